@@ -135,6 +135,8 @@ def work(case):
         if not case.get("causal", True):
             right = (L - 1 - p).clamp(max=w - 1)
         far = (p - left).clamp(max=sinks)
+        if not case.get("causal", True):  # sinks past the window
+            far = far + (min(sinks, L) - (p + right + 1)).clamp(min=0)
         pairs += float((left + 1 + right + far).sum())
         rows += p.numel()
         first = float(p[0] - left[0])
@@ -335,16 +337,18 @@ def _visible(p, j, case):
     return (near & (j < p + w)) | first
 
 
-def _windowed(q, k, v, p0, case, step, attend):
+def _windowed(q, k, v, p0, case, step):
     """Rows at positions p0, p0 + 1, ... of q [Hq, n, D] against keys 0 .. L - 1, `step` rows at
-    a time, each against the keys that one of them sees."""
+    a time, against the keys that one of them sees."""
     L, n, grp = k.shape[1], q.shape[1], q.shape[0] // k.shape[0]
     w, sinks = case["window"], case["sinks"]
     out = []
     for a in range(0, n, step):
         z = min(n, a + step)
         lo = max(0, p0 + a - w + 1)
-        hi = p0 + z if case.get("causal", True) else min(L, p0 + z - 1 + w)
+        hi = p0 + z
+        if not case.get("causal", True):
+            hi = min(L, max(p0 + z - 1 + w, sinks))
         first = min(sinks, lo)
         j = torch.arange(lo, hi, device=DEV)
         kk, vv = k[:, lo:hi], v[:, lo:hi]
@@ -352,7 +356,7 @@ def _windowed(q, k, v, p0, case, step, attend):
             j = torch.cat([torch.arange(first, device=DEV), j])
             kk, vv = torch.cat([k[:, :first], kk], 1), torch.cat([v[:, :first], vv], 1)
         p = torch.arange(p0 + a, p0 + z, device=DEV)
-        out.append(attend(q[:, a:z], kk, vv, _visible(p, j, case), grp))
+        out.append(_attend(q[:, a:z], kk, vv, _visible(p, j, case), grp))
     return torch.cat([x[0] for x in out], 1), torch.cat([x[1] for x in out], 1)
 
 
@@ -373,7 +377,7 @@ def _run_plain(s):
             if n <= 0:
                 continue
             ob, lb = _windowed(q[b, :, :n].float(), k[b, :, :L].float(), v[b, :, :L].float(), p0,
-                               c, _rows_at_once(c, min(L, 2 * c["window"] + c["sinks"])), _attend)
+                               c, _rows_at_once(c, min(L, 2 * c["window"] + c["sinks"])))
             o[b, :, :n], lse[b, :, :n] = ob.bfloat16(), lb
         return {"o": o, "lse": lse}
     lens, table, cache = s["lens_list"], s["table"], s["cache"]
@@ -392,7 +396,7 @@ def _run_plain(s):
     for b, L in enumerate(lens):
         k, v = _plain_rows(cache, table[b], L, "k"), _plain_rows(cache, table[b], L, "v")
         ob, lse[b] = _windowed(q[b].float(), k, v, L - n, c,
-                               _rows_at_once(c, min(L, c["window"] + c["sinks"])), _attend)
+                               _rows_at_once(c, min(L, c["window"] + c["sinks"])))
         o[b] = ob.bfloat16()
     return {"o": o, "lse": lse}
 
@@ -416,18 +420,32 @@ def _held64(x, bits):
     return (small[..., None] + step[..., None] * code).reshape(H, n, D)
 
 
-def _attend64(q, k, v, mask, grp):
-    """One block of rows from the definition, a key/value head at a time."""
+def _rows64(q, k, v, start, case):
+    """Rows at positions start, start + 1, ... of q [Hq, n, D] over all keys they may see, from
+    the definition: one query head and 1024 rows at a time."""
+    Hq, n, D = q.shape
+    L, share = k.shape[1], Hq // k.shape[0]
+    two_sided = not case.get("causal", True)
+    reach, sinks = min(case["window"], L), min(case["sinks"], L)
     o = torch.zeros(q.shape, dtype=torch.float64, device=DEV)
-    lse = torch.zeros(q.shape[:2], dtype=torch.float64, device=DEV)
-    hidden = torch.zeros(mask.shape, dtype=torch.float64, device=DEV)
-    hidden[~mask] = -math.inf
-    for h in range(q.shape[0]):
-        x = torch.mm(q[h].double(), k[h // grp].double().t().contiguous())
-        x = x * q.shape[2] ** -0.5 + hidden
-        lse[h] = torch.logsumexp(x, 1)
-        shift = torch.where(lse[h] > -math.inf, lse[h], torch.zeros_like(lse[h]))
-        o[h] = torch.mm(torch.exp(x - shift[:, None]), v[h // grp].double())
+    lse = torch.zeros(Hq, n, dtype=torch.float64, device=DEV)
+    every = torch.arange(L, device=DEV)
+    for r0 in range(0, n, 1024):
+        r1 = min(n, r0 + 1024)
+        pos = torch.arange(start + r0, start + r1, device=DEV)
+        some = (every > start + r0 - reach) | (every < sinks)
+        some &= (every < start + r1 - 1 + reach) | (every < sinks) if two_sided else every < start + r1
+        at = every[some]
+        gap = at.unsqueeze(0) - pos.unsqueeze(1)
+        hidden = (gap.abs() >= reach) & (at < sinks).logical_not().unsqueeze(0)
+        if not two_sided:
+            hidden |= gap > 0
+        for h in range(Hq):
+            kh, vh = k[h // share][at].double(), v[h // share][at].double()
+            x = (q[h, r0:r1].double() @ kh.t().contiguous()) / math.sqrt(D)
+            x[hidden] = -math.inf
+            lse[h, r0:r1] = x.logsumexp(1)
+            o[h, r0:r1] = x.softmax(1) @ vh
     return o, lse
 
 
@@ -442,8 +460,8 @@ def exact(case, seed):
         for b, L in enumerate(lens):
             n = L - p0
             if n > 0:
-                o[b, :, :n], lse[b, :, :n] = _windowed(q[b, :, :n], k[b, :, :L], v[b, :, :L], p0,
-                                                       case, 2048, _attend64)
+                o[b, :, :n], lse[b, :, :n] = _rows64(q[b, :, :n], k[b, :, :L], v[b, :, :L], p0,
+                                                     case)
         return {"o": o, "lse": lse}
     if case["kind"] in ("store", "read"):
         k = torch.zeros(case["B"], case["Hkv"], max(lens), case["D"], dtype=torch.float64,
@@ -458,6 +476,6 @@ def exact(case, seed):
     lse = torch.zeros(q.shape[:3], dtype=torch.float64, device=DEV)
     for b, L in enumerate(lens):
         kb, vb = kv(b)
-        o[b], lse[b] = _windowed(q[b], _held64(kb[0], case["bits"]), _held64(vb[0], case["bits"]),
-                                 L - n, case, 2048, _attend64)
+        o[b], lse[b] = _rows64(q[b], _held64(kb[0], case["bits"]), _held64(vb[0], case["bits"]),
+                               L - n, case)
     return {"o": o, "lse": lse}
