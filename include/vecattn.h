@@ -408,6 +408,136 @@ vecattn_status vecattn_recall(const void* q, const vecattn_tdesc* qd, const void
                               float* kept, void* stream);
 
 /*
+ * Attention with a sliding window and a few first keys that stay visible
+ * (sinks), for the layers that look at a neighbourhood instead of a selection.
+ * Row r of q is at position p = r + Nk - Nq (the queries are the last Nq rows of
+ * the keys), and sees the keys
+ *   V(p) = { j < L : (p - window < j and (causal ? j <= p : j < p + window))
+ *                    or (j < sinks and (!causal or j <= p)) },
+ * L = lens[b] or Nk:  o = sum over V(p) of softmax_j(scale * <q, k_j>) v_j, and
+ * lse as for vecattn_sparse_attn.  A window of 1 is the row's own key; a window
+ * (or sinks) of Nk or more is all of them.
+ *   q, o : bf16 [B, Hq, Nq, D]     k, v : bf16 [B, Hkv, Nk, D], Nq <= Nk
+ *   lens : optional int32 [B] device memory (clamped to [0, Nk]): the keys of
+ *          sequence b that exist.  Rows at or past it are padding: they are not
+ *          read, and their o and lse are left as they were.  NULL: all Nk.
+ *   causal : the VECATTN_CAUSAL bit (other bits are invalid)
+ *   scale  : 0 means 1 / sqrt(D)
+ *   lse    : optional fp32 [B, Hq, Nq] contiguous output, may be NULL
+ * A key outside a row's V(p) never reaches that row, whatever it holds.
+ * Errors: INVALID_ARG (null pointer, shape mismatch, Nq > Nk, window < 1, sinks
+ * < 0, bad scale or bits, misalignment); UNSUPPORTED (D not in {64, 128}, more
+ * than 65535 sequences or query heads, a K or V row stride of 2^24 elements or
+ * more).
+ */
+vecattn_status vecattn_window_attn(const void* q, const vecattn_tdesc* qd, const void* k,
+                                   const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,
+                                   const int32_t* lens, int64_t window, int64_t sinks,
+                                   int32_t causal, float scale, void* o, const vecattn_tdesc* od,
+                                   float* lse, void* stream);
+
+/*
+ * A key/value cache in pages, held in 4 or 8 bits a value.  The tokens of a
+ * sequence lie in pages of `page` tokens: table[b][c] is the page of tokens
+ * [c * page, (c + 1) * page) of sequence b.  Every 64 values x of one token and
+ * head (a group) are held as codes u and one pair (m, s) in bf16,
+ *   m = min x,  s = bf16((max x - min x) / M),  u = min(M, rint((x - m) / s)),
+ * M = 2^bits - 1, in fp32 steps, ties to even; they stand for m + s u.  A step
+ * below 2^-100 is held as 0 (u = 0); a group with a NaN or an infinity, or whose
+ * range is past fp32, stands for NaN.  4.5 or 8.5 bits a value.
+ */
+typedef struct vecattn_cache {
+  void* data;    /* device memory, 16-byte aligned, vecattn_cache_size bytes; the
+                    layout inside is the library's.  Contents need not be
+                    initialised: only tokens below lens[b] are looked at */
+  int64_t pages; /* pages held */
+  int32_t H, D;  /* key/value heads; 64 or 128 */
+  int32_t page;  /* tokens per page: a power of two, 32 to 1024 */
+  int32_t bits;  /* 4 or 8 */
+} vecattn_cache;
+
+/*
+ * Bytes of a cache (its data pointer is not looked at).
+ * Errors: INVALID_ARG (null pointer, pages < 1, H < 1, a page size or bits other
+ * than above, more than 2^62 bytes); UNSUPPORTED (D not in {64, 128}, H > 65535).
+ */
+vecattn_status vecattn_cache_size(const vecattn_cache* cache, size_t* bytes);
+
+/*
+ * Quantises the rows of k and v into the cache: the last rows of each sequence.
+ *   k, v  : bf16 [B, H, n, D]
+ *   table : int32 [B, cols] device memory.  An entry outside [0, pages) holds no
+ *           page: its tokens are not written here, not read back by
+ *           vecattn_cache_read, and not visible to vecattn_cache_attn (so pages
+ *           that a window has left behind can be given away).  Tokens past
+ *           cols * page are held nowhere either.
+ *   lens  : int32 [B] device memory: tokens of each sequence, the new ones included
+ *   n_new : optional int32 [B] device memory (clamped to [0, n]): the rows of
+ *           sequence b that exist (a padded batch), rows [0, n_new[b]); NULL: all n.
+ * Row r is written at position lens[b] - n_new[b] + r; rows at a position below 0
+ * are skipped.  Tokens at other positions stay as they are.
+ * Sequences of one call, and calls that may overlap, must not write the same
+ * page (reading pages that several sequences share is fine).
+ * Errors: INVALID_ARG (null pointer, shape mismatch between k, v and the cache,
+ * cols < 1 or cols * page > 2^30, a bad cache, misalignment); UNSUPPORTED (D not
+ * in {64, 128}, n > 2^28, more than 65535 sequences or heads).
+ */
+vecattn_status vecattn_cache_write(const void* k, const vecattn_tdesc* kd, const void* v,
+                                   const vecattn_tdesc* vd, const vecattn_cache* cache,
+                                   const int32_t* table, int64_t cols, const int32_t* lens,
+                                   const int32_t* n_new, void* stream);
+
+/*
+ * The cache's tokens [start, start + N) of each sequence as bf16, m + s u rounded
+ * once (e.g. a cached prompt for vecattn_select and vecattn_sparse_attn).
+ *   k, v : bf16 [B, H, N, D] outputs; row r is token start + r.  Rows of tokens
+ *          at or past lens[b], and of tokens that no page holds, are left as they
+ *          were.
+ * Errors: as vecattn_cache_write (N > 2^28: UNSUPPORTED); INVALID_ARG for start
+ * < 0 or > 2^30.
+ */
+vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, int64_t start, void* k,
+                                  const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
+                                  void* stream);
+
+/*
+ * Attention of the last n tokens of each sequence over its cached tokens: one
+ * token (decoding), a few (drafts), or a chunk of a prompt.  Row r of q is at
+ * position p = lens[b] - n_new[b] + r and sees
+ *   V(p) = { j <= p : j > p - window or j < sinks }, less the tokens that no
+ * page holds; the values are m + s u unrounded, and o, lse as for
+ * vecattn_sparse_attn (a row that sees nothing: o = 0, lse = -inf).  The new
+ * tokens' own K and V are in the cache already (vecattn_cache_write with the
+ * same lens).
+ *   q, o   : bf16 [B, Hq, n, D], Hq a multiple of the cache's H
+ *   table, cols, lens, n_new : as for vecattn_cache_write; rows at or past
+ *            n_new[b] are left as they were
+ *   window : >= 1 (2^30: everything)      sinks : >= 0
+ *   scale  : 0 means 1 / sqrt(D)
+ *   lse    : optional fp32 [B, Hq, n] contiguous output, may be NULL
+ *   workspace : device memory (16-byte aligned) of at least
+ *            vecattn_cache_attn_workspace_size bytes for the same qd, cache, cols,
+ *            window and sinks (0: may be NULL); contents need not be initialised.
+ *            Calls that may overlap need one each.
+ * The result does not depend on the order of execution (no atomics).  What a
+ * call does follows lens, n_new and table on the device, so that a captured call
+ * can be replayed as they change.
+ * Errors: as vecattn_cache_write; INVALID_ARG for window < 1, sinks < 0, a bad
+ * scale, a misaligned workspace; CAPACITY (workspace too small); UNSUPPORTED
+ * (sizes past the launch limits: B * Hq * n > 2^31 or about 2^24 workgroups).
+ */
+vecattn_status vecattn_cache_attn_workspace_size(const vecattn_tdesc* qd,
+                                                 const vecattn_cache* cache, int64_t cols,
+                                                 int64_t window, int64_t sinks, size_t* bytes);
+vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
+                                  const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, const int32_t* n_new, int64_t window,
+                                  int64_t sinks, float scale, void* o, const vecattn_tdesc* od,
+                                  float* lse, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+/*
  * Per-head filter ratios, Eq. 5 (Sec. 3.1.2).  Host function (host memory, no
  * GPU).
  * For each of `heads` heads, n_cand candidate filter ratios were sampled

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from dataclasses import dataclass
 from typing import Optional, Tuple
 
 import torch
@@ -32,6 +33,11 @@ class TDesc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int64), ("H", ctypes.c_int64), ("N", ctypes.c_int64),
                 ("D", ctypes.c_int64), ("sB", ctypes.c_int64), ("sH", ctypes.c_int64),
                 ("sN", ctypes.c_int64)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("H", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("page", ctypes.c_int32), ("bits", ctypes.c_int32)]
 
 
 _lib = None
@@ -77,12 +83,23 @@ def load() -> ctypes.CDLL:
     lib.vecattn_head_sparsity.argtypes = [P, i64, i64, i64, i32, i32, P, P]
     lib.vecattn_recall.argtypes = [P, D, P, D, P, i64, P, i32, i32, f32, P, P]
     lib.vecattn_select_noalloc.argtypes = [P, D, P, D, i32, i32, i32, f64, P, i64, P, P, P]
+    C = ctypes.POINTER(CacheDesc)
+    lib.vecattn_window_attn.argtypes = [P, D, P, D, P, D, P, i64, i64, i32, f32, P, D, P, P]
+    lib.vecattn_cache_size.argtypes = [C, ctypes.POINTER(ctypes.c_size_t)]
+    lib.vecattn_cache_write.argtypes = [P, D, P, D, C, P, i64, P, P, P]
+    lib.vecattn_cache_read.argtypes = [C, P, i64, P, i64, P, D, P, D, P]
+    lib.vecattn_cache_attn_workspace_size.argtypes = [D, C, i64, i64, i64,
+                                                      ctypes.POINTER(ctypes.c_size_t)]
+    lib.vecattn_cache_attn.argtypes = [P, D, C, P, i64, P, P, i64, i64, f32, P, D, P, P,
+                                       ctypes.c_size_t, P]
     for name in ("vecattn_pool", "vecattn_select_max_count", "vecattn_select_workspace_size",
                  "vecattn_select", "vecattn_select_mins_tiled", "vecattn_sparse_attn",
                  "vecattn_plan_filter_ratios", "vecattn_select_per_head",
                  "vecattn_select_varlen", "vecattn_sparse_attn_varlen", "vecattn_check_lists",
                  "vecattn_head_sparsity", "vecattn_recall", "vecattn_select_noalloc",
-                 "vecattn_sparse_attn_ordered", "vecattn_attn_order"):
+                 "vecattn_sparse_attn_ordered", "vecattn_attn_order", "vecattn_window_attn",
+                 "vecattn_cache_size", "vecattn_cache_write", "vecattn_cache_read",
+                 "vecattn_cache_attn_workspace_size", "vecattn_cache_attn"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -475,4 +492,195 @@ def sparse_attn_varlen(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seq
         cu.ctypes.data_as(ctypes.c_void_p), int(len(cu) - 1), _ptr(idx), int(cap), _ptr(counts),
         int(block), int(bool(causal)), float(scale), _ptr(out), ctypes.byref(od), _ptr(lse),
         _stream(q)), "sparse_attn_varlen")
+    return (out, lse) if return_lse else out
+
+
+def _desc_any(t: torch.Tensor) -> TDesc:
+    """desc() with the strides of dimensions of size 1, which address nothing, set to ones that
+    pass the library's checks (a slice of a projection may carry any)."""
+    d = desc(t)
+    if d.N == 1:
+        d.sN = d.D
+    if d.H == 1:
+        d.sH = 0
+    if d.B == 1:
+        d.sB = 0
+    return d
+
+
+def _int32_on(t: torch.Tensor, shape, device, name: str):
+    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape) \
+            or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on {device}")
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} must be on {device}")
+
+
+_ALL_KEYS = 1 << 30  # a window that hides nothing
+
+
+def window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0,
+                causal: bool = False, scale: float = 0.0, lens: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """Attention of q [B, Hq, Nq, D] over k, v [B, Hkv, Nk, D] (the queries are the last Nq rows)
+    with a sliding ``window`` (a key per side and the row's own: |p - j| < window) and the first
+    ``sinks`` keys, vecattn_window_attn.  ``lens`` (int32 [B]): the keys of each sequence that
+    exist; padded rows of a given ``out`` are left as they were (0 in an ``out`` made here)."""
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _bf16_cuda(t, n)
+    if out is None:
+        new = torch.empty if lens is None else torch.zeros
+        out = new(q.shape, dtype=q.dtype, device=q.device)
+    _bf16_cuda(out, "out")
+    _same_device(q.device, k=k, v=v, out=out)
+    B, Hq, Nq, _ = q.shape
+    if lens is not None:
+        _int32_on(lens, (B,), q.device, "lens")
+    lse = None
+    if return_lse:
+        lse = (torch.empty if lens is None else torch.zeros)((B, Hq, Nq), dtype=torch.float32,
+                                                             device=q.device)
+    qd, kd, vd, od = _desc_any(q), _desc_any(k), _desc_any(v), _desc_any(out)
+    with torch.cuda.device(q.device):
+        _check(load().vecattn_window_attn(
+            _ptr(q), ctypes.byref(qd), _ptr(k), ctypes.byref(kd), _ptr(v), ctypes.byref(vd),
+            _ptr(lens), int(window), int(sinks), int(bool(causal)), float(scale), _ptr(out),
+            ctypes.byref(od), _ptr(lse), _stream(q)), "window_attn")
+    return (out, lse) if return_lse else out
+
+
+@dataclass
+class Cache:
+    """A key/value cache in pages of 4- or 8-bit values (vecattn_cache): ``data`` (uint8, the
+    library's layout) of ``pages`` pages of ``page`` tokens, ``heads`` x ``dim`` values each."""
+    data: torch.Tensor
+    pages: int
+    heads: int
+    dim: int
+    page: int
+    bits: int
+
+    def desc(self) -> CacheDesc:
+        return CacheDesc(self.data.data_ptr(), self.pages, self.heads, self.dim, self.page,
+                         self.bits)
+
+
+def cache_bytes(pages: int, heads: int, dim: int, page: int = 64, bits: int = 4) -> int:
+    """Bytes of a cache of these sizes."""
+    n = ctypes.c_size_t(0)
+    d = CacheDesc(None, int(pages), int(heads), int(dim), int(page), int(bits))
+    _check(load().vecattn_cache_size(ctypes.byref(d), ctypes.byref(n)), "cache_size")
+    return int(n.value)
+
+
+def cache_alloc(pages: int, heads: int, dim: int, page: int = 64, bits: int = 4,
+                device="cuda") -> Cache:
+    """A cache of ``pages`` pages of ``page`` tokens (a power of two, 32 to 1024), ``heads``
+    key/value heads of ``dim`` values, 4 or 8 bits each."""
+    n = cache_bytes(pages, heads, dim, page, bits)
+    return Cache(torch.empty(n, dtype=torch.uint8, device=device), int(pages), int(heads),
+                 int(dim), int(page), int(bits))
+
+
+def _cache_args(cache: Cache, table: torch.Tensor, lens: torch.Tensor, B: int,
+                n_new: Optional[torch.Tensor] = None):
+    dev = cache.data.device
+    if not cache.data.is_cuda or cache.data.dtype != torch.uint8 or not cache.data.is_contiguous() \
+            or cache.data.numel() < cache_bytes(cache.pages, cache.heads, cache.dim, cache.page,
+                                                cache.bits):
+        raise ValueError("the cache's data must be a contiguous uint8 CUDA tensor of cache_bytes")
+    if table.dim() != 2:
+        raise ValueError("table must be [B, cols]")
+    _int32_on(table, (B, table.shape[1]), dev, "table")
+    _int32_on(lens, (B,), dev, "lens")
+    if n_new is not None:
+        _int32_on(n_new, (B,), dev, "n_new")
+    return dev, cache.desc()
+
+
+def cache_write(cache: Cache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
+                lens: torch.Tensor, n_new: Optional[torch.Tensor] = None) -> None:
+    """Quantises k, v [B, heads, n, dim], the last rows of each sequence, into the cache
+    (vecattn_cache_write).  ``table`` int32 [B, cols]: the page of every ``page`` tokens (-1:
+    none); ``lens`` int32 [B]: tokens of each sequence, the new ones included; ``n_new`` int32
+    [B]: how many of the n rows each sequence has (all when not given)."""
+    _bf16_cuda(k, "k")
+    _bf16_cuda(v, "v")
+    kd, vd = _desc_any(k), _desc_any(v)
+    dev, cd = _cache_args(cache, table, lens, k.shape[0], n_new)
+    _same_device(dev, k=k, v=v)
+    with torch.cuda.device(dev):
+        _check(load().vecattn_cache_write(
+            _ptr(k), ctypes.byref(kd), _ptr(v), ctypes.byref(vd), ctypes.byref(cd), _ptr(table),
+            int(table.shape[1]), _ptr(lens), _ptr(n_new), _stream(cache.data)), "cache_write")
+
+
+def cache_read(cache: Cache, table: torch.Tensor, lens: torch.Tensor, n: int, start: int = 0,
+               out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None
+               ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Tokens [start, start + n) of each sequence back as bf16 k, v [B, heads, n, dim]
+    (vecattn_cache_read).  Rows of tokens that are not held are left as they were in a given
+    ``out`` pair, and 0 in one made here."""
+    B = table.shape[0]
+    dev, cd = _cache_args(cache, table, lens, B)
+    if out is None:
+        shape = (B, cache.heads, int(n), cache.dim)
+        out = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
+    k, v = out
+    for t, name in ((k, "k"), (v, "v")):
+        _bf16_cuda(t, name)
+        if tuple(t.shape) != (B, cache.heads, int(n), cache.dim):
+            raise ValueError("out must be a pair of [B, heads, n, dim] tensors")
+    _same_device(dev, k=k, v=v)
+    kd, vd = _desc_any(k), _desc_any(v)
+    with torch.cuda.device(dev):
+        _check(load().vecattn_cache_read(
+            ctypes.byref(cd), _ptr(table), int(table.shape[1]), _ptr(lens), int(start), _ptr(k),
+            ctypes.byref(kd), _ptr(v), ctypes.byref(vd), _stream(cache.data)), "cache_read")
+    return k, v
+
+
+def cache_attn_workspace_bytes(q: torch.Tensor, cache: Cache, cols: int,
+                               window: Optional[int] = None, sinks: int = 0) -> int:
+    """Workspace bytes of cache_attn for these shapes (a table of ``cols`` columns)."""
+    n = ctypes.c_size_t(0)
+    qd, cd = _desc_any(q), cache.desc()
+    _check(load().vecattn_cache_attn_workspace_size(
+        ctypes.byref(qd), ctypes.byref(cd), int(cols), _ALL_KEYS if window is None else int(window),
+        int(sinks), ctypes.byref(n)), "cache_attn_workspace_size")
+    return int(n.value)
+
+
+def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.Tensor,
+               n_new: Optional[torch.Tensor] = None, window: Optional[int] = None, sinks: int = 0,
+               scale: float = 0.0, out: Optional[torch.Tensor] = None, return_lse: bool = False,
+               workspace: Optional[torch.Tensor] = None):
+    """Attention of q [B, Hq, n, dim], the last n tokens of each sequence, over the cached tokens
+    (vecattn_cache_attn): causal, all of them or a sliding ``window`` and the first ``sinks``.
+    ``table``, ``lens``, ``n_new`` as for cache_write, which has put the new tokens' K and V there.
+    Padded rows of a given ``out`` are left as they were (0 in an ``out`` made here)."""
+    _bf16_cuda(q, "q")
+    B, Hq, n, _ = q.shape
+    dev, cd = _cache_args(cache, table, lens, B, n_new)
+    new = torch.empty if n_new is None else torch.zeros
+    if out is None:
+        out = new(q.shape, dtype=q.dtype, device=dev)
+    _bf16_cuda(out, "out")
+    _same_device(dev, q=q, out=out, workspace=workspace)
+    lse = new((B, Hq, n), dtype=torch.float32, device=dev) if return_lse else None
+    window = _ALL_KEYS if window is None else int(window)
+    need = cache_attn_workspace_bytes(q, cache, table.shape[1], window, sinks)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    nws = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    qd, od = _desc_any(q), _desc_any(out)
+    with torch.cuda.device(dev):
+        _check(load().vecattn_cache_attn(
+            _ptr(q), ctypes.byref(qd), ctypes.byref(cd), _ptr(table), int(table.shape[1]),
+            _ptr(lens), _ptr(n_new), window, int(sinks), float(scale), _ptr(out),
+            ctypes.byref(od), _ptr(lse), _ptr(workspace), nws, _stream(q)), "cache_attn")
     return (out, lse) if return_lse else out

@@ -14,6 +14,8 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kNegInf = -__builtin_inff();
 
@@ -56,6 +58,17 @@ __device__ __forceinline__ float wave_max_xor32(float x) {
 
 #define LDS_PTR(T, p) ((__attribute__((address_space(3))) T*)(p))
 
+// 16-byte copy per lane from a buffer (byte offset voff) to LDS (destination:
+// wave-uniform base + 16 * lane).  The 16-byte form exists only on gfx950;
+// the host pass of the compiler rejects it, so it is compiled for the device
+// side only.
+__device__ __forceinline__ void gather16_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t voff,
+                                                void* lds_base) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, lds_base), 16, voff, 0, 0, 0);
+#endif
+}
+
 // Chunk swizzle: 16-byte chunk c of row r lives at chunk c ^ swz(r).  LDS has
 // 64 banks of 4 bytes; a 16-byte read serves 16 lanes per cycle, an 8-byte
 // read 32.  K reads (16 lanes = 16 consecutive rows, one logical chunk) need
@@ -77,5 +90,8 @@ __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
+
+// Every vector-memory and LDS access of the wave so far.
+__device__ __forceinline__ void wait_all() { __builtin_amdgcn_s_waitcnt(7 << 4); }
 
 }  // namespace vecattn

@@ -117,6 +117,55 @@ struct RecallArgs {
 };
 hipError_t launch_recall(const RecallArgs& a, hipStream_t stream);
 
+// Attention with a sliding window and sinks.  Row r of q is at position
+// r + k.N - q.N; lens (int32 [B], or NULL) bounds each sequence's keys and rows.
+struct WindowArgs {
+  Tensor4 q, k, v;
+  void* o;
+  int64_t o_sB, o_sH, o_sN;
+  float* lse;
+  const int32_t* lens;
+  int64_t window, sinks;
+  int32_t causal;
+  float scale;
+};
+hipError_t launch_window_attn(const WindowArgs& a, hipStream_t stream);
+
+// The quantised key/value cache and the pages of a batch of sequences.
+struct CacheArgs {
+  void* data;
+  int64_t pages;
+  int32_t H, D, page, bits;
+  const int32_t* table;  // [B, cols] pages
+  int64_t cols;
+  const int32_t* lens;   // [B] tokens held
+};
+hipError_t launch_cache_write(const Tensor4& k, const Tensor4& v, const CacheArgs& c,
+                              const int32_t* n_new, hipStream_t stream);
+hipError_t launch_cache_read(const CacheArgs& c, int64_t start, const Tensor4& k, const Tensor4& v,
+                             hipStream_t stream);
+
+// Attention over the cache.  How the work is dealt out, and so the workspace,
+// follows from the shape.
+struct CacheAttnShape {
+  int64_t B, Hq, H, n, D;
+  int64_t cols, page, window, sinks;
+};
+struct CacheAttnArgs {
+  CacheAttnShape shape;
+  Tensor4 q;
+  CacheArgs cache;
+  const int32_t* n_new;
+  void* o;
+  int64_t o_sB, o_sH, o_sN;
+  float* lse;
+  float scale;
+  void* workspace;
+};
+bool cache_attn_grid_ok(const CacheAttnShape& s);
+size_t cache_attn_workspace_bytes(const CacheAttnShape& s);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t stream);
+
 // Host: per-head filter ratios by dynamic programming (Eq. 5).  Returns 0, or
 // 1 when no choice reaches the target.
 int plan_filter_ratios(int32_t H, int32_t C, const double* sp, const double* perf, double target,

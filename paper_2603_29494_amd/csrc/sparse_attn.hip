@@ -50,19 +50,6 @@ constexpr int kHerdUnit = 4096;
 // so they must be rare next to the gathers.
 constexpr int kHerdBatch = 16;
 
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
-// 16-byte copy per lane from a buffer (byte offset voff) to LDS (destination:
-// wave-uniform base + 16 * lane).  The 16-byte form exists only on gfx950;
-// the host pass of the compiler rejects it, so it is compiled for the device
-// side only.
-__device__ __forceinline__ void gather16_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t voff,
-                                                void* lds_base) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, LDS_PTR(void, lds_base), 16, voff, 0, 0, 0);
-#endif
-}
-
 // 4-byte copy per lane of a list entry to LDS through the list's buffer
 // resource: offsets past the list read 0, so no index can leave the list.
 __device__ __forceinline__ void ids_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t voff,

@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -186,7 +187,7 @@ vecattn_status select_impl(const void* q, const vecattn_tdesc* qd, const void* k
 
 extern "C" {
 
-int32_t vecattn_version(void) { return 101; }
+int32_t vecattn_version(void) { return 102; }
 
 const char* vecattn_status_string(vecattn_status s) {
   switch (s) {
@@ -389,6 +390,68 @@ vecattn_tdesc seq_desc(const vecattn_tdesc* d, int64_t n) {
   return r;
 }
 
+constexpr int64_t kMaxGridYZ = 65535;        // heads and sequences are grid dimensions
+constexpr int64_t kMaxCacheRows = int64_t(1) << 28;
+
+bool same_shape(const vecattn_tdesc* a, const vecattn_tdesc* b) {
+  return a->B == b->B && a->H == b->H && a->N == b->N && a->D == b->D;
+}
+
+size_t cache_page_bytes(const vecattn_cache* c) {
+  const size_t token = static_cast<size_t>(c->D) * c->bits / 8 + static_cast<size_t>(c->D) / 64 * 4;
+  return 2 * token * static_cast<size_t>(c->page) * static_cast<size_t>(c->H);
+}
+
+vecattn_status check_cache(const vecattn_cache* c, bool with_data) {
+  if (!c || c->pages < 1 || c->H < 1 || c->D < 1) return VECATTN_ERR_INVALID_ARG;
+  if (c->page < 32 || c->page > 1024 || (c->page & (c->page - 1)) != 0)
+    return VECATTN_ERR_INVALID_ARG;
+  if (c->bits != 4 && c->bits != 8) return VECATTN_ERR_INVALID_ARG;
+  if (with_data && (!c->data || !aligned16(c->data))) return VECATTN_ERR_INVALID_ARG;
+  if ((c->D != 64 && c->D != 128) || c->H > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
+  if (static_cast<size_t>(c->pages) > (size_t(1) << 62) / cache_page_bytes(c))
+    return VECATTN_ERR_INVALID_ARG;
+  return VECATTN_OK;
+}
+
+bool cols_ok(int64_t cols, int32_t page) { return cols >= 1 && cols <= kMaxN / page; }
+
+// The arguments that writing and reading back share.
+vecattn_status check_cache_rows(const void* k, const vecattn_tdesc* kd, const void* v,
+                                const vecattn_tdesc* vd, const vecattn_cache* c,
+                                const int32_t* table, int64_t cols, const int32_t* lens) {
+  vecattn_status st;
+  if ((st = check_desc(k, kd)) != VECATTN_OK) return st;
+  if ((st = check_desc(v, vd)) != VECATTN_OK) return st;
+  if ((st = check_cache(c, true)) != VECATTN_OK) return st;
+  if (!same_shape(kd, vd) || kd->H != c->H || kd->D != c->D) return VECATTN_ERR_INVALID_ARG;
+  if (!table || !lens || !cols_ok(cols, c->page)) return VECATTN_ERR_INVALID_ARG;
+  if (kd->B > kMaxGridYZ || kd->N > kMaxCacheRows) return VECATTN_ERR_UNSUPPORTED;
+  return VECATTN_OK;
+}
+
+vecattn_status check_cache_attn(const vecattn_tdesc* qd, const vecattn_cache* c, bool with_data,
+                                int64_t cols, int64_t window, int64_t sinks,
+                                vecattn::CacheAttnShape* s) {
+  const vecattn_status st = check_cache(c, with_data);
+  if (st != VECATTN_OK) return st;
+  if (!qd || qd->B < 1 || qd->H < 1 || qd->N < 1 || qd->D != c->D || qd->H % c->H != 0)
+    return VECATTN_ERR_INVALID_ARG;
+  if (!cols_ok(cols, c->page) || window < 1 || sinks < 0) return VECATTN_ERR_INVALID_ARG;
+  if (qd->B > kMaxGridYZ || qd->H > kMaxGridYZ || qd->N > kMaxCacheRows)
+    return VECATTN_ERR_UNSUPPORTED;
+  // A window or sinks past every position is all of it (and keeps the sums of
+  // positions in range).
+  *s = vecattn::CacheAttnShape{qd->B, qd->H, c->H, qd->N, qd->D, cols, c->page,
+                               std::min(window, int64_t(1) << 32), std::min(sinks, int64_t(1) << 32)};
+  return vecattn::cache_attn_grid_ok(*s) ? VECATTN_OK : VECATTN_ERR_UNSUPPORTED;
+}
+
+vecattn::CacheArgs to_cache(const vecattn_cache* c, const int32_t* table, int64_t cols,
+                            const int32_t* lens) {
+  return vecattn::CacheArgs{c->data, c->pages, c->H, c->D, c->page, c->bits, table, cols, lens};
+}
+
 const void* seq_ptr(const void* p, const vecattn_tdesc* d, int64_t row) {
   return static_cast<const char*>(p) + row * d->sN * 2;  // bf16 elements
 }
@@ -464,6 +527,98 @@ vecattn_status vecattn_sparse_attn_varlen(const void* q, const vecattn_tdesc* qd
                             o, od->sB, od->sH, od->sN, lse, idx, counts, cap, block,
                             (causal & kCausal) ? 1 : 0, scale, nullptr};
   hipError_t e = vecattn::launch_sparse_attn_varlen(a, cu_seqlens, nseq, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_window_attn(const void* q, const vecattn_tdesc* qd, const void* k,
+                                   const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,
+                                   const int32_t* lens, int64_t window, int64_t sinks,
+                                   int32_t causal, float scale, void* o, const vecattn_tdesc* od,
+                                   float* lse, void* stream) {
+  vecattn_status st;
+  if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
+  if ((st = check_desc(k, kd)) != VECATTN_OK) return st;
+  if ((st = check_desc(v, vd)) != VECATTN_OK) return st;
+  if ((st = check_desc(o, od)) != VECATTN_OK) return st;
+  if (kd->B != qd->B || kd->D != qd->D || qd->N > kd->N || qd->H % kd->H != 0)
+    return VECATTN_ERR_INVALID_ARG;
+  if (vd->B != kd->B || vd->H != kd->H || vd->N != kd->N || vd->D != kd->D || !same_shape(od, qd))
+    return VECATTN_ERR_INVALID_ARG;
+  if (window < 1 || sinks < 0 || !std::isfinite(scale) || scale < 0.0f || (causal & ~kCausal) != 0)
+    return VECATTN_ERR_INVALID_ARG;
+  if (qd->B > kMaxGridYZ || qd->H > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
+  // A tile's 64 rows are addressed with 32-bit byte offsets.
+  if (kd->N > 1 && (kd->sN >= (int64_t(1) << 24) || vd->sN >= (int64_t(1) << 24)))
+    return VECATTN_ERR_UNSUPPORTED;
+  vecattn::WindowArgs a{to_tensor(q, qd), to_tensor(k, kd), to_tensor(v, vd), o, od->sB, od->sH,
+                        od->sN, lse, lens, window, sinks, causal, scale};
+  hipError_t e = vecattn::launch_window_attn(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_size(const vecattn_cache* cache, size_t* bytes) {
+  if (!bytes) return VECATTN_ERR_INVALID_ARG;
+  const vecattn_status st = check_cache(cache, false);
+  if (st != VECATTN_OK) return st;
+  *bytes = static_cast<size_t>(cache->pages) * cache_page_bytes(cache);
+  return VECATTN_OK;
+}
+
+vecattn_status vecattn_cache_write(const void* k, const vecattn_tdesc* kd, const void* v,
+                                   const vecattn_tdesc* vd, const vecattn_cache* cache,
+                                   const int32_t* table, int64_t cols, const int32_t* lens,
+                                   const int32_t* n_new, void* stream) {
+  vecattn_status st = check_cache_rows(k, kd, v, vd, cache, table, cols, lens);
+  if (st != VECATTN_OK) return st;
+  hipError_t e = vecattn::launch_cache_write(to_tensor(k, kd), to_tensor(v, vd),
+                                             to_cache(cache, table, cols, lens), n_new,
+                                             static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, int64_t start, void* k,
+                                  const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
+                                  void* stream) {
+  vecattn_status st = check_cache_rows(k, kd, v, vd, cache, table, cols, lens);
+  if (st != VECATTN_OK) return st;
+  if (start < 0 || start > kMaxN) return VECATTN_ERR_INVALID_ARG;
+  hipError_t e = vecattn::launch_cache_read(to_cache(cache, table, cols, lens), start,
+                                            to_tensor(k, kd), to_tensor(v, vd),
+                                            static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_attn_workspace_size(const vecattn_tdesc* qd,
+                                                 const vecattn_cache* cache, int64_t cols,
+                                                 int64_t window, int64_t sinks, size_t* bytes) {
+  if (!bytes) return VECATTN_ERR_INVALID_ARG;
+  vecattn::CacheAttnShape s;
+  const vecattn_status st = check_cache_attn(qd, cache, false, cols, window, sinks, &s);
+  if (st != VECATTN_OK) return st;
+  *bytes = vecattn::cache_attn_workspace_bytes(s);
+  return VECATTN_OK;
+}
+
+vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
+                                  const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, const int32_t* n_new, int64_t window,
+                                  int64_t sinks, float scale, void* o, const vecattn_tdesc* od,
+                                  float* lse, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+  vecattn_status st;
+  if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
+  if ((st = check_desc(o, od)) != VECATTN_OK) return st;
+  vecattn::CacheAttnShape s;
+  if ((st = check_cache_attn(qd, cache, true, cols, window, sinks, &s)) != VECATTN_OK) return st;
+  if (!table || !lens || !same_shape(od, qd) || !std::isfinite(scale) || scale < 0.0f)
+    return VECATTN_ERR_INVALID_ARG;
+  const size_t need = vecattn::cache_attn_workspace_bytes(s);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return VECATTN_ERR_CAPACITY;
+  if (workspace && !aligned16(workspace)) return VECATTN_ERR_INVALID_ARG;
+  vecattn::CacheAttnArgs a{s, to_tensor(q, qd), to_cache(cache, table, cols, lens), n_new, o,
+                           od->sB, od->sH, od->sN, lse, scale, workspace};
+  hipError_t e = vecattn::launch_cache_attn(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 

@@ -1,0 +1,301 @@
+// Attention with a sliding window and sinks: query position p sees the keys
+// j with p - window < j (and j <= p causal, or j < p + window), and the first
+// `sinks` keys (causal: those at or before p).
+//
+// One workgroup owns 128 query rows of one head (four waves of 32) and walks the
+// tiles of 64 keys that one of its rows sees: those of the sinks, then those of
+// the window.  A tile's K and V rows go straight from memory to LDS (16 bytes per
+// lane) while the tile before is worked on, stored with the swizzle of
+// device_common.h.  Each wave computes S^T = K Q^T and O^T += V^T P^T for the
+// whole tile on v_mfma_f32_32x32x16_bf16 (lane layout as in sparse_attn.hip) with
+// the softmax state in registers.  Only tiles that some row of a wave does not
+// see whole are masked, and tiles that none of its rows sees are skipped by it.
+#include <algorithm>
+
+#include "device_common.h"
+#include "launch.h"
+
+namespace vecattn {
+namespace {
+
+constexpr int kTile = 64;
+constexpr int kRows = 128;   // query rows per workgroup
+constexpr float kUnseen = -3.4028234663852886e38f;
+
+struct WindowParams {
+  const uint16_t *q, *k, *v;
+  int64_t q_sB, q_sH, q_sN, k_sB, k_sH, k_sN, v_sB, v_sH, v_sN;
+  uint16_t* o;
+  int64_t o_sB, o_sH, o_sN;
+  float* lse;
+  const int32_t* lens;
+  int32_t Hq, group, Nq, Nk, window, sinks, causal, row_tiles;
+  float scale_log2;
+};
+
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_window_attn(
+    const WindowParams a) {
+  constexpr int CH = D / 8;
+  constexpr int U = kTile * CH / 256;   // direct-load instructions per wave and matrix
+  constexpr int DS = D / 16, DB = D / 32, RB = 2 * D;
+  __shared__ __align__(16) uint16_t k_s0[kTile * D];
+  __shared__ __align__(16) uint16_t k_s1[kTile * D];
+  __shared__ __align__(16) uint16_t v_s0[kTile * D];
+  __shared__ __align__(16) uint16_t v_s1[kTile * D];
+  auto kbuf = [&](int st) __attribute__((always_inline)) { return st ? k_s1 : k_s0; };
+  auto vbuf = [&](int st) __attribute__((always_inline)) { return st ? v_s1 : v_s0; };
+
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rt = blockIdx.x;
+  const int h = blockIdx.y, b = blockIdx.z, hk = h / a.group;
+  const int off = a.Nk - a.Nq;                       // position of row 0
+  const int len = a.lens ? min(max(a.lens[b], 0), a.Nk) : a.Nk;
+  const int rows_end = min(a.Nq, len - off);         // rows past it are padding
+  const int row0 = rt * kRows;
+  if (row0 >= rows_end) return;
+  const int p_lo = row0 + off, p_hi = min(row0 + kRows, rows_end) - 1 + off;
+  // Keys of the window, [near, far] (with two-sided sinks past it), and the tiles:
+  // ns of the sinks before it, then from nt0.
+  const int near = max(0, p_lo - a.window + 1);
+  const int far = a.causal ? p_hi : min(len, max(p_hi + a.window, a.sinks)) - 1;
+  const int nt0 = near / kTile;
+  const int ns = min(nt0, (min(a.sinks, near) + kTile - 1) / kTile);
+  const int ntiles = ns + far / kTile + 1 - nt0;
+  auto tile_key = [&](int t) __attribute__((always_inline)) {
+    return (t < ns ? t : nt0 + (t - ns)) * kTile;
+  };
+
+  const uint16_t* kh = a.k + b * a.k_sB + hk * a.k_sH;
+  const uint16_t* vh = a.v + b * a.v_sB + hk * a.v_sH;
+  const uint32_t k_rowb = static_cast<uint32_t>(a.k_sN) * 2u;
+  const uint32_t v_rowb = static_cast<uint32_t>(a.v_sN) * 2u;
+  // The tile's rows as buffer resources (rows at or past len read 0).
+  auto gather = [&](int j0, int st) __attribute__((always_inline)) {
+    const int rows = min(kTile, len - j0);
+    const __amdgpu_buffer_rsrc_t krs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t*>(kh + j0 * a.k_sN), 0, (rows - 1) * k_rowb + RB, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vrs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t*>(vh + j0 * a.v_sN), 0, (rows - 1) * v_rowb + RB, 0x00020000);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = (wave * U + u) * 64 + lane, r = i / CH;
+      const uint32_t c = 16u * ((i % CH) ^ swz<D>(r));
+      gather16_to_lds(krs, r * k_rowb + c, kbuf(st) + (wave * U + u) * 64 * 8);
+      gather16_to_lds(vrs, r * v_rowb + c, vbuf(st) + (wave * U + u) * 64 * 8);
+    }
+  };
+
+  const int my_row = row0 + 32 * wave + ln;
+  const int my_pos = my_row + off;
+  const bool have = my_row < rows_end;
+  bf16x8 qf[DS];
+  {
+    const u32x4* qr = reinterpret_cast<const u32x4*>(
+        a.q + b * a.q_sB + h * a.q_sH + static_cast<int64_t>(have ? my_row : row0) * a.q_sN);
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+      const u32x4 t = have ? qr[2 * s + g] : u32x4{0, 0, 0, 0};
+      qf[s] = __builtin_bit_cast(bf16x8, t);
+    }
+  }
+  // Positions of the wave's rows that exist (w_hi < w_lo: none).
+  const int w_lo = row0 + 32 * wave + off, w_hi = min(w_lo + 31, rows_end - 1 + off);
+
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+  float m_run = kUnseen, l_run = 0.0f;
+
+  const int j16 = lane & 15, tq = j16 >> 2, tp = j16 & 3, vhalf = (lane >> 4) & 1;
+  uint32_t koff[DS], voff[DB][2];
+#pragma unroll
+  for (int s2 = 0; s2 < DS; ++s2) koff[s2] = ln * RB + 16 * ((2 * s2 + g) ^ swz<D>(ln));
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int hi = 0; hi < 2; ++hi) {
+      const int d = 32 * db + 16 * vhalf + 4 * tp;
+      const int k0 = 4 * g + tq + 8 * hi;
+      voff[db][hi] = k0 * RB + 16 * ((d >> 3) ^ swz<D>(k0)) + 8 * ((d >> 2) & 1);
+    }
+
+  auto step = [&](int j0, int st) __attribute__((always_inline)) {
+    // What the wave's rows see of keys j0 .. j0 + 63: nothing, all, or a part.
+    const bool in_sinks = j0 < a.sinks && !(a.causal && j0 > w_hi);
+    const bool in_near = j0 + kTile - 1 > w_lo - a.window &&
+                         (a.causal ? j0 <= w_hi : j0 < w_hi + a.window);
+    if (w_hi < w_lo || !(in_sinks || in_near)) return;
+    const bool whole =
+        j0 + kTile <= len && (!a.causal || j0 + kTile - 1 <= w_lo) &&
+        (j0 + kTile <= a.sinks ||
+         (j0 > w_hi - a.window && (a.causal || j0 + kTile - 1 < w_lo + a.window)));
+    const char* kb = reinterpret_cast<const char*>(kbuf(st));
+    const char* vb = reinterpret_cast<const char*>(vbuf(st));
+    f32x16 s[2];
+#pragma unroll
+    for (int kh2 = 0; kh2 < 2; ++kh2) {
+      s[kh2] = f32x16{};
+#pragma unroll
+      for (int s2 = 0; s2 < DS; ++s2) {
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + koff[s2] + kh2 * 32 * RB);
+        s[kh2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[s2],
+                                                         s[kh2], 0, 0, 0);
+      }
+    }
+    auto sees = [&](int j) __attribute__((always_inline)) {
+      const bool nr = j > my_pos - a.window && (a.causal || j < my_pos + a.window);
+      return j < len && (nr || j < a.sinks) && (!a.causal || j <= my_pos);
+    };
+    if (!whole) {
+#pragma unroll
+      for (int kh2 = 0; kh2 < 2; ++kh2)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + 32 * kh2 + 8 * (e / 4) + 4 * g + e % 4;
+          s[kh2][e] = sees(j) ? s[kh2][e] : kNegInf;
+        }
+    }
+    float top = kNegInf;
+#pragma unroll
+    for (int kh2 = 0; kh2 < 2; ++kh2)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kh2][e]);
+    top = wave_max_xor32(top) * a.scale_log2;
+    if (__any(top > m_run + 8.0f)) {
+      const float m_new = top > m_run + 8.0f ? top : m_run;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+    }
+    auto vread = [&](int ks, int db) __attribute__((always_inline)) {
+      const char* a0 = vb + voff[db][0] + 16 * ks * RB;
+      const char* a1 = vb + voff[db][1] + 16 * ks * RB;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a0));
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a1));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // In a tile that is not seen whole, a NaN or an infinity of a V row must not
+    // reach the rows that do not see it through 0 * NaN: such values are taken out
+    // of the product and added to the rows that see them.
+    bool odd = false;
+    if (!whole) {
+      uint32_t hot = 0;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const i16x8 x = vread(ks, db);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            hot |= (static_cast<uint16_t>(x[e]) & 0x7F80u) == 0x7F80u ? 1u : 0u;
+        }
+      odd = __any(hot != 0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      f32x8 p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[ks >> 1][8 * (ks & 1) + e], a.scale_log2, -m_run));
+        l_run += p[e];
+      }
+      const bf16x8 pb = __builtin_convertvector(p, bf16x8);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        i16x8 x = vread(ks, db);
+        if (odd) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            x[e] = (static_cast<uint16_t>(x[e]) & 0x7F80u) == 0x7F80u ? short(0) : x[e];
+        }
+        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb,
+                                                           oacc[db], 0, 0, 0);
+      }
+    }
+    if (odd) {
+      for (int j = 0; j < kTile; ++j) {
+        if (!sees(j0 + j)) continue;
+        const char* row = vb + j * RB;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int d = 32 * db + 8 * (e / 4) + 4 * g + e % 4;
+            const uint16_t x = *reinterpret_cast<const uint16_t*>(
+                row + 16 * ((d >> 3) ^ swz<D>(j)) + 2 * (d & 7));
+            if ((x & 0x7F80u) == 0x7F80u) oacc[db][e] += bf16_bits_to_f32(x);
+          }
+      }
+    }
+  };
+
+  gather(tile_key(0), 0);
+  for (int t = 0; t < ntiles; t += 2) {
+    wait_all();
+    __builtin_amdgcn_s_barrier();
+    if (t + 1 < ntiles) gather(tile_key(t + 1), 1);
+    step(tile_key(t), 0);
+    if (t + 1 >= ntiles) break;
+    wait_all();
+    __builtin_amdgcn_s_barrier();
+    if (t + 2 < ntiles) gather(tile_key(t + 2), 0);
+    step(tile_key(t + 1), 1);
+  }
+
+  l_run += __shfl_xor(l_run, 32);
+  if (!have) return;
+  const float inv = 1.0f / l_run;   // a row sees its own key at least
+  if (a.lse && g == 0)
+    a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.Nq + my_row] =
+        (m_run + __builtin_log2f(l_run)) * 0.69314718055994531f;
+  uint16_t* orow = a.o + b * a.o_sB + h * a.o_sH + static_cast<int64_t>(my_row) * a.o_sN;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int vq = 0; vq < 4; ++vq) {
+      f32x4 r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = oacc[db][4 * vq + e] * inv;
+      *reinterpret_cast<bf16x4*>(orow + 32 * db + 8 * vq + 4 * g) = __builtin_convertvector(r, bf16x4);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_window_attn(const WindowArgs& x, hipStream_t stream) {
+  WindowParams a;
+  a.q = static_cast<const uint16_t*>(x.q.ptr);
+  a.k = static_cast<const uint16_t*>(x.k.ptr);
+  a.v = static_cast<const uint16_t*>(x.v.ptr);
+  a.q_sB = x.q.sB, a.q_sH = x.q.sH, a.q_sN = x.q.sN;
+  a.k_sB = x.k.sB, a.k_sH = x.k.sH, a.k_sN = x.k.sN;
+  a.v_sB = x.v.sB, a.v_sH = x.v.sH, a.v_sN = x.v.sN;
+  a.o = static_cast<uint16_t*>(x.o);
+  a.o_sB = x.o_sB, a.o_sH = x.o_sH, a.o_sN = x.o_sN;
+  a.lse = x.lse;
+  a.lens = x.lens;
+  a.Hq = static_cast<int32_t>(x.q.H);
+  a.group = static_cast<int32_t>(x.q.H / x.k.H);
+  a.Nq = static_cast<int32_t>(x.q.N);
+  a.Nk = static_cast<int32_t>(x.k.N);
+  // A window or sinks past the keys is all of them (and keeps the positions'
+  // sums and differences in range: N <= 2^30).
+  a.window = static_cast<int32_t>(std::min(x.window, x.k.N));
+  a.sinks = static_cast<int32_t>(std::min(x.sinks, x.k.N));
+  a.causal = x.causal;
+  a.row_tiles = static_cast<int32_t>((x.q.N + kRows - 1) / kRows);
+  const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(x.q.D));
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const dim3 grid(static_cast<unsigned>(a.row_tiles), static_cast<unsigned>(x.q.H),
+                  static_cast<unsigned>(x.q.B));
+  if (x.q.D == 128) hipLaunchKernelGGL(k_window_attn<128>, grid, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL(k_window_attn<64>, grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace vecattn

@@ -1,0 +1,170 @@
+"""Window attention (sliding window and sinks) against a plain 64-bit form; bounds in
+window_reference."""
+import math
+
+import pytest
+import torch
+
+import paper_2603_29494_amd as va
+import window_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def rows(seed, B, H, N, D, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(B, H, N, D, generator=g) * scale).bfloat16().cuda()
+
+
+def case(seed, B, Hq, Hkv, Nq, Nk, D):
+    q = rows(seed, B, Hq, Nq, D, 1.5)
+    return q, rows(seed + 1, B, Hkv, Nk, D), rows(seed + 2, B, Hkv, Nk, D)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("B,Hq,Hkv,Nq,Nk,D,window,sinks", [
+    (1, 1, 1, 1, 1, 64, 1, 0),
+    (1, 2, 1, 1, 700, 128, 100, 4),        # one query at the end of the keys
+    (2, 4, 2, 65, 65, 64, 7, 0),
+    (1, 3, 3, 130, 130, 128, 1, 0),        # each row its own key
+    (1, 3, 1, 130, 130, 128, 1, 1),
+    (1, 7, 1, 333, 333, 128, 64, 64),      # sinks to a tile's end
+    (1, 2, 2, 333, 333, 64, 65, 63),
+    (1, 2, 2, 500, 500, 128, 129, 130),
+    (1, 2, 1, 257, 1001, 64, 200, 5),      # a chunk at the end
+    (1, 2, 1, 128, 900, 128, 1 << 40, 0),  # everything
+    (1, 2, 1, 200, 200, 128, 10, 1 << 40), # all keys are sinks
+    (1, 2, 2, 700, 700, 64, 300, 400),     # sinks that meet the window
+])
+def test_against_64_bits(gpu, B, Hq, Hkv, Nq, Nk, D, window, sinks, causal):
+    q, k, v = case(Nq + Nk + window % 97, B, Hq, Hkv, Nq, Nk, D)
+    o, lse = va.window_attn(q, k, v, window, sinks, causal, return_lse=True)
+    torch.cuda.synchronize()
+    w, s = min(window, 1 << 30), min(sinks, 1 << 30)
+    ref.check(o, lse, ref.window_attn(q, k, v, w, s, causal))
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("Nq,lens", [(300, [300, 0, 129, 1]), (100, [200, 201, 260, 300])])
+def test_padded_batch(gpu, Nq, lens, causal):
+    """Keys at or past lens are not seen whatever they hold, and padded rows stay as they were."""
+    q, k, v = case(5, 4, 4, 2, Nq, 300, 128)
+    for b, L in enumerate(lens):
+        k[b, :, L:] = math.nan
+        v[b, :, L:] = math.inf
+        q[b, :, max(0, L - (300 - Nq)):] = math.nan
+    t = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, 7.0)
+    o, lse = va.window_attn(q, k, v, 50, 3, causal, lens=t, out=out, return_lse=True)
+    torch.cuda.synchronize()
+    q[q.isnan()] = 0
+    r = ref.window_attn(q, k, v, 50, 3, causal, lens)
+    ref.check(o, lse, r)
+    pad = torch.isnan(r[1])
+    assert (o.cpu()[pad] == 7.0).all() and (lse.cpu()[pad] == 0).all()
+    fresh = va.window_attn(q, k, v, 50, 3, causal, lens=t)
+    assert torch.equal(fresh.cpu()[~pad], o.cpu()[~pad]) and (fresh.cpu()[pad] == 0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_layouts_and_scale(gpu, D):
+    """Token-major projections, a packed QKV view, an output in a wider buffer."""
+    B, Hq, Hkv, N = 2, 6, 2, 211
+    g = torch.Generator().manual_seed(3)
+    qkv = torch.randn(B, N, Hq + 2 * Hkv, D, generator=g).bfloat16().cuda()
+    q, k, v = (t.transpose(1, 2) for t in qkv.split([Hq, Hkv, Hkv], 2))
+    buf = torch.zeros(B, Hq, N, D + 16, dtype=torch.bfloat16, device="cuda")
+    o, lse = va.window_attn(q, k, v, 40, 2, True, scale=0.3, out=buf[..., 8:8 + D], return_lse=True)
+    torch.cuda.synchronize()
+    ref.check(o, lse, ref.window_attn(q, k, v, 40, 2, True, scale=0.3))
+    assert (buf[..., :8] == 0).all() and (buf[..., 8 + D:] == 0).all()
+    o2 = va.window_attn(q.contiguous(), k.contiguous(), v.contiguous(), 40, 2, True, scale=0.3)
+    assert torch.equal(o, o2)
+
+
+@pytest.mark.parametrize("what", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+def test_hidden_keys_never_reach_a_row(gpu, D, causal, what):
+    """A NaN or infinity in a key's row changes only the rows that see it."""
+    N, window, sinks, at = 300, 40, 2, 150
+    q, k, v = case(11, 1, 2, 1, N, N, D)
+    clean = va.window_attn(q, k, v, window, sinks, causal)
+    x = float(what)
+    v[:, :, at, 5] = x
+    o = va.window_attn(q, k, v, window, sinks, causal).float()
+    mask = ref.sees(torch.arange(N), torch.arange(N), window, sinks, causal, N)[:, at].cuda()
+    assert torch.equal(o[:, :, ~mask], clean.float()[:, :, ~mask])
+    hit = o[:, :, mask, 5]
+    assert (hit.isnan() if what == "nan" else hit == x).all()
+    other = torch.arange(D) != 5
+    assert torch.equal(o[:, :, mask][..., other], clean.float()[:, :, mask][..., other])
+    v[:, :, at, 5] = 0
+    k[:, :, at, 3] = x
+    o = va.window_attn(q, k, v, window, sinks, causal)
+    assert o[:, :, ~mask].isfinite().all()
+    k[:, :, at, 3] = 0
+    again = va.window_attn(q, k, v, window, sinks, causal)
+    assert torch.equal(o[:, :, ~mask], again[:, :, ~mask])
+
+
+def test_large_scores(gpu):
+    """References move by hundreds along a row; no weight overflows."""
+    q, k, v = case(21, 1, 2, 2, 400, 400, 128)
+    k *= torch.linspace(0.1, 30, 400, device="cuda").bfloat16()[None, None, :, None]
+    for order in (k, k.flip(2)):
+        o, lse = va.window_attn(q, order.contiguous(), v, 300, 1, False, return_lse=True)
+        ref.check(o, lse, ref.window_attn(q, order, v, 300, 1, False))
+
+
+def test_everything_matches_sparse_attention_of_all_keys(gpu):
+    """A window that hides nothing is causal dense attention: vector-sparse attention with every
+    key listed, within both kernels' bounds."""
+    q, k, v = case(31, 1, 4, 2, 320, 320, 64)
+    idx, cnt = va.select(q, k, 64, "topk", 1.0, True)
+    a, la = va.sparse_attn(q, k, v, idx, cnt, 64, True, return_lse=True)
+    o, lse = va.window_attn(q, k, v, 320, 0, True, return_lse=True)
+    r = ref.window_attn(q, k, v, 320, 0, True)
+    ref.check(o, lse, r)
+    assert ((a.double() - o.double()).abs().cpu() <= 2 * r[2]).all()
+    assert ((la.double() - lse.double()).abs().cpu() <= 2 * r[3]).all()
+
+
+def test_other_stream_and_replayed_graph(gpu):
+    q, k, v = case(41, 2, 4, 2, 200, 200, 128)
+    lens = torch.tensor([200, 77], dtype=torch.int32, device="cuda")
+    want = va.window_attn(q, k, v, 30, 2, True, lens=lens)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        o = va.window_attn(q, k, v, 30, 2, True, lens=lens)
+    side.synchronize()
+    assert torch.equal(o, want)
+    out = torch.zeros_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        va.window_attn(q, k, v, 30, 2, True, lens=lens, out=out)
+    for step, ln in enumerate(([200, 77], [1, 200], [150, 0])):
+        lens.copy_(torch.tensor(ln, dtype=torch.int32))
+        q.copy_(rows(90 + step, 2, 4, 200, 128))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, va.window_attn(q, k, v, 30, 2, True, lens=lens))
+
+
+def test_long_rows_past_32_bit_offsets(gpu):
+    """Keys whose rows span more than 2^32 bytes (one head of a wide token-major buffer)."""
+    N, D, W = 70000, 64, 1 << 15   # 70000 * 65536 bytes
+    buf = torch.empty(N * W, dtype=torch.bfloat16, device="cuda")
+    wide = buf.view(1, N, W // D, D).transpose(1, 2)
+    k, v = wide[:, 3:4], wide[:, W // D - 1:]
+    k.copy_(rows(51, 1, 1, N, D))
+    v.copy_(rows(52, 1, 1, N, D))
+    q = rows(53, 1, 2, 150, D, 1.5)
+    o, lse = va.window_attn(q, k, v, 333, 9, True, return_lse=True)
+    near = torch.cat([torch.arange(9), torch.arange(N - 150 - 333, N)])
+    # the same keys packed: the first 9, then all that some row's window holds
+    kk, vv = k[:, :, near].contiguous(), v[:, :, near].contiguous()
+    r = ref.window_attn(q, kk, vv, 333, 9, True)
+    ref.check(o, lse, r)
