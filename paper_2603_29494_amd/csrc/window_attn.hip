@@ -121,47 +121,52 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       voff[db][hi] = k0 * RB + 16 * ((d >> 3) ^ swz<D>(k0)) + 8 * ((d >> 2) & 1);
     }
 
-  auto step = [&](int j0, int st) __attribute__((always_inline)) {
-    // What the wave's rows see of keys j0 .. j0 + 63: nothing, all, or a part.
+  // This lane's row sees the keys in (v_lo, v_hi] and those up to v_first.
+  const int v_lo = my_pos - a.window;
+  const int v_hi = min(len - 1, a.causal ? my_pos : my_pos + a.window - 1);
+  const int v_first = min(a.causal ? min(a.sinks - 1, my_pos) : a.sinks - 1, len - 1);
+  // What the wave's rows see of keys j0 .. j0 + 63: nothing, all, or a part.
+  auto none = [&](int j0) __attribute__((always_inline)) {
     const bool in_sinks = j0 < a.sinks && !(a.causal && j0 > w_hi);
     const bool in_near = j0 + kTile - 1 > w_lo - a.window &&
                          (a.causal ? j0 <= w_hi : j0 < w_hi + a.window);
-    if (w_hi < w_lo || !(in_sinks || in_near)) return;
-    const bool whole =
-        j0 + kTile <= len && (!a.causal || j0 + kTile - 1 <= w_lo) &&
-        (j0 + kTile <= a.sinks ||
-         (j0 > w_hi - a.window && (a.causal || j0 + kTile - 1 < w_lo + a.window)));
+    return w_hi < w_lo || !(in_sinks || in_near);
+  };
+  auto whole = [&](int j0) __attribute__((always_inline)) {
+    return j0 + kTile <= len && (!a.causal || j0 + kTile - 1 <= w_lo) &&
+           (j0 + kTile <= a.sinks ||
+            (j0 > w_hi - a.window && (a.causal || j0 + kTile - 1 < w_lo + a.window)));
+  };
+  auto scores = [&](f32x16 (&s)[2], int st) __attribute__((always_inline)) {
     const char* kb = reinterpret_cast<const char*>(kbuf(st));
-    const char* vb = reinterpret_cast<const char*>(vbuf(st));
-    f32x16 s[2];
 #pragma unroll
-    for (int kh2 = 0; kh2 < 2; ++kh2) {
-      s[kh2] = f32x16{};
+    for (int hf = 0; hf < 2; ++hf) {
+      s[hf] = f32x16{};
 #pragma unroll
       for (int s2 = 0; s2 < DS; ++s2) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + koff[s2] + kh2 * 32 * RB);
-        s[kh2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[s2],
-                                                         s[kh2], 0, 0, 0);
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + koff[s2] + hf * 32 * RB);
+        s[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[s2],
+                                                        s[hf], 0, 0, 0);
       }
     }
-    auto sees = [&](int j) __attribute__((always_inline)) {
-      const bool nr = j > my_pos - a.window && (a.causal || j < my_pos + a.window);
-      return j < len && (nr || j < a.sinks) && (!a.causal || j <= my_pos);
-    };
-    if (!whole) {
+  };
+  auto mask = [&](f32x16 (&s)[2], int j0) __attribute__((always_inline)) {
+    const int lo = v_lo - j0 - 4 * g, hi = v_hi - j0 - 4 * g, first = v_first - j0 - 4 * g;
 #pragma unroll
-      for (int kh2 = 0; kh2 < 2; ++kh2)
+    for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + 32 * kh2 + 8 * (e / 4) + 4 * g + e % 4;
-          s[kh2][e] = sees(j) ? s[kh2][e] : kNegInf;
-        }
-    }
+      for (int e = 0; e < 16; ++e) {
+        const int j = 32 * hf + 8 * (e / 4) + e % 4;
+        s[hf][e] = (j > lo && j <= hi) || j <= first ? s[hf][e] : kNegInf;
+      }
+  };
+  // A row's reference moves when its maximum has grown by more than 8 (log2 units).
+  auto refer = [&](const f32x16 (&s)[2]) __attribute__((always_inline)) {
     float top = kNegInf;
 #pragma unroll
-    for (int kh2 = 0; kh2 < 2; ++kh2)
+    for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kh2][e]);
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[hf][e]);
     top = wave_max_xor32(top) * a.scale_log2;
     if (__any(top > m_run + 8.0f)) {
       const float m_new = top > m_run + 8.0f ? top : m_run;
@@ -171,69 +176,42 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
     }
-    auto vread = [&](int ks, int db) __attribute__((always_inline)) {
-      const char* a0 = vb + voff[db][0] + 16 * ks * RB;
-      const char* a1 = vb + voff[db][1] + 16 * ks * RB;
-      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a0));
-      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a1));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    // In a tile that is not seen whole, a NaN or an infinity of a V row must not
-    // reach the rows that do not see it through 0 * NaN: such values are taken out
-    // of the product and added to the rows that see them.
-    bool odd = false;
-    if (!whole) {
-      uint32_t hot = 0;
+  };
+  auto vread = [&](int ks, int db, int st) __attribute__((always_inline)) {
+    const char* vb = reinterpret_cast<const char*>(vbuf(st));
+    const char* a0 = vb + voff[db][0] + 16 * ks * RB;  // the swizzle repeats every 16 rows
+    const char* a1 = vb + voff[db][1] + 16 * ks * RB;
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a0));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a1));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto weights = [&](const f32x16 (&s)[2], int ks) __attribute__((always_inline)) {
+    f32x8 p;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const i16x8 x = vread(ks, db);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            hot |= (static_cast<uint16_t>(x[e]) & 0x7F80u) == 0x7F80u ? 1u : 0u;
-        }
-      odd = __any(hot != 0);
-    }
+    for (int e = 0; e < 8; ++e)
+      p[e] = __builtin_amdgcn_exp2f(
+          __builtin_fmaf(s[ks >> 1][8 * (ks & 1) + e], a.scale_log2, -m_run));
+    l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    return __builtin_convertvector(p, bf16x8);
+  };
+  auto step = [&](int j0, int st) __attribute__((always_inline)) {
+    if (none(j0)) return;
+    f32x16 s[2];
+    scores(s, st);
+    if (!whole(j0)) mask(s, j0);
+    refer(s);
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      f32x8 p;
+      const bf16x8 pb = weights(s, ks);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(s[ks >> 1][8 * (ks & 1) + e], a.scale_log2, -m_run));
-        l_run += p[e];
-      }
-      const bf16x8 pb = __builtin_convertvector(p, bf16x8);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        i16x8 x = vread(ks, db);
-        if (odd) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            x[e] = (static_cast<uint16_t>(x[e]) & 0x7F80u) == 0x7F80u ? short(0) : x[e];
-        }
-        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb,
-                                                           oacc[db], 0, 0, 0);
-      }
-    }
-    if (odd) {
-      for (int j = 0; j < kTile; ++j) {
-        if (!sees(j0 + j)) continue;
-        const char* row = vb + j * RB;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int d = 32 * db + 8 * (e / 4) + 4 * g + e % 4;
-            const uint16_t x = *reinterpret_cast<const uint16_t*>(
-                row + 16 * ((d >> 3) ^ swz<D>(j)) + 2 * (d & 7));
-            if ((x & 0x7F80u) == 0x7F80u) oacc[db][e] += bf16_bits_to_f32(x);
-          }
-      }
+      for (int db = 0; db < DB; ++db)
+        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, vread(ks, db, st)), pb, oacc[db], 0, 0, 0);
     }
   };
 
+  __shared__ int s_redo;
+  if (tid == 0) s_redo = 0;
   gather(tile_key(0), 0);
   for (int t = 0; t < ntiles; t += 2) {
     wait_all();
@@ -245,6 +223,66 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     __builtin_amdgcn_s_barrier();
     if (t + 2 < ntiles) gather(tile_key(t + 2), 0);
     step(tile_key(t + 1), 1);
+  }
+
+  // A NaN or an infinity of a V row reaches rows of its tile that do not see it
+  // (0 * NaN in the product).  So a workgroup with anything not finite walks its
+  // tiles again, with such values taken out of the products and added to the rows
+  // that see them.
+  float fin = 0.0f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) fin = __builtin_fmaf(oacc[db][e], 0.0f, fin);
+  __syncthreads();
+  if (__any(have && fin != 0.0f) && lane == 0) s_redo = 1;
+  __syncthreads();
+  if (__builtin_amdgcn_readfirstlane(s_redo)) {
+    auto not_finite = [](uint16_t x) __attribute__((always_inline)) {
+      return (x & 0x7F80u) == 0x7F80u;
+    };
+    m_run = kUnseen;
+    l_run = 0.0f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+    for (int t = 0; t < ntiles; ++t) {
+      const int j0 = tile_key(t);
+      __syncthreads();
+      gather(j0, 0);
+      wait_all();
+      __syncthreads();
+      if (none(j0)) continue;
+      f32x16 s[2];
+      scores(s, 0);
+      mask(s, j0);
+      refer(s);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        const bf16x8 pb = weights(s, ks);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          i16x8 x = vread(ks, db, 0);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = not_finite(x[e]) ? short(0) : x[e];
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb,
+                                                             oacc[db], 0, 0, 0);
+        }
+      }
+#pragma unroll 1
+      for (int j = 0; j < kTile; ++j) {
+        if (!((j0 + j > v_lo && j0 + j <= v_hi) || j0 + j <= v_first)) continue;
+        const char* row = reinterpret_cast<const char*>(v_s0) + j * RB;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int d = 32 * db + 8 * (e / 4) + 4 * g + e % 4;
+            const uint16_t x = *reinterpret_cast<const uint16_t*>(
+                row + 16 * ((d >> 3) ^ swz<D>(j)) + 2 * (d & 7));
+            if (not_finite(x)) oacc[db][e] += bf16_bits_to_f32(x);
+          }
+      }
+    }
   }
 
   l_run += __shfl_xor(l_run, 32);
