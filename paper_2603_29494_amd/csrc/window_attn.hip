@@ -11,6 +11,7 @@
 // the softmax state in registers.  Only tiles that some row of a wave does not
 // see whole are masked, and tiles that none of its rows sees are skipped by it.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.h"
 #include "launch.h"
@@ -71,20 +72,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const uint16_t* vh = a.v + b * a.v_sB + hk * a.v_sH;
   const uint32_t k_rowb = static_cast<uint32_t>(a.k_sN) * 2u;
   const uint32_t v_rowb = static_cast<uint32_t>(a.v_sN) * 2u;
-  // The tile's rows as buffer resources (rows at or past len read 0).
-  auto gather = [&](int j0, int st) __attribute__((always_inline)) {
-    const int rows = min(kTile, len - j0);
-    const __amdgpu_buffer_rsrc_t krs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t*>(kh + j0 * a.k_sN), 0, (rows - 1) * k_rowb + RB, 0x00020000);
-    const __amdgpu_buffer_rsrc_t vrs = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint16_t*>(vh + j0 * a.v_sN), 0, (rows - 1) * v_rowb + RB, 0x00020000);
+  // The tile's rows through a buffer resource of their own (rows at or past len
+  // read 0).
+  auto gather = [&](const uint16_t* base, int64_t sN, uint32_t rowb, int j0, uint16_t* dst)
+                    __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint16_t*>(base + j0 * sN), 0, (min(kTile, len - j0) - 1) * rowb + RB,
+        0x00020000);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = (wave * U + u) * 64 + lane, r = i / CH;
-      const uint32_t c = 16u * ((i % CH) ^ swz<D>(r));
-      gather16_to_lds(krs, r * k_rowb + c, kbuf(st) + (wave * U + u) * 64 * 8);
-      gather16_to_lds(vrs, r * v_rowb + c, vbuf(st) + (wave * U + u) * 64 * 8);
+      gather16_to_lds(rs, r * rowb + 16u * ((i % CH) ^ swz<D>(r)), dst + (wave * U + u) * 64 * 8);
     }
+  };
+  auto gather_k = [&](int j0, int st) __attribute__((always_inline)) {
+    gather(kh, a.k_sN, k_rowb, j0, kbuf(st));
+  };
+  auto gather_v = [&](int j0, int st) __attribute__((always_inline)) {
+    gather(vh, a.v_sN, v_rowb, j0, vbuf(st));
   };
 
   const int my_row = row0 + 32 * wave + ln;
@@ -125,29 +130,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int v_lo = my_pos - a.window;
   const int v_hi = min(len - 1, a.causal ? my_pos : my_pos + a.window - 1);
   const int v_first = min(a.causal ? min(a.sinks - 1, my_pos) : a.sinks - 1, len - 1);
-  // What the wave's rows see of keys j0 .. j0 + 63: nothing, all, or a part.
-  auto none = [&](int j0) __attribute__((always_inline)) {
-    const bool in_sinks = j0 < a.sinks && !(a.causal && j0 > w_hi);
-    const bool in_near = j0 + kTile - 1 > w_lo - a.window &&
-                         (a.causal ? j0 <= w_hi : j0 < w_hi + a.window);
-    return w_hi < w_lo || !(in_sinks || in_near);
-  };
+  // Every row of the wave sees keys j0 .. j0 + 63.
   auto whole = [&](int j0) __attribute__((always_inline)) {
     return j0 + kTile <= len && (!a.causal || j0 + kTile - 1 <= w_lo) &&
            (j0 + kTile <= a.sinks ||
             (j0 > w_hi - a.window && (a.causal || j0 + kTile - 1 < w_lo + a.window)));
   };
-  auto scores = [&](f32x16 (&s)[2], int st) __attribute__((always_inline)) {
-    const char* kb = reinterpret_cast<const char*>(kbuf(st));
+  // S^T of keys 32 hf .. + 31 of the tile in stage st.
+  auto score = [&](f32x16& s, int st, int hf) __attribute__((always_inline)) {
+    const char* kb = reinterpret_cast<const char*>(kbuf(st)) + hf * 32 * RB;
+    s = f32x16{};
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      s[hf] = f32x16{};
-#pragma unroll
-      for (int s2 = 0; s2 < DS; ++s2) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + koff[s2] + hf * 32 * RB);
-        s[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[s2],
-                                                        s[hf], 0, 0, 0);
-      }
+    for (int s2 = 0; s2 < DS; ++s2) {
+      const u32x4 kf = *reinterpret_cast<const u32x4*>(kb + koff[s2]);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), qf[s2], s, 0, 0,
+                                                  0);
     }
   };
   auto mask = [&](f32x16 (&s)[2], int j0) __attribute__((always_inline)) {
@@ -161,15 +158,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       }
   };
   // A row's reference moves when its maximum has grown by more than 8 (log2 units).
-  auto refer = [&](const f32x16 (&s)[2]) __attribute__((always_inline)) {
+  auto refer = [&](const f32x16 (&s)[2], bool mine) __attribute__((always_inline)) {
     float top = kNegInf;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[hf][e]);
     top = wave_max_xor32(top) * a.scale_log2;
-    if (__any(top > m_run + 8.0f)) {
-      const float m_new = top > m_run + 8.0f ? top : m_run;
+    const bool up = mine && top > m_run + 8.0f;
+    if (__any(up)) {
+      const float m_new = up ? top : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
       l_run *= alpha;
@@ -185,51 +183,109 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, a1));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto weights = [&](const f32x16 (&s)[2], int ks) __attribute__((always_inline)) {
+  // Weights above 256 went into O and l as they are; the row's reference moves up by
+  // a power of two for the tiles to come.  A weight past fp32 range leaves O or l
+  // infinite, which the end of the walk sees.
+  auto move = [&](float tsum) __attribute__((always_inline)) {
+    if (__any(tsum > 256.0f)) {
+      const float top = wave_max_xor32(tsum);
+      const int up = top > 256.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
+      const float alpha = __builtin_amdgcn_ldexpf(1.0f, -up);
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      m_run += static_cast<float>(up);
+    }
+  };
+  // The weights of keys 16 ks .. + 15 of a tile, and their sum.
+  auto weigh = [&](const f32x16 (&s)[2], int ks, float& sum) __attribute__((always_inline)) {
     f32x8 p;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       p[e] = __builtin_amdgcn_exp2f(
           __builtin_fmaf(s[ks >> 1][8 * (ks & 1) + e], a.scale_log2, -m_run));
-    l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     return __builtin_convertvector(p, bf16x8);
   };
-  auto step = [&](int j0, int st) __attribute__((always_inline)) {
-    if (none(j0)) return;
-    f32x16 s[2];
-    scores(s, st);
-    if (!whole(j0)) mask(s, j0);
-    refer(s);
-#pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const bf16x8 pb = weights(s, ks);
+  // One step: the scores of tile t + 1 (K of stage st ^ 1) while tile t (scores cur,
+  // V of stage st) is weighed and multiplied, so that the matrix instructions of
+  // one run beside the exponentials of the other.
+  auto step = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], int st, auto more_tag)
+                  __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more_tag)::value;
+    float sum[4];
+    bf16x8 pb[4];
+    auto product = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
       for (int db = 0; db < DB; ++db)
         oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, vread(ks, db, st)), pb, oacc[db], 0, 0, 0);
+            __builtin_bit_cast(bf16x8, vread(ks, db, st)), pb[ks], oacc[db], 0, 0, 0);
+    };
+    if constexpr (MORE) score(nxt[0], st ^ 1, 0);
+    pb[0] = weigh(cur, 0, sum[0]);
+    if constexpr (MORE) score(nxt[1], st ^ 1, 1);
+    pb[1] = weigh(cur, 1, sum[1]);
+    product(0);
+    pb[2] = weigh(cur, 2, sum[2]);
+    product(1);
+    pb[3] = weigh(cur, 3, sum[3]);
+    product(2);
+    product(3);
+    const float tsum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    l_run += tsum;
+    move(tsum);
+  };
+  int settled = 0;   // every row of the wave has a reference
+  auto ready = [&](f32x16 (&s)[2], int j0) __attribute__((always_inline)) {
+    if (!whole(j0)) mask(s, j0);
+    if (!settled) {
+      refer(s, true);
+      settled = __builtin_amdgcn_readfirstlane(!__any(m_run == kUnseen));
     }
   };
 
   __shared__ int s_redo;
   if (tid == 0) s_redo = 0;
-  gather(tile_key(0), 0);
-  for (int t = 0; t < ntiles; t += 2) {
+  // K runs one tile ahead of V.
+  f32x16 sa[2], sb[2];
+  gather_k(tile_key(0), 0);
+  gather_v(tile_key(0), 0);
+  wait_all();
+  __builtin_amdgcn_s_barrier();
+  if (ntiles > 1) gather_k(tile_key(1), 1);
+  score(sa[0], 0, 0);
+  score(sa[1], 0, 1);
+  ready(sa, tile_key(0));
+  int t = 0;
+  auto turn = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], int st) __attribute__((always_inline)) {
     wait_all();
     __builtin_amdgcn_s_barrier();
-    if (t + 1 < ntiles) gather(tile_key(t + 1), 1);
-    step(tile_key(t), 0);
-    if (t + 1 >= ntiles) break;
+    if (t + 2 < ntiles) gather_k(tile_key(t + 2), st);
+    gather_v(tile_key(t + 1), st ^ 1);
+    step(cur, nxt, st, std::true_type{});
+    ready(nxt, tile_key(t + 1));
+    ++t;
+  };
+  while (t + 2 < ntiles) {
+    turn(sa, sb, 0);
+    turn(sb, sa, 1);
+  }
+  if (t + 1 < ntiles) {
+    turn(sa, sb, 0);
     wait_all();
     __builtin_amdgcn_s_barrier();
-    if (t + 2 < ntiles) gather(tile_key(t + 2), 0);
-    step(tile_key(t + 1), 1);
+    step(sb, sa, 1, std::false_type{});
+  } else {
+    wait_all();
+    __builtin_amdgcn_s_barrier();
+    step(sa, sb, 0, std::false_type{});
   }
 
   // A NaN or an infinity of a V row reaches rows of its tile that do not see it
   // (0 * NaN in the product).  So a workgroup with anything not finite walks its
   // tiles again, with such values taken out of the products and added to the rows
   // that see them.
-  float fin = 0.0f;
+  float fin = l_run * 0.0f;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -243,28 +299,44 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     };
     m_run = kUnseen;
     l_run = 0.0f;
+    settled = 0;
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-    for (int t = 0; t < ntiles; ++t) {
+    for (t = 0; t < ntiles; ++t) {
       const int j0 = tile_key(t);
       __syncthreads();
-      gather(j0, 0);
+      gather_k(j0, 0);
+      gather_v(j0, 0);
       wait_all();
       __syncthreads();
-      if (none(j0)) continue;
       f32x16 s[2];
-      scores(s, 0);
-      mask(s, j0);
-      refer(s);
+      score(s[0], 0, 0);
+      score(s[1], 0, 1);
+      ready(s, j0);
+      // A row with weights near the end of fp32 range takes its reference from the
+      // tile first; the others go as before, to the same bits.
+      float sum[4];
+      bf16x8 pb[4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) pb[ks] = weigh(s, ks, sum[ks]);
+      float tsum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      const int far_up = !(tsum <= 1e30f);
+      const bool over = (far_up | __shfl_xor(far_up, 32)) != 0;
+      if (__any(over)) {
+        refer(s, over);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) pb[ks] = weigh(s, ks, sum[ks]);
+        tsum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+      l_run += tsum;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
-        const bf16x8 pb = weights(s, ks);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           i16x8 x = vread(ks, db, 0);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = not_finite(x[e]) ? short(0) : x[e];
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb,
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb[ks],
                                                              oacc[db], 0, 0, 0);
         }
       }
@@ -282,6 +354,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             if (not_finite(x)) oacc[db][e] += bf16_bits_to_f32(x);
           }
       }
+      move(tsum);
     }
   }
 
