@@ -30,7 +30,8 @@ struct WindowParams {
   int64_t o_sB, o_sH, o_sN;
   float* lse;
   const int32_t* lens;
-  int32_t Hq, group, Nq, Nk, window, sinks, causal, row_tiles;
+  int32_t Hq, Hkv, group, Nq, Nk, window, sinks, causal, row_tiles, run;
+  int64_t items;
   float scale_log2;
 };
 
@@ -49,8 +50,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rt = blockIdx.x;
-  const int h = blockIdx.y, b = blockIdx.z, hk = h / a.group;
+  // Work item: batch and key/value head, then row tile, then the query heads that
+  // share them.  The hardware deals workgroup x to XCD x % 8; an XCD takes `run`
+  // consecutive items at a time, whose windows overlap, so that it finds most of
+  // their keys in its own L2.
+  const int64_t slot = blockIdx.x >> 3;
+  int64_t item = (slot / a.run * 8 + (blockIdx.x & 7)) * a.run + slot % a.run;
+  if (item >= a.items) return;
+  const int hg = static_cast<int>(item % a.group);
+  item /= a.group;
+  const int rt = static_cast<int>(item % a.row_tiles);
+  item /= a.row_tiles;
+  const int hk = static_cast<int>(item % a.Hkv), h = hk * a.group + hg;
+  const int64_t b = item / a.Hkv;
   const int off = a.Nk - a.Nq;                       // position of row 0
   const int len = a.lens ? min(max(a.lens[b], 0), a.Nk) : a.Nk;
   const int rows_end = min(a.Nq, len - off);         // rows past it are padding
@@ -72,24 +84,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const uint16_t* vh = a.v + b * a.v_sB + hk * a.v_sH;
   const uint32_t k_rowb = static_cast<uint32_t>(a.k_sN) * 2u;
   const uint32_t v_rowb = static_cast<uint32_t>(a.v_sN) * 2u;
-  // The tile's rows through a buffer resource of their own (rows at or past len
-  // read 0).
-  auto gather = [&](const uint16_t* base, int64_t sN, uint32_t rowb, int j0, uint16_t* dst)
+  // Direct-load instruction u of this wave for the tile at key j0, through a buffer
+  // resource of the tile's own (rows at or past len read 0).
+  auto gather = [&](const uint16_t* base, int64_t sN, uint32_t rowb, int j0, int u, uint16_t* dst)
                     __attribute__((always_inline)) {
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         const_cast<uint16_t*>(base + j0 * sN), 0, (min(kTile, len - j0) - 1) * rowb + RB,
         0x00020000);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = (wave * U + u) * 64 + lane, r = i / CH;
-      gather16_to_lds(rs, r * rowb + 16u * ((i % CH) ^ swz<D>(r)), dst + (wave * U + u) * 64 * 8);
-    }
+    const int i = (wave * U + u) * 64 + lane, r = i / CH;
+    gather16_to_lds(rs, r * rowb + 16u * ((i % CH) ^ swz<D>(r)), dst + (wave * U + u) * 64 * 8);
   };
-  auto gather_k = [&](int j0, int st) __attribute__((always_inline)) {
-    gather(kh, a.k_sN, k_rowb, j0, kbuf(st));
+  auto gather_k = [&](int j0, int u, int st) __attribute__((always_inline)) {
+    gather(kh, a.k_sN, k_rowb, j0, u, kbuf(st));
   };
-  auto gather_v = [&](int j0, int st) __attribute__((always_inline)) {
-    gather(vh, a.v_sN, v_rowb, j0, vbuf(st));
+  auto gather_v = [&](int j0, int u, int st) __attribute__((always_inline)) {
+    gather(vh, a.v_sN, v_rowb, j0, u, vbuf(st));
   };
 
   const int my_row = row0 + 32 * wave + ln;
@@ -208,29 +217,65 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     return __builtin_convertvector(p, bf16x8);
   };
   // One step: the scores of tile t + 1 (K of stage st ^ 1) while tile t (scores cur,
-  // V of stage st) is weighed and multiplied, so that the matrix instructions of
-  // one run beside the exponentials of the other.
-  auto step = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], int st, auto more_tag)
+  // V of stage st) is weighed and multiplied, so that matrix instructions run beside
+  // exponentials.  The order is fixed: between two matrix instructions one operand
+  // read kAhead instructions ahead of its use, one weight (two where the product
+  // waits for them) and, in the first half, one of the gathers.
+  auto step = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], int st, auto more_tag, auto&& fetch)
                   __attribute__((always_inline)) {
     constexpr bool MORE = decltype(more_tag)::value;
+    constexpr int NS = MORE ? 2 * DS : 0, NP = 4 * DB;   // matrix instructions of either kind
+    constexpr int kAhead = 4;
+    i16x8 ring[kAhead];
+    f32x8 p[4];
     float sum[4];
     bf16x8 pb[4];
-    auto product = [&](int ks) __attribute__((always_inline)) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8, vread(ks, db, st)), pb[ks], oacc[db], 0, 0, 0);
+    auto read = [&](int i) __attribute__((always_inline)) {   // operand of instruction i
+      if (i < NS) {
+        const char* kb = reinterpret_cast<const char*>(kbuf(st ^ 1)) + i / DS * 32 * RB;
+        ring[i % kAhead] = *reinterpret_cast<const i16x8*>(kb + koff[i % DS]);
+      } else if (i < NS + NP) {
+        ring[i % kAhead] = vread((i - NS) / DB, (i - NS) % DB, st);
+      }
     };
-    if constexpr (MORE) score(nxt[0], st ^ 1, 0);
-    pb[0] = weigh(cur, 0, sum[0]);
-    if constexpr (MORE) score(nxt[1], st ^ 1, 1);
-    pb[1] = weigh(cur, 1, sum[1]);
-    product(0);
-    pb[2] = weigh(cur, 2, sum[2]);
-    product(1);
-    pb[3] = weigh(cur, 3, sum[3]);
-    product(2);
-    product(3);
+    auto weight = [&](int e) __attribute__((always_inline)) {   // of element e of 32
+      if (e >= 32) return;
+      const int ks = e / 8;
+      p[ks][e % 8] =
+          __builtin_amdgcn_exp2f(__builtin_fmaf(cur[e / 16][e % 16], a.scale_log2, -m_run));
+      if (e % 8 == 7) {
+        sum[ks] = ((p[ks][0] + p[ks][1]) + (p[ks][2] + p[ks][3])) +
+                  ((p[ks][4] + p[ks][5]) + (p[ks][6] + p[ks][7]));
+        pb[ks] = __builtin_convertvector(p[ks], bf16x8);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) read(i);
+    if constexpr (!MORE) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) weight(e);
+    }
+    if constexpr (MORE) nxt[0] = nxt[1] = f32x16{};
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      nxt[i / DS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8, ring[i % kAhead]), qf[i % DS], nxt[i / DS], 0, 0, 0);
+      read(i + kAhead);
+      fetch(i);
+#pragma unroll
+      for (int x = 0; x < 16 / NS; ++x) weight(16 / NS * i + x);
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      oacc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8, ring[(NS + i) % kAhead]), pb[i / DB], oacc[i % DB], 0, 0, 0);
+      read(NS + i + kAhead);
+#pragma unroll
+      for (int x = 0; x < 32 / NP; ++x) weight(16 + 32 / NP * i + x);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     const float tsum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     l_run += tsum;
     move(tsum);
@@ -248,11 +293,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (tid == 0) s_redo = 0;
   // K runs one tile ahead of V.
   f32x16 sa[2], sb[2];
-  gather_k(tile_key(0), 0);
-  gather_v(tile_key(0), 0);
+#pragma unroll
+  for (int u = 0; u < U; ++u) gather_k(tile_key(0), u, 0);
+#pragma unroll
+  for (int u = 0; u < U; ++u) gather_v(tile_key(0), u, 0);
   wait_all();
   __builtin_amdgcn_s_barrier();
-  if (ntiles > 1) gather_k(tile_key(1), 1);
+  if (ntiles > 1) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) gather_k(tile_key(1), u, 1);
+  }
   score(sa[0], 0, 0);
   score(sa[1], 0, 1);
   ready(sa, tile_key(0));
@@ -260,9 +310,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   auto turn = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], int st) __attribute__((always_inline)) {
     wait_all();
     __builtin_amdgcn_s_barrier();
-    if (t + 2 < ntiles) gather_k(tile_key(t + 2), st);
-    gather_v(tile_key(t + 1), st ^ 1);
-    step(cur, nxt, st, std::true_type{});
+    // Past the last tile K is fetched once more (into a buffer nothing reads).
+    const int jk = tile_key(min(t + 2, ntiles - 1)), jv = tile_key(t + 1);
+    step(cur, nxt, st, std::true_type{}, [&](int i) __attribute__((always_inline)) {
+      if (i < U) gather_v(jv, i, st ^ 1);
+      else if (i < 2 * U) gather_k(jk, i - U, st);
+    });
     ready(nxt, tile_key(t + 1));
     ++t;
   };
@@ -274,11 +327,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     turn(sa, sb, 0);
     wait_all();
     __builtin_amdgcn_s_barrier();
-    step(sb, sa, 1, std::false_type{});
+    step(sb, sa, 1, std::false_type{}, [](int) {});
   } else {
     wait_all();
     __builtin_amdgcn_s_barrier();
-    step(sa, sb, 0, std::false_type{});
+    step(sa, sb, 0, std::false_type{}, [](int) {});
   }
 
   // A NaN or an infinity of a V row reaches rows of its tile that do not see it
@@ -305,8 +358,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (t = 0; t < ntiles; ++t) {
       const int j0 = tile_key(t);
       __syncthreads();
-      gather_k(j0, 0);
-      gather_v(j0, 0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        gather_k(j0, u, 0);
+        gather_v(j0, u, 0);
+      }
       wait_all();
       __syncthreads();
       f32x16 s[2];
@@ -362,7 +418,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (!have) return;
   const float inv = 1.0f / l_run;   // a row sees its own key at least
   if (a.lse && g == 0)
-    a.lse[(static_cast<int64_t>(b) * a.Hq + h) * a.Nq + my_row] =
+    a.lse[(b * a.Hq + h) * a.Nq + my_row] =
         (m_run + __builtin_log2f(l_run)) * 0.69314718055994531f;
   uint16_t* orow = a.o + b * a.o_sB + h * a.o_sH + static_cast<int64_t>(my_row) * a.o_sN;
 #pragma unroll
@@ -391,7 +447,8 @@ hipError_t launch_window_attn(const WindowArgs& x, hipStream_t stream) {
   a.lse = x.lse;
   a.lens = x.lens;
   a.Hq = static_cast<int32_t>(x.q.H);
-  a.group = static_cast<int32_t>(x.q.H / x.k.H);
+  a.Hkv = static_cast<int32_t>(x.k.H);
+  a.group = a.Hq / a.Hkv;
   a.Nq = static_cast<int32_t>(x.q.N);
   a.Nk = static_cast<int32_t>(x.k.N);
   // A window or sinks past the keys is all of them (and keeps the positions'
@@ -402,8 +459,12 @@ hipError_t launch_window_attn(const WindowArgs& x, hipStream_t stream) {
   a.row_tiles = static_cast<int32_t>((x.q.N + kRows - 1) / kRows);
   const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(x.q.D));
   a.scale_log2 = scale * 1.4426950408889634f;
-  const dim3 grid(static_cast<unsigned>(a.row_tiles), static_cast<unsigned>(x.q.H),
-                  static_cast<unsigned>(x.q.B));
+  a.items = x.q.B * a.Hq * static_cast<int64_t>(a.row_tiles);
+  // Runs of the 64 workgroups that an XCD holds at a time, shorter ones where that
+  // would leave an XCD fewer than four.
+  a.run = static_cast<int32_t>(std::min<int64_t>(64, std::max<int64_t>(1, a.items / 32)));
+  const int64_t rounds = (a.items + 8 * a.run - 1) / (8 * a.run);
+  const dim3 grid(static_cast<unsigned>(rounds * 8 * a.run));
   if (x.q.D == 128) hipLaunchKernelGGL(k_window_attn<128>, grid, dim3(256), 0, stream, a);
   else hipLaunchKernelGGL(k_window_attn<64>, grid, dim3(256), 0, stream, a);
   return hipGetLastError();
