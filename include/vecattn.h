@@ -427,8 +427,8 @@ vecattn_status vecattn_recall(const void* q, const vecattn_tdesc* qd, const void
  * A key outside a row's V(p) never reaches that row, whatever it holds.
  * Errors: INVALID_ARG (null pointer, shape mismatch, Nq > Nk, window < 1, sinks
  * < 0, bad scale or bits, misalignment); UNSUPPORTED (D not in {64, 128}, more
- * than 65535 sequences or query heads, a K or V row stride of 2^24 elements or
- * more).
+ * than 65535 sequences or query heads or 2^23 tiles of 128 rows in all, a K or V
+ * row stride of 2^24 elements or more).
  */
 vecattn_status vecattn_window_attn(const void* q, const vecattn_tdesc* qd, const void* k,
                                    const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,

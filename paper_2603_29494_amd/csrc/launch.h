@@ -119,6 +119,7 @@ hipError_t launch_recall(const RecallArgs& a, hipStream_t stream);
 
 // Attention with a sliding window and sinks.  Row r of q is at position
 // r + k.N - q.N; lens (int32 [B], or NULL) bounds each sequence's keys and rows.
+constexpr int32_t kWindowRows = 128;  // query rows per workgroup
 struct WindowArgs {
   Tensor4 q, k, v;
   void* o;

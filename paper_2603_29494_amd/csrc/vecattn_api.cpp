@@ -390,7 +390,7 @@ vecattn_tdesc seq_desc(const vecattn_tdesc* d, int64_t n) {
   return r;
 }
 
-constexpr int64_t kMaxGridYZ = 65535;        // heads and sequences are grid dimensions
+constexpr int64_t kMaxGridYZ = 65535;   // heads and sequences (grid dimensions)
 constexpr int64_t kMaxCacheRows = int64_t(1) << 28;
 
 bool same_shape(const vecattn_tdesc* a, const vecattn_tdesc* b) {
@@ -546,7 +546,9 @@ vecattn_status vecattn_window_attn(const void* q, const vecattn_tdesc* qd, const
     return VECATTN_ERR_INVALID_ARG;
   if (window < 1 || sinks < 0 || !std::isfinite(scale) || scale < 0.0f || (causal & ~kCausal) != 0)
     return VECATTN_ERR_INVALID_ARG;
-  if (qd->B > kMaxGridYZ || qd->H > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
+  if (qd->B > kMaxGridYZ || qd->H > kMaxGridYZ ||
+      qd->B * qd->H * num_blocks(qd->N, vecattn::kWindowRows) > (int64_t(1) << 23))
+    return VECATTN_ERR_UNSUPPORTED;
   // A tile's 64 rows are addressed with 32-bit byte offsets.
   if (kd->N > 1 && (kd->sN >= (int64_t(1) << 24) || vd->sN >= (int64_t(1) << 24)))
     return VECATTN_ERR_UNSUPPORTED;

@@ -20,7 +20,7 @@ namespace vecattn {
 namespace {
 
 constexpr int kTile = 64;
-constexpr int kRows = 128;   // query rows per workgroup
+constexpr int kRows = kWindowRows;
 constexpr float kUnseen = -3.4028234663852886e38f;
 
 struct WindowParams {

@@ -47,6 +47,8 @@ def test_window_attn_rejects_bad_arguments():
     big = 70000
     assert win(scale=0.0, qd=desc(big, 2, 8, 64), kd=desc(big, 2, 8, 64), vd=desc(big, 2, 8, 64),
                od=desc(big, 2, 8, 64)) == UNSUPPORTED
+    many = desc(60000, 64, 300, 64)
+    assert win(scale=0.0, qd=many, kd=many, vd=many, od=many) == UNSUPPORTED
     wide = desc(1, 2, 128, 128, sN=1 << 24)
     assert win(scale=0.0, kd=wide) == UNSUPPORTED and win(scale=0.0, vd=wide) == UNSUPPORTED
 
