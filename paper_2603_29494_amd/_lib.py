@@ -7,7 +7,9 @@ cannot be loaded, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -495,22 +497,24 @@ def sparse_attn_varlen(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seq
     return (out, lse) if return_lse else out
 
 
-def _desc_any(t: torch.Tensor) -> TDesc:
-    """desc() with the strides of dimensions of size 1, which address nothing, set to ones that
-    pass the library's checks (a slice of a projection may carry any)."""
-    d = desc(t)
-    if d.N == 1:
-        d.sN = d.D
-    if d.H == 1:
-        d.sH = 0
-    if d.B == 1:
-        d.sB = 0
-    return d
+@functools.lru_cache(maxsize=4096)
+def _tdesc(shape, strides):
+    """A [B, H, N, D] tensor's descriptor by reference.  The strides of dimensions of size 1, which
+    address nothing, are set to ones that pass the library's checks (a slice of a projection may
+    carry any)."""
+    if len(shape) != 4:
+        raise ValueError("expected a [B, H, N, D] tensor")
+    if strides[3] != 1 and shape[3] != 1:
+        raise ValueError("the D dimension must be contiguous")
+    B, H, N, Dd = shape
+    sB, sH, sN = strides[:3]
+    return ctypes.byref(TDesc(B, H, N, Dd, 0 if B == 1 else sB, 0 if H == 1 else sH,
+                              Dd if N == 1 else sN))
 
 
 def _int32_on(t: torch.Tensor, shape, device, name: str):
-    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape) \
-            or t.device != device:
+    if t.dtype is not torch.int32 or t.shape != shape or t.device != device \
+            or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on {device}")
 
 
@@ -518,6 +522,15 @@ def _same_device(device, **tensors):
     for name, t in tensors.items():
         if t is not None and t.device != device:
             raise ValueError(f"{name} must be on {device}")
+
+
+def _call(device: torch.device, what: str, fn, *args):
+    """fn(*args, stream) on the device's current stream, with that device current."""
+    with contextlib.nullcontext() if torch.cuda.current_device() == device.index \
+            else torch.cuda.device(device):
+        status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if status != OK:
+        raise VecattnError(status, what)
 
 
 _ALL_KEYS = 1 << 30  # a window that hides nothing
@@ -532,28 +545,24 @@ def window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, 
     exist; padded rows of a given ``out`` are left as they were (0 in an ``out`` made here)."""
     for t, n in ((q, "q"), (k, "k"), (v, "v")):
         _bf16_cuda(t, n)
+    dev = q.device
+    new = torch.empty if lens is None else torch.zeros
     if out is None:
-        new = torch.empty if lens is None else torch.zeros
-        out = new(q.shape, dtype=q.dtype, device=q.device)
+        out = new(q.shape, dtype=torch.bfloat16, device=dev)
     _bf16_cuda(out, "out")
-    _same_device(q.device, k=k, v=v, out=out)
-    B, Hq, Nq, _ = q.shape
+    _same_device(dev, k=k, v=v, out=out)
     if lens is not None:
-        _int32_on(lens, (B,), q.device, "lens")
-    lse = None
-    if return_lse:
-        lse = (torch.empty if lens is None else torch.zeros)((B, Hq, Nq), dtype=torch.float32,
-                                                             device=q.device)
-    qd, kd, vd, od = _desc_any(q), _desc_any(k), _desc_any(v), _desc_any(out)
-    with torch.cuda.device(q.device):
-        _check(load().vecattn_window_attn(
-            _ptr(q), ctypes.byref(qd), _ptr(k), ctypes.byref(kd), _ptr(v), ctypes.byref(vd),
-            _ptr(lens), int(window), int(sinks), int(bool(causal)), float(scale), _ptr(out),
-            ctypes.byref(od), _ptr(lse), _stream(q)), "window_attn")
+        _int32_on(lens, q.shape[:1], dev, "lens")
+    lse = new(q.shape[:3], dtype=torch.float32, device=dev) if return_lse else None
+    _call(dev, "window_attn", load().vecattn_window_attn,
+          q.data_ptr(), _tdesc(q.shape, q.stride()), k.data_ptr(), _tdesc(k.shape, k.stride()),
+          v.data_ptr(), _tdesc(v.shape, v.stride()), None if lens is None else lens.data_ptr(),
+          window, sinks, 1 if causal else 0, scale, out.data_ptr(),
+          _tdesc(out.shape, out.stride()), None if lse is None else lse.data_ptr())
     return (out, lse) if return_lse else out
 
 
-@dataclass
+@dataclass(frozen=True)
 class Cache:
     """A key/value cache in pages of 4- or 8-bit values (vecattn_cache): ``data`` (uint8, the
     library's layout) of ``pages`` pages of ``page`` tokens, ``heads`` x ``dim`` values each."""
@@ -564,9 +573,20 @@ class Cache:
     page: int
     bits: int
 
-    def desc(self) -> CacheDesc:
-        return CacheDesc(self.data.data_ptr(), self.pages, self.heads, self.dim, self.page,
-                         self.bits)
+    def __post_init__(self):
+        need = cache_bytes(self.pages, self.heads, self.dim, self.page, self.bits)
+        if self.data.dtype is not torch.uint8 or not self.data.is_contiguous() \
+                or self.data.numel() < need:
+            raise ValueError(f"data must be a contiguous uint8 tensor of {need} bytes")
+
+    def desc(self):
+        return _cache_desc(self.data.data_ptr(), self.pages, self.heads, self.dim, self.page,
+                           self.bits)
+
+
+@functools.lru_cache(maxsize=256)
+def _cache_desc(*fields):
+    return ctypes.byref(CacheDesc(*fields))
 
 
 def cache_bytes(pages: int, heads: int, dim: int, page: int = 64, bits: int = 4) -> int:
@@ -587,19 +607,17 @@ def cache_alloc(pages: int, heads: int, dim: int, page: int = 64, bits: int = 4,
 
 
 def _cache_args(cache: Cache, table: torch.Tensor, lens: torch.Tensor, B: int,
-                n_new: Optional[torch.Tensor] = None):
+                n_new: Optional[torch.Tensor] = None) -> torch.device:
     dev = cache.data.device
-    if not cache.data.is_cuda or cache.data.dtype != torch.uint8 or not cache.data.is_contiguous() \
-            or cache.data.numel() < cache_bytes(cache.pages, cache.heads, cache.dim, cache.page,
-                                                cache.bits):
-        raise ValueError("the cache's data must be a contiguous uint8 CUDA tensor of cache_bytes")
+    if dev.type != "cuda":
+        raise ValueError("the cache's data must be a CUDA tensor")
     if table.dim() != 2:
         raise ValueError("table must be [B, cols]")
     _int32_on(table, (B, table.shape[1]), dev, "table")
     _int32_on(lens, (B,), dev, "lens")
     if n_new is not None:
         _int32_on(n_new, (B,), dev, "n_new")
-    return dev, cache.desc()
+    return dev
 
 
 def cache_write(cache: Cache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
@@ -610,13 +628,12 @@ def cache_write(cache: Cache, k: torch.Tensor, v: torch.Tensor, table: torch.Ten
     [B]: how many of the n rows each sequence has (all when not given)."""
     _bf16_cuda(k, "k")
     _bf16_cuda(v, "v")
-    kd, vd = _desc_any(k), _desc_any(v)
-    dev, cd = _cache_args(cache, table, lens, k.shape[0], n_new)
+    dev = _cache_args(cache, table, lens, k.shape[0], n_new)
     _same_device(dev, k=k, v=v)
-    with torch.cuda.device(dev):
-        _check(load().vecattn_cache_write(
-            _ptr(k), ctypes.byref(kd), _ptr(v), ctypes.byref(vd), ctypes.byref(cd), _ptr(table),
-            int(table.shape[1]), _ptr(lens), _ptr(n_new), _stream(cache.data)), "cache_write")
+    _call(dev, "cache_write", load().vecattn_cache_write,
+          k.data_ptr(), _tdesc(k.shape, k.stride()), v.data_ptr(), _tdesc(v.shape, v.stride()),
+          cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(),
+          None if n_new is None else n_new.data_ptr())
 
 
 def cache_read(cache: Cache, table: torch.Tensor, lens: torch.Tensor, n: int, start: int = 0,
@@ -626,33 +643,38 @@ def cache_read(cache: Cache, table: torch.Tensor, lens: torch.Tensor, n: int, st
     (vecattn_cache_read).  Rows of tokens that are not held are left as they were in a given
     ``out`` pair, and 0 in one made here."""
     B = table.shape[0]
-    dev, cd = _cache_args(cache, table, lens, B)
+    dev = _cache_args(cache, table, lens, B)
+    shape = (B, cache.heads, n, cache.dim)
     if out is None:
-        shape = (B, cache.heads, int(n), cache.dim)
         out = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
     k, v = out
     for t, name in ((k, "k"), (v, "v")):
         _bf16_cuda(t, name)
-        if tuple(t.shape) != (B, cache.heads, int(n), cache.dim):
+        if t.shape != shape:
             raise ValueError("out must be a pair of [B, heads, n, dim] tensors")
     _same_device(dev, k=k, v=v)
-    kd, vd = _desc_any(k), _desc_any(v)
-    with torch.cuda.device(dev):
-        _check(load().vecattn_cache_read(
-            ctypes.byref(cd), _ptr(table), int(table.shape[1]), _ptr(lens), int(start), _ptr(k),
-            ctypes.byref(kd), _ptr(v), ctypes.byref(vd), _stream(cache.data)), "cache_read")
+    _call(dev, "cache_read", load().vecattn_cache_read,
+          cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(), start,
+          k.data_ptr(), _tdesc(k.shape, k.stride()), v.data_ptr(), _tdesc(v.shape, v.stride()))
     return k, v
+
+
+@functools.lru_cache(maxsize=4096)
+def _attn_workspace(shape, pages, heads, dim, page, bits, cols, window, sinks) -> int:
+    n = ctypes.c_size_t(0)
+    B, H, N, Dd = shape
+    qd, cd = TDesc(B, H, N, Dd, 0, 0, Dd), CacheDesc(None, pages, heads, dim, page, bits)
+    _check(load().vecattn_cache_attn_workspace_size(
+        ctypes.byref(qd), ctypes.byref(cd), cols, window, sinks, ctypes.byref(n)),
+        "cache_attn_workspace_size")
+    return n.value
 
 
 def cache_attn_workspace_bytes(q: torch.Tensor, cache: Cache, cols: int,
                                window: Optional[int] = None, sinks: int = 0) -> int:
     """Workspace bytes of cache_attn for these shapes (a table of ``cols`` columns)."""
-    n = ctypes.c_size_t(0)
-    qd, cd = _desc_any(q), cache.desc()
-    _check(load().vecattn_cache_attn_workspace_size(
-        ctypes.byref(qd), ctypes.byref(cd), int(cols), _ALL_KEYS if window is None else int(window),
-        int(sinks), ctypes.byref(n)), "cache_attn_workspace_size")
-    return int(n.value)
+    return _attn_workspace(q.shape, cache.pages, cache.heads, cache.dim, cache.page, cache.bits,
+                           cols, _ALL_KEYS if window is None else window, sinks)
 
 
 def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.Tensor,
@@ -664,23 +686,23 @@ def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.T
     ``table``, ``lens``, ``n_new`` as for cache_write, which has put the new tokens' K and V there.
     Padded rows of a given ``out`` are left as they were (0 in an ``out`` made here)."""
     _bf16_cuda(q, "q")
-    B, Hq, n, _ = q.shape
-    dev, cd = _cache_args(cache, table, lens, B, n_new)
+    dev = _cache_args(cache, table, lens, q.shape[0], n_new)
     new = torch.empty if n_new is None else torch.zeros
     if out is None:
-        out = new(q.shape, dtype=q.dtype, device=dev)
+        out = new(q.shape, dtype=torch.bfloat16, device=dev)
     _bf16_cuda(out, "out")
     _same_device(dev, q=q, out=out, workspace=workspace)
-    lse = new((B, Hq, n), dtype=torch.float32, device=dev) if return_lse else None
-    window = _ALL_KEYS if window is None else int(window)
-    need = cache_attn_workspace_bytes(q, cache, table.shape[1], window, sinks)
+    lse = new(q.shape[:3], dtype=torch.float32, device=dev) if return_lse else None
+    if window is None:
+        window = _ALL_KEYS
+    cols = table.shape[1]
+    need = cache_attn_workspace_bytes(q, cache, cols, window, sinks)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    nws = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    qd, od = _desc_any(q), _desc_any(out)
-    with torch.cuda.device(dev):
-        _check(load().vecattn_cache_attn(
-            _ptr(q), ctypes.byref(qd), ctypes.byref(cd), _ptr(table), int(table.shape[1]),
-            _ptr(lens), _ptr(n_new), window, int(sinks), float(scale), _ptr(out),
-            ctypes.byref(od), _ptr(lse), _ptr(workspace), nws, _stream(q)), "cache_attn")
+    _call(dev, "cache_attn", load().vecattn_cache_attn,
+          q.data_ptr(), _tdesc(q.shape, q.stride()), cache.desc(), table.data_ptr(), cols,
+          lens.data_ptr(), None if n_new is None else n_new.data_ptr(), window, sinks, scale,
+          out.data_ptr(), _tdesc(out.shape, out.stride()), None if lse is None else lse.data_ptr(),
+          None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel() * workspace.element_size())
     return (out, lse) if return_lse else out

@@ -133,7 +133,7 @@ def test_cache_attn_rejects_bad_arguments():
 
 def test_workspace_follows_what_a_row_can_see():
     q = torch.empty(1, 4, 1, 128, dtype=torch.bfloat16)
-    c = va.Cache(torch.empty(0, dtype=torch.uint8), 4096, 4, 128, 64, 4)
+    c = va.Cache(torch.empty(va.cache_bytes(4096, 4, 128), dtype=torch.uint8), 4096, 4, 128, 64, 4)
     whole = va.cache_attn_workspace_bytes(q, c, 2048)
     assert whole > va.cache_attn_workspace_bytes(q, c, 2048, window=4096) > 0
     assert va.cache_attn_workspace_bytes(q, c, 2048, window=100) == 0
@@ -152,6 +152,8 @@ def test_binding_rejects_what_is_not_on_the_gpu():
         va.cache_attn(x, c, table, lens)
     with pytest.raises(ValueError):
         va.cache_read(c, table, lens, 4)
+    with pytest.raises(ValueError):
+        va.Cache(c.data[:-1], 2, 2, 128, 64, 4)     # a byte short
 
 
 # ---- the 64-bit forms themselves, on small cases ----
