@@ -471,7 +471,8 @@ vecattn_status vecattn_cache_size(const vecattn_cache* cache, size_t* bytes);
  *           vecattn_cache_read, and not visible to vecattn_cache_attn (so pages
  *           that a window has left behind can be given away).  Tokens past
  *           cols * page are held nowhere either.
- *   lens  : int32 [B] device memory: tokens of each sequence, the new ones included
+ *   lens  : int32 [B] device memory: tokens of each sequence, the new ones
+ *           included (below 0: none; at most 2^30)
  *   n_new : optional int32 [B] device memory (clamped to [0, n]): the rows of
  *           sequence b that exist (a padded batch), rows [0, n_new[b]); NULL: all n.
  * Row r is written at position lens[b] - n_new[b] + r; rows at a position below 0
@@ -525,7 +526,7 @@ vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* tab
  * can be replayed as they change.
  * Errors: as vecattn_cache_write; INVALID_ARG for window < 1, sinks < 0, a bad
  * scale, a misaligned workspace; CAPACITY (workspace too small); UNSUPPORTED
- * (sizes past the launch limits: B * Hq * n > 2^31 or about 2^24 workgroups).
+ * (sizes past the launch limits: B * Hq * n >= 2^24, or about 2^23 workgroups).
  */
 vecattn_status vecattn_cache_attn_workspace_size(const vecattn_tdesc* qd,
                                                  const vecattn_cache* cache, int64_t cols,

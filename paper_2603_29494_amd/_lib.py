@@ -528,7 +528,7 @@ def _call(device: torch.device, what: str, fn, *args):
     """fn(*args, stream) on the device's current stream, with that device current."""
     with contextlib.nullcontext() if torch.cuda.current_device() == device.index \
             else torch.cuda.device(device):
-        status = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
     if status != OK:
         raise VecattnError(status, what)
 
@@ -546,14 +546,14 @@ def window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, 
     for t, n in ((q, "q"), (k, "k"), (v, "v")):
         _bf16_cuda(t, n)
     dev = q.device
-    new = torch.empty if lens is None else torch.zeros
+    new = q.new_empty if lens is None else q.new_zeros
     if out is None:
-        out = new(q.shape, dtype=torch.bfloat16, device=dev)
+        out = new(q.shape)
     _bf16_cuda(out, "out")
     _same_device(dev, k=k, v=v, out=out)
     if lens is not None:
         _int32_on(lens, q.shape[:1], dev, "lens")
-    lse = new(q.shape[:3], dtype=torch.float32, device=dev) if return_lse else None
+    lse = new(q.shape[:3], dtype=torch.float32) if return_lse else None
     _call(dev, "window_attn", load().vecattn_window_attn,
           q.data_ptr(), _tdesc(q.shape, q.stride()), k.data_ptr(), _tdesc(k.shape, k.stride()),
           v.data_ptr(), _tdesc(v.shape, v.stride()), None if lens is None else lens.data_ptr(),
@@ -687,12 +687,12 @@ def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.T
     Padded rows of a given ``out`` are left as they were (0 in an ``out`` made here)."""
     _bf16_cuda(q, "q")
     dev = _cache_args(cache, table, lens, q.shape[0], n_new)
-    new = torch.empty if n_new is None else torch.zeros
+    new = q.new_empty if n_new is None else q.new_zeros
     if out is None:
-        out = new(q.shape, dtype=torch.bfloat16, device=dev)
+        out = new(q.shape)
     _bf16_cuda(out, "out")
     _same_device(dev, q=q, out=out, workspace=workspace)
-    lse = new(q.shape[:3], dtype=torch.float32, device=dev) if return_lse else None
+    lse = new(q.shape[:3], dtype=torch.float32) if return_lse else None
     if window is None:
         window = _ALL_KEYS
     cols = table.shape[1]

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void k_cache_write(
   constexpr int RPP = 256 / CH;           // rows per pass
   const int64_t b = blockIdx.z;
   const int h = blockIdx.y;
-  const int64_t len = lens[b];
+  const int64_t len = min(max(lens[b], 0), 1 << 30);
   const int64_t nb = n_new ? min(max(n_new[b], 0), n) : n;
   const int64_t p0 = len - nb;            // position of row 0
   const int64_t jb = (max(p0, int64_t(0)) >> 5) + blockIdx.x;
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void k_cache_read(
   constexpr int RPP = 256 / CH;
   const int64_t b = blockIdx.z;
   const int h = blockIdx.y;
-  const int64_t len = lens[b];
+  const int64_t len = min(max(lens[b], 0), 1 << 30);
   const int64_t jb = (start >> 5) + blockIdx.x;
   const int64_t j0 = jb * kCacheBlock;
   if (j0 >= len) return;

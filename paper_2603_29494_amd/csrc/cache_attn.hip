@@ -14,12 +14,13 @@
 //
 // The query heads that share a key/value head and the new tokens of a sequence
 // are the rows (row = token * group + head), R tiles of 16 of them per
-// workgroup; four waves take every fourth block of 32 tokens each.  A long
+// workgroup; its waves take blocks of 32 tokens in turn.  A long
 // sequence is split over workgroups of `chunk` blocks, joined by k_cache_merge.
 //
 // MFMA 16x16x32 lane layout (lane l = 16 g + n): A: row n, K-slots 8 g .. 8 g + 7;
 // B: column n, the same slots; C: column n, rows 4 g .. 4 g + 3.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_common.h"
 
@@ -27,6 +28,7 @@ namespace vecattn {
 namespace {
 
 constexpr float kUnseen = -3.4028234663852886e38f;  // reference of a row that has met no key
+constexpr int32_t kMaxLen = 1 << 30;                 // positions stay in 32 bits
 constexpr float kLn2 = 0.69314718055994531f;
 
 struct AttnParams {
@@ -40,8 +42,8 @@ struct AttnParams {
   const int32_t* lens;
   const int32_t* n_new;
   float* part;       // [work item][16 R] (m, l), then [work item][16 R][D] sums
-  int64_t cols, pages;
-  int64_t window, sinks;
+  int32_t cols, pages;   // pages past the first 2^31 - 1 cannot be named
+  int32_t window, sinks;
   int32_t H, n, group, page_shift;
   int32_t tiles;     // row tiles per head
   int32_t splits;    // workgroups a row tile's keys are split over
@@ -52,52 +54,55 @@ struct AttnParams {
 // What one row tile sees, in blocks of 32 tokens: the first `ns` blocks (sinks),
 // then blocks nb0 ..; `total` of both.
 struct Span {
-  int64_t p_first;   // position of the sequence's row 0
-  int64_t p_lo, p_hi;   // positions of the tile's rows
-  int64_t ns, nb0, total;
-  int32_t rows;      // rows of the sequence (all tiles)
+  int32_t p_first;      // position of the sequence's row 0
+  int32_t p_lo, p_hi;   // positions of the tile's rows
+  int32_t ns, nb0, total;
+  int32_t rows;         // rows of the sequence (all tiles)
 };
 
 __device__ __forceinline__ Span span_of(const AttnParams& a, int64_t b, int row0, int nrows) {
   Span s;
-  const int64_t len = a.lens[b];
-  const int64_t nb = a.n_new ? min(max(a.n_new[b], 0), a.n) : a.n;
+  const int len = min(max(a.lens[b], 0), kMaxLen);
+  const int nb = a.n_new ? min(max(a.n_new[b], 0), a.n) : a.n;
   s.p_first = len - nb;
-  s.rows = static_cast<int32_t>(nb) * a.group;
+  s.rows = nb * a.group;
   s.p_lo = s.p_first + row0 / a.group;
   s.p_hi = s.p_first + (min(row0 + nrows, s.rows) - 1) / a.group;
   s.ns = s.nb0 = s.total = 0;
   if (row0 >= s.rows || s.p_hi < 0) return s;
-  const int64_t near = max(int64_t(0), s.p_lo - a.window + 1);
+  const int near = max(0, s.p_lo - a.window + 1);
   s.nb0 = near >> 5;
   s.ns = min(s.nb0, (min(a.sinks, near) + 31) >> 5);
   // Tokens past the table are held nowhere.
-  const int64_t held = a.cols << (a.page_shift - 5);
-  const int64_t end = min((s.p_hi >> 5) + 1, held);
+  const int held = a.cols << (a.page_shift - 5);
+  const int end = min((s.p_hi >> 5) + 1, held);
   s.ns = min(s.ns, held);
-  s.total = s.ns + max(int64_t(0), end - s.nb0);
+  s.total = s.ns + max(0, end - s.nb0);
   return s;
 }
 
+// Eight codes as bf16.  `ones` is kOnes in a vector register that the compiler does
+// not see through: with both constants in scalar registers it takes two instructions
+// for (x & mask) | ones instead of one.
 template <int BITS>
 struct Unpack;
 template <>
 struct Unpack<4> {
   static constexpr float kOff = 16.0f;
-  static __device__ __forceinline__ bf16x8 get(const uint32_t* w) {
+  static constexpr uint32_t kOnes = 0x41804180u;   // a pair of 16.0
+  static __device__ __forceinline__ bf16x8 get(const uint32_t* w, uint32_t ones) {
+    constexpr uint32_t mask = 0x00780078u;
     const uint32_t x = w[0];
-    u32x4 r;
-    r[0] = ((x << 3) & 0x00780078u) | 0x41804180u;
-    r[1] = ((x >> 1) & 0x00780078u) | 0x41804180u;
-    r[2] = ((x >> 5) & 0x00780078u) | 0x41804180u;
-    r[3] = ((x >> 9) & 0x00780078u) | 0x41804180u;
+    const u32x4 r = {((x << 3) & mask) | ones, ((x >> 1) & mask) | ones, ((x >> 5) & mask) | ones,
+                     ((x >> 9) & mask) | ones};
     return __builtin_bit_cast(bf16x8, r);
   }
 };
 template <>
 struct Unpack<8> {
   static constexpr float kOff = 0.0f;
-  static __device__ __forceinline__ bf16x8 get(const uint32_t* w) {
+  static constexpr uint32_t kOnes = 0;
+  static __device__ __forceinline__ bf16x8 get(const uint32_t* w, uint32_t) {
     u32x4 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -120,10 +125,44 @@ __device__ __forceinline__ float col_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int D, int BITS, int R>
-__global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
+// What a wave holds of a block: its lanes' codes and the (m, s) of the tokens of
+// their C-layout rows.
+template <int D, int BITS>
+struct Block {
+  using L = CacheLayout<D, BITS>;
+  uint32_t kc[L::kRun], vc[L::kRun], kp[2][4 * L::kG], vp[2][4 * L::kG];
+  __device__ __forceinline__ void load(const uint8_t* blk, int lane) {
+#pragma unroll
+    for (int c = 0; c < L::kRun / 4; ++c)
+      *reinterpret_cast<u32x4*>(kc + 4 * c) =
+          *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
+#pragma unroll
+    for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+      for (int c = 0; c < L::kG; ++c)
+        *reinterpret_cast<u32x4*>(kp[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
+            blk + L::kCodes + (16 * tl + 4 * (lane >> 4)) * L::kG * 4 + 16 * c);
+    blk += L::kHalf;
+#pragma unroll
+    for (int c = 0; c < L::kRun / 4; ++c)
+      *reinterpret_cast<u32x4*>(vc + 4 * c) =
+          *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
+#pragma unroll
+    for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+      for (int c = 0; c < L::kG; ++c)
+        *reinterpret_cast<u32x4*>(vp[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
+            blk + L::kCodes + (16 * tl + 4 * (lane >> 4)) * L::kG * 4 + 16 * c);
+  }
+};
+
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+
+template <int D, int BITS, int R, int W>
+__global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, ST = D / 32, DB = D / 16;
+  constexpr bool kAhead = R == 1;   // registers for a second block
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -137,14 +176,37 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
   const int row0 = tile * 16 * R;
   const Span s = span_of(a, b, row0, 16 * R);
   if (row0 >= s.rows) return;
-  const int64_t t0 = static_cast<int64_t>(split) * a.chunk;
-  const int64_t t1 = min(s.total, t0 + a.chunk);
+  const int t0 = split * a.chunk;
+  const int t1 = min(s.total, t0 + a.chunk);
   if (split > 0 && t0 >= t1) return;
+
+  // The t-th block this row tile sees, and its page; where no page is held, or past
+  // the last block, a block that can be read and is not used.
+  const int sh = a.page_shift - 5;
+  const ScalarInts pages = (ScalarInts)(a.table + b * a.cols);
+  auto block_of = [&](int t) __attribute__((always_inline)) {
+    t = min(t, t1 - 1);
+    return t < s.ns ? t : s.nb0 + (t - s.ns);
+  };
+  auto page_of = [&](int t) __attribute__((always_inline)) { return pages[block_of(t) >> sh]; };
+  auto held = [&](int page) __attribute__((always_inline)) { return page >= 0 && page < a.pages; };
+  auto address = [&](int t, int page) __attribute__((always_inline)) {
+    const int64_t pg = held(page) ? page : 0;
+    return a.data + (((pg * a.H + h) << sh) + (block_of(t) & ((1 << sh) - 1))) * L::kBytes;
+  };
+  int t = t0 + wave;
+  Block<D, BITS> cur, nxt;
+  int page = -1, page1 = -1;
+  if (kAhead && t0 < t1) {
+    page = page_of(t);
+    page1 = page_of(t + W);
+    cur.load(address(t, page), lane);
+  }
 
   // Rows of this lane's columns.
   bf16x8 qf[R][ST];
   float qs[R][G];
-  int64_t pos[R];
+  int pos[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = row0 + 16 * r + n;
@@ -181,39 +243,14 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
       pm[r][gi] = 0.0f;
     }
   }
+  uint32_t ones = Unpack<BITS>::kOnes;
+  asm volatile("" : "+v"(ones));
   const bf16x8 minus_off = {-16.0f, -16.0f, -16.0f, -16.0f, -16.0f, -16.0f, -16.0f, -16.0f};
 
-  const int sh = a.page_shift - 5;
-  for (int64_t t = t0 + wave; t < t1; t += 4) {
-    const int64_t jb = t < s.ns ? t : s.nb0 + (t - s.ns);
-    const int64_t page = a.table[b * a.cols + (jb >> sh)];
-    if (page < 0 || page >= a.pages) continue;
-    const uint8_t* blk =
-        a.data + (((page * a.H + h) << sh) + (jb & ((int64_t(1) << sh) - 1))) * L::kBytes;
-    uint32_t kc[L::kRun], vc[L::kRun], kp[2][4 * G], vp[2][4 * G];
-#pragma unroll
-    for (int c = 0; c < L::kRun / 4; ++c) {
-      *reinterpret_cast<u32x4*>(kc + 4 * c) =
-          *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
-      *reinterpret_cast<u32x4*>(vc + 4 * c) =
-          *reinterpret_cast<const u32x4*>(blk + L::kHalf + (c * 64 + lane) * 16);
-    }
-#pragma unroll
-    for (int tl = 0; tl < 2; ++tl)
-#pragma unroll
-      for (int c = 0; c < G; ++c) {
-        const int at = L::kCodes + (16 * tl + 4 * g) * G * 4 + 16 * c;
-        *reinterpret_cast<u32x4*>(kp[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(blk + at);
-        *reinterpret_cast<u32x4*>(vp[tl] + 4 * c) =
-            *reinterpret_cast<const u32x4*>(blk + L::kHalf + at);
-      }
-    const int64_t j0 = jb * kCacheBlock;
+  auto work = [&](const Block<D, BITS>& x, int t) __attribute__((always_inline)) {
+    const int j0 = block_of(t) * kCacheBlock;
     // Every row of the tile sees the whole block, or masks are needed.
     const bool masked = j0 + 31 > s.p_lo || (j0 <= s.p_hi - a.window && j0 + 31 >= a.sinks);
-
-    bf16x8 vf[DB];
-#pragma unroll
-    for (int db = 0; db < DB; ++db) vf[db] = Unpack<BITS>::get(vc + db * DW);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float sc[2][4];
@@ -228,38 +265,57 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
 #pragma unroll
         for (int st = 0; st < ST; ++st)
           acc[st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              Unpack<BITS>::get(kc + (tl * ST + st) * DW), qf[r][st], acc[st / 2], 0, 0, 0);
+              Unpack<BITS>::get(x.kc + (tl * ST + st) * DW, ones), qf[r][st], acc[st / 2], 0, 0, 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float x = 0.0f;
+          float y = 0.0f;
 #pragma unroll
           for (int gi = 0; gi < G; ++gi) {
-            const uint32_t w = kp[tl][e * G + gi];
-            x = __builtin_fmaf(__uint_as_float(w & 0xFFFF0000u), acc[gi][e], x);
-            x = __builtin_fmaf(__uint_as_float(w << 16), qs[r][gi], x);
+            const uint32_t w = x.kp[tl][e * G + gi];
+            y = __builtin_fmaf(__uint_as_float(w & 0xFFFF0000u), acc[gi][e], y);
+            y = __builtin_fmaf(__uint_as_float(w << 16), qs[r][gi], y);
           }
-          sc[tl][e] = x;
+          sc[tl][e] = y;
         }
       }
-      uint32_t ok = 0xFFu;
+      uint32_t vp[2][4 * G];
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+        for (int e = 0; e < 4 * G; ++e) vp[tl][e] = x.vp[tl][e];
       if (masked) {
-        ok = 0;
+        // What a hidden token holds must not reach the row: its weight is 0, and so
+        // are its m and s.
 #pragma unroll
         for (int tl = 0; tl < 2; ++tl)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int64_t j = j0 + 16 * tl + 4 * g + e;
+            const int j = j0 + 16 * tl + 4 * g + e;
             const bool see = j <= pos[r] && (j > pos[r] - a.window || j < a.sinks);
-            ok |= see ? 1u << (4 * tl + e) : 0u;
             sc[tl][e] = see ? sc[tl][e] : kNegInf;
+#pragma unroll
+            for (int gi = 0; gi < G; ++gi) vp[tl][e * G + gi] = see ? vp[tl][e * G + gi] : 0u;
           }
       }
-      float top = kNegInf;
+      // Weights against the reference as it is; where a lane's sum is past 256 (a row
+      // that had none among them) the row's reference moves to its maximum first.
+      float p[2][4], sum;
+      auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(sc[0][e], sc[1][e]));
-      top = col_max(top) * a.scale_log2;
-      if (__any(top > m_run[r] + 8.0f)) {  // references move rarely, by steps of 8 (log2 units)
-        const float m_new = top > m_run[r] + 8.0f ? top : m_run[r];
+        for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            p[tl][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[tl][e], a.scale_log2, -m_run[r]));
+        sum = ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) +
+              ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
+      };
+      weigh();
+      if (__any(sum > 256.0f)) {
+        float top = kNegInf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(sc[0][e], sc[1][e]));
+        top = col_max(top) * a.scale_log2;
+        const float m_new = fmaxf(m_run[r], top);
         const float alpha = __builtin_amdgcn_exp2f(m_run[r] - m_new);
         m_run[r] = m_new;
         l_run[r] *= alpha;
@@ -270,15 +326,9 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
           off[r][gi] *= alpha;
           pm[r][gi] *= alpha;
         }
+        weigh();
       }
-      float p[2][4];
-#pragma unroll
-      for (int tl = 0; tl < 2; ++tl)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[tl][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[tl][e], a.scale_log2, -m_run[r]));
-          l_run[r] += p[tl][e];
-        }
+      l_run[r] += sum;
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
         f32x8 y;
@@ -286,8 +336,7 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
         for (int tl = 0; tl < 2; ++tl)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            uint32_t w = vp[tl][e * G + gi];
-            if (masked && !(ok >> (4 * tl + e) & 1u)) w = 0;  // whatever a hidden token holds
+            const uint32_t w = vp[tl][e * G + gi];
             y[4 * tl + e] = p[tl][e] * __uint_as_float(w & 0xFFFF0000u);
             pm[r][gi] = __builtin_fmaf(p[tl][e], __uint_as_float(w << 16), pm[r][gi]);
           }
@@ -296,15 +345,40 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
           off[r][gi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(minus_off, pb, off[r][gi], 0, 0, 0);
 #pragma unroll
         for (int db = 4 * gi; db < 4 * gi + 4; ++db)
-          oacc[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], pb, oacc[r][db], 0, 0, 0);
+          oacc[r][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              Unpack<BITS>::get(x.vc + db * DW, ones), pb, oacc[r][db], 0, 0, 0);
       }
     }
+  };
+  // Each block is fetched while the one before is worked on, its page's entry one
+  // block earlier still.
+  if constexpr (!kAhead) {
+    for (; t < t1; t += W) {
+      page = page_of(t);
+      if (!held(page)) continue;
+      cur.load(address(t, page), lane);
+      work(cur, t);
+    }
+  }
+  while (kAhead && t < t1) {
+    nxt.load(address(t + W, page1), lane);
+    int page2 = page_of(t + 2 * W);
+    if (held(page)) work(cur, t);
+    t += W;
+    if (t >= t1) break;
+    cur.load(address(t + W, page2), lane);
+    page = page_of(t + 2 * W);
+    if (held(page1)) work(nxt, t);
+    t += W;
+    page1 = page;
+    page = page2;
   }
 
-  // Join the four waves: each scales its sums to the largest reference and adds
-  // what the codes' sums leave out.
-  __shared__ float s_m[4][16 * R], s_l[4][16 * R];
-  __shared__ float s_o[4][16][D + 4];
+  // Join the waves: each scales its sums to the largest reference and adds what the
+  // codes' sums leave out.
+  constexpr int kPad = D + 4;
+  __shared__ float s_m[W][16 * R], s_l[W][16 * R];
+  __shared__ __align__(16) float s_o[W][16][kPad];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     l_run[r] = col_sum(l_run[r]);
@@ -314,7 +388,9 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int c = 16 * r + n;
-    const float m = fmaxf(fmaxf(s_m[0][c], s_m[1][c]), fmaxf(s_m[2][c], s_m[3][c]));
+    float m = s_m[0][c];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, s_m[w][c]);
     const float alpha = __builtin_amdgcn_exp2f(m_run[r] - m);
     if (g == 0) s_l[wave][c] = l_run[r] * alpha;
 #pragma unroll
@@ -328,24 +404,23 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
       *reinterpret_cast<f32x4*>(&s_o[wave][n][16 * db + 4 * g]) = y;
     }
     __syncthreads();
-    // 256 threads: row threadIdx / 16, every sixteenth group of four values.
-    const int rr = threadIdx.x >> 4, cc = threadIdx.x & 15;
-    const int row = row0 + 16 * r + rr;
-    const float l = (s_l[0][16 * r + rr] + s_l[1][16 * r + rr]) +
-                    (s_l[2][16 * r + rr] + s_l[3][16 * r + rr]);
-    const float mr = fmaxf(fmaxf(s_m[0][16 * r + rr], s_m[1][16 * r + rr]),
-                           fmaxf(s_m[2][16 * r + rr], s_m[3][16 * r + rr]));
-    const int tok = row / a.group, hq = h * a.group + row % a.group;
-    const bool have = row < s.rows;
-#pragma unroll
-    for (int d = 4 * cc; d < D; d += 64) {
+    // Four values of a row per thread.
+    for (int i = threadIdx.x; i < 4 * D; i += 64 * W) {
+      const int rr = i / (D / 4), d = i % (D / 4) * 4;
+      const int row = row0 + 16 * r + rr;
+      if (row >= s.rows) break;
+      float l = 0.0f, mr = s_m[0][16 * r + rr];
       f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int w = 0; w < 4; ++w) y += *reinterpret_cast<const f32x4*>(&s_o[w][rr][d]);
-      if (!have) continue;
+      for (int w = 0; w < W; ++w) {
+        l += s_l[w][16 * r + rr];
+        mr = fmaxf(mr, s_m[w][16 * r + rr]);
+        y += *reinterpret_cast<const f32x4*>(&s_o[w][rr][d]);
+      }
+      const int tok = row / a.group, hq = h * a.group + row % a.group;
       if (a.splits > 1) {
-        *reinterpret_cast<f32x4*>(a.part + (static_cast<int64_t>(gridDim.x) * 2 +
-                                            item * D) * (16 * R) + (16 * r + rr) * D + d) = y;
+        *reinterpret_cast<f32x4*>(a.part + (static_cast<int64_t>(gridDim.x) * 2 + item * D) *
+                                               (16 * R) + (16 * r + rr) * D + d) = y;
         if (d == 0) {
           float* ml = a.part + (item * 16 * R + 16 * r + rr) * 2;
           ml[0] = mr;
@@ -361,47 +436,57 @@ __global__ __launch_bounds__(256) void k_cache_attn(const AttnParams a) {
               l == 0.0f ? kNegInf : (mr + __builtin_log2f(l)) * kLn2;
       }
     }
-    __syncthreads();
+    if (r + 1 < R) __syncthreads();
   }
 }
 
-// Joins the splits of a row: one wave per row.
+// Joins the splits of a row: a workgroup per row, its four waves taking every
+// fourth split, a lane D / 64 values.
 template <int D>
 __global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t tile_rows,
-                                                     int64_t items, int64_t total_rows) {
-  const int64_t id = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (id >= total_rows) return;
+                                                     int64_t items) {
+  constexpr int V = D / 64;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int rows_all = a.n * a.group;
-  const int row = static_cast<int>(id % rows_all);
-  const int64_t bh = id / rows_all;
+  const int row = static_cast<int>(blockIdx.x % rows_all);
+  const int64_t bh = blockIdx.x / rows_all;
   const int h = static_cast<int>(bh % a.H);
   const int64_t b = bh / a.H;
   const int tile = row / tile_rows;
   const Span s = span_of(a, b, tile * tile_rows, tile_rows);
   const int tok = row / a.group, hq = h * a.group + row % a.group;
   if (row >= s.rows) return;
-  const int used = static_cast<int>(max(int64_t(1), (s.total + a.chunk - 1) / a.chunk));
+  const int used = max(1, (s.total + a.chunk - 1) / a.chunk);
   const int64_t item0 = (bh * a.tiles + tile) * a.splits;
   const int in_tile = row - tile * tile_rows;
+  const float* ml = a.part + (item0 * tile_rows + in_tile) * 2;
+  const float* src = a.part + (items * 2 + item0 * D) * tile_rows + in_tile * D + V * lane;
   float m = kUnseen;
-  for (int i = 0; i < used; ++i)
-    m = fmaxf(m, a.part[((item0 + i) * tile_rows + in_tile) * 2]);
-  float l = 0.0f, y[D / 64] = {};
-  for (int i = 0; i < used; ++i) {
-    const float* ml = a.part + ((item0 + i) * tile_rows + in_tile) * 2;
-    const float alpha = __builtin_amdgcn_exp2f(ml[0] - m);
-    l += ml[1] * alpha;
-    const float* src = a.part + (items * 2 + (item0 + i) * D) * tile_rows + in_tile * D;
+  for (int i = lane; i < used; i += 64) m = fmaxf(m, ml[static_cast<int64_t>(i) * tile_rows * 2]);
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x) y[x] = __builtin_fmaf(src[64 * x + lane], alpha, y[x]);
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float l = 0.0f, y[V] = {};
+#pragma unroll 4
+  for (int i = wave; i < used; i += 4) {
+    const int64_t at = static_cast<int64_t>(i) * tile_rows;
+    const float alpha = __builtin_amdgcn_exp2f(ml[at * 2] - m);
+    l = __builtin_fmaf(ml[at * 2 + 1], alpha, l);
+#pragma unroll
+    for (int x = 0; x < V; ++x) y[x] = __builtin_fmaf(src[at * D + x], alpha, y[x]);
   }
-  const float inv = l > 0.0f ? 1.0f / l : l;
+  __shared__ float s_y[4][D + 1];
 #pragma unroll
-  for (int x = 0; x < D / 64; ++x)
-    reinterpret_cast<__bf16*>(a.o)[b * a.o_sB + hq * a.o_sH + tok * a.o_sN + 64 * x + lane] =
-        static_cast<__bf16>(y[x] * inv);
-  if (a.lse && lane == 0)
+  for (int x = 0; x < V; ++x) s_y[wave][V * lane + x] = y[x];
+  if (lane == 0) s_y[wave][D] = l;
+  __syncthreads();
+  if (threadIdx.x >= D) return;
+  const int d = threadIdx.x;
+  l = (s_y[0][D] + s_y[1][D]) + (s_y[2][D] + s_y[3][D]);
+  const float v = (s_y[0][d] + s_y[1][d]) + (s_y[2][d] + s_y[3][d]);
+  const float inv = l > 0.0f ? 1.0f / l : l;
+  reinterpret_cast<__bf16*>(a.o)[b * a.o_sB + hq * a.o_sH + tok * a.o_sN + d] =
+      static_cast<__bf16>(v * inv);
+  if (a.lse && d == 0)
     a.lse[(b * a.H * a.group + hq) * a.n + tok] =
         l == 0.0f ? kNegInf : (m + __builtin_log2f(l)) * kLn2;
 }
@@ -409,14 +494,14 @@ __global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t
 // How a call is dealt out; depends on its shapes alone, so that the workspace
 // query and the launch agree.
 struct Deal {
-  int32_t R, tiles, splits, chunk;
+  int32_t R, W, tiles, splits, chunk;
   int64_t items;
 };
 
 Deal deal(const CacheAttnShape& s) {
   Deal d;
   const int64_t rows = s.n * (s.Hq / s.H);
-  d.R = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  d.R = rows <= 16 ? 1 : 2;
   d.tiles = static_cast<int32_t>((rows + 16 * d.R - 1) / (16 * d.R));
   const int64_t base = s.B * s.H * d.tiles;
   // Blocks a row tile can see: the table's, or the window's and the sinks'.
@@ -424,7 +509,8 @@ Deal deal(const CacheAttnShape& s) {
   const int64_t seen = std::min(held, (std::min<int64_t>(s.window, held * 32) +
                                        std::min<int64_t>(s.n, 16 * d.R) + 31) / 32 + 1 +
                                           (std::min<int64_t>(s.sinks, held * 32) + 31) / 32);
-  constexpr int64_t kTarget = 1024, kLeast = 16;
+  d.W = d.R == 1 ? 8 : 4;
+  constexpr int64_t kTarget = 512, kLeast = 32;
   const int64_t want = std::max<int64_t>(1, kTarget / base);
   const int64_t chunk = std::max<int64_t>(kLeast, (seen + want - 1) / want);
   d.chunk = static_cast<int32_t>(chunk);
@@ -442,9 +528,9 @@ size_t cache_attn_workspace_bytes(const CacheAttnShape& s) {
 }
 
 bool cache_attn_grid_ok(const CacheAttnShape& s) {
-  if (s.Hq * s.n > (int64_t(1) << 30) || s.B * s.Hq * s.n > (int64_t(1) << 31)) return false;
+  if (s.Hq * s.n > (int64_t(1) << 30) || s.B * s.Hq * s.n >= (int64_t(1) << 24)) return false;
   const Deal d = deal(s);
-  return d.items < (int64_t(1) << 24);
+  return d.items < (int64_t(1) << 23);
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
@@ -461,8 +547,9 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
   a.lens = c.lens;
   a.n_new = x.n_new;
   a.part = static_cast<float*>(x.workspace);
-  a.cols = c.cols, a.pages = c.pages;
-  a.window = x.shape.window, a.sinks = x.shape.sinks;
+  a.cols = static_cast<int32_t>(c.cols);
+  a.pages = static_cast<int32_t>(std::min<int64_t>(c.pages, INT32_MAX));
+  a.window = static_cast<int32_t>(x.shape.window), a.sinks = static_cast<int32_t>(x.shape.sinks);
   a.H = c.H;
   a.n = static_cast<int32_t>(x.shape.n);
   a.group = static_cast<int32_t>(x.shape.Hq / x.shape.H);
@@ -470,28 +557,30 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
   a.tiles = d.tiles, a.splits = d.splits, a.chunk = d.chunk;
   const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(c.D));
   a.scale_log2 = scale * 1.4426950408889634f;
-  auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(d.items)), dim3(256), 0, stream, a);
+  auto launch = [&](auto kernel, int waves) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(d.items)), dim3(64 * waves), 0, stream,
+                       a);
   };
-  auto pick = [&](auto bits) {
-    constexpr int BITS = decltype(bits)::value;
-    if (c.D == 128)
-      d.R == 1 ? run(k_cache_attn<128, BITS, 1>)
-               : d.R == 2 ? run(k_cache_attn<128, BITS, 2>) : run(k_cache_attn<128, BITS, 4>);
-    else
-      d.R == 1 ? run(k_cache_attn<64, BITS, 1>)
-               : d.R == 2 ? run(k_cache_attn<64, BITS, 2>) : run(k_cache_attn<64, BITS, 4>);
+  auto pick = [&](auto dim, auto bits) {
+    constexpr int D = decltype(dim)::value, BITS = decltype(bits)::value;
+    if (d.R == 1 && d.W == 8) launch(k_cache_attn<D, BITS, 1, 8>, 8);
+    else if (d.R == 1) launch(k_cache_attn<D, BITS, 1, 4>, 4);
+    else launch(k_cache_attn<D, BITS, 2, 4>, 4);
   };
-  if (c.bits == 4) pick(std::integral_constant<int, 4>{});
-  else pick(std::integral_constant<int, 8>{});
+  using std::integral_constant;
+  if (c.D == 128)
+    c.bits == 4 ? pick(integral_constant<int, 128>{}, integral_constant<int, 4>{})
+                : pick(integral_constant<int, 128>{}, integral_constant<int, 8>{});
+  else
+    c.bits == 4 ? pick(integral_constant<int, 64>{}, integral_constant<int, 4>{})
+                : pick(integral_constant<int, 64>{}, integral_constant<int, 8>{});
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || d.splits == 1) return e;
-  const int64_t rows = x.shape.B * x.shape.Hq * x.shape.n;
-  const dim3 grid(static_cast<unsigned>((rows + 3) / 4));
+  const dim3 grid(static_cast<unsigned>(x.shape.B * x.shape.Hq * x.shape.n));
   if (c.D == 128)
-    hipLaunchKernelGGL(k_cache_merge<128>, grid, dim3(256), 0, stream, a, 16 * d.R, d.items, rows);
+    hipLaunchKernelGGL(k_cache_merge<128>, grid, dim3(256), 0, stream, a, 16 * d.R, d.items);
   else
-    hipLaunchKernelGGL(k_cache_merge<64>, grid, dim3(256), 0, stream, a, 16 * d.R, d.items, rows);
+    hipLaunchKernelGGL(k_cache_merge<64>, grid, dim3(256), 0, stream, a, 16 * d.R, d.items);
   return hipGetLastError();
 }
 

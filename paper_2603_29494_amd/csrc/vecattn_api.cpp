@@ -443,7 +443,7 @@ vecattn_status check_cache_attn(const vecattn_tdesc* qd, const vecattn_cache* c,
   // A window or sinks past every position is all of it (and keeps the sums of
   // positions in range).
   *s = vecattn::CacheAttnShape{qd->B, qd->H, c->H, qd->N, qd->D, cols, c->page,
-                               std::min(window, int64_t(1) << 32), std::min(sinks, int64_t(1) << 32)};
+                               std::min(window, kMaxN), std::min(sinks, kMaxN)};
   return vecattn::cache_attn_grid_ok(*s) ? VECATTN_OK : VECATTN_ERR_UNSUPPORTED;
 }
 
