@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void k_cache_write(
       uint32_t dw[L::kDw] = {};
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (BITS == 4) dw[0] |= static_cast<uint32_t>(u[e]) << (4 * nibble_of(e));
+        if constexpr (BITS == 4) dw[0] |= static_cast<uint32_t>(u[e]) << (4 * k_nibble(e));
         else dw[e >> 2] |= static_cast<uint32_t>(u[e]) << (8 * (e & 3));
       }
       const int w0 = ((key >> 4) * (D / 32) + (c >> 2)) * L::kDw, l = (c & 3) * 16 + (key & 15);
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256) void k_cache_write(
       const int64_t r = j0 + key - p0;
       const bool have = r >= 0 && r < nb;
       const uint32_t u = codes[key][d];
-      const int x = BITS == 4 ? 0 : e >> 2, sh = BITS == 4 ? 4 * nibble_of(e) : 8 * (e & 3);
+      const int x = BITS == 4 ? 0 : e >> 2, sh = BITS == 4 ? 4 * v_nibble(e) : 8 * (e & 3);
       if (have) {
         dw[x] |= u << sh;
         mask[x] |= (BITS == 4 ? 0xFu : 0xFFu) << sh;
@@ -178,11 +178,11 @@ __device__ __forceinline__ u32x4 values8(uint32_t par, const int (&u)[8]) {
   return out;
 }
 
-template <int BITS>
+template <int BITS, bool V>
 __device__ __forceinline__ void unpack8(const uint32_t (&dw)[BITS / 4], int (&u)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if constexpr (BITS == 4) u[e] = (dw[0] >> (4 * nibble_of(e))) & 0xF;
+    if constexpr (BITS == 4) u[e] = (dw[0] >> (4 * (V ? v_nibble(e) : k_nibble(e)))) & 0xF;
     else u[e] = (dw[e >> 2] >> (8 * (e & 3))) & 0xFF;
   }
 }
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256) void k_cache_read(
       dw[x] = *reinterpret_cast<const uint32_t*>(
           blk + L::kHalf + code_byte((d >> 4) * L::kDw + x, g * 16 + (d & 15)));
     int u[8];
-    unpack8<BITS>(dw, u);
+    unpack8<BITS, true>(dw, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) codes[(e >> 2) * 16 + 4 * g + (e & 3)][d] = static_cast<uint8_t>(u[e]);
   }
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256) void k_cache_read(
 #pragma unroll
     for (int x = 0; x < L::kDw; ++x)
       dw[x] = *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + x, l));
-    unpack8<BITS>(dw, u);
+    unpack8<BITS, false>(dw, u);
     const int gi = key * L::kG + c / 8;
     *reinterpret_cast<u32x4*>(k + b * k_sB + h * k_sH + r * k_sN + 8 * c) =
         values8(reinterpret_cast<const uint32_t*>(blk + L::kCodes)[gi], u);

@@ -5,17 +5,26 @@
 // A key's value is m + s u per group of 64 head-dim values (cache_common.h), so
 //   q . k = sum_G s_G (q_G . u_G) + m_G sum(q_G),
 //   sum_j p_j v_j = sum_j (p_j s_jG) u_j + sum_j p_j m_jG,
-// and the codes go into the matrix instructions as they are: exact in bf16.
-// Codes of 4 bits become 16 + u there (one shift and one and-or per pair); the
-// 16 is taken out by starting the score accumulators at -16 sum(q_G) and by
-// summing -16 times the rounded weights p_j s_jG with a matrix instruction of
-// its own, so that no rounding but that of p_j s_jG to bf16 (half a step, 2^-9)
-// remains.  The normaliser and the m_jG terms take the fp32 weights.
+// and the codes go into the matrix instructions as they are, exactly.
+//   K, 4 bits: a code's byte is u 2^-9 read as fp8 (e4m3: a subnormal up to 7, the
+//     first binade from 8), so masks are all the unpacking; the row of q, scaled by a
+//     power of two, is the sum of three bf8 (e5m2) parts, exact to 2^-30 of its
+//     largest value.
+//   V, 4 bits: 16 + u in bf16 (a shift and an and-or per pair); the 16 is taken out by
+//     summing -16 times the rounded weights with a matrix instruction of its own.
+//   8 bits: bf16 holds integers to 256.
+// No rounding remains but that of p_j s_jG to bf16 (half a step, 2^-9 at most of
+// it); the normaliser and the m_jG terms take the fp32 weights.
 //
 // The query heads that share a key/value head and the new tokens of a sequence
-// are the rows (row = token * group + head), R tiles of 16 of them per
-// workgroup; its waves take blocks of 32 tokens in turn.  A long
-// sequence is split over workgroups of `chunk` blocks, joined by k_cache_merge.
+// are the rows (row = token * group + head), up to 32 of them per workgroup; its
+// waves take blocks of 32 tokens in turn.  Where eight rows are all, the 16 columns
+// of the matrix instructions hold them twice, once for either 16 tokens of a block,
+// which halves the work per score.
+//
+// How the keys are dealt out follows the lengths on the device: every workgroup
+// sums what the sequences see, takes chunks of such a size that the workgroups fill
+// the chip, and finds its own chunk; k_cache_merge joins the chunks of a row.
 //
 // MFMA 16x16x32 lane layout (lane l = 16 g + n): A: row n, K-slots 8 g .. 8 g + 7;
 // B: column n, the same slots; C: column n, rows 4 g .. 4 g + 3.
@@ -41,13 +50,15 @@ struct AttnParams {
   const int32_t* table;
   const int32_t* lens;
   const int32_t* n_new;
-  float* part;       // [work item][16 R] (m, l), then [work item][16 R][D] sums
+  float* part;       // [item][rows of a tile][D] sums, then [item][rows of a tile] (m, l)
   int32_t cols, pages;   // pages past the first 2^31 - 1 cannot be named
   int32_t window, sinks;
   int32_t H, n, group, page_shift;
   int32_t tiles;     // row tiles per head
-  int32_t splits;    // workgroups a row tile's keys are split over
-  int32_t chunk;     // blocks of 32 keys per split
+  int32_t units;     // row tiles of all sequences
+  int32_t items;     // chunks that partial results have room for
+  int32_t target;    // chunks to aim at (0: one per row tile)
+  int32_t least;     // blocks of a chunk at least
   float scale_log2;
 };
 
@@ -81,14 +92,72 @@ __device__ __forceinline__ Span span_of(const AttnParams& a, int64_t b, int row0
   return s;
 }
 
-// Eight codes as bf16.  `ones` is kOnes in a vector register that the compiler does
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// Blocks per chunk, so that all row tiles together make about `target` chunks.
+// Every wave of every workgroup computes the same (64 row tiles at a time).
+__device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows) {
+  if (a.target == 0) return kMaxLen;
+  const int lane = threadIdx.x & 63;
+  int sum = 0;   // <= 256 row tiles of 2^25 blocks, in units of 8 blocks
+  for (int u = lane; u < a.units; u += 64)
+    sum += (span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows).total + 7) >> 3;
+  sum = __builtin_amdgcn_readfirstlane(wave_sum(sum));
+  const int64_t blocks = static_cast<int64_t>(sum) * 8 * a.H;
+  const int chunk = static_cast<int>((blocks + a.target - 1) / a.target);
+  return (max(chunk, a.least) + 7) & ~7;
+}
+
+// Row tile `unit`'s chunks are those from `first` on, `count` of them.
+struct Share {
+  int32_t unit, first, count;
+};
+
+__device__ __forceinline__ int chunks_in(const Span& s, int chunk) {
+  return max(1, (s.total + chunk - 1) / chunk);
+}
+
+// The share that chunk `index` belongs to (by_chunk), or that of row tile `index`;
+// unit < 0 if there is none.
+__device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, int chunk,
+                                            int index, bool by_chunk) {
+  if (a.target == 0) return Share{index < a.units ? index : -1, index, 1};
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int u0 = 0; u0 < a.units; u0 += 64) {
+    const int u = u0 + lane;
+    int count = 0;
+    if (u < a.units)
+      count = chunks_in(span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows), chunk);
+    int incl = count;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(incl, o);
+      if (lane >= o) incl += y;
+    }
+    const int first = before + incl - count;
+    const bool here = u < a.units && (by_chunk ? index >= first && index < first + count : index == u);
+    const uint64_t at = __ballot(here);
+    if (at) {
+      const int l = __builtin_ctzll(at);
+      return Share{u0 + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(count, l)};
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return Share{-1, 0, 0};
+}
+
+// Eight codes of V (of K as well with 8 bits) as bf16.  `ones` is kOnes in a vector register that the compiler does
 // not see through: with both constants in scalar registers it takes two instructions
 // for (x & mask) | ones instead of one.
 template <int BITS>
 struct Unpack;
 template <>
 struct Unpack<4> {
-  static constexpr float kOff = 16.0f;
   static constexpr uint32_t kOnes = 0x41804180u;   // a pair of 16.0
   static __device__ __forceinline__ bf16x8 get(const uint32_t* w, uint32_t ones) {
     constexpr uint32_t mask = 0x00780078u;
@@ -100,7 +169,6 @@ struct Unpack<4> {
 };
 template <>
 struct Unpack<8> {
-  static constexpr float kOff = 0.0f;
   static constexpr uint32_t kOnes = 0;
   static __device__ __forceinline__ bf16x8 get(const uint32_t* w, uint32_t) {
     u32x4 r;
@@ -125,60 +193,147 @@ __device__ __forceinline__ float col_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// What a wave holds of a block: its lanes' codes and the (m, s) of the tokens of
-// their C-layout rows.
-template <int D, int BITS>
+// What a wave holds of a block: its lanes' codes and the (m, s) of its tokens in
+// the scores' C layout (with HALF of the 16 tokens that the lane's column is for).
+template <int D, int BITS, bool HALF>
 struct Block {
   using L = CacheLayout<D, BITS>;
-  uint32_t kc[L::kRun], vc[L::kRun], kp[2][4 * L::kG], vp[2][4 * L::kG];
+  static constexpr int NT = HALF ? 1 : 2;
+  uint32_t kc[L::kRun], vc[L::kRun], kp[NT][4 * L::kG], vp[NT][4 * L::kG];
+  static __device__ __forceinline__ void codes(uint32_t* to, const uint8_t* from, int lane) {
+#pragma unroll
+    for (int c = 0; c < L::kRun / 4; ++c)
+      *reinterpret_cast<u32x4*>(to + 4 * c) =
+          *reinterpret_cast<const u32x4*>(from + (c * 64 + lane) * 16);
+  }
+  static __device__ __forceinline__ void params(uint32_t (&to)[NT][4 * L::kG], const uint8_t* from,
+                                                int lane) {
+#pragma unroll
+    for (int tl = 0; tl < NT; ++tl) {
+      const int tile = HALF ? (lane >> 3) & 1 : tl;
+#pragma unroll
+      for (int c = 0; c < L::kG; ++c)
+        *reinterpret_cast<u32x4*>(to[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
+            from + (16 * tile + 4 * (lane >> 4)) * L::kG * 4 + 16 * c);
+    }
+  }
   __device__ __forceinline__ void load(const uint8_t* blk, int lane) {
+    codes(kc, blk, lane);
+    params(kp, blk + L::kCodes, lane);
+    codes(vc, blk + L::kHalf, lane);
+    params(vp, blk + L::kHalf + L::kCodes, lane);
+  }
+};
+
+// Rows of q as the score products take them: with 8 bits bf16 as they came, with 4
+// bits scaled by 2^k and split into three bf8 parts.  sum: of a group's values, in
+// the products' scale; unscale: from that scale to scores.
+template <int D, int BITS>
+struct Rows {
+  static constexpr int G = D / kCacheGroup, ST = D / 32;
+  bf16x8 q[BITS == 8 ? ST : 1];
+  long part[BITS == 4 ? 3 : 1][BITS == 4 ? ST : 1];
+  float sum[G], unscale;
+
+  __device__ __forceinline__ void load(const uint16_t* src, bool have, int g) {
+    u32x4 w[ST];
 #pragma unroll
-    for (int c = 0; c < L::kRun / 4; ++c)
-      *reinterpret_cast<u32x4*>(kc + 4 * c) =
-          *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
+    for (int st = 0; st < ST; ++st) {
+      w[st] = u32x4{0, 0, 0, 0};
+      if (have) w[st] = *reinterpret_cast<const u32x4*>(src + 32 * st + 8 * g);
+    }
+    float x[ST][8], top = 0.0f;
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl)
+    for (int st = 0; st < ST; ++st)
 #pragma unroll
-      for (int c = 0; c < L::kG; ++c)
-        *reinterpret_cast<u32x4*>(kp[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
-            blk + L::kCodes + (16 * tl + 4 * (lane >> 4)) * L::kG * 4 + 16 * c);
-    blk += L::kHalf;
+      for (int e = 0; e < 4; ++e) {
+        x[st][2 * e] = __uint_as_float(w[st][e] << 16);
+        x[st][2 * e + 1] = __uint_as_float(w[st][e] & 0xFFFF0000u);
+        top = fmaxf(top, fmaxf(fabsf(x[st][2 * e]), fabsf(x[st][2 * e + 1])));
+      }
 #pragma unroll
-    for (int c = 0; c < L::kRun / 4; ++c)
-      *reinterpret_cast<u32x4*>(vc + 4 * c) =
-          *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
+    for (int gi = 0; gi < G; ++gi) sum[gi] = 0.0f;
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl)
+    for (int st = 0; st < ST; ++st)
 #pragma unroll
-      for (int c = 0; c < L::kG; ++c)
-        *reinterpret_cast<u32x4*>(vp[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
-            blk + L::kCodes + (16 * tl + 4 * (lane >> 4)) * L::kG * 4 + 16 * c);
+      for (int e = 0; e < 8; ++e) sum[st / 2] += x[st][e];
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) sum[gi] = col_sum(sum[gi]);
+    if constexpr (BITS == 8) {
+#pragma unroll
+      for (int st = 0; st < ST; ++st) q[st] = __builtin_bit_cast(bf16x8, w[st]);
+      unscale = 1.0f;
+    } else {
+      // The largest value between 2^14 and 2^15.
+      const int k = 15 - __builtin_amdgcn_frexp_expf(fmaxf(col_max(top), 0x1p-100f));
+#pragma unroll
+      for (int st = 0; st < ST; ++st) {
+        uint32_t d[3][2];
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          float y[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_ldexpf(x[st][e + i], k);
+#pragma unroll
+          for (int pt = 0; pt < 3; ++pt) {
+            int c = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], 0, false);
+            c = __builtin_amdgcn_cvt_pk_bf8_f32(y[2], y[3], c, true);
+            d[pt][e / 4] = c;
+            y[0] -= __builtin_amdgcn_cvt_f32_bf8(c, 0);
+            y[1] -= __builtin_amdgcn_cvt_f32_bf8(c, 1);
+            y[2] -= __builtin_amdgcn_cvt_f32_bf8(c, 2);
+            y[3] -= __builtin_amdgcn_cvt_f32_bf8(c, 3);
+          }
+        }
+#pragma unroll
+        for (int pt = 0; pt < 3; ++pt)
+          part[pt][st] = static_cast<long>((static_cast<uint64_t>(d[pt][1]) << 32) | d[pt][0]);
+      }
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi) sum[gi] = __builtin_amdgcn_ldexpf(sum[gi], k - 9);
+      unscale = __builtin_amdgcn_ldexpf(1.0f, 9 - k);
+    }
+  }
+
+  // acc + q . u over 32 head-dim values of 16 tokens.
+  __device__ __forceinline__ f32x4 dot(const uint32_t* codes, int st, f32x4 acc) const {
+    if constexpr (BITS == 8) {
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(Unpack<8>::get(codes, 0), q[st], acc, 0, 0, 0);
+    } else {
+      const uint64_t lo = codes[0] & 0x0F0F0F0Fu, hi = (codes[0] >> 4) & 0x0F0F0F0Fu;
+      const long u = static_cast<long>(hi << 32 | lo);
+#pragma unroll
+      for (int pt = 0; pt < 3; ++pt)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_fp8_bf8(u, part[pt][st], acc, 0, 0, 0);
+      return acc;
+    }
   }
 };
 
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
-template <int D, int BITS, int R, int W>
+// R tiles of 16 rows, or (HALF, R = 1) 8 rows; W waves.
+template <int D, int BITS, int R, bool HALF, int W>
 __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, ST = D / 32, DB = D / 16;
-  constexpr bool kAhead = R == 1;   // registers for a second block
+  constexpr int NT = HALF ? 1 : 2;             // groups of four tokens whose scores a lane holds
+  constexpr int RW = HALF ? 8 : 16;            // rows per tile of columns
+  constexpr int kRows = R * RW;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const int64_t item = blockIdx.x;   // ((b * H + h) * tiles + tile) * splits + split
-  const int split = static_cast<int>(item % a.splits);
-  int64_t rest = item / a.splits;
-  const int tile = static_cast<int>(rest % a.tiles);
-  rest /= a.tiles;
-  const int h = static_cast<int>(rest % a.H);
-  const int64_t b = rest / a.H;
-  const int row0 = tile * 16 * R;
-  const Span s = span_of(a, b, row0, 16 * R);
+  const int h = blockIdx.x % a.H;
+  const int index = blockIdx.x / a.H;
+  const int chunk = chunk_of(a, kRows);
+  const Share share = find_share(a, kRows, chunk, index, true);
+  if (share.unit < 0) return;
+  const int64_t b = share.unit / a.tiles;
+  const int row0 = share.unit % a.tiles * kRows;
+  const Span s = span_of(a, b, row0, kRows);
   if (row0 >= s.rows) return;
-  const int t0 = split * a.chunk;
-  const int t1 = min(s.total, t0 + a.chunk);
-  if (split > 0 && t0 >= t1) return;
+  const int t0 = (index - share.first) * (share.count > 1 ? chunk : 0);
+  const int t1 = share.count > 1 ? min(s.total, t0 + chunk) : s.total;
 
   // The t-th block this row tile sees, and its page; where no page is held, or past
   // the last block, a block that can be read and is not used.
@@ -194,39 +349,19 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
     const int64_t pg = held(page) ? page : 0;
     return a.data + (((pg * a.H + h) << sh) + (block_of(t) & ((1 << sh) - 1))) * L::kBytes;
   };
-  int t = t0 + wave;
-  Block<D, BITS> cur, nxt;
-  int page = -1, page1 = -1;
-  if (kAhead && t0 < t1) {
-    page = page_of(t);
-    page1 = page_of(t + W);
-    cur.load(address(t, page), lane);
-  }
 
   // Rows of this lane's columns.
-  bf16x8 qf[R][ST];
-  float qs[R][G];
+  Rows<D, BITS> rows[R];
   int pos[R];
+  float to_log2[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int row = row0 + 16 * r + n;
+    const int row = row0 + RW * r + n % RW;
     const int tok = row / a.group, hq = h * a.group + row % a.group;
     const bool have = row < s.rows;
     pos[r] = have ? s.p_first + tok : -1;
-    const uint16_t* src = a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN;
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi) qs[r][gi] = 0.0f;
-#pragma unroll
-    for (int st = 0; st < ST; ++st) {
-      u32x4 w = {0, 0, 0, 0};
-      if (have) w = *reinterpret_cast<const u32x4*>(src + 32 * st + 8 * g);
-      qf[r][st] = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        qs[r][st / 2] += __uint_as_float(w[e] << 16) + __uint_as_float(w[e] & 0xFFFF0000u);
-    }
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi) qs[r][gi] = col_sum(qs[r][gi]);
+    rows[r].load(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN, have, g);
+    to_log2[r] = a.scale_log2 * rows[r].unscale;
   }
 
   f32x4 oacc[R][DB], off[R][G];
@@ -246,51 +381,53 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
   uint32_t ones = Unpack<BITS>::kOnes;
   asm volatile("" : "+v"(ones));
   const bf16x8 minus_off = {-16.0f, -16.0f, -16.0f, -16.0f, -16.0f, -16.0f, -16.0f, -16.0f};
+  const bool second = HALF && (n & 8);   // the lane's columns are for the block's last 16 tokens
 
-  auto work = [&](const Block<D, BITS>& x, int t) __attribute__((always_inline)) {
+  auto work = [&](const Block<D, BITS, HALF>& x, int t) __attribute__((always_inline)) {
     const int j0 = block_of(t) * kCacheBlock;
     // Every row of the tile sees the whole block, or masks are needed.
     const bool masked = j0 + 31 > s.p_lo || (j0 <= s.p_hi - a.window && j0 + 31 >= a.sinks);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float sc[2][4];
+      float sc[NT][4];
+      {
+        f32x4 acc[2][G];
 #pragma unroll
-      for (int tl = 0; tl < 2; ++tl) {
-        f32x4 acc[G];
+        for (int tl = 0; tl < 2; ++tl) {
 #pragma unroll
-        for (int gi = 0; gi < G; ++gi) {
-          const float z = -Unpack<BITS>::kOff * qs[r][gi];
-          acc[gi] = f32x4{z, z, z, z};
+          for (int gi = 0; gi < G; ++gi) acc[tl][gi] = f32x4{};
+#pragma unroll
+          for (int st = 0; st < ST; ++st)
+            acc[tl][st / 2] = rows[r].dot(x.kc + (tl * ST + st) * DW, st, acc[tl][st / 2]);
         }
 #pragma unroll
-        for (int st = 0; st < ST; ++st)
-          acc[st / 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              Unpack<BITS>::get(x.kc + (tl * ST + st) * DW, ones), qf[r][st], acc[st / 2], 0, 0, 0);
+        for (int tl = 0; tl < NT; ++tl)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float y = 0.0f;
+          for (int e = 0; e < 4; ++e) {
+            float y = 0.0f;
 #pragma unroll
-          for (int gi = 0; gi < G; ++gi) {
-            const uint32_t w = x.kp[tl][e * G + gi];
-            y = __builtin_fmaf(__uint_as_float(w & 0xFFFF0000u), acc[gi][e], y);
-            y = __builtin_fmaf(__uint_as_float(w << 16), qs[r][gi], y);
+            for (int gi = 0; gi < G; ++gi) {
+              const uint32_t w = x.kp[tl][e * G + gi];
+              const float c = HALF ? (second ? acc[1][gi][e] : acc[0][gi][e]) : acc[tl][gi][e];
+              y = __builtin_fmaf(__uint_as_float(w & 0xFFFF0000u), c, y);
+              y = __builtin_fmaf(__uint_as_float(w << 16), rows[r].sum[gi], y);
+            }
+            sc[tl][e] = y;
           }
-          sc[tl][e] = y;
-        }
       }
-      uint32_t vp[2][4 * G];
+      uint32_t vp[NT][4 * G];
 #pragma unroll
-      for (int tl = 0; tl < 2; ++tl)
+      for (int tl = 0; tl < NT; ++tl)
 #pragma unroll
         for (int e = 0; e < 4 * G; ++e) vp[tl][e] = x.vp[tl][e];
       if (masked) {
         // What a hidden token holds must not reach the row: its weight is 0, and so
         // are its m and s.
 #pragma unroll
-        for (int tl = 0; tl < 2; ++tl)
+        for (int tl = 0; tl < NT; ++tl)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int j = j0 + 16 * tl + 4 * g + e;
+            const int j = j0 + (HALF ? 2 * (n & 8) : 16 * tl) + 4 * g + e;
             const bool see = j <= pos[r] && (j > pos[r] - a.window || j < a.sinks);
             sc[tl][e] = see ? sc[tl][e] : kNegInf;
 #pragma unroll
@@ -299,22 +436,25 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
       }
       // Weights against the reference as it is; where a lane's sum is past 256 (a row
       // that had none among them) the row's reference moves to its maximum first.
-      float p[2][4], sum;
+      float p[NT][4], sum;
       auto weigh = [&]() __attribute__((always_inline)) {
+        sum = 0.0f;
 #pragma unroll
-        for (int tl = 0; tl < 2; ++tl)
+        for (int tl = 0; tl < NT; ++tl) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            p[tl][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[tl][e], a.scale_log2, -m_run[r]));
-        sum = ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) +
-              ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
+            p[tl][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[tl][e], to_log2[r], -m_run[r]));
+          sum += (p[tl][0] + p[tl][1]) + (p[tl][2] + p[tl][3]);
+        }
       };
       weigh();
       if (__any(sum > 256.0f)) {
         float top = kNegInf;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(sc[0][e], sc[1][e]));
-        top = col_max(top) * a.scale_log2;
+        for (int tl = 0; tl < NT; ++tl)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, sc[tl][e]);
+        top = col_max(top) * to_log2[r];
         const float m_new = fmaxf(m_run[r], top);
         const float alpha = __builtin_amdgcn_exp2f(m_run[r] - m_new);
         m_run[r] = m_new;
@@ -331,16 +471,24 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
       l_run[r] += sum;
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
-        f32x8 y;
+        u32x2 y2[NT];
 #pragma unroll
-        for (int tl = 0; tl < 2; ++tl)
+        for (int tl = 0; tl < NT; ++tl) {
+          f32x4 y;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t w = vp[tl][e * G + gi];
-            y[4 * tl + e] = p[tl][e] * __uint_as_float(w & 0xFFFF0000u);
+            y[e] = p[tl][e] * __uint_as_float(w & 0xFFFF0000u);
             pm[r][gi] = __builtin_fmaf(p[tl][e], __uint_as_float(w << 16), pm[r][gi]);
           }
-        const bf16x8 pb = __builtin_convertvector(y, bf16x8);
+          y2[tl] = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+        }
+        u32x4 yb;
+        if constexpr (HALF)
+          yb = u32x4{second ? 0u : y2[0][0], second ? 0u : y2[0][1], second ? y2[0][0] : 0u,
+                     second ? y2[0][1] : 0u};
+        else yb = u32x4{y2[0][0], y2[0][1], y2[NT - 1][0], y2[NT - 1][1]};
+        const bf16x8 pb = __builtin_bit_cast(bf16x8, yb);
         if constexpr (BITS == 4)
           off[r][gi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(minus_off, pb, off[r][gi], 0, 0, 0);
 #pragma unroll
@@ -350,35 +498,28 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
       }
     }
   };
-  // Each block is fetched while the one before is worked on, its page's entry one
-  // block earlier still.
-  if constexpr (!kAhead) {
-    for (; t < t1; t += W) {
-      page = page_of(t);
-      if (!held(page)) continue;
-      cur.load(address(t, page), lane);
-      work(cur, t);
-    }
-  }
-  while (kAhead && t < t1) {
-    nxt.load(address(t + W, page1), lane);
-    int page2 = page_of(t + 2 * W);
-    if (held(page)) work(cur, t);
-    t += W;
-    if (t >= t1) break;
-    cur.load(address(t + W, page2), lane);
-    page = page_of(t + 2 * W);
-    if (held(page1)) work(nxt, t);
-    t += W;
-    page1 = page;
-    page = page2;
+  Block<D, BITS, HALF> cur;
+  for (int t = t0 + wave; t < t1; t += W) {
+    const int page = page_of(t);
+    if (!held(page)) continue;
+    cur.load(address(t, page), lane);
+    work(cur, t);
   }
 
-  // Join the waves: each scales its sums to the largest reference and adds what the
-  // codes' sums leave out.
-  constexpr int kPad = D + 4;
+  // Join the waves (and the two halves of the columns): each scales its sums to the
+  // largest reference and adds what the codes' sums leave out.
   __shared__ float s_m[W][16 * R], s_l[W][16 * R];
-  __shared__ __align__(16) float s_o[W][16][kPad];
+  __shared__ __align__(16) float s_o[W][16][D + 4];
+  auto top_ref = [&](int row) __attribute__((always_inline)) {   // row of the tile, 0 .. kRows - 1
+    const int c = row / RW * 16 + row % RW;
+    float m = kUnseen;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      m = fmaxf(m, s_m[w][c]);
+      if (HALF) m = fmaxf(m, s_m[w][c + 8]);
+    }
+    return m;
+  };
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     l_run[r] = col_sum(l_run[r]);
@@ -387,12 +528,8 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int c = 16 * r + n;
-    float m = s_m[0][c];
-#pragma unroll
-    for (int w = 1; w < W; ++w) m = fmaxf(m, s_m[w][c]);
-    const float alpha = __builtin_amdgcn_exp2f(m_run[r] - m);
-    if (g == 0) s_l[wave][c] = l_run[r] * alpha;
+    const float alpha = __builtin_amdgcn_exp2f(m_run[r] - top_ref(RW * r + n % RW));
+    if (g == 0) s_l[wave][16 * r + n] = l_run[r] * alpha;
 #pragma unroll
     for (int gi = 0; gi < G; ++gi) pm[r][gi] = col_sum(pm[r][gi]);
 #pragma unroll
@@ -405,25 +542,27 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
     }
     __syncthreads();
     // Four values of a row per thread.
-    for (int i = threadIdx.x; i < 4 * D; i += 64 * W) {
+    for (int i = threadIdx.x; i < RW * (D / 4); i += 64 * W) {
       const int rr = i / (D / 4), d = i % (D / 4) * 4;
-      const int row = row0 + 16 * r + rr;
+      const int row = row0 + RW * r + rr;
       if (row >= s.rows) break;
-      float l = 0.0f, mr = s_m[0][16 * r + rr];
+      float l = 0.0f;
       f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        l += s_l[w][16 * r + rr];
-        mr = fmaxf(mr, s_m[w][16 * r + rr]);
-        y += *reinterpret_cast<const f32x4*>(&s_o[w][rr][d]);
-      }
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int hf = 0; hf < (HALF ? 2 : 1); ++hf) {
+          l += s_l[w][16 * r + rr + 8 * hf];
+          y += *reinterpret_cast<const f32x4*>(&s_o[w][rr + 8 * hf][d]);
+        }
+      const float m = top_ref(RW * r + rr);
       const int tok = row / a.group, hq = h * a.group + row % a.group;
-      if (a.splits > 1) {
-        *reinterpret_cast<f32x4*>(a.part + (static_cast<int64_t>(gridDim.x) * 2 + item * D) *
-                                               (16 * R) + (16 * r + rr) * D + d) = y;
+      if (share.count > 1) {
+        const int64_t at = static_cast<int64_t>(blockIdx.x) * kRows + RW * r + rr;
+        *reinterpret_cast<f32x4*>(a.part + at * D + d) = y;
         if (d == 0) {
-          float* ml = a.part + (item * 16 * R + 16 * r + rr) * 2;
-          ml[0] = mr;
+          float* ml = a.part + static_cast<int64_t>(a.items) * kRows * D + at * 2;
+          ml[0] = m;
           ml[1] = l;
         }
       } else {
@@ -433,46 +572,46 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
             __builtin_convertvector(y, bf16x4);
         if (a.lse && d == 0)
           a.lse[(b * a.H * a.group + hq) * a.n + tok] =
-              l == 0.0f ? kNegInf : (mr + __builtin_log2f(l)) * kLn2;
+              l == 0.0f ? kNegInf : (m + __builtin_log2f(l)) * kLn2;
       }
     }
     if (r + 1 < R) __syncthreads();
   }
 }
 
-// Joins the splits of a row: a workgroup per row, its four waves taking every
-// fourth split, a lane D / 64 values.
+// Joins the chunks of a row: a workgroup per row, its four waves taking every
+// fourth chunk, a lane D / 64 values.  Rows of one chunk are done already.
 template <int D>
-__global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t tile_rows,
-                                                     int64_t items) {
+__global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t tile_rows) {
   constexpr int V = D / 64;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int rows_all = a.n * a.group;
   const int row = static_cast<int>(blockIdx.x % rows_all);
-  const int64_t bh = blockIdx.x / rows_all;
-  const int h = static_cast<int>(bh % a.H);
+  const int bh = static_cast<int>(blockIdx.x / rows_all);
+  const int h = bh % a.H;
   const int64_t b = bh / a.H;
   const int tile = row / tile_rows;
+  const Share share = find_share(a, tile_rows, chunk_of(a, tile_rows),
+                                 static_cast<int>(b) * a.tiles + tile, false);
+  if (share.count <= 1) return;
   const Span s = span_of(a, b, tile * tile_rows, tile_rows);
   const int tok = row / a.group, hq = h * a.group + row % a.group;
   if (row >= s.rows) return;
-  const int used = max(1, (s.total + a.chunk - 1) / a.chunk);
-  const int64_t item0 = (bh * a.tiles + tile) * a.splits;
-  const int in_tile = row - tile * tile_rows;
-  const float* ml = a.part + (item0 * tile_rows + in_tile) * 2;
-  const float* src = a.part + (items * 2 + item0 * D) * tile_rows + in_tile * D + V * lane;
+  const int64_t at0 = (static_cast<int64_t>(share.first) * a.H + h) * tile_rows + row % tile_rows;
+  const int64_t step = static_cast<int64_t>(a.H) * tile_rows;
+  const float* src = a.part + at0 * D + V * lane;
+  const float* ml = a.part + static_cast<int64_t>(a.items) * tile_rows * D + at0 * 2;
   float m = kUnseen;
-  for (int i = lane; i < used; i += 64) m = fmaxf(m, ml[static_cast<int64_t>(i) * tile_rows * 2]);
+  for (int i = lane; i < share.count; i += 64) m = fmaxf(m, ml[i * step * 2]);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   float l = 0.0f, y[V] = {};
 #pragma unroll 4
-  for (int i = wave; i < used; i += 4) {
-    const int64_t at = static_cast<int64_t>(i) * tile_rows;
-    const float alpha = __builtin_amdgcn_exp2f(ml[at * 2] - m);
-    l = __builtin_fmaf(ml[at * 2 + 1], alpha, l);
+  for (int i = wave; i < share.count; i += 4) {
+    const float alpha = __builtin_amdgcn_exp2f(ml[i * step * 2] - m);
+    l = __builtin_fmaf(ml[i * step * 2 + 1], alpha, l);
 #pragma unroll
-    for (int x = 0; x < V; ++x) y[x] = __builtin_fmaf(src[at * D + x], alpha, y[x]);
+    for (int x = 0; x < V; ++x) y[x] = __builtin_fmaf(src[i * step * D + x], alpha, y[x]);
   }
   __shared__ float s_y[4][D + 1];
 #pragma unroll
@@ -494,28 +633,32 @@ __global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t
 // How a call is dealt out; depends on its shapes alone, so that the workspace
 // query and the launch agree.
 struct Deal {
-  int32_t R, W, tiles, splits, chunk;
-  int64_t items;
+  bool half;
+  int32_t R, W, rows, tiles, target, least;
+  int64_t units, items;
+  bool merge;
 };
 
 Deal deal(const CacheAttnShape& s) {
   Deal d;
   const int64_t rows = s.n * (s.Hq / s.H);
+  d.half = rows <= 8;
   d.R = rows <= 16 ? 1 : 2;
-  d.tiles = static_cast<int32_t>((rows + 16 * d.R - 1) / (16 * d.R));
-  const int64_t base = s.B * s.H * d.tiles;
+  d.W = 4;
+  d.rows = d.half ? 8 : 16 * d.R;
+  d.tiles = static_cast<int32_t>((rows + d.rows - 1) / d.rows);
+  d.units = s.B * d.tiles;
   // Blocks a row tile can see: the table's, or the window's and the sinks'.
   const int64_t held = s.cols * (s.page / kCacheBlock);
   const int64_t seen = std::min(held, (std::min<int64_t>(s.window, held * 32) +
-                                       std::min<int64_t>(s.n, 16 * d.R) + 31) / 32 + 1 +
+                                       std::min<int64_t>(s.n, d.rows) + 31) / 32 + 1 +
                                           (std::min<int64_t>(s.sinks, held * 32) + 31) / 32);
-  d.W = d.R == 1 ? 8 : 4;
-  constexpr int64_t kTarget = 512, kLeast = 32;
-  const int64_t want = std::max<int64_t>(1, kTarget / base);
-  const int64_t chunk = std::max<int64_t>(kLeast, (seen + want - 1) / want);
-  d.chunk = static_cast<int32_t>(chunk);
-  d.splits = static_cast<int32_t>((seen + chunk - 1) / chunk);
-  d.items = base * d.splits;
+  constexpr int64_t kTarget = 1024, kLeast = 16, kMaxUnits = 256;
+  d.least = kLeast;
+  d.merge = seen > kLeast && d.units <= kMaxUnits;
+  d.target = d.merge ? kTarget : 0;
+  d.items = d.units * s.H;
+  if (d.merge) d.items = std::min(d.items + kTarget, d.items * ((seen + kLeast - 1) / kLeast));
   return d;
 }
 
@@ -523,8 +666,8 @@ Deal deal(const CacheAttnShape& s) {
 
 size_t cache_attn_workspace_bytes(const CacheAttnShape& s) {
   const Deal d = deal(s);
-  if (d.splits == 1) return 0;
-  return static_cast<size_t>(d.items) * 16 * d.R * (s.D + 2) * sizeof(float);
+  if (!d.merge) return 0;
+  return static_cast<size_t>(d.items) * d.rows * (s.D + 2) * sizeof(float);
 }
 
 bool cache_attn_grid_ok(const CacheAttnShape& s) {
@@ -554,34 +697,31 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
   a.n = static_cast<int32_t>(x.shape.n);
   a.group = static_cast<int32_t>(x.shape.Hq / x.shape.H);
   a.page_shift = __builtin_ctz(static_cast<unsigned>(c.page));
-  a.tiles = d.tiles, a.splits = d.splits, a.chunk = d.chunk;
+  a.tiles = d.tiles, a.units = static_cast<int32_t>(d.units);
+  a.items = static_cast<int32_t>(d.items), a.target = d.target, a.least = d.least;
   const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(c.D));
   a.scale_log2 = scale * 1.4426950408889634f;
-  auto launch = [&](auto kernel, int waves) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(d.items)), dim3(64 * waves), 0, stream,
-                       a);
-  };
   auto pick = [&](auto dim, auto bits) {
     constexpr int D = decltype(dim)::value, BITS = decltype(bits)::value;
-    if (d.R == 1 && d.W == 8) launch(k_cache_attn<D, BITS, 1, 8>, 8);
-    else if (d.R == 1) launch(k_cache_attn<D, BITS, 1, 4>, 4);
-    else launch(k_cache_attn<D, BITS, 2, 4>, 4);
+    auto launch = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(d.items)), dim3(64 * d.W), 0, stream, a);
+    };
+    if (d.half) launch(k_cache_attn<D, BITS, 1, true, 4>);
+    else if (d.R == 1) launch(k_cache_attn<D, BITS, 1, false, 4>);
+    else launch(k_cache_attn<D, BITS, 2, false, 4>);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !d.merge) return e;
+    hipLaunchKernelGGL(k_cache_merge<D>,
+                       dim3(static_cast<unsigned>(x.shape.B * x.shape.Hq * x.shape.n)), dim3(256), 0,
+                       stream, a, d.rows);
+    return hipGetLastError();
   };
   using std::integral_constant;
   if (c.D == 128)
-    c.bits == 4 ? pick(integral_constant<int, 128>{}, integral_constant<int, 4>{})
-                : pick(integral_constant<int, 128>{}, integral_constant<int, 8>{});
-  else
-    c.bits == 4 ? pick(integral_constant<int, 64>{}, integral_constant<int, 4>{})
-                : pick(integral_constant<int, 64>{}, integral_constant<int, 8>{});
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || d.splits == 1) return e;
-  const dim3 grid(static_cast<unsigned>(x.shape.B * x.shape.Hq * x.shape.n));
-  if (c.D == 128)
-    hipLaunchKernelGGL(k_cache_merge<128>, grid, dim3(256), 0, stream, a, 16 * d.R, d.items);
-  else
-    hipLaunchKernelGGL(k_cache_merge<64>, grid, dim3(256), 0, stream, a, 16 * d.R, d.items);
-  return hipGetLastError();
+    return c.bits == 4 ? pick(integral_constant<int, 128>{}, integral_constant<int, 4>{})
+                       : pick(integral_constant<int, 128>{}, integral_constant<int, 8>{});
+  return c.bits == 4 ? pick(integral_constant<int, 64>{}, integral_constant<int, 4>{})
+                     : pick(integral_constant<int, 64>{}, integral_constant<int, 8>{});
 }
 
 }  // namespace vecattn

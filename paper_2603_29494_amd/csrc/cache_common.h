@@ -16,9 +16,10 @@
 //   V: dword db * kDw + x holds codes of head-dim value 16 db + n, tokens
 //      4 g + 0..3 and 16 + 4 g + 0..3 (A operand: rows head-dim values, K-slots
 //      tokens, in the order in which the scores' C layout leaves the weights).
-// Eight codes of 4 bits: slot 2 i in nibble i, slot 2 i + 1 in nibble i + 4, so
-// that one shift and one and-or give the pair (2 i, 2 i + 1).  Of 8 bits: slots
-// 0..3 in the first dword's bytes, 4..7 in the second's.
+// Eight codes of 4 bits: of K slot e in nibble 2 e and slot 4 + e in nibble 2 e + 1
+// (e < 4: a mask makes bytes of either four); of V slot 2 i in nibble i, slot 2 i + 1
+// in nibble i + 4 (a shift and an and-or make the bf16 pair (2 i, 2 i + 1)).  Of 8
+// bits: slots 0..3 in the first dword's bytes, 4..7 in the second's.
 #pragma once
 
 #include "device_common.h"
@@ -45,7 +46,8 @@ __host__ __device__ __forceinline__ constexpr int code_byte(int w, int l) {
   return ((w >> 2) * 64 + l) * 16 + (w & 3) * 4;
 }
 
-// Nibble of slot e (0..7).
-__host__ __device__ __forceinline__ constexpr int nibble_of(int e) { return (e >> 1) + 4 * (e & 1); }
+// Nibble of slot e (0..7) of K's and of V's dwords.
+__host__ __device__ __forceinline__ constexpr int k_nibble(int e) { return 2 * (e & 3) + (e >> 2); }
+__host__ __device__ __forceinline__ constexpr int v_nibble(int e) { return (e >> 1) + 4 * (e & 1); }
 
 }  // namespace vecattn
