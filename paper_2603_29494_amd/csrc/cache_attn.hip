@@ -112,7 +112,8 @@ __device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows) {
   return (max(chunk, a.least) + 7) & ~7;
 }
 
-// Row tile `unit`'s chunks are those from `first` on, `count` of them.
+// Row tile `unit`'s chunks are those from `first` on, `count` of them (stored for the
+// join behind the partial results).
 struct Share {
   int32_t unit, first, count;
 };
@@ -121,10 +122,9 @@ __device__ __forceinline__ int chunks_in(const Span& s, int chunk) {
   return max(1, (s.total + chunk - 1) / chunk);
 }
 
-// The share that chunk `index` belongs to (by_chunk), or that of row tile `index`;
-// unit < 0 if there is none.
+// The share that chunk `index` belongs to; unit < 0 if there is none.
 __device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, int chunk,
-                                            int index, bool by_chunk) {
+                                            int index) {
   if (a.target == 0) return Share{index < a.units ? index : -1, index, 1};
   const int lane = threadIdx.x & 63;
   int before = 0;
@@ -140,8 +140,7 @@ __device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, 
       if (lane >= o) incl += y;
     }
     const int first = before + incl - count;
-    const bool here = u < a.units && (by_chunk ? index >= first && index < first + count : index == u);
-    const uint64_t at = __ballot(here);
+    const uint64_t at = __ballot(u < a.units && index >= first && index < first + count);
     if (at) {
       const int l = __builtin_ctzll(at);
       return Share{u0 + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(count, l)};
@@ -149,6 +148,10 @@ __device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, 
     before += __builtin_amdgcn_readlane(incl, 63);
   }
   return Share{-1, 0, 0};
+}
+
+__device__ __forceinline__ int2* shares_of(const AttnParams& a, int tile_rows, int D) {
+  return reinterpret_cast<int2*>(a.part + static_cast<int64_t>(a.items) * tile_rows * (D + 2));
 }
 
 // Eight codes of V (of K as well with 8 bits) as bf16.  `ones` is kOnes in a vector register that the compiler does
@@ -314,7 +317,7 @@ typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 // R tiles of 16 rows, or (HALF, R = 1) 8 rows; W waves.
 template <int D, int BITS, int R, bool HALF, int W>
-__global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2 : 1))) void k_cache_attn(const AttnParams a) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, ST = D / 32, DB = D / 16;
   constexpr int NT = HALF ? 1 : 2;             // groups of four tokens whose scores a lane holds
@@ -326,8 +329,10 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
   const int h = blockIdx.x % a.H;
   const int index = blockIdx.x / a.H;
   const int chunk = chunk_of(a, kRows);
-  const Share share = find_share(a, kRows, chunk, index, true);
+  const Share share = find_share(a, kRows, chunk, index);
   if (share.unit < 0) return;
+  if (a.target && h == 0 && index == share.first && threadIdx.x == 0)
+    shares_of(a, kRows, D)[share.unit] = int2{share.first, share.count};
   const int64_t b = share.unit / a.tiles;
   const int row0 = share.unit % a.tiles * kRows;
   const Span s = span_of(a, b, row0, kRows);
@@ -499,11 +504,37 @@ __global__ __launch_bounds__(64 * W) void k_cache_attn(const AttnParams a) {
     }
   };
   Block<D, BITS, HALF> cur;
-  for (int t = t0 + wave; t < t1; t += W) {
-    const int page = page_of(t);
-    if (!held(page)) continue;
-    cur.load(address(t, page), lane);
-    work(cur, t);
+  int t = t0 + wave;
+  if constexpr (HALF) {
+    // Each block is fetched while the one before is worked on, its page's entry one
+    // block earlier still.
+    Block<D, BITS, HALF> nxt;
+    int page = -1, page1 = -1;
+    if (t < t1) {
+      page = page_of(t);
+      page1 = page_of(t + W);
+      cur.load(address(t, page), lane);
+    }
+    while (t < t1) {
+      nxt.load(address(t + W, page1), lane);
+      const int page2 = page_of(t + 2 * W);
+      if (held(page)) work(cur, t);
+      t += W;
+      if (t >= t1) break;
+      cur.load(address(t + W, page2), lane);
+      page = page_of(t + 2 * W);
+      if (held(page1)) work(nxt, t);
+      t += W;
+      page1 = page;
+      page = page2;
+    }
+  } else {
+    for (; t < t1; t += W) {
+      const int page = page_of(t);
+      if (!held(page)) continue;
+      cur.load(address(t, page), lane);
+      work(cur, t);
+    }
   }
 
   // Join the waves (and the two halves of the columns): each scales its sums to the
@@ -591,23 +622,23 @@ __global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t
   const int h = bh % a.H;
   const int64_t b = bh / a.H;
   const int tile = row / tile_rows;
-  const Share share = find_share(a, tile_rows, chunk_of(a, tile_rows),
-                                 static_cast<int>(b) * a.tiles + tile, false);
-  if (share.count <= 1) return;
-  const Span s = span_of(a, b, tile * tile_rows, tile_rows);
+  const int2 share = shares_of(a, tile_rows, D)[b * a.tiles + tile];   // first, count
+  const int count = share.y;
+  if (count <= 1) return;
+  const int nb = a.n_new ? min(max(a.n_new[b], 0), a.n) : a.n;
   const int tok = row / a.group, hq = h * a.group + row % a.group;
-  if (row >= s.rows) return;
-  const int64_t at0 = (static_cast<int64_t>(share.first) * a.H + h) * tile_rows + row % tile_rows;
+  if (tok >= nb) return;
+  const int64_t at0 = (static_cast<int64_t>(share.x) * a.H + h) * tile_rows + row % tile_rows;
   const int64_t step = static_cast<int64_t>(a.H) * tile_rows;
   const float* src = a.part + at0 * D + V * lane;
   const float* ml = a.part + static_cast<int64_t>(a.items) * tile_rows * D + at0 * 2;
   float m = kUnseen;
-  for (int i = lane; i < share.count; i += 64) m = fmaxf(m, ml[i * step * 2]);
+  for (int i = lane; i < count; i += 64) m = fmaxf(m, ml[i * step * 2]);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   float l = 0.0f, y[V] = {};
 #pragma unroll 4
-  for (int i = wave; i < share.count; i += 4) {
+  for (int i = wave; i < count; i += 4) {
     const float alpha = __builtin_amdgcn_exp2f(ml[i * step * 2] - m);
     l = __builtin_fmaf(ml[i * step * 2 + 1], alpha, l);
 #pragma unroll
@@ -644,8 +675,9 @@ Deal deal(const CacheAttnShape& s) {
   const int64_t rows = s.n * (s.Hq / s.H);
   d.half = rows <= 8;
   d.R = rows <= 16 ? 1 : 2;
-  d.W = 4;
   d.rows = d.half ? 8 : 16 * d.R;
+  // Few row tiles: more waves on each, and half the chunks to join.
+  d.W = d.half && s.B * s.H <= 128 ? 8 : 4;
   d.tiles = static_cast<int32_t>((rows + d.rows - 1) / d.rows);
   d.units = s.B * d.tiles;
   // Blocks a row tile can see: the table's, or the window's and the sinks'.
@@ -653,12 +685,12 @@ Deal deal(const CacheAttnShape& s) {
   const int64_t seen = std::min(held, (std::min<int64_t>(s.window, held * 32) +
                                        std::min<int64_t>(s.n, d.rows) + 31) / 32 + 1 +
                                           (std::min<int64_t>(s.sinks, held * 32) + 31) / 32);
-  constexpr int64_t kTarget = 1024, kLeast = 16, kMaxUnits = 256;
+  constexpr int64_t kTarget = 512, kLeast = 32, kMaxUnits = 256;
   d.least = kLeast;
   d.merge = seen > kLeast && d.units <= kMaxUnits;
-  d.target = d.merge ? kTarget : 0;
+  d.target = d.merge ? kTarget * 4 / d.W : 0;
   d.items = d.units * s.H;
-  if (d.merge) d.items = std::min(d.items + kTarget, d.items * ((seen + kLeast - 1) / kLeast));
+  if (d.merge) d.items = std::min(d.items + d.target, d.items * ((seen + kLeast - 1) / kLeast));
   return d;
 }
 
@@ -667,7 +699,8 @@ Deal deal(const CacheAttnShape& s) {
 size_t cache_attn_workspace_bytes(const CacheAttnShape& s) {
   const Deal d = deal(s);
   if (!d.merge) return 0;
-  return static_cast<size_t>(d.items) * d.rows * (s.D + 2) * sizeof(float);
+  return static_cast<size_t>(d.items) * d.rows * (s.D + 2) * sizeof(float) +
+         static_cast<size_t>(d.units) * 2 * sizeof(int32_t);
 }
 
 bool cache_attn_grid_ok(const CacheAttnShape& s) {
@@ -706,7 +739,8 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
     auto launch = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(d.items)), dim3(64 * d.W), 0, stream, a);
     };
-    if (d.half) launch(k_cache_attn<D, BITS, 1, true, 4>);
+    if (d.half && d.W == 8) launch(k_cache_attn<D, BITS, 1, true, 8>);
+    else if (d.half) launch(k_cache_attn<D, BITS, 1, true, 4>);
     else if (d.R == 1) launch(k_cache_attn<D, BITS, 1, false, 4>);
     else launch(k_cache_attn<D, BITS, 2, false, 4>);
     const hipError_t e = hipGetLastError();
