@@ -7,7 +7,6 @@ cannot be loaded, every call raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import os
@@ -526,9 +525,10 @@ def _same_device(device, **tensors):
 
 def _call(device: torch.device, what: str, fn, *args):
     """fn(*args, stream) on the device's current stream, with that device current."""
-    with contextlib.nullcontext() if torch.cuda.current_device() == device.index \
-            else torch.cuda.device(device):
-        status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _call(device, what, fn, *args)
+    status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
     if status != OK:
         raise VecattnError(status, what)
 

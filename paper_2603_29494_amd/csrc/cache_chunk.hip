@@ -1,0 +1,484 @@
+// Attention of many rows over the quantised cache (a chunk of a prompt, or drafts of
+// many heads): the cache's values are rebuilt once per 128 rows.
+//
+// A workgroup owns 128 rows (row = token * group + head; four waves of 32) and walks
+// its chunk of the tokens in tiles of 64 (two blocks of the cache).  The codes of a
+// tile are fetched two tiles ahead, turned into fp16 values m + s u (rounded once, by
+// one packed fma per pair) and put into LDS one tile ahead, in the order in which the
+// matrix instructions take them: K as [eight head-dim values][token], V as [eight
+// tokens][head-dim value], 16 bytes each, which is how the cache holds them, so that
+// neither needs a transpose.  S^T = K Q^T and O^T += V^T P^T run on
+// v_mfma_f32_32x32x16_f16.
+//
+// fp16 has eight times bf16's precision (a value and a weight are off by at most
+// 2^-11), and its range is made to fit by powers of two: a row of q is scaled to its
+// largest value, a tile of K to its largest (the scores take the power back), V to
+// the largest tile so far (O follows, and takes the power back at the end), and the
+// softmax weights to 2^7 at a row's maximum.
+//
+// MFMA 32x32x16 lane layout as in sparse_attn.hip: A: row l % 32, K-slots 8 g ..
+// 8 g + 7 (g = l / 32); B: column l % 32, the same slots; C: column l % 32, rows
+// 8 * (v / 4) + 4 g + v % 4.
+#include "cache_plan.h"
+
+namespace vecattn {
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
+
+constexpr int kTile = 64;       // tokens per tile
+constexpr float kBias = 7.0f;   // log2 of the weight at a row's reference
+
+__device__ __forceinline__ f16x2 to_f16(float x, float y) {
+  return __builtin_convertvector(f32x2{x, y}, f16x2);
+}
+
+// (m, s) of a group.
+__device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Eight codes as 1024 + u in fp16 (exact), in slot order.
+template <int BITS, bool V>
+__device__ __forceinline__ void spread8(const uint32_t* w, uint32_t (&r)[4]) {
+  if constexpr (BITS == 8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r[i] = __builtin_amdgcn_perm(0x64646464u, w[i >> 1], i & 1 ? 0x04030402u : 0x04010400u);
+  } else if constexpr (V) {   // slots (2 i, 2 i + 1) in nibbles i and i + 4
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = ((w[0] >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
+  } else {                    // slots 0..3 in the even nibbles, 4..7 in the odd
+    const uint32_t lo = w[0] & 0x0F0F0F0Fu, hi = (w[0] >> 4) & 0x0F0F0F0Fu;
+    r[0] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
+    r[1] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
+    r[2] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
+    r[3] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
+  }
+}
+
+template <int D, int BITS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_cache_chunk(
+    const AttnParams a) {
+  using L = CacheLayout<D, BITS>;
+  constexpr int G = L::kG, DW = L::kDw, DS = D / 16, DB = D / 32;
+  constexpr int kChunks = L::kRun / 4;      // 1 KB pieces of a block's K or V codes
+  constexpr int kUnits = 2 * kChunks;       // of a tile's
+  constexpr bool kSplit = kUnits < 4;       // two waves take K, two take V
+  constexpr int kPer = kSplit ? 1 : kUnits / 4;   // pieces a wave takes of either
+  constexpr int kItems = 4 / DW;            // octets of codes in a lane's 16 bytes
+  __shared__ __align__(16) f16x8 k_s[2][D / 8][kTile];
+  __shared__ __align__(16) f16x8 v_s[2][2][4][D];
+
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
+  const int n16 = lane & 15, g16 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  const int h = blockIdx.x % a.H;
+  const int index = blockIdx.x / a.H;
+  const int chunk = chunk_of(a, kChunkRows);
+  const Share share = find_share(a, kChunkRows, chunk, index);
+  if (share.unit < 0) return;
+  if (a.target && h == 0 && index == share.first && tid == 0)
+    shares_of(a, kChunkRows, D)[share.unit] = int2{share.first, share.count};
+  const int64_t b = share.unit / a.tiles;
+  const int row0 = share.unit % a.tiles * kChunkRows;
+  const Span s = span_of(a, b, row0, kChunkRows);
+  if (row0 >= s.rows) return;
+  const int t0 = (index - share.first) * (share.count > 1 ? chunk : 0);   // a multiple of 8
+  const int t1 = share.count > 1 ? min(s.total, t0 + chunk) : s.total;
+  const int ntiles = (t1 - t0 + 1) / 2;
+
+  // This lane's row.
+  const int row = row0 + 32 * wave + ln;
+  const int tok = row / a.group, hq = h * a.group + row % a.group;
+  const bool have = row < s.rows;
+  const int pos = have ? s.p_first + tok : -1;
+  // Positions of the wave's rows that exist.
+  const int w_lo = s.p_first + (row0 + 32 * wave) / a.group;
+  const int w_hi = s.p_first + (min(row0 + 32 * wave + 32, s.rows) - 1) / a.group;
+  f16x8 qf[DS];
+  float to_log2;
+  {
+    const u32x4* src =
+        reinterpret_cast<const u32x4*>(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN);
+    u32x4 w[DS];
+    float top = 0x1p-100f;
+#pragma unroll
+    for (int st = 0; st < DS; ++st) {
+      w[st] = u32x4{0, 0, 0, 0};
+      if (have) w[st] = src[2 * st + g];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        top = fmaxf(top, fmaxf(fabsf(low_of(w[st][e])), fabsf(step_of(w[st][e]))));
+    }
+    const int k = 15 - __builtin_amdgcn_frexp_expf(wave_max_xor32(top));
+#pragma unroll
+    for (int st = 0; st < DS; ++st) {
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = __builtin_bit_cast(
+            uint32_t, to_f16(__builtin_amdgcn_ldexpf(low_of(w[st][e]), k),
+                             __builtin_amdgcn_ldexpf(step_of(w[st][e]), k)));
+      qf[st] = __builtin_bit_cast(f16x8, x);
+    }
+    to_log2 = a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, -k);
+  }
+
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+  float m_run = kUnseen, l_run = 0.0f;
+  int v_exp = -200;   // O is in units of 2^v_exp
+
+  const int sh = a.page_shift - 5;
+  const ScalarInts pages = (ScalarInts)(a.table + b * a.cols);
+  // A block of the chunk: its first token, and where it lies (NULL: not held, or past
+  // the chunk).
+  auto first_token = [&](int t) __attribute__((always_inline)) {
+    return (t < s.ns ? t : s.nb0 + (t - s.ns)) * kCacheBlock;
+  };
+  auto place = [&](int t) __attribute__((always_inline)) -> const uint8_t* {
+    if (t >= t1) return nullptr;
+    const int jb = first_token(t) / kCacheBlock;
+    const int page = pages[jb >> sh];
+    if (page < 0 || page >= a.pages) return nullptr;
+    return a.data + (((static_cast<int64_t>(page) * a.H + h) << sh) + (jb & ((1 << sh) - 1))) *
+                        L::kBytes;
+  };
+
+  // What a wave holds of a tile before it is rebuilt: its pieces' codes, the (m, s)
+  // they need, and every token's, one per lane, for the tile's largest value.
+  struct Raw {
+    u32x4 kc[kPer], vc[kPer];
+    uint32_t kp[kPer][kItems], vp[kPer][8], km[G], vm[G];
+    uint32_t held;   // bit per block
+  };
+  // Which piece: block u / kChunks, 1 KB u % kChunks.
+  auto k_unit = [&](int i) __attribute__((always_inline)) { return kSplit ? wave & 1 : wave * kPer + i; };
+  const bool do_k = !kSplit || wave < 2, do_v = !kSplit || wave >= 2;
+  // Of octet i of a K piece: the 16 tokens it is of, and its 32 head-dim values.
+  auto k_token16 = [&](int c, int i) __attribute__((always_inline)) { return (c * kItems + i) / (D / 32); };
+  auto k_step = [&](int c, int i) __attribute__((always_inline)) { return (c * kItems + i) % (D / 32); };
+
+  auto fetch = [&](Raw& x, int tile) __attribute__((always_inline)) {
+    const uint8_t* at[2] = {place(t0 + 2 * tile), place(t0 + 2 * tile + 1)};
+    x.held = (at[0] ? 1u : 0u) | (at[1] ? 2u : 0u);
+    // A block that is not held is read from the cache's start and not used.
+    const uint8_t* blk[2] = {at[0] ? at[0] : a.data, at[1] ? at[1] : a.data};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int u = k_unit(i), c = u % kChunks;
+      const uint8_t* p = u / kChunks ? blk[1] : blk[0];
+      const uint32_t* par = reinterpret_cast<const uint32_t*>(p + L::kCodes);
+      if (do_k) {
+        x.kc[i] = *reinterpret_cast<const u32x4*>(p + (c * 64 + lane) * 16);
+#pragma unroll
+        for (int it = 0; it < kItems; ++it)
+          x.kp[i][it] = par[(16 * k_token16(c, it) + n16) * G + k_step(c, it) / 2];
+      }
+      if (do_v) {
+        p += L::kHalf;
+        par += L::kHalf / 4;
+        x.vc[i] = *reinterpret_cast<const u32x4*>(p + (c * 64 + lane) * 16);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          x.vp[i][e] = par[((e >> 2) * 16 + 4 * g16 + (e & 3)) * G + c / DW];
+      }
+    }
+    const uint8_t* p = (lane & 32 ? blk[1] : blk[0]) + L::kCodes + ln * G * 4;
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) {
+      x.km[gi] = *reinterpret_cast<const uint32_t*>(p + 4 * gi);
+      x.vm[gi] = *reinterpret_cast<const uint32_t*>(p + L::kHalf + 4 * gi);
+    }
+  };
+  const int end = s.p_hi + 1;   // tokens from here on are nobody's
+  auto live = [&](const Raw& x, int tile, int bl, int token) __attribute__((always_inline)) {
+    return (x.held >> bl & 1u) && first_token(t0 + 2 * tile + bl) + token < end;
+  };
+  // Power of two above every |m| and |m + s M| of the tile's tokens.
+  auto exponent = [&](const uint32_t (&w)[G], bool on) __attribute__((always_inline)) {
+    constexpr float M = BITS == 4 ? 15.0f : 255.0f;
+    float top = 0x1p-110f;
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) {
+      const float m = low_of(w[gi]), hi = __builtin_fmaf(step_of(w[gi]), M, m);
+      top = fmaxf(top, on ? fmaxf(fabsf(m), fabsf(hi)) : 0.0f);   // NaN: left out
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    return __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
+  };
+  // Rebuilds a tile into stage st; careful: groups that stand for NaN become 0 in V.
+  // Returns K's power; raises v_next to V's.
+  auto rebuild = [&](const Raw& x, int tile, int st, int& v_next, bool careful)
+                     __attribute__((always_inline)) {
+    const bool on = live(x, tile, g, ln);
+    const int ke = exponent(x.km, on) - 15;
+    v_next = max(v_next, exponent(x.vm, on) - 15);
+    const f16x2 minus = {_Float16(-1024.0f), _Float16(-1024.0f)};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int u = k_unit(i), c = u % kChunks, bl = u / kChunks;
+      if (do_k) {
+#pragma unroll
+        for (int it = 0; it < kItems; ++it) {
+          const int t16 = k_token16(c, it), st32 = k_step(c, it);
+          const uint32_t w = live(x, tile, bl, 16 * t16 + n16) ? x.kp[i][it] : 0u;
+          const float m = __builtin_amdgcn_ldexpf(low_of(w), -ke);
+          const float d = __builtin_amdgcn_ldexpf(step_of(w), -ke);
+          const f16x2 m2 = to_f16(m, m), d2 = to_f16(d, d);
+          uint32_t r[4];
+          uint32_t cw[DW];
+#pragma unroll
+          for (int e = 0; e < DW; ++e) cw[e] = x.kc[i][it * DW + e];
+          spread8<BITS, false>(cw, r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f16x2 y = __builtin_bit_cast(f16x2, r[e]) + minus;
+            r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, d2, m2));
+          }
+          k_s[st][4 * st32 + g16][32 * bl + 16 * t16 + n16] =
+              __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
+        }
+      }
+      if (do_v) {
+        f16x2 m2[4], d2[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float m[2], d[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int token = (e >> 1) * 16 + 4 * g16 + 2 * (e & 1) + y;
+            uint32_t w = live(x, tile, bl, token) ? x.vp[i][2 * e + y] : 0u;
+            if (careful && !(low_of(w) == low_of(w))) w = 0u;
+            m[y] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
+            d[y] = __builtin_amdgcn_ldexpf(step_of(w), -v_next);
+          }
+          m2[e] = to_f16(m[0], m[1]);
+          d2[e] = to_f16(d[0], d[1]);
+        }
+#pragma unroll
+        for (int it = 0; it < kItems; ++it) {
+          uint32_t r[4], cw[DW];
+#pragma unroll
+          for (int e = 0; e < DW; ++e) cw[e] = x.vc[i][it * DW + e];
+          spread8<BITS, true>(cw, r);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const f16x2 y = __builtin_bit_cast(f16x2, r[e]) + minus;
+            r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, d2[e], m2[e]));
+          }
+          v_s[st][bl][g16][16 * (c * kItems + it) + n16] =
+              __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
+        }
+      }
+    }
+    return ke;
+  };
+
+  auto sees = [&](int j) __attribute__((always_inline)) {
+    return j <= pos && (j > pos - a.window || j < a.sinks);
+  };
+  // Tile `tile` in stage st: scores (K in units of 2^ke), weights, products.
+  auto work = [&](int tile, int st, int ke, uint32_t blocks) __attribute__((always_inline)) {
+    f32x16 sc[2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      sc[hf] = f32x16{};
+#pragma unroll
+      for (int s2 = 0; s2 < DS; ++s2)
+        sc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_s[st][2 * s2 + g][32 * hf + ln], qf[s2],
+                                                        sc[hf], 0, 0, 0);
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int j0 = first_token(t0 + 2 * tile + hf);
+      const bool held = blocks >> hf & 1u;
+      if (held && j0 + 31 <= w_lo && (j0 > w_hi - a.window || j0 + 31 < a.sinks)) continue;
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        sc[hf][e] = held && sees(j0 + 8 * (e / 4) + 4 * g + e % 4) ? sc[hf][e] : kNegInf;
+    }
+    const float scale = to_log2 * __builtin_amdgcn_ldexpf(1.0f, ke);
+    f32x16 p[2];
+    float sum;
+    auto weigh = [&]() __attribute__((always_inline)) {
+      sum = 0.0f;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          p[hf][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[hf][e], scale, -m_run));
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          sum += (p[hf][e] + p[hf][e + 1]) + (p[hf][e + 2] + p[hf][e + 3]);
+      }
+    };
+    weigh();
+    // A row that has met no key, or whose weights would leave fp16, takes its
+    // reference from the tile's maximum first.
+    if (__any(sum > 32768.0f)) {
+      float top = kNegInf;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[hf][e]);
+      top = wave_max_xor32(top) * scale - kBias;
+      const float m_new = fmaxf(m_run, top);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      weigh();
+    }
+    l_run += sum;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int step = 0; step < 2; ++step) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int v0 = 8 * (e >> 1) + 4 * step + 2 * (e & 1);
+          w[e] = __builtin_bit_cast(uint32_t, to_f16(p[hf][v0], p[hf][v0 + 1]));
+        }
+        const f16x8 pb = __builtin_bit_cast(f16x8, w);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_s[st][hf][2 * step + g][32 * db + ln],
+                                                            pb, oacc[db], 0, 0, 0);
+      }
+  };
+  // O follows V's power.
+  auto follow = [&](int v_next) __attribute__((always_inline)) {
+    if (v_next == v_exp) return;
+    const float f = __builtin_amdgcn_ldexpf(1.0f, v_exp - v_next);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] *= f;
+    v_exp = v_next;
+  };
+
+  __shared__ int s_redo;
+  if (tid == 0) s_redo = 0;
+  if (ntiles > 0) {
+    Raw raw;
+    int v_next = v_exp;
+    fetch(raw, 0);
+    int ke = rebuild(raw, 0, 0, v_next, false);
+    uint32_t blocks = raw.held;
+    if (ntiles > 1) fetch(raw, 1);
+    for (int t = 0; t < ntiles; ++t) {
+      const int st = t & 1;
+      __syncthreads();
+      follow(v_next);
+      int ke1 = 0;
+      uint32_t blocks1 = 0;
+      if (t + 1 < ntiles) {
+        ke1 = rebuild(raw, t + 1, st ^ 1, v_next, false);
+        blocks1 = raw.held;
+        if (t + 2 < ntiles) fetch(raw, t + 2);
+      }
+      work(t, st, ke, blocks);
+      ke = ke1;
+      blocks = blocks1;
+    }
+  }
+
+  // A group of V that stands for NaN reaches rows that do not see its token (0 * NaN
+  // in the product).  So a workgroup with anything not finite walks its tiles again,
+  // with such groups taken out of the products and added to the rows that see them.
+  float fin = l_run * 0.0f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) fin = __builtin_fmaf(oacc[db][e], 0.0f, fin);
+  __syncthreads();
+  if (__any(have && fin != 0.0f) && lane == 0) s_redo = 1;
+  __syncthreads();
+  if (__builtin_amdgcn_readfirstlane(s_redo)) {
+    m_run = kUnseen;
+    l_run = 0.0f;
+    v_exp = -200;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
+#pragma unroll 1
+    for (int t = 0; t < ntiles; ++t) {
+      Raw raw;
+      int v_next = v_exp;
+      fetch(raw, t);
+      __syncthreads();
+      const int ke = rebuild(raw, t, 0, v_next, true);
+      __syncthreads();
+      follow(v_next);
+      work(t, 0, ke, raw.held);
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi) {
+        const bool nan = live(raw, t, g, ln) && !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));
+        for (uint64_t left = __ballot(nan); left; left &= left - 1) {
+          const int i = __builtin_ctzll(left);
+          if (!sees(first_token(t0 + 2 * t + (i >> 5)) + (i & 31))) continue;
+#pragma unroll
+          for (int db = 2 * gi; db < 2 * gi + 2; ++db)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) oacc[db][e] = __builtin_nanf("");
+        }
+      }
+    }
+  }
+
+  l_run += __shfl_xor(l_run, 32);
+  if (!have) return;
+  const float back = __builtin_amdgcn_ldexpf(1.0f, v_exp);
+  if (share.count > 1) {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kChunkRows + 32 * wave + ln;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int vq = 0; vq < 4; ++vq) {
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = oacc[db][4 * vq + e] * back;
+        *reinterpret_cast<f32x4*>(a.part + at * D + 32 * db + 8 * vq + 4 * g) = y;
+      }
+    if (g == 0) {
+      float* ml = a.part + static_cast<int64_t>(a.items) * kChunkRows * D + at * 2;
+      ml[0] = m_run;
+      ml[1] = l_run;
+    }
+    return;
+  }
+  const float inv = (l_run > 0.0f ? 1.0f / l_run : l_run);   // no key: 0; NaN stays
+  uint16_t* orow = a.o + b * a.o_sB + hq * a.o_sH + tok * a.o_sN;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int vq = 0; vq < 4; ++vq) {
+      f32x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = oacc[db][4 * vq + e] * inv * back;
+      *reinterpret_cast<bf16x4*>(orow + 32 * db + 8 * vq + 4 * g) = __builtin_convertvector(y, bf16x4);
+    }
+  if (a.lse && g == 0)
+    a.lse[(b * a.H * a.group + hq) * a.n + tok] =
+        l_run == 0.0f ? kNegInf : (m_run + __builtin_log2f(l_run)) * kLn2;
+}
+
+}  // namespace
+
+hipError_t launch_cache_chunk(const AttnParams& a, int32_t D, int32_t bits, int64_t items,
+                              hipStream_t stream) {
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(items)), dim3(256), 0, stream, a);
+  };
+  if (D == 128) bits == 4 ? run(k_cache_chunk<128, 4>) : run(k_cache_chunk<128, 8>);
+  else bits == 4 ? run(k_cache_chunk<64, 4>) : run(k_cache_chunk<64, 8>);
+  return hipGetLastError();
+}
+
+}  // namespace vecattn

@@ -1,0 +1,142 @@
+// How the attention over the cache deals its work out: what a row tile sees of a
+// sequence's tokens, and the chunks that the blocks of all row tiles are cut into.
+// Shared by the kernels of a few rows (cache_attn.hip) and of many (cache_chunk.hip).
+#pragma once
+
+#include "cache_common.h"
+
+namespace vecattn {
+
+constexpr float kUnseen = -3.4028234663852886e38f;  // reference of a row that has met no key
+constexpr int32_t kMaxLen = 1 << 30;                 // positions stay in 32 bits
+constexpr float kLn2 = 0.69314718055994531f;
+
+struct AttnParams {
+  const uint16_t* q;
+  int64_t q_sB, q_sH, q_sN;
+  uint16_t* o;
+  int64_t o_sB, o_sH, o_sN;
+  float* lse;
+  const uint8_t* data;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* n_new;
+  float* part;       // [item][rows of a tile][D] sums, then [item][rows of a tile] (m, l)
+  int32_t cols, pages;   // pages past the first 2^31 - 1 cannot be named
+  int32_t window, sinks;
+  int32_t H, n, group, page_shift;
+  int32_t tiles;     // row tiles per head
+  int32_t units;     // row tiles of all sequences
+  int32_t items;     // chunks that partial results have room for
+  int32_t target;    // chunks to aim at (0: one per row tile)
+  int32_t least;     // blocks of a chunk at least
+  float scale_log2;
+};
+
+// What one row tile sees, in blocks of 32 tokens: the first `ns` blocks (sinks),
+// then blocks nb0 ..; `total` of both.
+struct Span {
+  int32_t p_first;      // position of the sequence's row 0
+  int32_t p_lo, p_hi;   // positions of the tile's rows
+  int32_t ns, nb0, total;
+  int32_t rows;         // rows of the sequence (all tiles)
+};
+
+__device__ __forceinline__ Span span_of(const AttnParams& a, int64_t b, int row0, int nrows) {
+  Span s;
+  const int len = min(max(a.lens[b], 0), kMaxLen);
+  const int nb = a.n_new ? min(max(a.n_new[b], 0), a.n) : a.n;
+  s.p_first = len - nb;
+  s.rows = nb * a.group;
+  s.p_lo = s.p_first + row0 / a.group;
+  s.p_hi = s.p_first + (min(row0 + nrows, s.rows) - 1) / a.group;
+  s.ns = s.nb0 = s.total = 0;
+  if (row0 >= s.rows || s.p_hi < 0) return s;
+  const int near = max(0, s.p_lo - a.window + 1);
+  s.nb0 = near >> 5;
+  s.ns = min(s.nb0, (min(a.sinks, near) + 31) >> 5);
+  // Tokens past the table are held nowhere.
+  const int held = a.cols << (a.page_shift - 5);
+  const int end = min((s.p_hi >> 5) + 1, held);
+  s.ns = min(s.ns, held);
+  s.total = s.ns + max(0, end - s.nb0);
+  return s;
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// Blocks per chunk, so that all row tiles together make about `target` chunks.
+// Every wave of every workgroup computes the same (64 row tiles at a time).
+__device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows) {
+  if (a.target == 0) return kMaxLen;
+  const int lane = threadIdx.x & 63;
+  int sum = 0;   // <= 256 row tiles of 2^25 blocks, in units of 8 blocks
+  for (int u = lane; u < a.units; u += 64)
+    sum += (span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows).total + 7) >> 3;
+  sum = __builtin_amdgcn_readfirstlane(wave_sum(sum));
+  const int64_t blocks = static_cast<int64_t>(sum) * 8 * a.H;
+  const int chunk = static_cast<int>((blocks + a.target - 1) / a.target);
+  return (max(chunk, a.least) + 7) & ~7;
+}
+
+// Row tile `unit`'s chunks are those from `first` on, `count` of them (stored for the
+// join behind the partial results).
+struct Share {
+  int32_t unit, first, count;
+};
+
+__device__ __forceinline__ int chunks_in(const Span& s, int chunk) {
+  return max(1, (s.total + chunk - 1) / chunk);
+}
+
+// The share that chunk `index` belongs to; unit < 0 if there is none.
+__device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, int chunk,
+                                            int index) {
+  if (a.target == 0) return Share{index < a.units ? index : -1, index, 1};
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int u0 = 0; u0 < a.units; u0 += 64) {
+    const int u = u0 + lane;
+    int count = 0;
+    if (u < a.units)
+      count = chunks_in(span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows), chunk);
+    int incl = count;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(incl, o);
+      if (lane >= o) incl += y;
+    }
+    const int first = before + incl - count;
+    const uint64_t at = __ballot(u < a.units && index >= first && index < first + count);
+    if (at) {
+      const int l = __builtin_ctzll(at);
+      return Share{u0 + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(count, l)};
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return Share{-1, 0, 0};
+}
+
+__device__ __forceinline__ int2* shares_of(const AttnParams& a, int tile_rows, int D) {
+  return reinterpret_cast<int2*>(a.part + static_cast<int64_t>(a.items) * tile_rows * (D + 2));
+}
+
+// How a call is dealt out; depends on its shapes alone, so that the workspace
+// query and the launch agree.
+struct Deal {
+  bool many, half;   // which kernel takes it
+  int32_t R, W, rows, tiles, target, least;
+  int64_t units, items;
+  bool merge;
+};
+
+hipError_t launch_cache_chunk(const AttnParams& a, int32_t D, int32_t bits, int64_t items,
+                              hipStream_t stream);
+
+constexpr int kChunkRows = 128;   // rows per workgroup of that kernel
+
+}  // namespace vecattn

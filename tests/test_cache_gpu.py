@@ -243,10 +243,11 @@ def test_pages_that_are_not_there(gpu, n, window, sinks):
     assert (lse[1] == -math.inf).all()
 
 
+@pytest.mark.parametrize("n", [4, 40])
 @pytest.mark.parametrize("D,bits", [(128, 4), (64, 8)])
-def test_hidden_tokens_never_reach_a_row(gpu, D, bits):
+def test_hidden_tokens_never_reach_a_row(gpu, D, bits, n):
     """NaN groups outside a row's window change nothing; inside they make it NaN."""
-    L, n, window = 300, 4, 60
+    L, window = 300, 60
     table, pages = paged([L], 32)
     k, v = rows(601, 1, 1, L, D), rows(602, 1, 1, L, D)
     q = rows(603, 1, 2, n, D)
@@ -257,7 +258,7 @@ def test_hidden_tokens_never_reach_a_row(gpu, D, bits):
         va.cache_write(cache, kk, vv, table, lens)
         return va.cache_attn(q, cache, table, lens, window=window, sinks=1)
     clean = run(k, v)
-    at = L - n - window + 3     # rows see from L - n + r - window + 1 on: row r sees it if r <= 2
+    at = L - n - window + 3     # row r sees from L - n + r - window + 1 on: the first three do
     seen = torch.tensor([L - n + r - window < at for r in range(n)]).cuda()
     assert seen.any() and not seen.all()
     for bad in ("k", "v"):
@@ -381,3 +382,27 @@ def test_a_model_layer_in_use(gpu, bits):
     assert same(gk, bf16_value(k[:, :, :N], bits)) and same(gv, bf16_value(v[:, :, :N], bits))
     idx, cnt = va.select(q, gk, 64, "topk", 0.2, True)
     assert va.check_lists(idx, cnt, N) == 0
+
+
+@pytest.mark.parametrize("D,bits,page", FORMATS)
+@pytest.mark.parametrize("n,Hq,H,window,sinks", [(33, 1, 1, None, 0), (150, 2, 1, None, 0),
+                                                 (64, 7, 1, 100, 40), (300, 1, 1, 1, 5)])
+def test_chunks_of_a_prompt(gpu, n, Hq, H, window, sinks, D, bits, page):
+    """More than 32 rows per key/value head, over sequences that end in a block's middle; split
+    over the keys where they are long."""
+    attn_case(800, [n + 1, 2500, n], Hq, H, n, D, bits, page, window, sinks)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -60, 1e-6, 3e4, 2.0 ** 60])
+@pytest.mark.parametrize("n", [1, 20, 50])
+def test_magnitudes(gpu, n, scale):
+    """Values far from 1, in K against 1 / scale in Q, in V, and growing along a sequence."""
+    L, D = 700, 128
+    table, pages = paged([L], 64)
+    g = torch.linspace(-6, 0, L).exp2().bfloat16().cuda()[None, None, :, None]
+    k, v = rows(851, 1, 1, L, D) * scale, rows(852, 1, 1, L, D) * scale * g
+    q = rows(853, 1, 2, n, D) / scale
+    cache = fresh_cache(pages, 1, D, 64, 4)
+    va.cache_write(cache, k, v, table, int32([L]))
+    o, lse = va.cache_attn(q, cache, table, int32([L]), return_lse=True)
+    ref.check(o, lse, ref.cache_attn(q, [k[0].cpu()], [v[0].cpu()], 4, [L]))

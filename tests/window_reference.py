@@ -9,13 +9,17 @@ x_j = v_j (bf16 rows) or s_j u_j = v_j - m_j (the cache), and e the error of a s
 relative error is about e, and the normaliser's again).  A score of D products accumulated in
 fp32 is off by at most (D + 8) 2^-23 of the sum of its terms' magnitudes (2^-23 a step, so that
 truncating additions are covered too); the cache's 4-bit codes enter as 16 + u, so their terms
-are |q| s (16 + u) and 16 |q| s.  The sums over keys add n 2^-23 of theirs.  lse is off by e, the
+are |q| s (16 + u) and 16 |q| s.  Calls of more than 32 rows per key/value head take the cache's
+values and the weights rounded to fp16 (half a step: 2^-11; scaled by powers of two so that what
+lies below its normal range is under 2^-29 of the largest): 2^-11 |q k| more in a score, and
+2 * 2^-11 sum_j w_j |v_j| in place of 2^-8 sum_j w_j |x_j|.  The sums over keys add n 2^-23 of theirs.  lse is off by e, the
 normaliser's n 2^-23 and four ulps of its own fp32 value."""
 import math
 
 import torch
 
 HALF = 2.0 ** -8
+HALF16 = 2.0 ** -11
 STEP = 2.0 ** -23
 GROUP = 64
 
@@ -55,7 +59,7 @@ def sees(p, j, window, sinks, causal, L):
     return (near | (j < sinks)) & (j < L) & ((j <= p) if causal else torch.ones_like(near))
 
 
-def attend(q, k, v, mask, scale, kmag=None, vmag=None, vround=None):
+def attend(q, k, v, mask, scale, kmag=None, vmag=None, vround=None, fp16=False):
     """One head: q [n, D], k, v [L, D] float64 where mask [n, L].  Returns o, lse and their
     bounds.  kmag, vmag: magnitudes that enter the fp32 sums in place of |k|, |v|; vround: what
     the rounded weights multiply."""
@@ -69,12 +73,15 @@ def attend(q, k, v, mask, scale, kmag=None, vmag=None, vround=None):
     x = (q @ k.t()) * scale
     x = x.masked_fill(~mask, -math.inf)
     err = ((q.abs() @ kmag.t()) * scale * (D + 8) * STEP).masked_fill(~mask, 0.0)
+    if fp16:
+        err += ((q.abs() @ k.abs().t()) * scale * HALF16 * (1 + HALF)).masked_fill(~mask, 0.0)
     e = err.amax(1, keepdim=True) if mask.shape[1] else torch.zeros(n, 1, dtype=torch.float64)
     lse = torch.logsumexp(x, 1)
     w = torch.exp(x - torch.where(lse == -math.inf, torch.zeros_like(lse), lse)[:, None])
     o = w @ v
     cnt = mask.sum(1, keepdim=True).double()
-    bound = (HALF * (w @ vround) * (1 + HALF) + HALF * o.abs() * (1 + 2 * HALF)
+    rounded = 2 * HALF16 * (w @ v.abs()) if fp16 else HALF * (w @ vround)
+    bound = (rounded * (1 + HALF) + HALF * o.abs() * (1 + 2 * HALF)
              + (2 * e + (cnt + 16) * STEP) * (w @ vmag) + 1e-30)
     finite = torch.where(torch.isfinite(lse), lse.abs(), torch.zeros_like(lse))
     lse_bound = e[:, 0] + (cnt[:, 0] + 8) * STEP + 8 * STEP * finite
@@ -135,7 +142,8 @@ def cache_attn(q, k, v, bits, lens, n_new=None, window=1 << 30, sinks=0, scale=0
             kmag = spread(km).abs() + spread(ks) * (ku + 2 * off)
             vmag = spread(vm).abs() + spread(vs) * (vu + 2 * off)
             for h in range(g * (Hq // Hkv), (g + 1) * (Hq // Hkv)):
-                r = attend(q[b, h, :nb], kk, vv, mask, scale, kmag, vmag, spread(vs) * vu)
+                r = attend(q[b, h, :nb], kk, vv, mask, scale, kmag, vmag, spread(vs) * vu,
+                           fp16=n * (Hq // Hkv) > 32)
                 o[b, h, :nb], lse[b, h, :nb], ob[b, h, :nb], lb[b, h, :nb] = r
     return o, lse, ob, lb
 
