@@ -562,7 +562,7 @@ Deal deal(const CacheAttnShape& s) {
   constexpr int64_t kTarget = 512, kLeast = 32, kMaxUnits = 256;
   d.least = kLeast;
   d.merge = seen > kLeast && d.units <= kMaxUnits;
-  d.target = d.merge ? kTarget * 4 / d.W : 0;
+  d.target = d.merge ? d.many ? 1024 : kTarget * 4 / d.W : 0;
   d.items = d.units * s.H;
   if (d.merge) d.items = std::min(d.items + d.target, d.items * ((seen + kLeast - 1) / kLeast));
   return d;

@@ -19,6 +19,8 @@
 // MFMA 32x32x16 lane layout as in sparse_attn.hip: A: row l % 32, K-slots 8 g ..
 // 8 g + 7 (g = l / 32); B: column l % 32, the same slots; C: column l % 32, rows
 // 8 * (v / 4) + 4 g + v % 4.
+#include <type_traits>
+
 #include "cache_plan.h"
 
 namespace vecattn {
@@ -39,6 +41,32 @@ __device__ __forceinline__ f16x2 to_f16(float x, float y) {
 // (m, s) of a group.
 __device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Largest value over the wave, on every lane (a scalar).
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    const int y = __builtin_amdgcn_update_dpp(static_cast<int>(x), static_cast<int>(x),
+                                              decltype(ctrl)::value, decltype(rows)::value, 0xf,
+                                              false);
+    x = max(x, static_cast<uint32_t>(y));
+  };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});   // row_shr:1
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // row_bcast:15
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Barrier for LDS alone: the wave's loads from memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // Eight codes as 1024 + u in fp16 (exact), in slot order.
 template <int BITS, bool V>
@@ -154,7 +182,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   // they need, and every token's, one per lane, for the tile's largest value.
   struct Raw {
     u32x4 kc[kPer], vc[kPer];
-    uint32_t kp[kPer][kItems], vp[kPer][8], km[G], vm[G];
+    uint32_t kp[kPer][kItems], vp[8], km[G], vm[G];   // a wave's V pieces share a block and a group
     uint32_t held;   // bit per block
   };
   // Which piece: block u / kChunks, 1 KB u % kChunks.
@@ -184,9 +212,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         p += L::kHalf;
         par += L::kHalf / 4;
         x.vc[i] = *reinterpret_cast<const u32x4*>(p + (c * 64 + lane) * 16);
+        if (i == 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          x.vp[i][e] = par[((e >> 2) * 16 + 4 * g16 + (e & 3)) * G + c / DW];
+          for (int e = 0; e < 8; ++e)
+            x.vp[e] = par[((e >> 2) * 16 + 4 * g16 + (e & 3)) * G + c / DW];
+        }
       }
     }
     const uint8_t* p = (lane & 32 ? blk[1] : blk[0]) + L::kCodes + ln * G * 4;
@@ -197,30 +227,60 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
   };
   const int end = s.p_hi + 1;   // tokens from here on are nobody's
-  auto live = [&](const Raw& x, int tile, int bl, int token) __attribute__((always_inline)) {
-    return (x.held >> bl & 1u) && first_token(t0 + 2 * tile + bl) + token < end;
+  auto left_in = [&](const Raw& x, int tile, int bl) __attribute__((always_inline)) {
+    return x.held >> bl & 1u ? min(kCacheBlock, end - first_token(t0 + 2 * tile + bl)) : 0;
   };
   // Power of two above every |m| and |m + s M| of the tile's tokens.
-  auto exponent = [&](const uint32_t (&w)[G], bool on) __attribute__((always_inline)) {
+  auto exponent = [&](const uint32_t (&w)[G]) __attribute__((always_inline)) {
     constexpr float M = BITS == 4 ? 15.0f : 255.0f;
     float top = 0x1p-110f;
 #pragma unroll
     for (int gi = 0; gi < G; ++gi) {
       const float m = low_of(w[gi]), hi = __builtin_fmaf(step_of(w[gi]), M, m);
-      top = fmaxf(top, on ? fmaxf(fabsf(m), fabsf(hi)) : 0.0f);   // NaN: left out
+      top = fmaxf(top, fmaxf(fabsf(m), fabsf(hi)));   // NaN: left out
     }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    return __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(top));
+    return __builtin_amdgcn_frexp_expf(__uint_as_float(wave_max(__float_as_uint(top))));
   };
   // Rebuilds a tile into stage st; careful: groups that stand for NaN become 0 in V.
   // Returns K's power; raises v_next to V's.
-  auto rebuild = [&](const Raw& x, int tile, int st, int& v_next, bool careful)
+  auto rebuild = [&](Raw& x, int tile, int st, int& v_next, bool careful)
                      __attribute__((always_inline)) {
-    const bool on = live(x, tile, g, ln);
-    const int ke = exponent(x.km, on) - 15;
-    v_next = max(v_next, exponent(x.vm, on) - 15);
+    // Tokens of no page and past the rows' last: as if m = s = 0.
+    const int left[2] = {left_in(x, tile, 0), left_in(x, tile, 1)};
+    if (min(left[0], left[1]) < kCacheBlock) {
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi)
+        if (ln >= (g ? left[1] : left[0])) x.km[gi] = x.vm[gi] = 0u;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int u = k_unit(i), lim = u / kChunks ? left[1] : left[0];
+#pragma unroll
+        for (int it = 0; it < kItems; ++it)
+          if (16 * k_token16(u % kChunks, it) + n16 >= lim) x.kp[i][it] = 0u;
+        if (i == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if ((e >> 2) * 16 + 4 * g16 + (e & 3) >= lim) x.vp[e] = 0u;
+        }
+      }
+    }
+    const int ke = exponent(x.km) - 15;
+    v_next = max(v_next, exponent(x.vm) - 15);
     const f16x2 minus = {_Float16(-1024.0f), _Float16(-1024.0f)};
+    f16x2 m2[4], d2[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float m[2], d[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        uint32_t w = x.vp[2 * e + y];
+        if (careful && !(low_of(w) == low_of(w))) w = 0u;
+        m[y] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
+        d[y] = __builtin_amdgcn_ldexpf(step_of(w), -v_next);
+      }
+      m2[e] = to_f16(m[0], m[1]);
+      d2[e] = to_f16(d[0], d[1]);
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int u = k_unit(i), c = u % kChunks, bl = u / kChunks;
@@ -228,10 +288,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
         for (int it = 0; it < kItems; ++it) {
           const int t16 = k_token16(c, it), st32 = k_step(c, it);
-          const uint32_t w = live(x, tile, bl, 16 * t16 + n16) ? x.kp[i][it] : 0u;
+          const uint32_t w = x.kp[i][it];
           const float m = __builtin_amdgcn_ldexpf(low_of(w), -ke);
           const float d = __builtin_amdgcn_ldexpf(step_of(w), -ke);
-          const f16x2 m2 = to_f16(m, m), d2 = to_f16(d, d);
+          const f16x2 km2 = to_f16(m, m), kd2 = to_f16(d, d);
           uint32_t r[4];
           uint32_t cw[DW];
 #pragma unroll
@@ -240,28 +300,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const f16x2 y = __builtin_bit_cast(f16x2, r[e]) + minus;
-            r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, d2, m2));
+            r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, kd2, km2));
           }
           k_s[st][4 * st32 + g16][32 * bl + 16 * t16 + n16] =
               __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
         }
       }
       if (do_v) {
-        f16x2 m2[4], d2[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float m[2], d[2];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int token = (e >> 1) * 16 + 4 * g16 + 2 * (e & 1) + y;
-            uint32_t w = live(x, tile, bl, token) ? x.vp[i][2 * e + y] : 0u;
-            if (careful && !(low_of(w) == low_of(w))) w = 0u;
-            m[y] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
-            d[y] = __builtin_amdgcn_ldexpf(step_of(w), -v_next);
-          }
-          m2[e] = to_f16(m[0], m[1]);
-          d2[e] = to_f16(d[0], d[1]);
-        }
 #pragma unroll
         for (int it = 0; it < kItems; ++it) {
           uint32_t r[4], cw[DW];
@@ -375,7 +420,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     if (ntiles > 1) fetch(raw, 1);
     for (int t = 0; t < ntiles; ++t) {
       const int st = t & 1;
-      __syncthreads();
+      lds_barrier();
       follow(v_next);
       int ke1 = 0;
       uint32_t blocks1 = 0;
@@ -419,7 +464,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       work(t, 0, ke, raw.held);
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
-        const bool nan = live(raw, t, g, ln) && !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));
+        const bool nan = !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));   // 0 where hidden
         for (uint64_t left = __ballot(nan); left; left &= left - 1) {
           const int i = __builtin_ctzll(left);
           if (!sees(first_token(t0 + 2 * t + (i >> 5)) + (i & 31))) continue;
