@@ -210,8 +210,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2
 
   const int h = blockIdx.x % a.H;
   const int index = blockIdx.x / a.H;
-  const int chunk = chunk_of(a, kRows);
-  const Share share = find_share(a, kRows, chunk, index);
+  const Share share = find_share(a, kRows, index);
   if (share.unit < 0) return;
   if (a.target && h == 0 && index == share.first && threadIdx.x == 0)
     shares_of(a, kRows, D)[share.unit] = int2{share.first, share.count};
@@ -219,8 +218,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2
   const int row0 = share.unit % a.tiles * kRows;
   const Span s = span_of(a, b, row0, kRows);
   if (row0 >= s.rows) return;
-  const int t0 = (index - share.first) * (share.count > 1 ? chunk : 0);
-  const int t1 = share.count > 1 ? min(s.total, t0 + chunk) : s.total;
+  const int t0 = (index - share.first) * (share.count > 1 ? share.chunk : 0);
+  const int t1 = share.count > 1 ? min(s.total, t0 + share.chunk) : s.total;
 
   // The t-th block this row tile sees, and its page; where no page is held, or past
   // the last block, a block that can be read and is not used.
@@ -492,15 +491,18 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2
   }
 }
 
-// Joins the chunks of a row: a workgroup per row, its four waves taking every
-// fourth chunk, a lane D / 64 values.  Rows of one chunk are done already.
-template <int D>
-__global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t tile_rows) {
-  constexpr int V = D / 64;
+// Joins the chunks of a row: WAVES waves per row take every WAVES-th chunk, a lane
+// D / 64 values.  Rows of one chunk are done already.
+template <int D, int WAVES>
+__global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t tile_rows,
+                                                     int64_t total_rows) {
+  constexpr int V = D / 64, kRowsPer = 4 / WAVES;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int rows_all = a.n * a.group;
-  const int row = static_cast<int>(blockIdx.x % rows_all);
-  const int bh = static_cast<int>(blockIdx.x / rows_all);
+  const int64_t id = static_cast<int64_t>(blockIdx.x) * kRowsPer + wave / WAVES;
+  if (id >= total_rows) return;   // whole workgroups with four waves per row
+  const int row = static_cast<int>(id % rows_all);
+  const int bh = static_cast<int>(id / rows_all);
   const int h = bh % a.H;
   const int64_t b = bh / a.H;
   const int tile = row / tile_rows;
@@ -520,25 +522,34 @@ __global__ __launch_bounds__(256) void k_cache_merge(const AttnParams a, int32_t
   for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
   float l = 0.0f, y[V] = {};
 #pragma unroll 4
-  for (int i = wave; i < count; i += 4) {
+  for (int i = wave % WAVES; i < count; i += WAVES) {
     const float alpha = __builtin_amdgcn_exp2f(ml[i * step * 2] - m);
     l = __builtin_fmaf(ml[i * step * 2 + 1], alpha, l);
 #pragma unroll
     for (int x = 0; x < V; ++x) y[x] = __builtin_fmaf(src[i * step * D + x], alpha, y[x]);
   }
-  __shared__ float s_y[4][D + 1];
+  if constexpr (WAVES > 1) {
+    __shared__ float s_y[WAVES][D + 1];
 #pragma unroll
-  for (int x = 0; x < V; ++x) s_y[wave][V * lane + x] = y[x];
-  if (lane == 0) s_y[wave][D] = l;
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  const int d = threadIdx.x;
-  l = (s_y[0][D] + s_y[1][D]) + (s_y[2][D] + s_y[3][D]);
-  const float v = (s_y[0][d] + s_y[1][d]) + (s_y[2][d] + s_y[3][d]);
+    for (int x = 0; x < V; ++x) s_y[wave][V * lane + x] = y[x];
+    if (lane == 0) s_y[wave][D] = l;
+    __syncthreads();
+    if (wave > 0) return;
+    l = 0.0f;
+#pragma unroll
+    for (int x = 0; x < V; ++x) y[x] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      l += s_y[w][D];
+#pragma unroll
+      for (int x = 0; x < V; ++x) y[x] += s_y[w][V * lane + x];
+    }
+  }
   const float inv = l > 0.0f ? 1.0f / l : l;
-  reinterpret_cast<__bf16*>(a.o)[b * a.o_sB + hq * a.o_sH + tok * a.o_sN + d] =
-      static_cast<__bf16>(v * inv);
-  if (a.lse && d == 0)
+  __bf16* orow = reinterpret_cast<__bf16*>(a.o) + b * a.o_sB + hq * a.o_sH + tok * a.o_sN;
+#pragma unroll
+  for (int x = 0; x < V; ++x) orow[V * lane + x] = static_cast<__bf16>(y[x] * inv);
+  if (a.lse && lane == 0)
     a.lse[(b * a.H * a.group + hq) * a.n + tok] =
         l == 0.0f ? kNegInf : (m + __builtin_log2f(l)) * kLn2;
 }
@@ -559,12 +570,19 @@ Deal deal(const CacheAttnShape& s) {
   const int64_t seen = std::min(held, (std::min<int64_t>(s.window, held * 32) +
                                        std::min<int64_t>(s.n, d.rows) + 31) / 32 + 1 +
                                           (std::min<int64_t>(s.sinks, held * 32) + 31) / 32);
-  constexpr int64_t kTarget = 512, kLeast = 32, kMaxUnits = 256;
+  constexpr int64_t kLeast = 32;
   d.least = kLeast;
   d.merge = seen > kLeast && d.units <= kMaxUnits;
-  d.target = d.merge ? d.many ? 1024 : kTarget * 4 / d.W : 0;
   d.items = d.units * s.H;
-  if (d.merge) d.items = std::min(d.items + d.target, d.items * ((seen + kLeast - 1) / kLeast));
+  d.target = 0;
+  if (d.merge) {
+    // Workgroups that run at a time (two of four waves per CU, or one of eight), once,
+    // or twice where a workgroup's work is long, and at least twice the row tiles.
+    const int64_t slots = 256 * 8 / d.W;
+    const int64_t rounds = std::max<int64_t>(d.many ? 2 : 1, (2 * d.items + slots - 1) / slots);
+    d.target = static_cast<int32_t>(slots * rounds);
+    d.items = std::min<int64_t>(d.target, d.items * ((seen + kLeast - 1) / kLeast));
+  }
   return d;
 }
 
@@ -622,9 +640,14 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
     else launch(k_cache_attn<D, BITS, 2, false, 4>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !d.merge) return e;
-    hipLaunchKernelGGL(k_cache_merge<D>,
-                       dim3(static_cast<unsigned>(x.shape.B * x.shape.Hq * x.shape.n)), dim3(256), 0,
-                       stream, a, d.rows);
+    // A wave per row where rows fill the chip, four where they do not.
+    const int64_t n = x.shape.B * x.shape.Hq * x.shape.n;
+    if (n > 2048)
+      hipLaunchKernelGGL((k_cache_merge<D, 1>), dim3(static_cast<unsigned>((n + 3) / 4)), dim3(256),
+                         0, stream, a, d.rows, n);
+    else
+      hipLaunchKernelGGL((k_cache_merge<D, 4>), dim3(static_cast<unsigned>(n)), dim3(256), 0, stream,
+                         a, d.rows, n);
     return hipGetLastError();
   };
   using std::integral_constant;

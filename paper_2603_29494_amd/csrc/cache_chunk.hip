@@ -106,8 +106,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
   const int h = blockIdx.x % a.H;
   const int index = blockIdx.x / a.H;
-  const int chunk = chunk_of(a, kChunkRows);
-  const Share share = find_share(a, kChunkRows, chunk, index);
+  const Share share = find_share(a, kChunkRows, index);
   if (share.unit < 0) return;
   if (a.target && h == 0 && index == share.first && tid == 0)
     shares_of(a, kChunkRows, D)[share.unit] = int2{share.first, share.count};
@@ -115,8 +114,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int row0 = share.unit % a.tiles * kChunkRows;
   const Span s = span_of(a, b, row0, kChunkRows);
   if (row0 >= s.rows) return;
-  const int t0 = (index - share.first) * (share.count > 1 ? chunk : 0);   // a multiple of 8
-  const int t1 = share.count > 1 ? min(s.total, t0 + chunk) : s.total;
+  const int t0 = (index - share.first) * (share.count > 1 ? share.chunk : 0);   // a multiple of 8
+  const int t1 = share.count > 1 ? min(s.total, t0 + share.chunk) : s.total;
   const int ntiles = (t1 - t0 + 1) / 2;
 
   // This lane's row.

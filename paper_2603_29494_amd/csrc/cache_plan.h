@@ -28,10 +28,25 @@ struct AttnParams {
   int32_t tiles;     // row tiles per head
   int32_t units;     // row tiles of all sequences
   int32_t items;     // chunks that partial results have room for
-  int32_t target;    // chunks to aim at (0: one per row tile)
+  int32_t target;    // most chunks, of all heads (0: one per row tile)
   int32_t least;     // blocks of a chunk at least
   float scale_log2;
 };
+
+// Inclusive prefix sum over the wave with DPP moves (see select_common.h), and its
+// last value.
+__device__ __forceinline__ int wave_incl_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
+  return x;
+}
+__device__ __forceinline__ int wave_total(int x) {
+  return __builtin_amdgcn_readlane(wave_incl_scan(x), 63);
+}
 
 // What one row tile sees, in blocks of 32 tokens: the first `ns` blocks (sinks),
 // then blocks nb0 ..; `total` of both.
@@ -63,62 +78,59 @@ __device__ __forceinline__ Span span_of(const AttnParams& a, int64_t b, int row0
   return s;
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-  return x;
-}
-
-// Blocks per chunk, so that all row tiles together make about `target` chunks.
-// Every wave of every workgroup computes the same (64 row tiles at a time).
-__device__ __forceinline__ int chunk_of(const AttnParams& a, int tile_rows) {
-  if (a.target == 0) return kMaxLen;
-  const int lane = threadIdx.x & 63;
-  int sum = 0;   // <= 256 row tiles of 2^25 blocks, in units of 8 blocks
-  for (int u = lane; u < a.units; u += 64)
-    sum += (span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows).total + 7) >> 3;
-  sum = __builtin_amdgcn_readfirstlane(wave_sum(sum));
-  const int64_t blocks = static_cast<int64_t>(sum) * 8 * a.H;
-  const int chunk = static_cast<int>((blocks + a.target - 1) / a.target);
-  return (max(chunk, a.least) + 7) & ~7;
-}
-
-// Row tile `unit`'s chunks are those from `first` on, `count` of them (stored for the
-// join behind the partial results).
+// Row tile `unit`'s chunks of `chunk` blocks are those from `first` on, `count` of them
+// (stored for the join behind the partial results).
 struct Share {
-  int32_t unit, first, count;
+  int32_t unit, first, count, chunk;
 };
 
-__device__ __forceinline__ int chunks_in(const Span& s, int chunk) {
-  return max(1, (s.total + chunk - 1) / chunk);
-}
+constexpr int kMaxUnits = 256;   // row tiles that are dealt out by their lengths
 
-// The share that chunk `index` belongs to; unit < 0 if there is none.
-__device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, int chunk,
-                                            int index) {
-  if (a.target == 0) return Share{index < a.units ? index : -1, index, 1};
+// The share that chunk `index` belongs to; unit < 0 if there is none.  Every wave of
+// every workgroup computes the same from the lengths: chunks of a size that makes at
+// most `target` of them for all heads.
+__device__ __forceinline__ Share find_share(const AttnParams& a, int tile_rows, int index) {
+  if (a.target == 0) return Share{index < a.units ? index : -1, index, 1, kMaxLen};
+  constexpr int kPasses = kMaxUnits / 64;
   const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int u0 = 0; u0 < a.units; u0 += 64) {
-    const int u = u0 + lane;
-    int count = 0;
-    if (u < a.units)
-      count = chunks_in(span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows), chunk);
-    int incl = count;
+  int total[kPasses], sum = 0;   // a sum of 256 x 2^25 blocks, in units of 8
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(incl, o);
-      if (lane >= o) incl += y;
-    }
+  for (int i = 0; i < kPasses; ++i) {
+    const int u = 64 * i + lane;
+    total[i] = 0;
+    if (64 * i < a.units && u < a.units)
+      total[i] = span_of(a, u / a.tiles, u % a.tiles * tile_rows, tile_rows).total;
+    sum += (total[i] + 7) >> 3;
+  }
+  const int64_t blocks = static_cast<int64_t>(wave_total(sum)) * 8 * a.H;
+  auto count_of = [&](int i, int chunk) __attribute__((always_inline)) {
+    return 64 * i + lane < a.units ? max(1, (total[i] + chunk - 1) / chunk) : 0;
+  };
+  auto chunk_for = [&](int parts) __attribute__((always_inline)) {
+    return (max(static_cast<int>((blocks + parts - 1) / parts), a.least) + 7) & ~7;
+  };
+  // As many blocks per chunk as fill `target`, unless the row tiles' last chunks make
+  // more of them; the second size cannot (each row tile adds less than one).
+  int chunk = chunk_for(a.target), chunks = 0;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) chunks += count_of(i, chunk);
+  if (static_cast<int64_t>(wave_total(chunks)) * a.H > a.target)
+    chunk = chunk_for(a.target - a.units * a.H);
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    if (64 * i >= a.units) break;
+    const int count = count_of(i, chunk), incl = wave_incl_scan(count);
     const int first = before + incl - count;
-    const uint64_t at = __ballot(u < a.units && index >= first && index < first + count);
+    const uint64_t at = __ballot(index >= first && index < first + count);
     if (at) {
       const int l = __builtin_ctzll(at);
-      return Share{u0 + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(count, l)};
+      return Share{64 * i + l, __builtin_amdgcn_readlane(first, l),
+                   __builtin_amdgcn_readlane(count, l), chunk};
     }
     before += __builtin_amdgcn_readlane(incl, 63);
   }
-  return Share{-1, 0, 0};
+  return Share{-1, 0, 0, 0};
 }
 
 __device__ __forceinline__ int2* shares_of(const AttnParams& a, int tile_rows, int D) {
