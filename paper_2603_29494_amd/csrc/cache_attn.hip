@@ -560,9 +560,10 @@ Deal deal(const CacheAttnShape& s) {
   d.half = rows <= 8;
   d.many = rows > 32;
   d.R = rows <= 16 ? 1 : 2;
-  d.rows = d.many ? kChunkRows : d.half ? 8 : 16 * d.R;
-  // Few row tiles: more waves on each, and half the chunks to join.
-  d.W = d.half && s.B * s.H <= 128 ? 8 : 4;
+  // Few row tiles: more waves on each, and half the chunks to join.  Many rows: eight
+  // waves share what rebuilding a tile costs.
+  d.W = d.many ? (rows > 128 ? 8 : 4) : d.half && s.B * s.H <= 128 ? 8 : 4;
+  d.rows = d.many ? 32 * d.W : d.half ? 8 : 16 * d.R;
   d.tiles = static_cast<int32_t>((rows + d.rows - 1) / d.rows);
   d.units = s.B * d.tiles;
   // Blocks a row tile can see: the table's, or the window's and the sinks'.
@@ -632,7 +633,7 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
       hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(d.items)), dim3(64 * d.W), 0, stream, a);
     };
     if (d.many) {
-      const hipError_t e = launch_cache_chunk(a, D, BITS, d.items, stream);
+      const hipError_t e = launch_cache_chunk(a, D, BITS, d.W, d.items, stream);
       if (e != hipSuccess) return e;
     } else if (d.half && d.W == 8) launch(k_cache_attn<D, BITS, 1, true, 8>);
     else if (d.half) launch(k_cache_attn<D, BITS, 1, true, 4>);

@@ -87,15 +87,17 @@ __device__ __forceinline__ void spread8(const uint32_t* w, uint32_t (&r)[4]) {
   }
 }
 
-template <int D, int BITS>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_cache_chunk(
+// W waves of 32 rows.
+template <int D, int BITS, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void k_cache_chunk(
     const AttnParams a) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, DS = D / 16, DB = D / 32;
   constexpr int kChunks = L::kRun / 4;      // 1 KB pieces of a block's K or V codes
   constexpr int kUnits = 2 * kChunks;       // of a tile's
-  constexpr bool kSplit = kUnits < 4;       // two waves take K, two take V
-  constexpr int kPer = kSplit ? 1 : kUnits / 4;   // pieces a wave takes of either
+  constexpr bool kSplit = 2 * kUnits <= W;  // a wave takes a piece of K or one of V
+  constexpr int kPer = kSplit ? 1 : kUnits / W;   // pieces a wave takes of either
+  constexpr int kRows = 32 * W;
   constexpr int kItems = 4 / DW;            // octets of codes in a lane's 16 bytes
   __shared__ __align__(16) f16x8 k_s[2][D / 8][kTile];
   __shared__ __align__(16) f16x8 v_s[2][2][4][D];
@@ -106,13 +108,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
   const int h = blockIdx.x % a.H;
   const int index = blockIdx.x / a.H;
-  const Share share = find_share(a, kChunkRows, index);
+  const Share share = find_share(a, kRows, index);
   if (share.unit < 0) return;
   if (a.target && h == 0 && index == share.first && tid == 0)
-    shares_of(a, kChunkRows, D)[share.unit] = int2{share.first, share.count};
+    shares_of(a, kRows, D)[share.unit] = int2{share.first, share.count};
   const int64_t b = share.unit / a.tiles;
-  const int row0 = share.unit % a.tiles * kChunkRows;
-  const Span s = span_of(a, b, row0, kChunkRows);
+  const int row0 = share.unit % a.tiles * kRows;
+  const Span s = span_of(a, b, row0, kRows);
   if (row0 >= s.rows) return;
   const int t0 = (index - share.first) * (share.count > 1 ? share.chunk : 0);   // a multiple of 8
   const int t1 = share.count > 1 ? min(s.total, t0 + share.chunk) : s.total;
@@ -185,8 +187,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     uint32_t held;   // bit per block
   };
   // Which piece: block u / kChunks, 1 KB u % kChunks.
-  auto k_unit = [&](int i) __attribute__((always_inline)) { return kSplit ? wave & 1 : wave * kPer + i; };
-  const bool do_k = !kSplit || wave < 2, do_v = !kSplit || wave >= 2;
+  auto k_unit = [&](int i) __attribute__((always_inline)) { return kSplit ? wave % kUnits : wave * kPer + i; };
+  const bool do_k = !kSplit || wave < kUnits;
+  const bool do_v = !kSplit || (wave >= kUnits && wave < 2 * kUnits);
   // Of octet i of a K piece: the 16 tokens it is of, and its 32 head-dim values.
   auto k_token16 = [&](int c, int i) __attribute__((always_inline)) { return (c * kItems + i) / (D / 32); };
   auto k_step = [&](int c, int i) __attribute__((always_inline)) { return (c * kItems + i) % (D / 32); };
@@ -480,7 +483,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (!have) return;
   const float back = __builtin_amdgcn_ldexpf(1.0f, v_exp);
   if (share.count > 1) {
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * kChunkRows + 32 * wave + ln;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kRows + 32 * wave + ln;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -491,7 +494,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         *reinterpret_cast<f32x4*>(a.part + at * D + 32 * db + 8 * vq + 4 * g) = y;
       }
     if (g == 0) {
-      float* ml = a.part + static_cast<int64_t>(a.items) * kChunkRows * D + at * 2;
+      float* ml = a.part + static_cast<int64_t>(a.items) * kRows * D + at * 2;
       ml[0] = m_run;
       ml[1] = l_run;
     }
@@ -515,13 +518,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
 }  // namespace
 
-hipError_t launch_cache_chunk(const AttnParams& a, int32_t D, int32_t bits, int64_t items,
-                              hipStream_t stream) {
+hipError_t launch_cache_chunk(const AttnParams& a, int32_t D, int32_t bits, int32_t waves,
+                              int64_t items, hipStream_t stream) {
   auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(items)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(items)),
+                       dim3(static_cast<unsigned>(64 * waves)), 0, stream, a);
   };
-  if (D == 128) bits == 4 ? run(k_cache_chunk<128, 4>) : run(k_cache_chunk<128, 8>);
-  else bits == 4 ? run(k_cache_chunk<64, 4>) : run(k_cache_chunk<64, 8>);
+  if (waves == 8) {
+    if (D == 128) bits == 4 ? run(k_cache_chunk<128, 4, 8>) : run(k_cache_chunk<128, 8, 8>);
+    else bits == 4 ? run(k_cache_chunk<64, 4, 8>) : run(k_cache_chunk<64, 8, 8>);
+  } else {
+    if (D == 128) bits == 4 ? run(k_cache_chunk<128, 4, 4>) : run(k_cache_chunk<128, 8, 4>);
+    else bits == 4 ? run(k_cache_chunk<64, 4, 4>) : run(k_cache_chunk<64, 8, 4>);
+  }
   return hipGetLastError();
 }
 

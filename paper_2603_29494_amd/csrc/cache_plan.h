@@ -146,9 +146,8 @@ struct Deal {
   bool merge;
 };
 
-hipError_t launch_cache_chunk(const AttnParams& a, int32_t D, int32_t bits, int64_t items,
-                              hipStream_t stream);
-
-constexpr int kChunkRows = 128;   // rows per workgroup of that kernel
+// The kernel of many rows: 32 of them per wave, four or eight waves.
+hipError_t launch_cache_chunk(const AttnParams& a, int32_t D, int32_t bits, int32_t waves,
+                              int64_t items, hipStream_t stream);
 
 }  // namespace vecattn
