@@ -243,9 +243,15 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     }
     return __builtin_amdgcn_frexp_expf(__uint_as_float(wave_max(__float_as_uint(top))));
   };
-  // Rebuilds a tile into stage st; careful: groups that stand for NaN become 0 in V.
-  // Returns K's power; raises v_next to V's.
-  auto rebuild = [&](Raw& x, int tile, int st, int& v_next, bool careful)
+  // Rebuilding a tile: prepare, then its pieces (octets of a lane's codes: kPer * kItems
+  // of K, as many of V).
+  struct Rebuilt {
+    f16x2 vm2[4], vd2[4];
+    int ke;   // K's power
+  };
+  const f16x2 minus = {_Float16(-1024.0f), _Float16(-1024.0f)};
+  // careful: groups that stand for NaN become 0 in V.  Raises v_next to V's power.
+  auto prepare = [&](Raw& x, Rebuilt& y, int tile, int& v_next, bool careful)
                      __attribute__((always_inline)) {
     // Tokens of no page and past the rows' last: as if m = s = 0.
     const int left[2] = {left_in(x, tile, 0), left_in(x, tile, 1)};
@@ -266,81 +272,83 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         }
       }
     }
-    const int ke = exponent(x.km) - 15;
+    y.ke = exponent(x.km) - 15;
     v_next = max(v_next, exponent(x.vm) - 15);
-    const f16x2 minus = {_Float16(-1024.0f), _Float16(-1024.0f)};
-    f16x2 m2[4], d2[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float m[2], d[2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        uint32_t w = x.vp[2 * e + y];
+      for (int i = 0; i < 2; ++i) {
+        uint32_t w = x.vp[2 * e + i];
         if (careful && !(low_of(w) == low_of(w))) w = 0u;
-        m[y] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
-        d[y] = __builtin_amdgcn_ldexpf(step_of(w), -v_next);
+        m[i] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
+        d[i] = __builtin_amdgcn_ldexpf(step_of(w), -v_next);
       }
-      m2[e] = to_f16(m[0], m[1]);
-      d2[e] = to_f16(d[0], d[1]);
+      y.vm2[e] = to_f16(m[0], m[1]);
+      y.vd2[e] = to_f16(d[0], d[1]);
     }
+  };
+  constexpr int kPieces = 2 * kPer * kItems;
+  auto piece = [&](const Raw& x, const Rebuilt& y, int i, int st) __attribute__((always_inline)) {
+    const int per = i % (kPer * kItems) / kItems, it = i % kItems;
+    const int u = k_unit(per), c = u % kChunks, bl = u / kChunks;
+    uint32_t r[4], cw[DW];
+    if (i < kPer * kItems) {
+      if (!do_k) return;
+      const int t16 = k_token16(c, it), st32 = k_step(c, it);
+      const uint32_t w = x.kp[per][it];
+      const float m = __builtin_amdgcn_ldexpf(low_of(w), -y.ke);
+      const float d = __builtin_amdgcn_ldexpf(step_of(w), -y.ke);
+      const f16x2 m2 = to_f16(m, m), d2 = to_f16(d, d);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int u = k_unit(i), c = u % kChunks, bl = u / kChunks;
-      if (do_k) {
+      for (int e = 0; e < DW; ++e) cw[e] = x.kc[per][it * DW + e];
+      spread8<BITS, false>(cw, r);
 #pragma unroll
-        for (int it = 0; it < kItems; ++it) {
-          const int t16 = k_token16(c, it), st32 = k_step(c, it);
-          const uint32_t w = x.kp[i][it];
-          const float m = __builtin_amdgcn_ldexpf(low_of(w), -ke);
-          const float d = __builtin_amdgcn_ldexpf(step_of(w), -ke);
-          const f16x2 km2 = to_f16(m, m), kd2 = to_f16(d, d);
-          uint32_t r[4];
-          uint32_t cw[DW];
+      for (int e = 0; e < 4; ++e)
+        r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(
+                                                __builtin_bit_cast(f16x2, r[e]) + minus, d2, m2));
+      k_s[st][4 * st32 + g16][32 * bl + 16 * t16 + n16] =
+          __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
+    } else {
+      if (!do_v) return;
 #pragma unroll
-          for (int e = 0; e < DW; ++e) cw[e] = x.kc[i][it * DW + e];
-          spread8<BITS, false>(cw, r);
+      for (int e = 0; e < DW; ++e) cw[e] = x.vc[per][it * DW + e];
+      spread8<BITS, true>(cw, r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f16x2 y = __builtin_bit_cast(f16x2, r[e]) + minus;
-            r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, kd2, km2));
-          }
-          k_s[st][4 * st32 + g16][32 * bl + 16 * t16 + n16] =
-              __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
-        }
-      }
-      if (do_v) {
-#pragma unroll
-        for (int it = 0; it < kItems; ++it) {
-          uint32_t r[4], cw[DW];
-#pragma unroll
-          for (int e = 0; e < DW; ++e) cw[e] = x.vc[i][it * DW + e];
-          spread8<BITS, true>(cw, r);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const f16x2 y = __builtin_bit_cast(f16x2, r[e]) + minus;
-            r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(y, d2[e], m2[e]));
-          }
-          v_s[st][bl][g16][16 * (c * kItems + it) + n16] =
-              __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
-        }
-      }
+      for (int e = 0; e < 4; ++e)
+        r[e] = __builtin_bit_cast(
+            uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, r[e]) + minus, y.vd2[e],
+                                                y.vm2[e]));
+      v_s[st][bl][g16][16 * (c * kItems + it) + n16] =
+          __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
     }
-    return ke;
   };
 
   auto sees = [&](int j) __attribute__((always_inline)) {
     return j <= pos && (j > pos - a.window || j < a.sinks);
   };
-  // Tile `tile` in stage st: scores (K in units of 2^ke), weights, products.
-  auto work = [&](int tile, int st, int ke, uint32_t blocks) __attribute__((always_inline)) {
-    f32x16 sc[2];
+  // Tile `tile` in stage st: scores (K in units of 2^ke), weights, products.  Operands
+  // are read four instructions ahead; `between` runs beside the score products.
+  constexpr int kAhead = 4;
+  auto work = [&](int tile, int st, int ke, uint32_t blocks, auto&& between)
+                  __attribute__((always_inline)) {
+    f32x16 sc[2] = {f32x16{}, f32x16{}};
+    {
+      f16x8 ring[kAhead];
+      auto read = [&](int i) __attribute__((always_inline)) {
+        if (i < 2 * DS) ring[i % kAhead] = k_s[st][2 * (i % DS) + g][32 * (i / DS) + ln];
+      };
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      sc[hf] = f32x16{};
+      for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-      for (int s2 = 0; s2 < DS; ++s2)
-        sc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_s[st][2 * s2 + g][32 * hf + ln], qf[s2],
-                                                        sc[hf], 0, 0, 0);
+      for (int i = 0; i < 2 * DS; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        sc[i / DS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], qf[i % DS],
+                                                            sc[i / DS], 0, 0, 0);
+        read(i + kAhead);
+        between(i);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
@@ -385,22 +393,31 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       weigh();
     }
     l_run += sum;
+    f16x8 pb[4], ring[kAhead];
+    auto read = [&](int i) __attribute__((always_inline)) {
+      const int k = i / DB;
+      if (k < 4) ring[i % kAhead] = v_s[st][k / 2][2 * (k % 2) + g][32 * (i % DB) + ln];
+    };
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
+    for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-      for (int step = 0; step < 2; ++step) {
-        u32x4 w;
+    for (int k = 0; k < 4; ++k) {
+      u32x4 w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int v0 = 8 * (e >> 1) + 4 * step + 2 * (e & 1);
-          w[e] = __builtin_bit_cast(uint32_t, to_f16(p[hf][v0], p[hf][v0 + 1]));
-        }
-        const f16x8 pb = __builtin_bit_cast(f16x8, w);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_s[st][hf][2 * step + g][32 * db + ln],
-                                                            pb, oacc[db], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) {
+        const int v0 = 8 * (e >> 1) + 4 * (k % 2) + 2 * (e & 1);
+        w[e] = __builtin_bit_cast(uint32_t, to_f16(p[k / 2][v0], p[k / 2][v0 + 1]));
       }
+      pb[k] = __builtin_bit_cast(f16x8, w);
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      oacc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], pb[i / DB],
+                                                            oacc[i % DB], 0, 0, 0);
+      read(i + kAhead);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
   // O follows V's power.
   auto follow = [&](int v_next) __attribute__((always_inline)) {
@@ -415,26 +432,37 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   if (tid == 0) s_redo = 0;
   if (ntiles > 0) {
     Raw raw;
+    Rebuilt re;
     int v_next = v_exp;
     fetch(raw, 0);
-    int ke = rebuild(raw, 0, 0, v_next, false);
+    prepare(raw, re, 0, v_next, false);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
+    int ke = re.ke;
     uint32_t blocks = raw.held;
     if (ntiles > 1) fetch(raw, 1);
-    for (int t = 0; t < ntiles; ++t) {
-      const int st = t & 1;
+    auto turn = [&](int t, int st) __attribute__((always_inline)) {
       lds_barrier();
       follow(v_next);
-      int ke1 = 0;
-      uint32_t blocks1 = 0;
-      if (t + 1 < ntiles) {
-        ke1 = rebuild(raw, t + 1, st ^ 1, v_next, false);
-        blocks1 = raw.held;
-        if (t + 2 < ntiles) fetch(raw, t + 2);
-      }
-      work(t, st, ke, blocks);
-      ke = ke1;
+      const bool more = t + 1 < ntiles;
+      if (more) prepare(raw, re, t + 1, v_next, false);
+      const uint32_t blocks1 = raw.held;
+      // The last tile rebuilds what the one before did, into a stage that nothing reads.
+      work(t, st, ke, blocks, [&](int i) __attribute__((always_inline)) {
+        constexpr int every = 2 * DS / kPieces;
+        static_assert(every * kPieces == 2 * DS, "pieces fit the score products");
+        if (i % every == every - 1) piece(raw, re, i / every, st ^ 1);
+        if (i == 2 * DS - 1 && t + 2 < ntiles) fetch(raw, t + 2);
+      });
+      ke = re.ke;
       blocks = blocks1;
+    };
+    int t = 0;
+    for (; t + 1 < ntiles; t += 2) {
+      turn(t, 0);
+      turn(t + 1, 1);
     }
+    if (t < ntiles) turn(t, 0);
   }
 
   // A group of V that stands for NaN reaches rows that do not see its token (0 * NaN
@@ -457,13 +485,16 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
 #pragma unroll 1
     for (int t = 0; t < ntiles; ++t) {
       Raw raw;
+      Rebuilt re;
       int v_next = v_exp;
       fetch(raw, t);
       __syncthreads();
-      const int ke = rebuild(raw, t, 0, v_next, true);
+      prepare(raw, re, t, v_next, true);
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
       __syncthreads();
       follow(v_next);
-      work(t, 0, ke, raw.held);
+      work(t, 0, re.ke, raw.held, [](int) {});
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
         const bool nan = !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));   // 0 where hidden
