@@ -38,34 +38,42 @@ __device__ __forceinline__ uint8_t* block_ptr(const PageMap& m, int64_t b, int h
   return m.data + (((page * m.H + h) << sh) + (jb & ((1 << sh) - 1))) * BYTES;
 }
 
-// Eight values of a token: codes (0..M) and, on every lane of the eight that
-// hold the group, its (m, s) dword.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+// bf16 bits as integers of the same order, and back, two at a time.
+__device__ __forceinline__ i16x2 ordered(uint32_t bits) {
+  const i16x2 b = __builtin_bit_cast(i16x2, bits);
+  return b ^ ((b >> 15) & short(0x7FFF));
+}
+
+// Half a group, 32 values of a token (the other half is on the lane beside): codes
+// (0..M) as bytes, four to a dword, and, on both lanes, the group's (m, s) dword.
 template <int BITS>
-__device__ __forceinline__ uint32_t quantise8(const u32x4 w, int (&u)[8]) {
+__device__ __forceinline__ uint32_t quantise32(const u32x4 (&w)[4], uint32_t (&bytes)[8]) {
   constexpr float M = BITS == 4 ? 15.0f : 255.0f;
-  float x[8];
+  // Extremes on the bits: bf16 pairs take one instruction, and NaN has its place.
+  i16x2 lo2 = ordered(w[0][0]), hi2 = lo2;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[2 * e] = __uint_as_float(w[e] << 16);
-    x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+  for (int e = 1; e < 16; ++e) {
+    const i16x2 k = ordered(w[e / 4][e % 4]);
+    lo2 = __builtin_elementwise_min(lo2, k);
+    hi2 = __builtin_elementwise_max(hi2, k);
   }
-  float lo = x[0], hi = x[0], bad = x[0] * 0.0f;  // bad: 0, or NaN
-#pragma unroll
-  for (int e = 1; e < 8; ++e) {
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
-    bad += x[e] * 0.0f;
-  }
-#pragma unroll
-  for (int o = 1; o < 8; o <<= 1) {
-    lo = fminf(lo, __shfl_xor(lo, o));
-    hi = fmaxf(hi, __shfl_xor(hi, o));
-    bad += __shfl_xor(bad, o);
-  }
+  auto beside = [](i16x2 x) __attribute__((always_inline)) {
+    const int y = __builtin_bit_cast(int, x);
+    return __builtin_bit_cast(i16x2, __builtin_amdgcn_update_dpp(y, y, 0xB1, 0xf, 0xf, false));
+  };
+  lo2 = __builtin_elementwise_min(lo2, beside(lo2));   // quad_perm [1, 0, 3, 2]
+  hi2 = __builtin_elementwise_max(hi2, beside(hi2));
+  const short lo_key = min(lo2[0], lo2[1]), hi_key = max(hi2[0], hi2[1]);
+  const uint32_t both = __builtin_bit_cast(
+      uint32_t, ordered(__builtin_bit_cast(uint32_t, i16x2{lo_key, hi_key})));
+  const float lo = __uint_as_float(both << 16), hi = __uint_as_float(both & 0xFFFF0000u);
   const float range = hi - lo;
-  if (!(bad == 0.0f) || !(range < INFINITY)) {
+  // Infinities (keys 0x7F80 and its mirror) and NaN lie outside the finite keys.
+  if (hi_key >= 0x7F80 || lo_key < -0x7F80 || !(range < INFINITY)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e] = 0;
+    for (int e = 0; e < 8; ++e) bytes[e] = 0;
     return 0x7FC07FC0u;
   }
   const __bf16 sb = static_cast<__bf16>(range / M);
@@ -75,93 +83,143 @@ __device__ __forceinline__ uint32_t quantise8(const u32x4 w, int (&u)[8]) {
     s = 0.0f;
     sbits = 0;
   }
+  // The nearest float to (x - m) / s from the nearest to 1 / s: one step with the
+  // exact remainder leaves the product off by 2^-46 of it before it is rounded, and a
+  // quotient by s, eight bits, is 2^-33 from the midpoint of two floats at least (none
+  // is one).  Adding 2^23 rounds it to an integer in the low bits, ties to even.
+  // s = 0: r = 0, u = 0.
+  const float r = s == 0.0f ? 0.0f : 1.0f / s;
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    u[e] = s == 0.0f ? 0 : static_cast<int>(fminf(M, __builtin_rintf((x[e] - lo) / s)));
-  return (__float_as_uint(lo) >> 16) | (sbits << 16);
+  for (int i = 0; i < 8; ++i) {
+    uint32_t u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t pair = w[i / 2][2 * (i % 2) + e / 2];
+      const float d = __uint_as_float(e % 2 ? pair & 0xFFFF0000u : pair << 16) - lo;
+      float q = d * r;
+      q = __builtin_fmaf(__builtin_fmaf(-q, s, d), r, q);
+      q = __uint_as_float(min(__float_as_uint(q), __float_as_uint(M)));   // neither below 0
+      u[e] = __float_as_uint(q + 8388608.0f);
+    }
+    bytes[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0C0C0400u),
+                                     __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0400u), 0x05040100u);
+  }
+  return (both & 0xFFFFu) | (sbits << 16);
 }
 
+// Half of a workgroup's threads take K, half V, each half a group of a token.  A whole
+// block is put together in LDS and stored 16 bytes a lane; of a part of one only the
+// new tokens' codes are stored, V's within the dwords they share with others.
 template <int D, int BITS>
-__global__ __launch_bounds__(256) void k_cache_write(
+__global__ __launch_bounds__(2 * D) void k_cache_write(
     const uint16_t* __restrict__ k, int64_t k_sB, int64_t k_sH, int64_t k_sN,
     const uint16_t* __restrict__ v, int64_t v_sB, int64_t v_sH, int64_t v_sN, int32_t n,
     const int32_t* __restrict__ lens, const int32_t* __restrict__ n_new, PageMap map) {
   using L = CacheLayout<D, BITS>;
-  constexpr int CH = D / 8;               // 8-value chunks per row
-  constexpr int RPP = 256 / CH;           // rows per pass
+  constexpr int PARTS = D / 32;   // threads per row
   const int64_t b = blockIdx.z;
   const int h = blockIdx.y;
-  const int64_t len = min(max(lens[b], 0), 1 << 30);
-  const int64_t nb = n_new ? min(max(n_new[b], 0), n) : n;
-  const int64_t p0 = len - nb;            // position of row 0
-  const int64_t jb = (max(p0, int64_t(0)) >> 5) + blockIdx.x;
-  const int64_t j0 = jb * kCacheBlock;
+  const int len = min(max(lens[b], 0), 1 << 30);
+  const int nb = n_new ? min(max(n_new[b], 0), n) : n;
+  const int p0 = len - nb;        // position of row 0
+  const int jb = (max(p0, 0) >> 5) + blockIdx.x;
+  const int j0 = jb * kCacheBlock;
   if (nb == 0 || j0 >= len) return;
   uint8_t* blk = block_ptr<L::kBytes>(map, b, h, jb);
   if (!blk) return;
-  __shared__ uint8_t codes[kCacheBlock][D];  // V's
+  // Tokens [from, to) of the block are written.
+  const int from = max(p0 - j0, 0), to = min(len - j0, kCacheBlock);
+  const bool whole = from == 0 && to == kCacheBlock;
+  __shared__ __align__(16) uint8_t image[L::kBytes];               // the block
+  __shared__ __align__(16) uint32_t codes[kCacheBlock][D / 4 + 4];   // V's, a byte each
 
-  const int c = threadIdx.x % CH;
+  const bool is_v = threadIdx.x >= D;
+  const int t = threadIdx.x % D, key = t / PARTS, part = t % PARTS;
+  if (key >= from && key < to) {
+    const int64_t row = j0 + key - p0;
+    const u32x4* src = reinterpret_cast<const u32x4*>(
+        is_v ? v + b * v_sB + h * v_sH + row * v_sN + 32 * part
+             : k + b * k_sB + h * k_sH + row * k_sN + 32 * part);
+    u32x4 w[4];
 #pragma unroll
-  for (int pass = 0; pass < kCacheBlock / RPP; ++pass) {
-    const int key = pass * RPP + threadIdx.x / CH;
-    const int64_t r = j0 + key - p0;
-    const bool have = r >= 0 && r < nb;   // the same for the lanes of a group
-    u32x4 kw = {0, 0, 0, 0}, vw = {0, 0, 0, 0};
-    if (have) {
-      kw = *reinterpret_cast<const u32x4*>(k + b * k_sB + h * k_sH + r * k_sN + 8 * c);
-      vw = *reinterpret_cast<const u32x4*>(v + b * v_sB + h * v_sH + r * v_sN + 8 * c);
+    for (int i = 0; i < 4; ++i) w[i] = src[i];
+    uint32_t bytes[8];
+    const uint32_t par = quantise32<BITS>(w, bytes);
+    uint8_t* to_blk = whole ? image : blk;
+    if (part % 2 == 0)
+      reinterpret_cast<uint32_t*>(to_blk + (is_v ? L::kHalf : 0) +
+                                  L::kCodes)[key * L::kG + part / 2] = par;
+    if (is_v) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *reinterpret_cast<u32x4*>(&codes[key][8 * part + 4 * i]) =
+            u32x4{bytes[4 * i], bytes[4 * i + 1], bytes[4 * i + 2], bytes[4 * i + 3]};
+    } else {
+      const int w0 = ((key >> 4) * PARTS + part) * L::kDw;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)   // eight values each
+#pragma unroll
+        for (int x = 0; x < L::kDw; ++x)
+          *reinterpret_cast<uint32_t*>(to_blk + code_byte(w0 + x, g * 16 + (key & 15))) =
+              BITS == 4 ? bytes[2 * g] | bytes[2 * g + 1] << 4 : bytes[2 * g + x];
     }
-    int u[8];
-    uint32_t par = quantise8<BITS>(kw, u);
-    if (have) {
-      uint32_t dw[L::kDw] = {};
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (BITS == 4) dw[0] |= static_cast<uint32_t>(u[e]) << (4 * k_nibble(e));
-        else dw[e >> 2] |= static_cast<uint32_t>(u[e]) << (8 * (e & 3));
-      }
-      const int w0 = ((key >> 4) * (D / 32) + (c >> 2)) * L::kDw, l = (c & 3) * 16 + (key & 15);
-#pragma unroll
-      for (int x = 0; x < L::kDw; ++x)
-        *reinterpret_cast<uint32_t*>(blk + code_byte(w0 + x, l)) = dw[x];
-      if (c % 8 == 0)
-        reinterpret_cast<uint32_t*>(blk + L::kCodes)[key * L::kG + c / 8] = par;
-    }
-    par = quantise8<BITS>(vw, u);
-    uint32_t pk[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) pk[e >> 2] |= static_cast<uint32_t>(u[e]) << (8 * (e & 3));
-    *reinterpret_cast<u32x2*>(&codes[key][8 * c]) = u32x2{pk[0], pk[1]};
-    if (have && c % 8 == 0)
-      reinterpret_cast<uint32_t*>(blk + L::kHalf + L::kCodes)[key * L::kG + c / 8] = par;
   }
   __syncthreads();
-  // V's codes, eight tokens of a head-dim value at a time; codes of tokens that
-  // this call does not write stay as they are.
-  for (int it = threadIdx.x; it < 4 * D; it += 256) {
-    const int d = it % D, g = it / D;
-    uint32_t dw[L::kDw] = {}, mask[L::kDw] = {};
+  // V's codes: eight tokens of four head-dim values at a time, as bytes transposed.
+  for (int it = threadIdx.x; it < D; it += 2 * D) {
+    const int d = it % (D / 4) * 4, g = it / (D / 4);
+    uint32_t c[8], have = 0;   // slot e: four values' codes; bit e: written
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int key = (e >> 2) * 16 + 4 * g + (e & 3);
-      const int64_t r = j0 + key - p0;
-      const bool have = r >= 0 && r < nb;
-      const uint32_t u = codes[key][d];
-      const int x = BITS == 4 ? 0 : e >> 2, sh = BITS == 4 ? 4 * v_nibble(e) : 8 * (e & 3);
-      if (have) {
-        dw[x] |= u << sh;
-        mask[x] |= (BITS == 4 ? 0xFu : 0xFFu) << sh;
-      }
+      const int token = (e >> 2) * 16 + 4 * g + (e & 3);
+      const bool here = token >= from && token < to;
+      c[e] = here ? codes[token][d / 4] : 0u;   // not written: undefined
+      have |= here ? 1u << e : 0u;
     }
 #pragma unroll
     for (int x = 0; x < L::kDw; ++x) {
-      if (mask[x] == 0) continue;
-      uint32_t* at = reinterpret_cast<uint32_t*>(
-          blk + L::kHalf + code_byte((d >> 4) * L::kDw + x, g * 16 + (d & 15)));
-      *at = mask[x] == 0xFFFFFFFFu ? dw[x] : (*at & ~mask[x]) | dw[x];
+      uint32_t p[4];   // byte i of the dwords to come, of four values
+      if constexpr (BITS == 4) {   // nibbles 2 i and 2 i + 1
+        p[0] = c[0] | c[2] << 4, p[1] = c[4] | c[6] << 4;
+        p[2] = c[1] | c[3] << 4, p[3] = c[5] | c[7] << 4;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = c[4 * x + i];
+      }
+      const uint32_t a0 = __builtin_amdgcn_perm(p[1], p[0], 0x05010400u);   // values 0, 1: bytes 0, 1
+      const uint32_t a1 = __builtin_amdgcn_perm(p[1], p[0], 0x07030602u);   // values 2, 3
+      const uint32_t b0 = __builtin_amdgcn_perm(p[3], p[2], 0x05010400u);
+      const uint32_t b1 = __builtin_amdgcn_perm(p[3], p[2], 0x07030602u);
+      const uint32_t out[4] = {__builtin_amdgcn_perm(b0, a0, 0x05040100u),
+                               __builtin_amdgcn_perm(b0, a0, 0x07060302u),
+                               __builtin_amdgcn_perm(b1, a1, 0x05040100u),
+                               __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
+      auto byte_of = [&](int i) __attribute__((always_inline)) {
+        return L::kHalf + code_byte((d + i) / 16 * L::kDw + x, g * 16 + (d + i) % 16);
+      };
+      if (whole) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(image + byte_of(i)) = out[i];
+        continue;
+      }
+      uint32_t mask = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (BITS == 4) mask |= have >> e & 1u ? 0xFu << (4 * v_nibble(e)) : 0u;
+        else if (e / 4 == x) mask |= have >> e & 1u ? 0xFFu << (8 * (e & 3)) : 0u;
+      }
+      if (mask == 0) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t* at = reinterpret_cast<uint32_t*>(blk + byte_of(i));
+        *at = (*at & ~mask) | (out[i] & mask);
+      }
     }
   }
+  if (!whole) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < L::kBytes / 16; i += 2 * D)
+    *reinterpret_cast<u32x4*>(blk + 16 * i) = *reinterpret_cast<const u32x4*>(image + 16 * i);
 }
 
 // m + s u for eight codes, rounded to bf16 once.
@@ -254,8 +312,8 @@ hipError_t launch_cache_write(const Tensor4& k, const Tensor4& v, const CacheArg
   const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(k.H),
                   static_cast<unsigned>(k.B));
   auto run = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, static_cast<const uint16_t*>(k.ptr),
-                       k.sB, k.sH, k.sN, static_cast<const uint16_t*>(v.ptr), v.sB, v.sH, v.sN,
+    hipLaunchKernelGGL(kernel, grid, dim3(static_cast<unsigned>(2 * c.D)), 0, stream,
+                       static_cast<const uint16_t*>(k.ptr), k.sB, k.sH, k.sN, static_cast<const uint16_t*>(v.ptr), v.sB, v.sH, v.sN,
                        static_cast<int32_t>(k.N), c.lens, n_new, page_map(c));
   };
   if (c.D == 128) c.bits == 4 ? run(k_cache_write<128, 4>) : run(k_cache_write<128, 8>);
