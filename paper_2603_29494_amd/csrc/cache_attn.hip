@@ -247,7 +247,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2
     const bool have = row < s.rows;
     pos[r] = have ? s.p_first + tok : -1;
     rows[r].load(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN, have, g);
-    to_log2[r] = a.scale_log2 * rows[r].unscale;
+    to_log2[r] = fmaxf(a.scale_log2 * rows[r].unscale, 0x1p-126f);   // -inf * 0 is no mask
   }
 
   f32x4 oacc[R][DB], off[R][G];

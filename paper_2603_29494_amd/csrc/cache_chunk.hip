@@ -359,7 +359,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       for (int e = 0; e < 16; ++e)
         sc[hf][e] = held && sees(j0 + 8 * (e / 4) + 4 * g + e % 4) ? sc[hf][e] : kNegInf;
     }
-    const float scale = to_log2 * __builtin_amdgcn_ldexpf(1.0f, ke);
+    // Not below fp32's normal numbers: -inf * 0 is no mask.
+    const float scale = fmaxf(to_log2 * __builtin_amdgcn_ldexpf(1.0f, ke), 0x1p-126f);
     f32x16 p[2];
     float sum;
     auto weigh = [&]() __attribute__((always_inline)) {

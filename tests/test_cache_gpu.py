@@ -406,3 +406,43 @@ def test_magnitudes(gpu, n, scale):
     va.cache_write(cache, k, v, table, int32([L]))
     o, lse = va.cache_attn(q, cache, table, int32([L]), return_lse=True)
     ref.check(o, lse, ref.cache_attn(q, [k[0].cpu()], [v[0].cpu()], 4, [L]))
+
+
+@pytest.mark.parametrize("n", [1, 12, 50])
+def test_zero_keys_and_tiny_queries(gpu, n):
+    """Blocks of zeros under queries near 0: scores of 0 and masks that stay masks."""
+    L, D = 200, 64
+    table, pages = paged([L], 32)
+    cache = fresh_cache(pages, 1, D, 32, 4)
+    k, v = torch.zeros(1, 1, L, D, dtype=torch.bfloat16, device="cuda"), rows(861, 1, 1, L, D)
+    va.cache_write(cache, k, v, table, int32([L]))
+    q = rows(862, 1, 2, n, D, scale=1e-6)
+    q[:, 1] = 0
+    o, lse = va.cache_attn(q, cache, table, int32([L]), window=70, sinks=2, scale=1e-6,
+                           return_lse=True)
+    ref.check(o, lse, ref.cache_attn(q, [k[0].cpu()], [v[0].cpu()], 4, [L], None, 70, 2, 1e-6))
+
+
+def test_many_sequences(gpu):
+    """More row tiles than the lengths are dealt out for: one chunk per sequence."""
+    lens = [(37 * i) % 211 for i in range(300)]
+    attn_case(870, lens, 2, 1, 1, 64, 4, 32)
+
+
+def test_two_calls_at_once(gpu):
+    """Calls on two streams, each with a workspace of its own."""
+    lens = [5000, 300]
+    cache, table, ks, vs = filled(880, lens, 2, 128, 64, 4)
+    qs = [rows(881 + i, 2, 8, 1, 128) for i in range(2)]
+    want = [va.cache_attn(q, cache, table, int32(lens)) for q in qs]
+    t = int32(lens)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(va.cache_attn(qs[i], cache, table, t))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in got[i])
