@@ -46,6 +46,15 @@ __device__ __forceinline__ i16x2 ordered(uint32_t bits) {
   return b ^ ((b >> 15) & short(0x7FFF));
 }
 
+// Eight codes from two dwords of bytes into the nibbles of their slots.
+__device__ __forceinline__ uint32_t nibbles(uint32_t lo, uint32_t hi) {
+  // Slots 0, 2, 4, 6 from nibble 0 on, slots 1, 3, 5, 7 from nibble 4 on.
+  const uint32_t even = __builtin_amdgcn_perm(hi, lo, 0x06040200u);
+  const uint32_t odd = __builtin_amdgcn_perm(hi, lo, 0x07050301u);
+  const uint32_t e = even | even >> 4, o = odd | odd >> 4;   // pairs in bytes 0 and 2
+  return __builtin_amdgcn_perm(o, e, 0x06040200u);
+}
+
 // Half a group, 32 values of a token (the other half is on the lane beside): codes
 // (0..M) as bytes, four to a dword, and, on both lanes, the group's (m, s) dword.
 template <int BITS>
@@ -161,7 +170,7 @@ __global__ __launch_bounds__(2 * D) void k_cache_write(
 #pragma unroll
         for (int x = 0; x < L::kDw; ++x)
           *reinterpret_cast<uint32_t*>(to_blk + code_byte(w0 + x, g * 16 + (key & 15))) =
-              BITS == 4 ? bytes[2 * g] | bytes[2 * g + 1] << 4 : bytes[2 * g + x];
+              BITS == 4 ? nibbles(bytes[2 * g], bytes[2 * g + 1]) : bytes[2 * g + x];
     }
   }
   __syncthreads();
@@ -205,7 +214,7 @@ __global__ __launch_bounds__(2 * D) void k_cache_write(
       uint32_t mask = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (BITS == 4) mask |= have >> e & 1u ? 0xFu << (4 * v_nibble(e)) : 0u;
+        if constexpr (BITS == 4) mask |= have >> e & 1u ? 0xFu << (4 * nibble_of(e)) : 0u;
         else if (e / 4 == x) mask |= have >> e & 1u ? 0xFFu << (8 * (e & 3)) : 0u;
       }
       if (mask == 0) continue;
@@ -236,11 +245,11 @@ __device__ __forceinline__ u32x4 values8(uint32_t par, const int (&u)[8]) {
   return out;
 }
 
-template <int BITS, bool V>
+template <int BITS>
 __device__ __forceinline__ void unpack8(const uint32_t (&dw)[BITS / 4], int (&u)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if constexpr (BITS == 4) u[e] = (dw[0] >> (4 * (V ? v_nibble(e) : k_nibble(e)))) & 0xF;
+    if constexpr (BITS == 4) u[e] = (dw[0] >> (4 * nibble_of(e))) & 0xF;
     else u[e] = (dw[e >> 2] >> (8 * (e & 3))) & 0xFF;
   }
 }
@@ -270,7 +279,7 @@ __global__ __launch_bounds__(256) void k_cache_read(
       dw[x] = *reinterpret_cast<const uint32_t*>(
           blk + L::kHalf + code_byte((d >> 4) * L::kDw + x, g * 16 + (d & 15)));
     int u[8];
-    unpack8<BITS, true>(dw, u);
+    unpack8<BITS>(dw, u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) codes[(e >> 2) * 16 + 4 * g + (e & 3)][d] = static_cast<uint8_t>(u[e]);
   }
@@ -287,7 +296,7 @@ __global__ __launch_bounds__(256) void k_cache_read(
 #pragma unroll
     for (int x = 0; x < L::kDw; ++x)
       dw[x] = *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + x, l));
-    unpack8<BITS, false>(dw, u);
+    unpack8<BITS>(dw, u);
     const int gi = key * L::kG + c / 8;
     *reinterpret_cast<u32x4*>(k + b * k_sB + h * k_sH + r * k_sN + 8 * c) =
         values8(reinterpret_cast<const uint32_t*>(blk + L::kCodes)[gi], u);

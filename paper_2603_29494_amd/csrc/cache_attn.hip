@@ -6,13 +6,12 @@
 //   q . k = sum_G s_G (q_G . u_G) + m_G sum(q_G),
 //   sum_j p_j v_j = sum_j (p_j s_jG) u_j + sum_j p_j m_jG,
 // and the codes go into the matrix instructions as they are, exactly.
-//   K, 4 bits: a code's byte is u 2^-9 read as fp8 (e4m3: a subnormal up to 7, the
-//     first binade from 8), so masks are all the unpacking; the row of q, scaled by a
-//     power of two, is the sum of three bf8 (e5m2) parts, exact to 2^-30 of its
-//     largest value.
+//   K: the code is the bits of a small fp16 number, so shifts and masks are all the
+//     unpacking; a row of q is scaled by a power of two, which fits bf16's eight bits
+//     into fp16 down to 2^-30 of its largest value.
 //   V, 4 bits: 16 + u in bf16 (a shift and an and-or per pair); the 16 is taken out by
 //     summing -16 times the rounded weights with a matrix instruction of its own.
-//   8 bits: bf16 holds integers to 256.
+//   V, 8 bits: bf16 holds integers to 256.
 // No rounding remains but that of p_j s_jG to bf16 (half a step, 2^-9 at most of
 // it); the normaliser and the m_jG terms take the fp32 weights.
 //
@@ -36,7 +35,7 @@
 namespace vecattn {
 namespace {
 
-// Eight codes of V (of K as well with 8 bits) as bf16.  `ones` is kOnes in a vector register that the compiler does
+// Eight codes of V as bf16.  `ones` is kOnes in a vector register that the compiler does
 // not see through: with both constants in scalar registers it takes two instructions
 // for (x & mask) | ones instead of one.
 template <int BITS>
@@ -110,88 +109,49 @@ struct Block {
   }
 };
 
-// Rows of q as the score products take them: with 8 bits bf16 as they came, with 4
-// bits scaled by 2^k and split into three bf8 parts.  sum: of a group's values, in
-// the products' scale; unscale: from that scale to scores.
+// Rows of q as the score products take them, scaled by 2^k.  sum: of a group's values,
+// in the products' scale; unscale: from that scale to scores.
 template <int D, int BITS>
 struct Rows {
   static constexpr int G = D / kCacheGroup, ST = D / 32;
-  bf16x8 q[BITS == 8 ? ST : 1];
-  long part[BITS == 4 ? 3 : 1][BITS == 4 ? ST : 1];
+  f16x8 q[ST];
   float sum[G], unscale;
 
   __device__ __forceinline__ void load(const uint16_t* src, bool have, int g) {
     u32x4 w[ST];
+    float top = 0x1p-100f;
 #pragma unroll
     for (int st = 0; st < ST; ++st) {
       w[st] = u32x4{0, 0, 0, 0};
       if (have) w[st] = *reinterpret_cast<const u32x4*>(src + 32 * st + 8 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        top = fmaxf(top, fmaxf(fabsf(low_of(w[st][e])), fabsf(high_of(w[st][e]))));
     }
-    float x[ST][8], top = 0.0f;
-#pragma unroll
-    for (int st = 0; st < ST; ++st)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[st][2 * e] = __uint_as_float(w[st][e] << 16);
-        x[st][2 * e + 1] = __uint_as_float(w[st][e] & 0xFFFF0000u);
-        top = fmaxf(top, fmaxf(fabsf(x[st][2 * e]), fabsf(x[st][2 * e + 1])));
-      }
+    // The largest value between 2^14 and 2^15.
+    const int k = 15 - __builtin_amdgcn_frexp_expf(col_max(top));
 #pragma unroll
     for (int gi = 0; gi < G; ++gi) sum[gi] = 0.0f;
 #pragma unroll
-    for (int st = 0; st < ST; ++st)
+    for (int st = 0; st < ST; ++st) {
+      u32x4 x;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[st / 2] += x[st][e];
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi) sum[gi] = col_sum(sum[gi]);
-    if constexpr (BITS == 8) {
-#pragma unroll
-      for (int st = 0; st < ST; ++st) q[st] = __builtin_bit_cast(bf16x8, w[st]);
-      unscale = 1.0f;
-    } else {
-      // The largest value between 2^14 and 2^15.
-      const int k = 15 - __builtin_amdgcn_frexp_expf(fmaxf(col_max(top), 0x1p-100f));
-#pragma unroll
-      for (int st = 0; st < ST; ++st) {
-        uint32_t d[3][2];
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          float y[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_ldexpf(x[st][e + i], k);
-#pragma unroll
-          for (int pt = 0; pt < 3; ++pt) {
-            int c = __builtin_amdgcn_cvt_pk_bf8_f32(y[0], y[1], 0, false);
-            c = __builtin_amdgcn_cvt_pk_bf8_f32(y[2], y[3], c, true);
-            d[pt][e / 4] = c;
-            y[0] -= __builtin_amdgcn_cvt_f32_bf8(c, 0);
-            y[1] -= __builtin_amdgcn_cvt_f32_bf8(c, 1);
-            y[2] -= __builtin_amdgcn_cvt_f32_bf8(c, 2);
-            y[3] -= __builtin_amdgcn_cvt_f32_bf8(c, 3);
-          }
-        }
-#pragma unroll
-        for (int pt = 0; pt < 3; ++pt)
-          part[pt][st] = static_cast<long>((static_cast<uint64_t>(d[pt][1]) << 32) | d[pt][0]);
+      for (int e = 0; e < 4; ++e) {
+        const float lo = low_of(w[st][e]), hi = high_of(w[st][e]);
+        sum[st / 2] += lo + hi;
+        x[e] = to_f16(__builtin_amdgcn_ldexpf(lo, k), __builtin_amdgcn_ldexpf(hi, k));
       }
-#pragma unroll
-      for (int gi = 0; gi < G; ++gi) sum[gi] = __builtin_amdgcn_ldexpf(sum[gi], k - 9);
-      unscale = __builtin_amdgcn_ldexpf(1.0f, 9 - k);
+      q[st] = __builtin_bit_cast(f16x8, x);
     }
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) sum[gi] = __builtin_amdgcn_ldexpf(col_sum(sum[gi]), k - kCodeExp<BITS>);
+    unscale = __builtin_amdgcn_ldexpf(1.0f, kCodeExp<BITS> - k);
   }
 
   // acc + q . u over 32 head-dim values of 16 tokens.
   __device__ __forceinline__ f32x4 dot(const uint32_t* codes, int st, f32x4 acc) const {
-    if constexpr (BITS == 8) {
-      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(Unpack<8>::get(codes, 0), q[st], acc, 0, 0, 0);
-    } else {
-      const uint64_t lo = codes[0] & 0x0F0F0F0Fu, hi = (codes[0] >> 4) & 0x0F0F0F0Fu;
-      const long u = static_cast<long>(hi << 32 | lo);
-#pragma unroll
-      for (int pt = 0; pt < 3; ++pt)
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_fp8_bf8(u, part[pt][st], acc, 0, 0, 0);
-      return acc;
-    }
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, codes_f16<BITS>(codes)),
+                                                  q[st], acc, 0, 0, 0);
   }
 };
 
@@ -295,8 +255,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2
             for (int gi = 0; gi < G; ++gi) {
               const uint32_t w = x.kp[tl][e * G + gi];
               const float c = HALF ? (second ? acc[1][gi][e] : acc[0][gi][e]) : acc[tl][gi][e];
-              y = __builtin_fmaf(__uint_as_float(w & 0xFFFF0000u), c, y);
-              y = __builtin_fmaf(__uint_as_float(w << 16), rows[r].sum[gi], y);
+              y = __builtin_fmaf(high_of(w), c, y);
+              y = __builtin_fmaf(low_of(w), rows[r].sum[gi], y);
             }
             sc[tl][e] = y;
           }
@@ -364,8 +324,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(HALF ? 2
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t w = vp[tl][e * G + gi];
-            y[e] = p[tl][e] * __uint_as_float(w & 0xFFFF0000u);
-            pm[r][gi] = __builtin_fmaf(p[tl][e], __uint_as_float(w << 16), pm[r][gi]);
+            y[e] = p[tl][e] * high_of(w);
+            pm[r][gi] = __builtin_fmaf(p[tl][e], low_of(w), pm[r][gi]);
           }
           y2[tl] = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
         }

@@ -1,20 +1,20 @@
 // Attention of many rows over the quantised cache (a chunk of a prompt, or drafts of
 // many heads): the cache's values are rebuilt once per 128 rows.
 //
-// A workgroup owns 128 rows (row = token * group + head; four waves of 32) and walks
+// A workgroup owns 128 or 256 rows (row = token * group + head; waves of 32) and walks
 // its chunk of the tokens in tiles of 64 (two blocks of the cache).  The codes of a
-// tile are fetched two tiles ahead, turned into fp16 values m + s u (rounded once, by
-// one packed fma per pair) and put into LDS one tile ahead, in the order in which the
-// matrix instructions take them: K as [eight head-dim values][token], V as [eight
-// tokens][head-dim value], 16 bytes each, which is how the cache holds them, so that
-// neither needs a transpose.  S^T = K Q^T and O^T += V^T P^T run on
-// v_mfma_f32_32x32x16_f16.
-//
-// fp16 has eight times bf16's precision (a value and a weight are off by at most
-// 2^-11), and its range is made to fit by powers of two: a row of q is scaled to its
-// largest value, a tile of K to its largest (the scores take the power back), V to
-// the largest tile so far (O follows, and takes the power back at the end), and the
-// softmax weights to 2^7 at a row's maximum.
+// tile are fetched two tiles ahead and put into LDS one tile ahead, in the order in
+// which the matrix instructions take them: K as [eight head-dim values][token], V as
+// [eight tokens][head-dim value], 16 bytes each, which is how the cache holds them, so
+// that neither needs a transpose.
+//   K goes in as it is, fp16 numbers whose bits are the code; its steps s are applied
+//   to the scores, and sum_G m_G sum(q_G) comes from a product of the m, bf16 as they
+//   are, with the sums in three bf16 parts: nothing is rounded but fp32 sums.
+//   V goes in as fp16 values m + s u (rounded once, 2^-11, by one packed fma per pair),
+//   in units of a power of two above the largest value of the tiles so far, which O
+//   follows; the softmax weights are fp16 too, 2^7 at a row's maximum.
+// S^T = K Q^T and O^T += V^T P^T run on v_mfma_f32_32x32x16_f16.  A row of q is scaled
+// by a power of two to its largest value.
 //
 // MFMA 32x32x16 lane layout as in sparse_attn.hip: A: row l % 32, K-slots 8 g ..
 // 8 g + 7 (g = l / 32); B: column l % 32, the same slots; C: column l % 32, rows
@@ -26,21 +26,10 @@
 namespace vecattn {
 namespace {
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 constexpr int kTile = 64;       // tokens per tile
 constexpr float kBias = 7.0f;   // log2 of the weight at a row's reference
-
-__device__ __forceinline__ f16x2 to_f16(float x, float y) {
-  return __builtin_convertvector(f32x2{x, y}, f16x2);
-}
-
-// (m, s) of a group.
-__device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float step_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // Largest value over the wave, on every lane (a scalar).
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
@@ -69,22 +58,10 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Eight codes as 1024 + u in fp16 (exact), in slot order.
-template <int BITS, bool V>
-__device__ __forceinline__ void spread8(const uint32_t* w, uint32_t (&r)[4]) {
-  if constexpr (BITS == 8) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      r[i] = __builtin_amdgcn_perm(0x64646464u, w[i >> 1], i & 1 ? 0x04030402u : 0x04010400u);
-  } else if constexpr (V) {   // slots (2 i, 2 i + 1) in nibbles i and i + 4
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = ((w[0] >> (4 * i)) & 0x000F000Fu) | 0x64006400u;
-  } else {                    // slots 0..3 in the even nibbles, 4..7 in the odd
-    const uint32_t lo = w[0] & 0x0F0F0F0Fu, hi = (w[0] >> 4) & 0x0F0F0F0Fu;
-    r[0] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
-    r[1] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
-    r[2] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
-    r[3] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
-  }
+template <int BITS>
+__device__ __forceinline__ u32x4 codes_1024(const uint32_t* w) {
+  const u32x4 x = codes_16<BITS>(w);
+  return u32x4{x[0] | 0x64006400u, x[1] | 0x64006400u, x[2] | 0x64006400u, x[3] | 0x64006400u};
 }
 
 // W waves of 32 rows.
@@ -100,6 +77,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   constexpr int kRows = 32 * W;
   constexpr int kItems = 4 / DW;            // octets of codes in a lane's 16 bytes
   __shared__ __align__(16) f16x8 k_s[2][D / 8][kTile];
+  // K's steps of the last group, and of the first in units of them.
+  __shared__ __align__(16) float step_s[2][kTile], ratio_s[2][kTile];
   __shared__ __align__(16) f16x8 v_s[2][2][4][D];
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
@@ -129,6 +108,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int w_lo = s.p_first + (row0 + 32 * wave) / a.group;
   const int w_hi = s.p_first + (min(row0 + 32 * wave + 32, s.rows) - 1) / a.group;
   f16x8 qf[DS];
+  bf16x8 q_sum;   // a group's sum of q in three parts, against (m, m) pairs (G = 1) or (m_0, m_1)
   float to_log2;
   {
     const u32x4* src =
@@ -141,20 +121,43 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       if (have) w[st] = src[2 * st + g];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        top = fmaxf(top, fmaxf(fabsf(low_of(w[st][e])), fabsf(step_of(w[st][e]))));
+        top = fmaxf(top, fmaxf(fabsf(low_of(w[st][e])), fabsf(high_of(w[st][e]))));
     }
     const int k = 15 - __builtin_amdgcn_frexp_expf(wave_max_xor32(top));
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int st = 0; st < DS; ++st) {
       u32x4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        x[e] = __builtin_bit_cast(
-            uint32_t, to_f16(__builtin_amdgcn_ldexpf(low_of(w[st][e]), k),
-                             __builtin_amdgcn_ldexpf(step_of(w[st][e]), k)));
+      for (int e = 0; e < 4; ++e) {
+        const float lo = low_of(w[st][e]), hi = high_of(w[st][e]);
+        sum[st / 4] += lo + hi;
+        x[e] = to_f16(__builtin_amdgcn_ldexpf(lo, k), __builtin_amdgcn_ldexpf(hi, k));
+      }
       qf[st] = __builtin_bit_cast(f16x8, x);
     }
-    to_log2 = a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, -k);
+    float part[2][3];
+#pragma unroll
+    for (int gi = 0; gi < 2; ++gi) {
+      float x = __builtin_amdgcn_ldexpf(sum[gi] + __shfl_xor(sum[gi], 32), k - kCodeExp<BITS>);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        part[gi][i] = static_cast<float>(static_cast<__bf16>(x));
+        x -= part[gi][i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q_sum[i] = static_cast<__bf16>(0.0f);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      if constexpr (G == 2) {
+        q_sum[2 * i] = static_cast<__bf16>(part[0][i]);
+        q_sum[2 * i + 1] = static_cast<__bf16>(part[1][i]);
+      } else {
+        q_sum[i] = static_cast<__bf16>(part[0][i]);
+      }
+    }
+    to_log2 = fmaxf(a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, kCodeExp<BITS> - k), 0x1p-126f);  // -inf * 0
   }
 
   f32x16 oacc[DB];
@@ -179,11 +182,11 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
                         L::kBytes;
   };
 
-  // What a wave holds of a tile before it is rebuilt: its pieces' codes, the (m, s)
-  // they need, and every token's, one per lane, for the tile's largest value.
+  // What a wave holds of a tile before it is rebuilt: its pieces' codes, the (m, s) that
+  // V's need (they share a block and a group), and every token's, one per lane.
   struct Raw {
     u32x4 kc[kPer], vc[kPer];
-    uint32_t kp[kPer][kItems], vp[8], km[G], vm[G];   // a wave's V pieces share a block and a group
+    uint32_t vp[8], km[G], vm[G];
     uint32_t held;   // bit per block
   };
   // Which piece: block u / kChunks, 1 KB u % kChunks.
@@ -203,16 +206,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     for (int i = 0; i < kPer; ++i) {
       const int u = k_unit(i), c = u % kChunks;
       const uint8_t* p = u / kChunks ? blk[1] : blk[0];
-      const uint32_t* par = reinterpret_cast<const uint32_t*>(p + L::kCodes);
-      if (do_k) {
-        x.kc[i] = *reinterpret_cast<const u32x4*>(p + (c * 64 + lane) * 16);
-#pragma unroll
-        for (int it = 0; it < kItems; ++it)
-          x.kp[i][it] = par[(16 * k_token16(c, it) + n16) * G + k_step(c, it) / 2];
-      }
+      if (do_k) x.kc[i] = *reinterpret_cast<const u32x4*>(p + (c * 64 + lane) * 16);
       if (do_v) {
         p += L::kHalf;
-        par += L::kHalf / 4;
+        const uint32_t* par = reinterpret_cast<const uint32_t*>(p + L::kCodes);
         x.vc[i] = *reinterpret_cast<const u32x4*>(p + (c * 64 + lane) * 16);
         if (i == 0) {
 #pragma unroll
@@ -238,7 +235,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     float top = 0x1p-110f;
 #pragma unroll
     for (int gi = 0; gi < G; ++gi) {
-      const float m = low_of(w[gi]), hi = __builtin_fmaf(step_of(w[gi]), M, m);
+      const float m = low_of(w[gi]), hi = __builtin_fmaf(high_of(w[gi]), M, m);
       top = fmaxf(top, fmaxf(fabsf(m), fabsf(hi)));   // NaN: left out
     }
     return __builtin_amdgcn_frexp_expf(__uint_as_float(wave_max(__float_as_uint(top))));
@@ -246,12 +243,12 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   // Rebuilding a tile: prepare, then its pieces (octets of a lane's codes: kPer * kItems
   // of K, as many of V).
   struct Rebuilt {
-    f16x2 vm2[4], vd2[4];
-    int ke;   // K's power
+    f16x2 m2[4], d2[4];   // V's
+    uint32_t km;          // K's m of this lane's token, as a pair for the product with q_sum
   };
   const f16x2 minus = {_Float16(-1024.0f), _Float16(-1024.0f)};
   // careful: groups that stand for NaN become 0 in V.  Raises v_next to V's power.
-  auto prepare = [&](Raw& x, Rebuilt& y, int tile, int& v_next, bool careful)
+  auto prepare = [&](Raw& x, Rebuilt& y, int tile, int st, int& v_next, bool careful)
                      __attribute__((always_inline)) {
     // Tokens of no page and past the rows' last: as if m = s = 0.
     const int left[2] = {left_in(x, tile, 0), left_in(x, tile, 1)};
@@ -259,20 +256,20 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
 #pragma unroll
       for (int gi = 0; gi < G; ++gi)
         if (ln >= (g ? left[1] : left[0])) x.km[gi] = x.vm[gi] = 0u;
+      const int lim = k_unit(0) / kChunks ? left[1] : left[0];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int u = k_unit(i), lim = u / kChunks ? left[1] : left[0];
-#pragma unroll
-        for (int it = 0; it < kItems; ++it)
-          if (16 * k_token16(u % kChunks, it) + n16 >= lim) x.kp[i][it] = 0u;
-        if (i == 0) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if ((e >> 2) * 16 + 4 * g16 + (e & 3) >= lim) x.vp[e] = 0u;
-        }
-      }
+      for (int e = 0; e < 8; ++e)
+        if ((e >> 2) * 16 + 4 * g16 + (e & 3) >= lim) x.vp[e] = 0u;
     }
-    y.ke = exponent(x.km) - 15;
+    if (wave == 0) {
+      // A last step far below the first is raised to 2^-40 of it, which adds nothing
+      // in fp32.  (NaN is in m too.)
+      const float first = high_of(x.km[0]);
+      const float step = fmaxf(high_of(x.km[G - 1]), first * 0x1p-40f);
+      step_s[st][lane] = step;
+      if (G == 2) ratio_s[st][lane] = step > 0.0f ? first / step : 0.0f;
+    }
+    y.km = __builtin_amdgcn_perm(x.km[G - 1], x.km[0], 0x05040100u);
     v_next = max(v_next, exponent(x.vm) - 15);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -282,73 +279,102 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         uint32_t w = x.vp[2 * e + i];
         if (careful && !(low_of(w) == low_of(w))) w = 0u;
         m[i] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
-        d[i] = __builtin_amdgcn_ldexpf(step_of(w), -v_next);
+        d[i] = __builtin_amdgcn_ldexpf(high_of(w), -v_next);
       }
-      y.vm2[e] = to_f16(m[0], m[1]);
-      y.vd2[e] = to_f16(d[0], d[1]);
+      y.m2[e] = __builtin_bit_cast(f16x2, to_f16(m[0], m[1]));
+      y.d2[e] = __builtin_bit_cast(f16x2, to_f16(d[0], d[1]));
     }
   };
   constexpr int kPieces = 2 * kPer * kItems;
   auto piece = [&](const Raw& x, const Rebuilt& y, int i, int st) __attribute__((always_inline)) {
     const int per = i % (kPer * kItems) / kItems, it = i % kItems;
     const int u = k_unit(per), c = u % kChunks, bl = u / kChunks;
-    uint32_t r[4], cw[DW];
+    uint32_t cw[DW];
     if (i < kPer * kItems) {
       if (!do_k) return;
-      const int t16 = k_token16(c, it), st32 = k_step(c, it);
-      const uint32_t w = x.kp[per][it];
-      const float m = __builtin_amdgcn_ldexpf(low_of(w), -y.ke);
-      const float d = __builtin_amdgcn_ldexpf(step_of(w), -y.ke);
-      const f16x2 m2 = to_f16(m, m), d2 = to_f16(d, d);
 #pragma unroll
       for (int e = 0; e < DW; ++e) cw[e] = x.kc[per][it * DW + e];
-      spread8<BITS, false>(cw, r);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        r[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(
-                                                __builtin_bit_cast(f16x2, r[e]) + minus, d2, m2));
-      k_s[st][4 * st32 + g16][32 * bl + 16 * t16 + n16] =
-          __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
+      k_s[st][4 * k_step(c, it) + g16][32 * bl + 16 * k_token16(c, it) + n16] =
+          __builtin_bit_cast(f16x8, codes_f16<BITS>(cw));
     } else {
       if (!do_v) return;
 #pragma unroll
       for (int e = 0; e < DW; ++e) cw[e] = x.vc[per][it * DW + e];
-      spread8<BITS, true>(cw, r);
+      u32x4 r = codes_1024<BITS>(cw);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        r[e] = __builtin_bit_cast(
-            uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, r[e]) + minus, y.vd2[e],
-                                                y.vm2[e]));
-      v_s[st][bl][g16][16 * (c * kItems + it) + n16] =
-          __builtin_bit_cast(f16x8, u32x4{r[0], r[1], r[2], r[3]});
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t pair = r[e];
+        r[e] = __builtin_bit_cast(uint32_t,
+                                  __builtin_elementwise_fma(__builtin_bit_cast(f16x2, pair) + minus,
+                                                            y.d2[e], y.m2[e]));
+      }
+      v_s[st][bl][g16][16 * (c * kItems + it) + n16] = __builtin_bit_cast(f16x8, r);
     }
   };
 
   auto sees = [&](int j) __attribute__((always_inline)) {
     return j <= pos && (j > pos - a.window || j < a.sinks);
   };
-  // Tile `tile` in stage st: scores (K in units of 2^ke), weights, products.  Operands
+  // Tile `tile` in stage st (km: its tokens' m): scores, weights, products.  Operands
   // are read four instructions ahead; `between` runs beside the score products.
   constexpr int kAhead = 4;
-  auto work = [&](int tile, int st, int ke, uint32_t blocks, auto&& between)
+  auto work = [&](int tile, int st, uint32_t km, uint32_t blocks, auto&& between)
                   __attribute__((always_inline)) {
-    f32x16 sc[2] = {f32x16{}, f32x16{}};
+    f32x16 sc[2];
     {
       f16x8 ring[kAhead];
+      f32x16 acc[2] = {f32x16{}, f32x16{}};
+      // Instruction i: half i / 4 % 2, 16 head-dim values of group i / 8.
       auto read = [&](int i) __attribute__((always_inline)) {
-        if (i < 2 * DS) ring[i % kAhead] = k_s[st][2 * (i % DS) + g][32 * (i / DS) + ln];
+        if (i < 2 * DS)
+          ring[i % kAhead] = k_s[st][2 * (i / 8 * 4 + i % 4) + g][32 * (i / 4 % 2) + ln];
+      };
+      auto of_tokens = [&](const float (&x)[kTile], int hf, int quad) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4*>(&x[32 * hf + 8 * quad + 4 * g]);
+      };
+      // The first group's sums into the second's steps, before those are added.
+      auto to_second = [&](int hf, int quad) __attribute__((always_inline)) {
+        const f32x4 r = of_tokens(ratio_s[st], hf, quad);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[hf][4 * quad + e] *= r[e];
+      };
+      // sum_G m_G sum(q_G): lanes 32 hf .. + 31 hold the half's tokens.
+      auto m_share = [&](int hf) __attribute__((always_inline)) {
+        const uint32_t m = g == hf ? km : 0u;
+        sc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            __builtin_bit_cast(bf16x8, u32x4{m, m, m, 0u}), q_sum, f32x16{}, 0, 0, 0);
+      };
+      auto finish = [&](int hf, int quad) __attribute__((always_inline)) {
+        const f32x4 step = of_tokens(step_s[st], hf, quad);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sc[hf][4 * quad + e] = __builtin_fmaf(acc[hf][4 * quad + e], step[e], sc[hf][4 * quad + e]);
       };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
       for (int i = 0; i < 2 * DS; ++i) {
+        const int hf = i / 4 % 2;
         __builtin_amdgcn_sched_barrier(0);
-        sc[i / DS] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], qf[i % DS],
-                                                            sc[i / DS], 0, 0, 0);
+        acc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], qf[i / 8 * 4 + i % 4],
+                                                         acc[hf], 0, 0, 0);
         read(i + kAhead);
         between(i);
+        // Beside the next four: what the four before need done, a quad or two each.
+        if (G == 2 && i >= 4 && i < 12) {
+          if (i % 4 > 0) to_second((i - 4) / 4, i % 4 - 1);
+          if (i % 4 == 3) to_second((i - 4) / 4, 3);
+        }
+        if (i >= 2 * DS - 4) {
+          if (i % 4 == 0) m_share(0);
+          else finish(0, i % 4 - 1);
+          if (i % 4 == 3) finish(0, 3);
+        }
       }
       __builtin_amdgcn_sched_barrier(0);
+      m_share(1);
+#pragma unroll
+      for (int quad = 0; quad < 4; ++quad) finish(1, quad);
     }
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
@@ -359,8 +385,6 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       for (int e = 0; e < 16; ++e)
         sc[hf][e] = held && sees(j0 + 8 * (e / 4) + 4 * g + e % 4) ? sc[hf][e] : kNegInf;
     }
-    // Not below fp32's normal numbers: -inf * 0 is no mask.
-    const float scale = fmaxf(to_log2 * __builtin_amdgcn_ldexpf(1.0f, ke), 0x1p-126f);
     f32x16 p[2];
     float sum;
     auto weigh = [&]() __attribute__((always_inline)) {
@@ -369,7 +393,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       for (int hf = 0; hf < 2; ++hf) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          p[hf][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[hf][e], scale, -m_run));
+          p[hf][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[hf][e], to_log2, -m_run));
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
           sum += (p[hf][e] + p[hf][e + 1]) + (p[hf][e + 2] + p[hf][e + 3]);
@@ -384,7 +408,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[hf][e]);
-      top = wave_max_xor32(top) * scale - kBias;
+      top = wave_max_xor32(top) * to_log2 - kBias;
       const float m_new = fmaxf(m_run, top);
       const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
       m_run = m_new;
@@ -407,7 +431,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int v0 = 8 * (e >> 1) + 4 * (k % 2) + 2 * (e & 1);
-        w[e] = __builtin_bit_cast(uint32_t, to_f16(p[k / 2][v0], p[k / 2][v0 + 1]));
+        w[e] = to_f16(p[k / 2][v0], p[k / 2][v0 + 1]);
       }
       pb[k] = __builtin_bit_cast(f16x8, w);
     }
@@ -436,26 +460,26 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     Rebuilt re;
     int v_next = v_exp;
     fetch(raw, 0);
-    prepare(raw, re, 0, v_next, false);
+    prepare(raw, re, 0, 0, v_next, false);
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
-    int ke = re.ke;
+    uint32_t km = re.km;
     uint32_t blocks = raw.held;
     if (ntiles > 1) fetch(raw, 1);
     auto turn = [&](int t, int st) __attribute__((always_inline)) {
       lds_barrier();
       follow(v_next);
       const bool more = t + 1 < ntiles;
-      if (more) prepare(raw, re, t + 1, v_next, false);
+      if (more) prepare(raw, re, t + 1, st ^ 1, v_next, false);
       const uint32_t blocks1 = raw.held;
       // The last tile rebuilds what the one before did, into a stage that nothing reads.
-      work(t, st, ke, blocks, [&](int i) __attribute__((always_inline)) {
+      work(t, st, km, blocks, [&](int i) __attribute__((always_inline)) {
         constexpr int every = 2 * DS / kPieces;
         static_assert(every * kPieces == 2 * DS, "pieces fit the score products");
         if (i % every == every - 1) piece(raw, re, i / every, st ^ 1);
         if (i == 2 * DS - 1 && t + 2 < ntiles) fetch(raw, t + 2);
       });
-      ke = re.ke;
+      km = re.km;
       blocks = blocks1;
     };
     int t = 0;
@@ -490,12 +514,12 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       int v_next = v_exp;
       fetch(raw, t);
       __syncthreads();
-      prepare(raw, re, t, v_next, true);
+      prepare(raw, re, t, 0, v_next, true);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
       __syncthreads();
       follow(v_next);
-      work(t, 0, re.ke, raw.held, [](int) {});
+      work(t, 0, re.km, raw.held, [](int) {});
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
         const bool nan = !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));   // 0 where hidden

@@ -9,10 +9,10 @@ x_j = v_j (bf16 rows) or s_j u_j = v_j - m_j (the cache), and e the error of a s
 relative error is about e, and the normaliser's again).  A score of D products accumulated in
 fp32 is off by at most (D + 8) 2^-23 of the sum of its terms' magnitudes (2^-23 a step, so that
 truncating additions are covered too); the cache's 4-bit codes enter as 16 + u, so their terms
-are |q| s (16 + u) and 16 |q| s.  Calls of more than 32 rows per key/value head take the cache's
-values and the weights rounded to fp16 (half a step: 2^-11; scaled by powers of two so that what
-lies below its normal range is under 2^-29 of the largest): 2^-11 |q k| more in a score, and
-2 * 2^-11 sum_j w_j |v_j| in place of 2^-8 sum_j w_j |x_j|.  The sums over keys add n 2^-23 of theirs.  lse is off by e, the
+are |q| s (16 + u) and 16 |q| s.  Calls of more than 32 rows per key/value head take V's values and
+the weights rounded to fp16 (half a step: 2^-11; scaled by powers of two so that what lies below its
+normal range is under 2^-29 of the largest): 2 * 2^-11 sum_j w_j |v_j| in place of 2^-8 sum_j w_j
+|x_j|.  The sums over keys add n 2^-23 of theirs.  lse is off by e, the
 normaliser's n 2^-23 and four ulps of its own fp32 value."""
 import math
 
@@ -73,8 +73,6 @@ def attend(q, k, v, mask, scale, kmag=None, vmag=None, vround=None, fp16=False):
     x = (q @ k.t()) * scale
     x = x.masked_fill(~mask, -math.inf)
     err = ((q.abs() @ kmag.t()) * scale * (D + 8) * STEP).masked_fill(~mask, 0.0)
-    if fp16:
-        err += ((q.abs() @ k.abs().t()) * scale * HALF16 * (1 + HALF)).masked_fill(~mask, 0.0)
     e = err.amax(1, keepdim=True) if mask.shape[1] else torch.zeros(n, 1, dtype=torch.float64)
     lse = torch.logsumexp(x, 1)
     w = torch.exp(x - torch.where(lse == -math.inf, torch.zeros_like(lse), lse)[:, None])
