@@ -557,7 +557,7 @@ def window_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, 
     _call(dev, "window_attn", load().vecattn_window_attn,
           q.data_ptr(), _tdesc(q.shape, q.stride()), k.data_ptr(), _tdesc(k.shape, k.stride()),
           v.data_ptr(), _tdesc(v.shape, v.stride()), None if lens is None else lens.data_ptr(),
-          window, sinks, 1 if causal else 0, scale, out.data_ptr(),
+          int(window), int(sinks), 1 if causal else 0, float(scale), out.data_ptr(),
           _tdesc(out.shape, out.stride()), None if lse is None else lse.data_ptr())
     return (out, lse) if return_lse else out
 
@@ -580,13 +580,8 @@ class Cache:
             raise ValueError(f"data must be a contiguous uint8 tensor of {need} bytes")
 
     def desc(self):
-        return _cache_desc(self.data.data_ptr(), self.pages, self.heads, self.dim, self.page,
-                           self.bits)
-
-
-@functools.lru_cache(maxsize=256)
-def _cache_desc(*fields):
-    return ctypes.byref(CacheDesc(*fields))
+        return ctypes.byref(CacheDesc(self.data.data_ptr(), self.pages, self.heads, self.dim,
+                                      self.page, self.bits))
 
 
 def cache_bytes(pages: int, heads: int, dim: int, page: int = 64, bits: int = 4) -> int:
@@ -654,7 +649,7 @@ def cache_read(cache: Cache, table: torch.Tensor, lens: torch.Tensor, n: int, st
             raise ValueError("out must be a pair of [B, heads, n, dim] tensors")
     _same_device(dev, k=k, v=v)
     _call(dev, "cache_read", load().vecattn_cache_read,
-          cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(), start,
+          cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(), int(start),
           k.data_ptr(), _tdesc(k.shape, k.stride()), v.data_ptr(), _tdesc(v.shape, v.stride()))
     return k, v
 
@@ -674,7 +669,7 @@ def cache_attn_workspace_bytes(q: torch.Tensor, cache: Cache, cols: int,
                                window: Optional[int] = None, sinks: int = 0) -> int:
     """Workspace bytes of cache_attn for these shapes (a table of ``cols`` columns)."""
     return _attn_workspace(q.shape, cache.pages, cache.heads, cache.dim, cache.page, cache.bits,
-                           cols, _ALL_KEYS if window is None else window, sinks)
+                           int(cols), _ALL_KEYS if window is None else int(window), int(sinks))
 
 
 def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.Tensor,
@@ -693,15 +688,14 @@ def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.T
     _bf16_cuda(out, "out")
     _same_device(dev, q=q, out=out, workspace=workspace)
     lse = new(q.shape[:3], dtype=torch.float32) if return_lse else None
-    if window is None:
-        window = _ALL_KEYS
+    window, sinks = _ALL_KEYS if window is None else int(window), int(sinks)
     cols = table.shape[1]
     need = cache_attn_workspace_bytes(q, cache, cols, window, sinks)
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(dev, "cache_attn", load().vecattn_cache_attn,
           q.data_ptr(), _tdesc(q.shape, q.stride()), cache.desc(), table.data_ptr(), cols,
-          lens.data_ptr(), None if n_new is None else n_new.data_ptr(), window, sinks, scale,
+          lens.data_ptr(), None if n_new is None else n_new.data_ptr(), window, sinks, float(scale),
           out.data_ptr(), _tdesc(out.shape, out.stride()), None if lse is None else lse.data_ptr(),
           None if workspace is None else workspace.data_ptr(),
           0 if workspace is None else workspace.numel() * workspace.element_size())

@@ -12,7 +12,8 @@
 //   are, with the sums in three bf16 parts: nothing is rounded but fp32 sums.
 //   V goes in as fp16 values m + s u (rounded once, 2^-11, by one packed fma per pair),
 //   in units of a power of two above the largest value of the tiles so far, which O
-//   follows; the softmax weights are fp16 too, 2^7 at a row's maximum.
+//   follows; the softmax weights are fp16 too, 2^7 at a row's maximum.  Where V's
+//   groups lie more than 2^16 apart the tiles are walked once per such range.
 // S^T = K Q^T and O^T += V^T P^T run on v_mfma_f32_32x32x16_f16.  A row of q is scaled
 // by a power of two to its largest value.
 //
@@ -30,6 +31,7 @@ typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 constexpr int kTile = 64;       // tokens per tile
 constexpr float kBias = 7.0f;   // log2 of the weight at a row's reference
+constexpr int kBand = 16;       // powers of two that V's fp16 values hold at once
 
 // Largest value over the wave, on every lane (a scalar).
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
@@ -64,10 +66,25 @@ __device__ __forceinline__ u32x4 codes_1024(const uint32_t* w) {
   return u32x4{x[0] | 0x64006400u, x[1] | 0x64006400u, x[2] | 0x64006400u, x[3] | 0x64006400u};
 }
 
-// W waves of 32 rows.
-template <int D, int BITS, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void k_cache_chunk(
-    const AttnParams a) {
+template <int D>
+struct Shared {
+  f16x8 k[2][D / 8][kTile];
+  // K's steps of the last group, and of the first in units of them.
+  __align__(16) float step[2][kTile], ratio[2][kTile];
+  f16x8 v[2][2][4][D];
+  uint32_t low[64];   // smallest magnitude of V's groups, by the lane that met it
+  int redo;
+};
+
+// A second walk's first and last power of two of V.
+struct Bands {
+  int low, top;
+};
+
+// A workgroup's work, W waves of 32 rows.  Not CAREFUL: false, and nothing is written,
+// if a careful walk has to follow.
+template <int D, int BITS, int W, bool CAREFUL>
+__device__ __forceinline__ bool walk(const AttnParams& a, Shared<D>& shared, Bands& bands) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, DS = D / 16, DB = D / 32;
   constexpr int kChunks = L::kRun / 4;      // 1 KB pieces of a block's K or V codes
@@ -76,10 +93,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   constexpr int kPer = kSplit ? 1 : kUnits / W;   // pieces a wave takes of either
   constexpr int kRows = 32 * W;
   constexpr int kItems = 4 / DW;            // octets of codes in a lane's 16 bytes
-  __shared__ __align__(16) f16x8 k_s[2][D / 8][kTile];
-  // K's steps of the last group, and of the first in units of them.
-  __shared__ __align__(16) float step_s[2][kTile], ratio_s[2][kTile];
-  __shared__ __align__(16) f16x8 v_s[2][2][4][D];
+  auto& k_s = shared.k;
+  auto& v_s = shared.v;
+  auto &step_s = shared.step, &ratio_s = shared.ratio;
 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ln = lane & 31;
   const int n16 = lane & 15, g16 = lane >> 4;
@@ -88,13 +104,13 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int h = blockIdx.x % a.H;
   const int index = blockIdx.x / a.H;
   const Share share = find_share(a, kRows, index);
-  if (share.unit < 0) return;
+  if (share.unit < 0) return true;
   if (a.target && h == 0 && index == share.first && tid == 0)
     shares_of(a, kRows, D)[share.unit] = int2{share.first, share.count};
   const int64_t b = share.unit / a.tiles;
   const int row0 = share.unit % a.tiles * kRows;
   const Span s = span_of(a, b, row0, kRows);
-  if (row0 >= s.rows) return;
+  if (row0 >= s.rows) return true;
   const int t0 = (index - share.first) * (share.count > 1 ? share.chunk : 0);   // a multiple of 8
   const int t1 = share.count > 1 ? min(s.total, t0 + share.chunk) : s.total;
   const int ntiles = (t1 - t0 + 1) / 2;
@@ -229,16 +245,15 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
   auto left_in = [&](const Raw& x, int tile, int bl) __attribute__((always_inline)) {
     return x.held >> bl & 1u ? min(kCacheBlock, end - first_token(t0 + 2 * tile + bl)) : 0;
   };
-  // Power of two above every |m| and |m + s M| of the tile's tokens.
-  auto exponent = [&](const uint32_t (&w)[G]) __attribute__((always_inline)) {
+  // The larger of a group's |m| and |m + s M|; NaN where it stands for NaN.
+  auto group_top = [&](uint32_t w) __attribute__((always_inline)) {
     constexpr float M = BITS == 4 ? 15.0f : 255.0f;
-    float top = 0x1p-110f;
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi) {
-      const float m = low_of(w[gi]), hi = __builtin_fmaf(high_of(w[gi]), M, m);
-      top = fmaxf(top, fmaxf(fabsf(m), fabsf(hi)));   // NaN: left out
-    }
-    return __builtin_amdgcn_frexp_expf(__uint_as_float(wave_max(__float_as_uint(top))));
+    const float m = low_of(w), hi = __builtin_fmaf(high_of(w), M, m);
+    return m == m ? fmaxf(fabsf(m), fabsf(hi)) : m;
+  };
+  constexpr float kTiny = 0x1p-110f, kHuge = 3.4028234663852886e38f;
+  auto exponent_of = [&](float top) __attribute__((always_inline)) {
+    return __builtin_amdgcn_frexp_expf(fminf(fmaxf(top, kTiny), kHuge));
   };
   // Rebuilding a tile: prepare, then its pieces (octets of a lane's codes: kPer * kItems
   // of K, as many of V).
@@ -247,19 +262,36 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     uint32_t km;          // K's m of this lane's token, as a pair for the product with q_sum
   };
   const f16x2 minus = {_Float16(-1024.0f), _Float16(-1024.0f)};
-  // careful: groups that stand for NaN become 0 in V.  Raises v_next to V's power.
-  auto prepare = [&](Raw& x, Rebuilt& y, int tile, int st, int& v_next, bool careful)
-                     __attribute__((always_inline)) {
-    // Tokens of no page and past the rows' last: as if m = s = 0.
+  // Raises v_next to V's power.  CAREFUL: V's groups that stand for NaN, and those of
+  // another magnitude than 2^band to 2^(band + kBand), become 0.
+  auto left_out = [&](uint32_t w, int band) __attribute__((always_inline)) {
+    const float t = group_top(w);
+    return CAREFUL && (!(t == t) || exponent_of(t) < band || exponent_of(t) > band + kBand);
+  };
+  auto prepare_k = [&](Raw& x, Rebuilt& y, int tile, int st) __attribute__((always_inline)) {
+    // Tokens of no page and those that no row of the workgroup sees: as if m = s = 0.
     const int left[2] = {left_in(x, tile, 0), left_in(x, tile, 1)};
-    if (min(left[0], left[1]) < kCacheBlock) {
+    const int j0[2] = {first_token(t0 + 2 * tile), first_token(t0 + 2 * tile + 1)};
+    // Tokens up to `gone` that are no sinks are behind every row's window.
+    const int gone = s.p_lo - a.window;
+    auto behind = [&](int j) __attribute__((always_inline)) { return j <= gone && j >= a.sinks; };
+    if (min(left[0], left[1]) < kCacheBlock || (j0[0] <= gone && j0[0] + 31 >= a.sinks) ||
+        (j0[1] <= gone && j0[1] + 31 >= a.sinks)) {
+      // (A lane number that is not seen through: nothing of this rare part is held over.)
+      int l = lane;
+      asm volatile("" : "+v"(l));
+      const bool no = (l & 31) >= (l & 32 ? left[1] : left[0]) ||
+                      behind((l & 32 ? j0[1] : j0[0]) + (l & 31));
 #pragma unroll
       for (int gi = 0; gi < G; ++gi)
-        if (ln >= (g ? left[1] : left[0])) x.km[gi] = x.vm[gi] = 0u;
-      const int lim = k_unit(0) / kChunks ? left[1] : left[0];
+        if (no) x.km[gi] = x.vm[gi] = 0u;
+      const int bl = k_unit(0) / kChunks;
+      const int lim = bl ? left[1] : left[0], first = bl ? j0[1] : j0[0];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if ((e >> 2) * 16 + 4 * g16 + (e & 3) >= lim) x.vp[e] = 0u;
+      for (int e = 0; e < 8; ++e) {
+        const int i = (e >> 2) * 16 + (l >> 4 << 2) + (e & 3);
+        if (i >= lim || behind(first + i)) x.vp[e] = 0u;
+      }
     }
     if (wave == 0) {
       // A last step far below the first is raised to 2^-40 of it, which adds nothing
@@ -267,23 +299,45 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       const float first = high_of(x.km[0]);
       const float step = fmaxf(high_of(x.km[G - 1]), first * 0x1p-40f);
       step_s[st][lane] = step;
-      if (G == 2) ratio_s[st][lane] = step > 0.0f ? first / step : 0.0f;
+      if (G == 2) ratio_s[st][lane] = step > 0.0f ? first * __builtin_amdgcn_rcpf(step) : 0.0f;
     }
     y.km = __builtin_amdgcn_perm(x.km[G - 1], x.km[0], 0x05040100u);
-    v_next = max(v_next, exponent(x.vm) - 15);
+  };
+  auto prepare_power = [&](const Raw& x, int& v_next, int band) __attribute__((always_inline)) {
+    float top = 0.0f, low = kHuge;   // of the token's groups that are not 0
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int gi = 0; gi < G; ++gi) {
+      const float t = left_out(x.vm[gi], band) ? 0.0f : group_top(x.vm[gi]);
+      top = fmaxf(top, t);   // NaN: left out
+      low = t > 0.0f ? fminf(low, t) : low;
+    }
+    if (!CAREFUL && wave == 1)
+      __hip_atomic_fetch_min(&shared.low[lane], __float_as_uint(low), __ATOMIC_RELAXED,
+                             __HIP_MEMORY_SCOPE_WORKGROUP);
+    v_next = max(v_next, exponent_of(__uint_as_float(wave_max(__float_as_uint(top)))) - 15);
+  };
+  auto prepare_v = [&](const Raw& x, Rebuilt& y, int half, int v_next, int band)
+                       __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 2 * half; e < 2 * half + 2; ++e) {
       float m[2], d[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         uint32_t w = x.vp[2 * e + i];
-        if (careful && !(low_of(w) == low_of(w))) w = 0u;
+        if (left_out(w, band)) w = 0u;
         m[i] = __builtin_amdgcn_ldexpf(low_of(w), -v_next);
         d[i] = __builtin_amdgcn_ldexpf(high_of(w), -v_next);
       }
       y.m2[e] = __builtin_bit_cast(f16x2, to_f16(m[0], m[1]));
       y.d2[e] = __builtin_bit_cast(f16x2, to_f16(d[0], d[1]));
     }
+  };
+  constexpr int kPrepare = 4;
+  auto prepare = [&](Raw& x, Rebuilt& y, int step, int tile, int st, int& v_next, int band)
+                     __attribute__((always_inline)) {
+    if (step == 0) prepare_k(x, y, tile, st);
+    else if (step == 1) prepare_power(x, v_next, band);
+    else prepare_v(x, y, step - 2, v_next, band);
   };
   constexpr int kPieces = 2 * kPer * kItems;
   auto piece = [&](const Raw& x, const Rebuilt& y, int i, int st) __attribute__((always_inline)) {
@@ -381,22 +435,26 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       const int j0 = first_token(t0 + 2 * tile + hf);
       const bool held = blocks >> hf & 1u;
       if (held && j0 + 31 <= w_lo && (j0 > w_hi - a.window || j0 + 31 < a.sinks)) continue;
+      int l = lane;
+      asm volatile("" : "+v"(l));
 #pragma unroll
       for (int e = 0; e < 16; ++e)
-        sc[hf][e] = held && sees(j0 + 8 * (e / 4) + 4 * g + e % 4) ? sc[hf][e] : kNegInf;
+        sc[hf][e] = held && sees(j0 + 8 * (e / 4) + (l >> 5 << 2) + e % 4) ? sc[hf][e] : kNegInf;
     }
-    f32x16 p[2];
+    u32x4 pw[4];   // the weights as operands: of 16 tokens each, pairs in the order of V's
     float sum;
     auto weigh = [&]() __attribute__((always_inline)) {
       sum = 0.0f;
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
+      for (int e = 0; e < 32; e += 4) {
+        float p[4];
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          p[hf][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[hf][e], to_log2, -m_run));
-#pragma unroll
-        for (int e = 0; e < 16; e += 4)
-          sum += (p[hf][e] + p[hf][e + 1]) + (p[hf][e + 2] + p[hf][e + 3]);
+        for (int i = 0; i < 4; ++i)
+          p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e / 16][e % 16 + i], to_log2, -m_run));
+        sum += (p[0] + p[1]) + (p[2] + p[3]);
+        const int k = 2 * (e / 16) + e / 4 % 2, at = 2 * (e % 16 / 8);
+        pw[k][at] = to_f16(p[0], p[1]);
+        pw[k][at + 1] = to_f16(p[2], p[3]);
       }
     };
     weigh();
@@ -418,7 +476,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       weigh();
     }
     l_run += sum;
-    f16x8 pb[4], ring[kAhead];
+    f16x8 ring[kAhead];
     auto read = [&](int i) __attribute__((always_inline)) {
       const int k = i / DB;
       if (k < 4) ring[i % kAhead] = v_s[st][k / 2][2 * (k % 2) + g][32 * (i % DB) + ln];
@@ -426,20 +484,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) read(i);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int v0 = 8 * (e >> 1) + 4 * (k % 2) + 2 * (e & 1);
-        w[e] = to_f16(p[k / 2][v0], p[k / 2][v0 + 1]);
-      }
-      pb[k] = __builtin_bit_cast(f16x8, w);
-    }
-#pragma unroll
     for (int i = 0; i < 4 * DB; ++i) {
       __builtin_amdgcn_sched_barrier(0);
-      oacc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], pb[i / DB],
-                                                            oacc[i % DB], 0, 0, 0);
+      oacc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+          ring[i % kAhead], __builtin_bit_cast(f16x8, pw[i / DB]), oacc[i % DB], 0, 0, 0);
       read(i + kAhead);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -453,92 +501,96 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     v_exp = v_next;
   };
 
-  __shared__ int s_redo;
-  if (tid == 0) s_redo = 0;
-  if (ntiles > 0) {
-    Raw raw;
-    Rebuilt re;
-    int v_next = v_exp;
-    fetch(raw, 0);
-    prepare(raw, re, 0, 0, v_next, false);
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
-    uint32_t km = re.km;
-    uint32_t blocks = raw.held;
-    if (ntiles > 1) fetch(raw, 1);
-    auto turn = [&](int t, int st) __attribute__((always_inline)) {
-      lds_barrier();
-      follow(v_next);
-      const bool more = t + 1 < ntiles;
-      if (more) prepare(raw, re, t + 1, st ^ 1, v_next, false);
-      const uint32_t blocks1 = raw.held;
-      // The last tile rebuilds what the one before did, into a stage that nothing reads.
-      work(t, st, km, blocks, [&](int i) __attribute__((always_inline)) {
-        constexpr int every = 2 * DS / kPieces;
-        static_assert(every * kPieces == 2 * DS, "pieces fit the score products");
-        if (i % every == every - 1) piece(raw, re, i / every, st ^ 1);
-        if (i == 2 * DS - 1 && t + 2 < ntiles) fetch(raw, t + 2);
-      });
-      km = re.km;
-      blocks = blocks1;
-    };
-    int t = 0;
-    for (; t + 1 < ntiles; t += 2) {
-      turn(t, 0);
-      turn(t + 1, 1);
-    }
-    if (t < ntiles) turn(t, 0);
-  }
-
-  // A group of V that stands for NaN reaches rows that do not see its token (0 * NaN
-  // in the product).  So a workgroup with anything not finite walks its tiles again,
-  // with such groups taken out of the products and added to the rows that see them.
-  float fin = l_run * 0.0f;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) fin = __builtin_fmaf(oacc[db][e], 0.0f, fin);
-  __syncthreads();
-  if (__any(have && fin != 0.0f) && lane == 0) s_redo = 1;
-  __syncthreads();
-  if (__builtin_amdgcn_readfirstlane(s_redo)) {
-    m_run = kUnseen;
-    l_run = 0.0f;
-    v_exp = -200;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-#pragma unroll 1
-    for (int t = 0; t < ntiles; ++t) {
+  if constexpr (!CAREFUL) {
+    if (tid == 0) shared.redo = 0;
+    if (wave == 1) shared.low[lane] = __float_as_uint(kHuge);
+    if (ntiles > 0) {
       Raw raw;
       Rebuilt re;
       int v_next = v_exp;
-      fetch(raw, t);
-      __syncthreads();
-      prepare(raw, re, t, 0, v_next, true);
+      fetch(raw, 0);
+#pragma unroll
+      for (int i = 0; i < kPrepare; ++i) prepare(raw, re, i, 0, 0, v_next, 0);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
-      __syncthreads();
-      follow(v_next);
-      work(t, 0, re.km, raw.held, [](int) {});
+      uint32_t km = re.km;
+      uint32_t blocks = raw.held;
+      if (ntiles > 1) fetch(raw, 1);
+      auto turn = [&](int t, int st) __attribute__((always_inline)) {
+        lds_barrier();
+        follow(v_next);
+        const uint32_t blocks1 = raw.held;
+        // The next tile is prepared and rebuilt: K's pieces in the first half, V's in the
+        // second.  The last tile does so with what it was itself, into a stage that
+        // nothing reads.
+        work(t, st, km, blocks, [&](int i) __attribute__((always_inline)) {
+          constexpr int every = 2 * DS / kPieces;
+          static_assert(every * kPieces == 2 * DS && kPrepare <= DS, "fits the score products");
+          if (i < kPrepare) prepare(raw, re, i, t + 1, st ^ 1, v_next, 0);
+          if (i % every == every - 1) piece(raw, re, i / every, st ^ 1);
+          if (i == 2 * DS - 1 && t + 2 < ntiles) fetch(raw, t + 2);
+        });
+        km = re.km;
+        blocks = blocks1;
+      };
+      int t = 0;
+      for (; t + 1 < ntiles; t += 2) {
+        turn(t, 0);
+        turn(t + 1, 1);
+      }
+      if (t < ntiles) turn(t, 0);
+    }
+    float fin = l_run * 0.0f;
 #pragma unroll
-      for (int gi = 0; gi < G; ++gi) {
-        const bool nan = !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));   // 0 where hidden
-        for (uint64_t left = __ballot(nan); left; left &= left - 1) {
-          const int i = __builtin_ctzll(left);
-          if (!sees(first_token(t0 + 2 * t + (i >> 5)) + (i & 31))) continue;
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int db = 2 * gi; db < 2 * gi + 2; ++db)
+      for (int e = 0; e < 16; ++e) fin = __builtin_fmaf(oacc[db][e], 0.0f, fin);
+    __syncthreads();
+    if (__any(have && fin != 0.0f) && lane == 0) shared.redo = 1;
+    __syncthreads();
+    bands.top = v_exp + 15;
+    bands.low = min(bands.top, exponent_of(__uint_as_float(~wave_max(~shared.low[lane]))));
+    if (__builtin_amdgcn_readfirstlane(shared.redo) || bands.low < bands.top - kBand) return false;
+  } else {
+#pragma unroll 1
+    for (int band = bands.low; band <= bands.top; band += kBand + 1) {
+      const float l_band = l_run;
+#pragma unroll 1
+      for (int t = 0; t < ntiles; ++t) {
+        Raw raw;
+        Rebuilt re;
+        int v_next = v_exp;
+        fetch(raw, t);
+        __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[db][e] = __builtin_nanf("");
+        for (int i = 0; i < kPrepare; ++i) prepare(raw, re, i, t, 0, v_next, band);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) piece(raw, re, i, 0);
+        __syncthreads();
+        follow(v_next);
+        work(t, 0, re.km, raw.held, [](int) {});
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+          const bool nan = !(low_of(raw.vm[gi]) == low_of(raw.vm[gi]));   // 0 where hidden
+          for (uint64_t left = __ballot(nan); left; left &= left - 1) {
+            const int i = __builtin_ctzll(left);
+            if (!sees(first_token(t0 + 2 * t + (i >> 5)) + (i & 31))) continue;
+#pragma unroll
+            for (int db = 2 * gi; db < 2 * gi + 2; ++db)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) oacc[db][e] = __builtin_nanf("");
+          }
         }
       }
+      // The weights' sums are whole after the first (and the references do not move).
+      if (band > bands.low) l_run = l_band;
     }
   }
 
   l_run += __shfl_xor(l_run, 32);
-  if (!have) return;
-  const float back = __builtin_amdgcn_ldexpf(1.0f, v_exp);
+  if (!have) return true;
   if (share.count > 1) {
+    const float back = __builtin_amdgcn_ldexpf(1.0f, v_exp);
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kRows + 32 * wave + ln;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -554,9 +606,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
       ml[0] = m_run;
       ml[1] = l_run;
     }
-    return;
+    return true;
   }
-  const float inv = (l_run > 0.0f ? 1.0f / l_run : l_run);   // no key: 0; NaN stays
+  // No key: 0; NaN stays.  2^60: O of a row that saw none of V's largest stays normal.
+  const float inv = (l_run > 0.0f ? 1.0f / l_run : l_run) * 0x1p60f;
   uint16_t* orow = a.o + b * a.o_sB + hq * a.o_sH + tok * a.o_sN;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -564,12 +617,26 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     for (int vq = 0; vq < 4; ++vq) {
       f32x4 y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = oacc[db][4 * vq + e] * inv * back;
+      for (int e = 0; e < 4; ++e) y[e] = __builtin_amdgcn_ldexpf(oacc[db][4 * vq + e] * inv, v_exp - 60);
       *reinterpret_cast<bf16x4*>(orow + 32 * db + 8 * vq + 4 * g) = __builtin_convertvector(y, bf16x4);
     }
   if (a.lse && g == 0)
     a.lse[(b * a.H * a.group + hq) * a.n + tok] =
         l_run == 0.0f ? kNegInf : (m_run + __builtin_log2f(l_run)) * kLn2;
+  return true;
+}
+
+// A group of V that stands for NaN reaches rows that do not see its token (0 * NaN in
+// the product), and one above 2^kBand times another costs that one bits in fp16.  So a
+// workgroup with anything not finite, or with V's magnitudes that far apart, walks its
+// tiles again: once for each kBand powers of two, the smallest first, with the other
+// groups taken out of V; NaN is added to the rows that see it.
+template <int D, int BITS, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void k_cache_chunk(
+    const AttnParams a) {
+  __shared__ __align__(16) Shared<D> shared;
+  Bands bands;
+  if (!walk<D, BITS, W, false>(a, shared, bands)) walk<D, BITS, W, true>(a, shared, bands);
 }
 
 }  // namespace

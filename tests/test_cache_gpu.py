@@ -446,3 +446,33 @@ def test_two_calls_at_once(gpu):
     torch.cuda.synchronize()
     for i in range(2):
         assert all(torch.equal(o, want[i]) for o in got[i])
+
+
+@pytest.mark.parametrize("D,bits", [(128, 4), (64, 4), (128, 8), (64, 8)])
+@pytest.mark.parametrize("n,Hq", [(3, 2), (50, 2), (50, 7)])
+def test_values_of_far_apart_magnitudes(gpu, D, bits, n, Hq):
+    """Tokens of V far above or below the others: rows that do not see them, other head-dim
+    groups and rows that see small ones alone keep their own values' precision."""
+    L, window = 700, 100
+    table, pages = paged([L], 32)
+    k, v0 = rows(891, 1, 1, L, D), rows(892, 1, 1, L, D)
+    q = rows(893, 1, Hq, n, D)
+    first = L - n - window + 1          # the first key that row 0 sees
+    g = torch.Generator().manual_seed(5)
+    spread = torch.randint(-40, 40, (L,), generator=g).float().exp2().bfloat16().cuda()
+    for what in ("behind", "seen by some", "half a row", "spread"):
+        v = v0.clone()
+        if what == "behind":
+            v[0, 0, first - 1] *= 1e30
+        elif what == "seen by some":
+            v[0, 0, first + 1] *= 1e30
+        elif what == "half a row":
+            v[..., :64] *= 2.0 ** -45
+            v[..., 70:] *= 2.0 ** 20
+        else:
+            v *= spread[None, None, :, None]
+        cache = fresh_cache(pages, 1, D, 32, bits)
+        va.cache_write(cache, k, v, table, int32([L]))
+        o, lse = va.cache_attn(q, cache, table, int32([L]), window=window, return_lse=True)
+        ref.check(o, lse, ref.cache_attn(q, [k[0].cpu()], [v[0].cpu()], bits, [L], None, window),
+                  what)
