@@ -10,7 +10,10 @@
 //
 // A workgroup takes one block of 32 tokens of one head, so that no two write the
 // same bytes (V's codes of eight tokens share a dword).  Both kernels are bound by
-// memory.
+// memory for long prompts: 32768 tokens, 4 heads of 128, 4 bits (86 MB) are written in
+// 19.5 us (4.4 TB/s) and read back in 15 (5.7, the codes still in cache), 131072 tokens
+// (344 MB) in 79 us (4.4 TB/s).  A call for single tokens takes 5 us, most of it the
+// chain of loads length, table, store.
 #include "cache_common.h"
 
 namespace vecattn {

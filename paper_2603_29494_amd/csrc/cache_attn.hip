@@ -25,6 +25,12 @@
 // sums what the sequences see, takes chunks of such a size that the workgroups fill
 // the chip, and finds its own chunk; k_cache_merge joins the chunks of a row.
 //
+// Bound by memory in long sequences: 28 query and 4 key/value heads of 128 over 4 x
+// 131072 tokens of 4 bits take 54 us (302 MB, 5.6 TB/s) and the join 5.  In short ones
+// by the chain of loads before the first codes (lengths, table, codes) and the join
+// after the last: 9 us for 700 tokens; 64 sequences of 37 to 8192 tokens, 8 heads, take
+// 32 us (105 MB, 3.3 TB/s).
+//
 // MFMA 16x16x32 lane layout (lane l = 16 g + n): A: row n, K-slots 8 g .. 8 g + 7;
 // B: column n, the same slots; C: column n, rows 4 g .. 4 g + 3.
 #include <algorithm>
@@ -520,8 +526,12 @@ Deal deal(const CacheAttnShape& s) {
   d.half = rows <= 8;
   d.many = rows > 32;
   d.R = rows <= 16 ? 1 : 2;
-  // Few row tiles: more waves on each, and half the chunks to join.  Many rows: eight
-  // waves share what rebuilding a tile costs.
+  // Eight rows at most: few row tiles take more waves on each, and have half the chunks
+  // to join (16 sequences x 4 heads, a window of 4096: 14.1 us, 16.8 with four waves);
+  // many fill the chip with four (64 x 8 heads: 117 us, 129 with eight).  Many rows:
+  // eight waves share what rebuilding a tile costs (136 rows: 66 us, 69 with four; 3584
+  // rows: 364 and 441), but not where half of them had no row (40 rows: 65, 111 with
+  // eight).  From 33 rows on rebuilding pays (24 rows: 37 us, 63 rebuilt).
   d.W = d.many ? (rows > 128 ? 8 : 4) : d.half && s.B * s.H <= 128 ? 8 : 4;
   d.rows = d.many ? 32 * d.W : d.half ? 8 : 16 * d.R;
   d.tiles = static_cast<int32_t>((rows + d.rows - 1) / d.rows);
@@ -531,18 +541,24 @@ Deal deal(const CacheAttnShape& s) {
   const int64_t seen = std::min(held, (std::min<int64_t>(s.window, held * 32) +
                                        std::min<int64_t>(s.n, d.rows) + 31) / 32 + 1 +
                                           (std::min<int64_t>(s.sinks, held * 32) + 31) / 32);
-  constexpr int64_t kLeast = 32;
-  d.least = kLeast;
-  d.merge = seen > kLeast && d.units <= kMaxUnits;
+  // Blocks that pay for a chunk's start and end (128 rows of 4 x 16k tokens rebuilt: 50
+  // us with 16, 60 with 24; 16 rows of 8 x 32k: 24 us with 32, 27 with 64).
+  d.least = d.many ? 16 : 32;
+  d.merge = seen > d.least && d.units <= kMaxUnits;
   d.items = d.units * s.H;
   d.target = 0;
   if (d.merge) {
-    // Workgroups that run at a time (two of four waves per CU, or one of eight), once,
-    // or twice where a workgroup's work is long, and at least twice the row tiles.
-    const int64_t slots = 256 * 8 / d.W;
-    const int64_t rounds = std::max<int64_t>(d.many ? 2 : 1, (2 * d.items + slots - 1) / slots);
+    // The workgroups that run at a time: two of four waves per CU, or one of eight, or
+    // one of 32 rows x 128 values, whose registers leave one wave per SIMD (32 rows of 8
+    // x 16k tokens: 38 us with 256, 46 with 512; of 64 values 44 and 35 with 32k).  Never
+    // fewer than two chunks per row tile, and two workgroups after each other where
+    // their work is long, so that those of hidden tokens even out (512 tokens over 33k:
+    // 364 us, 420 with one).
+    const int64_t slots = d.W == 8 || (!d.many && d.R == 2 && s.D == 128) ? 256 : 512;
+    int64_t rounds = std::max<int64_t>(1, (2 * d.items + slots - 1) / slots);
+    if (d.many && d.items * seen >= 64 * 2 * slots) rounds = std::max<int64_t>(2, rounds);
     d.target = static_cast<int32_t>(slots * rounds);
-    d.items = std::min<int64_t>(d.target, d.items * ((seen + kLeast - 1) / kLeast));
+    d.items = std::min<int64_t>(d.target, d.items * ((seen + d.least - 1) / d.least));
   }
   return d;
 }
@@ -601,7 +617,8 @@ hipError_t launch_cache_attn(const CacheAttnArgs& x, hipStream_t stream) {
     else launch(k_cache_attn<D, BITS, 2, false, 4>);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !d.merge) return e;
-    // A wave per row where rows fill the chip, four where they do not.
+    // A wave per row where rows fill the chip, four where they do not (14336 rows: 10 us
+    // less than with four; 256 rows of 64 chunks: 2 us less than with one).
     const int64_t n = x.shape.B * x.shape.Hq * x.shape.n;
     if (n > 2048)
       hipLaunchKernelGGL((k_cache_merge<D, 1>), dim3(static_cast<unsigned>((n + 3) / 4)), dim3(256),

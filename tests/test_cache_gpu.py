@@ -476,3 +476,10 @@ def test_values_of_far_apart_magnitudes(gpu, D, bits, n, Hq):
         o, lse = va.cache_attn(q, cache, table, int32([L]), window=window, return_lse=True)
         ref.check(o, lse, ref.cache_attn(q, [k[0].cpu()], [v[0].cpu()], bits, [L], None, window),
                   what)
+
+
+@pytest.mark.parametrize("D,bits,page", FORMATS)
+@pytest.mark.parametrize("n,Hq,H", [(4, 8, 1), (3, 14, 2), (12, 8, 1), (20, 16, 2)])
+def test_long_sequences_of_several_tokens(gpu, n, Hq, H, D, bits, page):
+    """32, 21, 96 and 160 rows per key/value head over sequences in many chunks."""
+    attn_case(895, [6001, 1700, n, 40], Hq, H, n, D, bits, page)

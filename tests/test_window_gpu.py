@@ -168,3 +168,10 @@ def test_long_rows_past_32_bit_offsets(gpu):
     kk, vv = k[:, :, near].contiguous(), v[:, :, near].contiguous()
     r = ref.window_attn(q, kk, vv, 333, 9, True)
     ref.check(o, lse, r)
+
+
+def test_scale_near_zero(gpu):
+    """Every visible key weighs the same, and none of the others."""
+    q, k, v = rows(91, 1, 2, 200, 128), rows(92, 1, 2, 200, 128), rows(93, 1, 2, 200, 128)
+    o, lse = va.window_attn(q, k, v, 30, 3, True, scale=1e-40, return_lse=True)
+    ref.check(o, lse, ref.window_attn(q, k, v, 30, 3, True, scale=1e-40))
