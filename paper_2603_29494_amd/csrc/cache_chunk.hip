@@ -43,10 +43,9 @@ constexpr int kBand = 16;       // powers of two that V's fp16 values hold at on
 // Largest value over the wave, on every lane (a scalar).
 __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
   auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
-    const int y = __builtin_amdgcn_update_dpp(static_cast<int>(x), static_cast<int>(x),
-                                              decltype(ctrl)::value, decltype(rows)::value, 0xf,
-                                              false);
-    x = max(x, static_cast<uint32_t>(y));
+    x = max(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+                0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false)),
+            x);   // 0 where no lane is read: max changes nothing, and takes the move in
   };
   using std::integral_constant;
   step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});   // row_shr:1
@@ -390,26 +389,32 @@ __device__ __forceinline__ bool walk(const AttnParams& a, Shared<D>& shared, Ban
         if (i < 2 * DS)
           ring[i % kAhead] = k_s[st][2 * (i / 8 * 4 + i % 4) + g][32 * (i / 4 % 2) + ln];
       };
-      auto of_tokens = [&](const float (&x)[kTile], int hf, int quad) __attribute__((always_inline)) {
-        return *reinterpret_cast<const f32x4*>(&x[32 * hf + 8 * quad + 4 * g]);
+      // What the scores need beside the products, four values of a lane at a time, one per
+      // instruction from the fifth on: with two groups first the first one's sums into the
+      // second's steps (before those are added), then the steps and the m's share.  The
+      // factors are read two instructions before.
+      constexpr int kJobs = 8 * G;
+      f32x4 factor[3];
+      auto read_factor = [&](int job) __attribute__((always_inline)) {
+        if (job < 0 || job >= kJobs) return;
+        const float* x = job < 8 * (G - 1) ? ratio_s[st] : step_s[st];
+        factor[job % 3] = *reinterpret_cast<const f32x4*>(x + 32 * (job / 4 % 2) + 8 * (job % 4) + 4 * g);
       };
-      // The first group's sums into the second's steps, before those are added.
-      auto to_second = [&](int hf, int quad) __attribute__((always_inline)) {
-        const f32x4 r = of_tokens(ratio_s[st], hf, quad);
+      auto apply = [&](int job) __attribute__((always_inline)) {
+        if (job < 0) return;
+        const int hf = job / 4 % 2;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[hf][4 * quad + e] *= r[e];
+        for (int e = 0; e < 4; ++e) {
+          const int at = 4 * (job % 4) + e;
+          if (job < 8 * (G - 1)) acc[hf][at] *= factor[job % 3][e];
+          else sc[hf][at] = __builtin_fmaf(acc[hf][at], factor[job % 3][e], sc[hf][at]);
+        }
       };
       // sum_G m_G sum(q_G): lanes 32 hf .. + 31 hold the half's tokens.
       auto m_share = [&](int hf) __attribute__((always_inline)) {
         const uint32_t m = g == hf ? km : 0u;
         sc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
             __builtin_bit_cast(bf16x8, u32x4{m, m, m, 0u}), q_sum, f32x16{}, 0, 0, 0);
-      };
-      auto finish = [&](int hf, int quad) __attribute__((always_inline)) {
-        const f32x4 step = of_tokens(step_s[st], hf, quad);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sc[hf][4 * quad + e] = __builtin_fmaf(acc[hf][4 * quad + e], step[e], sc[hf][4 * quad + e]);
       };
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) read(i);
@@ -420,22 +425,18 @@ __device__ __forceinline__ bool walk(const AttnParams& a, Shared<D>& shared, Ban
         acc[hf] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ring[i % kAhead], qf[i / 8 * 4 + i % 4],
                                                          acc[hf], 0, 0, 0);
         read(i + kAhead);
+        read_factor(i - 2);
         between(i);
-        // Beside the next four: what the four before need done, a quad or two each.
-        if (G == 2 && i >= 4 && i < 12) {
-          if (i % 4 > 0) to_second((i - 4) / 4, i % 4 - 1);
-          if (i % 4 == 3) to_second((i - 4) / 4, 3);
-        }
-        if (i >= 2 * DS - 4) {
-          if (i % 4 == 0) m_share(0);
-          else finish(0, i % 4 - 1);
-          if (i % 4 == 3) finish(0, 3);
-        }
+        apply(i - 4);
+        if (i == 2 * DS - 5) m_share(0);
       }
       __builtin_amdgcn_sched_barrier(0);
       m_share(1);
 #pragma unroll
-      for (int quad = 0; quad < 4; ++quad) finish(1, quad);
+      for (int i = 2 * DS; i < 2 * DS + 4; ++i) {
+        read_factor(i - 2);
+        apply(i - 4);
+      }
     }
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
