@@ -20,8 +20,8 @@
 // What bounds it: VALU work that runs beside the products only in part (per score two
 // scalings, an exponential with its argument, sum and rounding; the rebuilding), and
 // registers, all 256 of which are taken, so that two waves per SIMD are the most.  512
-// tokens of 28 query and 4 key/value heads of 128 over 33280 tokens of 8 bits: 362 us
-// with the join (242 GFLOP, 670 TFLOP/s), of which a walk with K rounded to fp16 values
+// tokens of 28 query and 4 key/value heads of 128 over 33280 tokens of 8 bits: 358 us
+// with the join (242 GFLOP, 677 TFLOP/s), of which a walk with K rounded to fp16 values
 // saves 20 and loses two digits of lse.
 //
 // MFMA 32x32x16 lane layout as in sparse_attn.hip: A: row l % 32, K-slots 8 g ..
