@@ -300,12 +300,17 @@ __device__ __forceinline__ bool walk(const AttnParams& a, Shared<D>& shared, Ban
       }
     }
     if (wave == 0) {
-      // A last step far below the first is raised to 2^-40 of it, which adds nothing
-      // in fp32.  (NaN is in m too.)
+      // Scores are step * (ratio * first group's + last group's).  Steps are 0 or from
+      // 2^-100 on, and the reciprocal takes no subnormal numbers: a last step of 0 (its
+      // codes are 0) is held as 2^-126.  One more than 2^100 below the first is raised
+      // to that, so that the ratio is at most 2^100.  (NaN is in m too.)
       const float first = high_of(x.km[0]);
-      const float step = fmaxf(high_of(x.km[G - 1]), first * 0x1p-40f);
+      float step = high_of(x.km[G - 1]);
+      if (G == 2) {
+        step = fmaxf(fmaxf(step, first * 0x1p-100f), 0x1p-126f);
+        ratio_s[st][lane] = first * __builtin_amdgcn_rcpf(step);
+      }
       step_s[st][lane] = step;
-      if (G == 2) ratio_s[st][lane] = step > 0.0f ? first * __builtin_amdgcn_rcpf(step) : 0.0f;
     }
     y.km = __builtin_amdgcn_perm(x.km[G - 1], x.km[0], 0x05040100u);
   };
