@@ -424,7 +424,8 @@ vecattn_status vecattn_recall(const void* q, const vecattn_tdesc* qd, const void
  *   causal : the VECATTN_CAUSAL bit (other bits are invalid)
  *   scale  : 0 means 1 / sqrt(D)
  *   lse    : optional fp32 [B, Hq, Nq] contiguous output, may be NULL
- * A key outside a row's V(p) never reaches that row, whatever it holds.
+ * A key outside a row's V(p) never reaches that row, whatever it holds.  The sums
+ * are fp32: finite |V| up to 2^100 leaves finite rows finite.
  * Errors: INVALID_ARG (null pointer, shape mismatch, Nq > Nk, window < 1, sinks
  * < 0, bad scale or bits, misalignment); UNSUPPORTED (D not in {64, 128}, more
  * than 65535 sequences or query heads or 2^23 tiles of 128 rows in all, a K or V

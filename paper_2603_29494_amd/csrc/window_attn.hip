@@ -202,8 +202,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
   // Weights above 256 went into O and l as they are; the row's reference moves up by
-  // a power of two for the tiles to come.  A weight past fp32 range leaves O or l
-  // infinite, which the end of the walk sees.
+  // a power of two for the tiles to come.  A weight, or its product with V, past fp32
+  // range leaves O or l infinite, which the end of the walk sees.
   auto move = [&](float tsum) __attribute__((always_inline)) {
     if (__any(tsum > 256.0f)) {
       const float top = wave_max_xor32(tsum);
@@ -215,13 +215,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       m_run += static_cast<float>(up);
     }
   };
-  // The weights of keys 16 ks .. + 15 of a tile, and their sum.
-  auto weigh = [&](const f32x16 (&s)[2], int ks, float& sum) __attribute__((always_inline)) {
+  // The weights of keys 16 ks .. + 15 of a tile, times alpha, and their sum.
+  auto weigh = [&](const f32x16 (&s)[2], int ks, float alpha, float& sum)
+                   __attribute__((always_inline)) {
     f32x8 p;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       p[e] = __builtin_amdgcn_exp2f(
-          __builtin_fmaf(s[ks >> 1][8 * (ks & 1) + e], a.scale_log2, -m_run));
+                 __builtin_fmaf(s[ks >> 1][8 * (ks & 1) + e], a.scale_log2, -m_run)) *
+             alpha;
     sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     return __builtin_convertvector(p, bf16x8);
   };
@@ -344,9 +346,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
 
   // A NaN or an infinity of a V row reaches rows of its tile that do not see it
-  // (0 * NaN in the product).  So a workgroup with anything not finite walks its
-  // tiles again, with such values taken out of the products and added to the rows
-  // that see them.
+  // (0 * NaN in the product), and a weight taken before its row's reference has moved
+  // may be past fp32 range, by itself or times V.  So a workgroup with anything not
+  // finite walks its tiles again, with such values taken out of the products and added
+  // to the rows that see them, and references moved first.
   float fin = l_run * 0.0f;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -378,21 +381,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       score(s[0], 0, 0);
       score(s[1], 0, 1);
       ready(s, j0);
-      // A row with weights near the end of fp32 range takes its reference from the
-      // tile first; the others go as before, to the same bits.
-      float sum[4];
+      // A row whose weights are past fp32 range takes its reference from the tile first.
+      // The others' references move as after a first walk's tile, by the same power of
+      // two, but before the products, which a large V would take past fp32 range:
+      // (O + P V) 2^-up = O 2^-up + (P 2^-up) V to the bit.
+      float sum[4], alpha = 1.0f;
       bf16x8 pb[4];
+      auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) pb[ks] = weigh(s, ks, sum[ks]);
-      float tsum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      const int far_up = !(tsum <= 1e30f);
-      const bool over = (far_up | __shfl_xor(far_up, 32)) != 0;
+        for (int ks = 0; ks < 4; ++ks) pb[ks] = weigh(s, ks, alpha, sum[ks]);
+        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      };
+      float tsum = weights();
+      const int past = !(tsum < INFINITY);
+      const bool over = (past | __shfl_xor(past, 32)) != 0;
       if (__any(over)) {
         refer(s, over);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) pb[ks] = weigh(s, ks, sum[ks]);
-        tsum = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tsum = weights();
       }
+      float shift = 0.0f;
+      if (__any(tsum > 256.0f)) {
+        const float top = wave_max_xor32(tsum);
+        const int up = top > 256.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
+        shift = static_cast<float>(up);
+        alpha = __builtin_amdgcn_ldexpf(1.0f, -up);
+        tsum = weights();
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+      }
+      m_run += shift;
       l_run += tsum;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
@@ -419,7 +437,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             if (not_finite(x)) oacc[db][e] += bf16_bits_to_f32(x);
           }
       }
-      move(tsum);
     }
   }
 
