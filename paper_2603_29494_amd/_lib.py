@@ -687,6 +687,8 @@ def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.T
         out = new(q.shape)
     _bf16_cuda(out, "out")
     _same_device(dev, q=q, out=out, workspace=workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     lse = new(q.shape[:3], dtype=torch.float32) if return_lse else None
     window, sinks = _ALL_KEYS if window is None else int(window), int(sinks)
     cols = table.shape[1]
