@@ -69,18 +69,19 @@ def cache_attn(q, k, v, bits, lens, window=1 << 30, sinks=0, scale=0.0, k_as=Non
     for b, L in enumerate(lens):
         mask = ref.sees(torch.arange(n) + L - n, torch.arange(L), window, sinks, True, L)
         group = Hq // k[b].shape[0]
-        for h in range(Hq):
-            u, m, s = ref.quantise(k[b][h // group].cpu(), bits)
+        many = n * group > 32
+        for g in range(k[b].shape[0]):
+            u, m, s = ref.quantise(k[b][g].cpu(), bits)
             su, m = ref.spread(s) * u.view(L, D), ref.spread(m)
             kk = m + su if k_as is None else (m + su).to(k_as).double()
-            vu, vm, vs = ref.quantise(v[b][h // group].cpu(), bits)
+            vu, vm, vs = ref.quantise(v[b][g].cpu(), bits)
             vu, vm, vs = (vu.long() & v_mask).view(L, D), ref.spread(vm), ref.spread(vs)
             vv = vm + vs * vu
-            many = n * group > 32
             rounded = 2 * HALF16 * vv.abs() if many else HALF * vs * vu
             summed = vv.abs() if many else vm.abs() + vs * (vu + (32 if bits == 4 else 0))
-            out.append(attend(q[b, h], kk, vv, q[b, h] ** 2 @ (su ** 2 + m ** 2).t(), mask, scale,
-                              rounded, summed))
+            for h in range(g * group, (g + 1) * group):
+                out.append(attend(q[b, h], kk, vv, q[b, h] ** 2 @ (su ** 2 + m ** 2).t(), mask,
+                                  scale, rounded, summed))
     return tuple(torch.stack(x).unflatten(0, (B, Hq)) for x in zip(*out))
 
 
