@@ -491,7 +491,9 @@ vecattn_status vecattn_cache_write(const void* k, const vecattn_tdesc* kd, const
 
 /*
  * The cache's tokens [start, start + N) of each sequence as bf16, m + s u rounded
- * once (e.g. a cached prompt for vecattn_select and vecattn_sparse_attn).
+ * once (e.g. a whole cached prompt for vecattn_select and vecattn_sparse_attn, which
+ * take as many rows of q as of k; a part of one for vecattn_window_attn, whose
+ * queries may be fewer than the keys).
  *   k, v : bf16 [B, H, N, D] outputs; row r is token start + r.  Rows of tokens
  *          at or past lens[b], and of tokens that no page holds, are left as they
  *          were.

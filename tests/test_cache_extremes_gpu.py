@@ -147,3 +147,16 @@ def test_two_graphs_with_one_workspace(gpu):
             graphs[i].replay()
             torch.cuda.synchronize()
             assert torch.equal(outs[i], va.cache_attn(qs[i], cache, table, lens)), (L2, i)
+
+
+@pytest.mark.parametrize("start", [0, 417])
+def test_a_cached_prompt_in_a_window_layer(gpu, start):
+    """New queries over the part of a cached prompt that their window holds, read back as bf16."""
+    L, n, window, D = 700, 150, 134, 128     # the first query sees from 417 on
+    k, v, q = rows(1, 1, 2, L, D), rows(2, 1, 2, L, D), rows(3, 1, 6, n, D)
+    cache, table, lens = cached(k, v, 8)
+    gk, gv = va.cache_read(cache, table, lens, L - start, start=start)
+    o, lse = va.window_attn(q, gk, gv, window, 0, True, return_lse=True)
+    hk, hv = (torch.stack([ref.held(h.cpu(), 8) for h in x[0]])[None].bfloat16() for x in (k, v))
+    assert torch.equal(gk.cpu(), hk[:, :, start:]) and torch.equal(gv.cpu(), hv[:, :, start:])
+    near(o, lse, sb.window_attn(q, hk, hv, window, 0, True))
