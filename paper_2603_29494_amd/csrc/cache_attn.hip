@@ -531,7 +531,14 @@ Deal deal(const CacheAttnShape& s) {
   // many fill the chip with four (64 x 8 heads: 117 us, 129 with eight).  Many rows:
   // eight waves share what rebuilding a tile costs (136 rows: 66 us, 69 with four; 3584
   // rows: 364 and 441), but not where half of them had no row (40 rows: 65, 111 with
-  // eight).  From 33 rows on rebuilding pays (24 rows: 37 us, 63 rebuilt).
+  // eight).
+  // Up to 32 rows the codes go in as they are (8 sequences of 16k tokens, 4 heads, 4 bits,
+  // 24 rows: 37 us, 60 rebuilt; 32 rows 38 and 60).  From 33 on rows take rebuilt tiles,
+  // which keep 11 bits of the weights and of V where the other way keeps 8 of the
+  // weights.  That is also the faster way for 65 rows and more over long sequences (96
+  // rows 68 us, 124 in tiles of 32 rows; 128 rows 73 and 105), but not for fewer (35 rows
+  // 62 and 59; of 64 values over 32k tokens 86 and 53) unless they are very many tokens (4
+  // x 131k: 201 and 215), nor over short ones (700 tokens: 27 and 15.5).
   d.W = d.many ? (rows > 128 ? 8 : 4) : d.half && s.B * s.H <= 128 ? 8 : 4;
   d.rows = d.many ? 32 * d.W : d.half ? 8 : 16 * d.R;
   d.tiles = static_cast<int32_t>((rows + d.rows - 1) / d.rows);
