@@ -513,7 +513,8 @@ vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* tab
  * page holds; the values are m + s u, and o, lse as for vecattn_sparse_attn (a
  * row that sees nothing: o = 0, lse = -inf).  Rounded are only the softmax weights
  * before they meet V (bf16's 8 bits times V's steps; with more than 32 rows, n * Hq
- * / H, fp16's 11 bits, and V's values to as many; lse is from what was not rounded)
+ * / H, fp16's 11 bits, down to 2^-32 of the row's largest weight, and V's values to
+ * as many, down to 2^-39 of the largest; lse is from what was not rounded)
  * and the output.  The sums are fp32: |q|, |K| and |V| up to 2^100.  The new tokens'
  * own K and V are in the cache already (vecattn_cache_write with the same lens).
  *   q, o   : bf16 [B, Hq, n, D], Hq a multiple of the cache's H

@@ -12,8 +12,9 @@
 //   are, with the sums in three bf16 parts: nothing is rounded but fp32 sums.
 //   V goes in as fp16 values m + s u (rounded once, 2^-11, by one packed fma per pair),
 //   in units of a power of two above the largest value of the tiles so far, which O
-//   follows; the softmax weights are fp16 too, 2^7 at a row's maximum.  Where V's
-//   groups lie more than 2^16 apart the tiles are walked once per such range.
+//   follows; the softmax weights are fp16 too, 2^7 at a row's maximum (below 2^-21 of
+//   that they lose bits, below 2^-32 they are 0).  Where V's groups lie more than 2^16
+//   apart the tiles are walked once per such range.
 // S^T = K Q^T and O^T += V^T P^T run on v_mfma_f32_32x32x16_f16.  A row of q is scaled
 // by a power of two to its largest value.
 //

@@ -14,8 +14,10 @@ after at most 16 additions among them: sqrt(keys / 64 + 16) 2^-23.
 
 o: the weights w are rounded before they meet V, independently of each other, to bf16 (half a step,
 2^-8, of w s u; of w v where V is bf16 rows) or, with more than 32 rows per key/value head, to fp16
-like V (2^-11 of w v, twice): that times the root of the sum of squares over the keys.  The result
-is rounded to bf16: 2^-8 |o|.  The weights' errors are lse's and the scores': two sizes, times sum
+like V (2^-11 of w v, twice): that times the root of the sum of squares over the keys.  The fp16
+weights are 2^7 and more at a row's largest, V 2^14 at its largest, and what lies below fp16's normal
+range is off by up to 2^-25: 2^-32 max |v| a key, as independently.  The result is rounded to bf16:
+2^-8 |o|.  The weights' errors are lse's and the scores': two sizes, times sum
 w |v|.  The fp32 sums: sqrt(keys) 2^-23 of sum w |v|, and of w s (16 + u) and w s 16 where 4-bit
 codes enter as 16 + u.
 
@@ -29,10 +31,10 @@ import window_reference as ref
 STEP, HALF, HALF16 = 2.0 ** -23, 2.0 ** -8, 2.0 ** -11
 
 
-def attend(q, k, v, terms2, mask, scale, rounded, summed):
+def attend(q, k, v, terms2, mask, scale, rounded, summed, fp16=False):
     """One head: q [n, D], k, v [L, D] float64 where mask [n, L]; terms2 [n, L]: ||t||^2; rounded
     [L, D]: what a rounded weight multiplies, times half a step; summed [L, D]: magnitudes of what
-    is summed to o.  Returns lse, its size, o, its size."""
+    is summed to o; fp16: weights and V are.  Returns lse, its size, o, its size."""
     x = ((q @ k.t()) * scale).masked_fill(~mask, -math.inf)
     lse = torch.logsumexp(x, 1)
     w = torch.exp(x - lse[:, None])
@@ -42,6 +44,8 @@ def attend(q, k, v, terms2, mask, scale, rounded, summed):
     o = w @ v
     osize = (w ** 2 @ rounded ** 2).sqrt() + HALF * o.abs() + 2 * size[:, None] * (w @ v.abs())
     osize += cnt.sqrt()[:, None] * STEP * (w @ summed) + 1e-30
+    if fp16:
+        osize += cnt.sqrt()[:, None] * 2.0 ** -32 * v[mask.any(0)].abs().max()
     return lse, size, o, osize
 
 
@@ -81,7 +85,7 @@ def cache_attn(q, k, v, bits, lens, window=1 << 30, sinks=0, scale=0.0, k_as=Non
             summed = vv.abs() if many else vm.abs() + vs * (vu + (32 if bits == 4 else 0))
             for h in range(g * group, (g + 1) * group):
                 out.append(attend(q[b, h], kk, vv, q[b, h] ** 2 @ (su ** 2 + m ** 2).t(), mask,
-                                  scale, rounded, summed))
+                                  scale, rounded, summed, many))
     return tuple(torch.stack(x).unflatten(0, (B, Hq)) for x in zip(*out))
 
 
