@@ -545,6 +545,186 @@ vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
                                   void* stream);
 
 /*
+ * What new tokens' attention puts on each cached token, added up: the measure by which
+ * a cache can drop what is not looked at.  For token j of a key/value head h,
+ *   w[b,h,j] = sum over the rows r of q, and the query heads that read h, that see j, of
+ *              exp(scale * <q_r, k_j> - lse_r),
+ * with lse from vecattn_cache_attn over the same cache and sequences, and
+ *   out[b,h,j] = w + decay * mass[b,h,j]      for tokens before the new ones,
+ *   out[b,h,j] = w                            for the new ones (mass is not read),
+ * j < lens[b].  A row whose lse is -inf adds nothing; a token that no page holds gets
+ * w = 0.  Entries at or past lens[b] are left as they were.
+ *   q, table, cols, lens, n_new, window, sinks, scale : as for vecattn_cache_attn
+ *   lse  : fp32 [B, Hq, n] contiguous
+ *   mass : optional fp32 [B, H, M] contiguous; NULL: 0.  May be out itself.
+ *   out  : fp32 [B, H, M] contiguous; tokens at or past M have no entry
+ * Sums are fp32, of one order (no atomics).  Asynchronous, one launch.
+ * Errors: as vecattn_cache_attn; INVALID_ARG for M < 1 or > 2^30, or a decay that is
+ * negative or not finite.
+ */
+vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const float* lse,
+                                  const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, const int32_t* n_new, int64_t window,
+                                  int64_t sinks, float scale, float decay, const float* mass,
+                                  float* out, int64_t M, void* stream);
+
+/*
+ * Which tokens of each sequence and head a budget keeps.  Candidates are the tokens
+ * j < min(lens[b], M) that a page holds; kept are min(budget, candidates) of them: those
+ * with j < sinks or j >= lens[b] - recent first, then by mass, the largest first, equal
+ * ones the lower index first (-0 equals 0; a NaN comes after all others).
+ *   mass : fp32 [B, H, M] contiguous        cache : its pages, H and page size
+ *   table, cols, lens : as for vecattn_cache_write
+ *   idx  : int32 [B, H, budget] output, ascending, -1 past the kept ones
+ *   kept : int32 [B] output, how many (the same for every head): lens of the pages
+ *          that vecattn_cache_gather fills
+ * Asynchronous, one launch.
+ * Errors: INVALID_ARG (null pointer, B < 1, M or budget < 1 or > 2^30, sinks or recent
+ * < 0, sinks + recent > budget, a bad cache, cols < 1 or cols * page > 2^30); UNSUPPORTED
+ * (more than 65535 sequences or heads).
+ */
+vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
+                                  const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, int64_t budget, int64_t sinks,
+                                  int64_t recent, int32_t* idx, int32_t* kept, void* stream);
+
+/*
+ * Moves chosen tokens, per head, into other pages: slot i < kept[b] of sequence b and
+ * head h takes token idx[b,h,i] of the same sequence and head, codes and (m, s) as they
+ * are.  Keys keep the rotary positions they were written with; a window of
+ * vecattn_cache_attn counts slots.
+ *   idx, kept : as from vecattn_cache_keep (any indices are accepted, in any order; one
+ *          that is negative or of a token that no page holds leaves a slot that stands for
+ *          NaN; kept is clamped to [0, budget])
+ *   to, to_table, to_cols : the cache (it may be the same one) and pages that take the
+ *          tokens.  No page of to_table may be one that this call reads.  Slots whose
+ *          entry names no page are not written; what the written pages' blocks of 32 slots
+ *          held past kept[b] is lost.
+ *   mass : optional fp32 [B, H, M] contiguous; with mass_out, fp32 [B, H, budget]
+ *          contiguous: mass_out[b,h,i] = mass[b,h,idx[b,h,i]] for i < kept[b] (NaN for an
+ *          index outside [0, M)), the rest left as it was.  Both or neither.
+ * Asynchronous, one launch.
+ * Errors: INVALID_ARG (null pointer, one of mass and mass_out alone, B < 1, budget or M
+ * < 1 or > 2^30, caches of other heads, D or bits, a bad cache, cols or to_cols < 1 or
+ * more than 2^30 tokens); UNSUPPORTED (more than 65535 sequences or heads).
+ */
+vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                    int64_t B, const int32_t* idx, const int32_t* kept,
+                                    int64_t budget, const vecattn_cache* to,
+                                    const int32_t* to_table, int64_t to_cols, const float* mass,
+                                    int64_t M, float* mass_out, void* stream);
+
+/*
+ * Attention of rows over another sequence's keys, such as an encoder's states (encoded
+ * text under a video layer, encoded frames under a decoder): every row sees the keys
+ *   V(b) = { j < lens[b] : mask[b][j] != 0 },
+ * o and lse as for vecattn_sparse_attn (where V(b) is empty: o = 0, lse = -inf).
+ *   q, o : bf16 [B, Hq, Nq, D]     k, v : bf16 [B, Hkv, Nk, D], any Nq and Nk
+ *   lens : optional int32 [B] device memory (clamped to [0, Nk]); NULL: all Nk.  Keys at
+ *          or past it are not read.
+ *   mask : optional bytes [B, Nk] device memory, mask_sB from one sequence to the next
+ *          (0: one for all); what a masked key holds, NaN and infinities too, reaches no row
+ *   n_q  : optional int32 [B] device memory (clamped to [0, Nq]): the rows of sequence b
+ *          that exist; those past it are left as they were.  NULL: all Nq.
+ *   scale : 0 means 1 / sqrt(D)
+ *   lse  : optional fp32 [B, Hq, Nq] contiguous output, may be NULL
+ *   workspace : device memory (16-byte aligned) of at least
+ *          vecattn_cross_attn_workspace_size bytes for the same qd and kd (0: may be
+ *          NULL); contents need not be initialised.  Calls that may overlap need one each.
+ * Scores and sums are fp32, the weights bf16 before they meet V.  The result does not
+ * depend on the order of execution (no atomics).  What a call does follows lens, mask and
+ * n_q on the device, so that a captured call can be replayed as they change.
+ * Errors: INVALID_ARG (null pointer, shape mismatch, Hq % Hkv != 0, mask_sB < 0, a bad
+ * scale, misalignment); CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128},
+ * Nq * Hq / Hkv > 2^30, more than 2^24 sequences times Hkv, about 2^23 workgroups, a K or
+ * V row stride of 2^24 elements or more).
+ */
+vecattn_status vecattn_cross_attn_workspace_size(const vecattn_tdesc* qd, const vecattn_tdesc* kd,
+                                                 size_t* bytes);
+vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const void* k,
+                                  const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,
+                                  const int32_t* lens, const uint8_t* mask, int64_t mask_sB,
+                                  const int32_t* n_q, float scale, void* o,
+                                  const vecattn_tdesc* od, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
+ * Rotary positions: pairs (a, b) of a row's first `rot` values are turned by the angle
+ * t = position * frequency of the pair,
+ *   a' = factor * (a cos t - b sin t),   b' = factor * (a sin t + b cos t);
+ * transposed, t is -t (with the same factor: the gradient of the turn, and with factor 1
+ * its inverse).  Values past rot stay as they are, bit for bit.
+ */
+typedef enum vecattn_rope_layout {
+  VECATTN_ROPE_HALF = 0,       /* pair i is values i and i + rot / 2 */
+  VECATTN_ROPE_INTERLEAVED = 1 /* pair i is values 2 i and 2 i + 1 */
+} vecattn_rope_layout;
+
+typedef enum vecattn_rope_scaling { /* for contexts longer than the trained one */
+  VECATTN_ROPE_NONE = 0,   /* f_i = base^(-2 i / rot) */
+  VECATTN_ROPE_LINEAR = 1, /* f_i / factor */
+  VECATTN_ROPE_NTK = 2,    /* base * factor^(rot / (rot - 2)) in place of base: the lowest
+                              frequency divided by factor, the highest as it was */
+  VECATTN_ROPE_PARTS = 3,  /* pairs up to the one that makes `fast` turns over `context`
+                              keep f_i, from the one that makes `slow` on f_i / factor, those
+                              between (both rounded outwards) a share of each that is linear
+                              in i; the turned values times 0.1 ln(factor) + 1 */
+  VECATTN_ROPE_BANDS = 4   /* the same, but the share is linear in the turns c f_i / 2 pi */
+} vecattn_rope_scaling;
+
+typedef struct vecattn_rope_spec {
+  int32_t rot;         /* values turned: even, 2 to D */
+  int32_t layout;      /* vecattn_rope_layout */
+  int32_t axes;        /* positions per token, 1 to 4 (e.g. time, height, width) */
+  int32_t transposed;  /* 0 or 1 */
+  double factor;
+  const double* freq;  /* host memory, rot / 2 frequencies in radians per position */
+  const int32_t* axis; /* host memory, rot / 2: which position turns each pair; NULL: the
+                          first */
+} vecattn_rope_spec;
+
+/*
+ * A ladder of frequencies (host function, no GPU) for vecattn_rope_spec.
+ *   fast, slow, context : of PARTS and BANDS (not read by the others); factor : of all but
+ *          NONE
+ *   freq : double [rot / 2] output       mfactor : output, factor for the spec
+ * Errors: INVALID_ARG (null output, rot odd or outside [2, 128], base <= 1, an unknown
+ * scaling, factor < 1, context <= 0, slow <= 0, fast <= slow, anything not finite).
+ */
+vecattn_status vecattn_rope_ladder(int32_t rot, double base, int32_t scaling, double factor,
+                                   double context, double fast, double slow, double* freq,
+                                   double* mfactor);
+
+/*
+ * Turns the rows of q, and of k if it is not NULL, by their positions.
+ *   q, qo : bf16 [B, Hq, N, D]      k, ko : bf16 [B, Hkv, N, D], both NULL or neither
+ *           (kd and kod too).  An output may be its input (the same pointer and strides); the
+ *           tensors must not overlap otherwise.
+ *   spec  : read during the call
+ *   positions of row r of sequence b, one of:
+ *     pos  : int32 device memory, pos[axis * pos_sA + b * pos_sB + r] (strides in
+ *            elements, >= 0; 0 shares one row of positions)
+ *     lens : int32 [B] device memory, lens[b] - n_new[b] + r on every axis, as
+ *            vecattn_cache_write places rows
+ *     neither: start + r on every axis
+ *   n_new : optional int32 [B] device memory (clamped to [0, N]): the rows of sequence b
+ *           that exist; those past it are left as they were.  NULL: all N.
+ * Angles are taken in 64 bits and reduced exactly, sines and cosines are good to fp32 at
+ * any position, and a result is rounded to bf16 once.  Asynchronous, one launch.
+ * Errors: INVALID_ARG (null pointer, shape mismatch, both pos and lens, |start| > 2^30,
+ * a bad stride, a spec outside what its comments allow, a factor or frequency that is not
+ * finite, |frequency| > 1024, an output that is its input with other strides,
+ * misalignment); UNSUPPORTED (D not in {64, 128}, more than 65535 heads in all, B * N >
+ * 2^30).
+ */
+vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* k,
+                            const vecattn_tdesc* kd, const vecattn_rope_spec* spec,
+                            const int32_t* pos, int64_t pos_sA, int64_t pos_sB,
+                            const int32_t* lens, const int32_t* n_new, int64_t start, void* qo,
+                            const vecattn_tdesc* qod, void* ko, const vecattn_tdesc* kod,
+                            void* stream);
+
+/*
  * Per-head filter ratios, Eq. 5 (Sec. 3.1.2).  Host function (host memory, no
  * GPU).
  * For each of `heads` heads, n_cand candidate filter ratios were sampled

@@ -41,6 +41,13 @@ class CacheDesc(ctypes.Structure):
                 ("D", ctypes.c_int32), ("page", ctypes.c_int32), ("bits", ctypes.c_int32)]
 
 
+class RopeSpec(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("layout", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("transposed", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("freq", ctypes.POINTER(ctypes.c_double)),
+                ("axis", ctypes.POINTER(ctypes.c_int32))]
+
+
 _lib = None
 
 
@@ -93,6 +100,15 @@ def load() -> ctypes.CDLL:
                                                       ctypes.POINTER(ctypes.c_size_t)]
     lib.vecattn_cache_attn.argtypes = [P, D, C, P, i64, P, P, i64, i64, f32, P, D, P, P,
                                        ctypes.c_size_t, P]
+    lib.vecattn_cache_mass.argtypes = [P, D, P, C, P, i64, P, P, i64, i64, f32, f32, P, P, i64, P]
+    lib.vecattn_cache_keep.argtypes = [P, i64, i64, C, P, i64, P, i64, i64, i64, P, P, P]
+    lib.vecattn_cache_gather.argtypes = [C, P, i64, i64, P, P, i64, C, P, i64, P, i64, P, P]
+    lib.vecattn_cross_attn_workspace_size.argtypes = [D, D, ctypes.POINTER(ctypes.c_size_t)]
+    lib.vecattn_cross_attn.argtypes = [P, D, P, D, P, D, P, P, i64, P, f32, P, D, P, P,
+                                       ctypes.c_size_t, P]
+    lib.vecattn_rope_ladder.argtypes = [i32, f64, i32, f64, f64, f64, f64, P, ctypes.POINTER(f64)]
+    lib.vecattn_rope.argtypes = [P, D, P, D, ctypes.POINTER(RopeSpec), P, i64, i64, P, P, i64, P, D,
+                                 P, D, P]
     for name in ("vecattn_pool", "vecattn_select_max_count", "vecattn_select_workspace_size",
                  "vecattn_select", "vecattn_select_mins_tiled", "vecattn_sparse_attn",
                  "vecattn_plan_filter_ratios", "vecattn_select_per_head",
@@ -100,7 +116,10 @@ def load() -> ctypes.CDLL:
                  "vecattn_head_sparsity", "vecattn_recall", "vecattn_select_noalloc",
                  "vecattn_sparse_attn_ordered", "vecattn_attn_order", "vecattn_window_attn",
                  "vecattn_cache_size", "vecattn_cache_write", "vecattn_cache_read",
-                 "vecattn_cache_attn_workspace_size", "vecattn_cache_attn"):
+                 "vecattn_cache_attn_workspace_size", "vecattn_cache_attn",
+                 "vecattn_cache_mass", "vecattn_cache_keep", "vecattn_cache_gather",
+                 "vecattn_cross_attn_workspace_size", "vecattn_cross_attn",
+                 "vecattn_rope_ladder", "vecattn_rope"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -702,3 +721,260 @@ def cache_attn(q: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.T
           None if workspace is None else workspace.data_ptr(),
           0 if workspace is None else workspace.numel() * workspace.element_size())
     return (out, lse) if return_lse else out
+
+
+def _fp32_on(t: torch.Tensor, shape, device, name: str):
+    if t.dtype is not torch.float32 or t.shape != shape or t.device != device \
+            or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor on {device}")
+
+
+def cache_mass(q: torch.Tensor, lse: torch.Tensor, cache: Cache, table: torch.Tensor,
+               lens: torch.Tensor, mass: Optional[torch.Tensor] = None,
+               n_new: Optional[torch.Tensor] = None, window: Optional[int] = None, sinks: int = 0,
+               scale: float = 0.0, decay: float = 1.0, out: Optional[torch.Tensor] = None
+               ) -> torch.Tensor:
+    """The attention weight that the new tokens of q [B, Hq, n, dim] put on each cached token, per
+    key/value head (vecattn_cache_mass), added to ``decay`` times ``mass`` (float32 [B, heads, M];
+    0 when not given, M then the table's tokens).  ``lse``: what cache_attn returned for the same
+    q, cache, ``window`` and ``sinks``.  ``out`` may be ``mass``; entries of tokens at or past
+    ``lens`` are left as they were in a given ``out``, and 0 in one made here."""
+    _bf16_cuda(q, "q")
+    B = q.shape[0]
+    dev = _cache_args(cache, table, lens, B, n_new)
+    cols = table.shape[1]
+    given = out if out is not None else mass
+    M = cols * cache.page if given is None or given.dim() != 3 else given.shape[2]
+    shape = (B, cache.heads, M)
+    if out is None:
+        out = q.new_zeros(shape, dtype=torch.float32)
+    _same_device(dev, q=q)
+    _fp32_on(lse, q.shape[:3], dev, "lse")
+    _fp32_on(out, shape, dev, "out")
+    if mass is not None:
+        _fp32_on(mass, shape, dev, "mass")
+    _call(dev, "cache_mass", load().vecattn_cache_mass,
+          q.data_ptr(), _tdesc(q.shape, q.stride()), lse.data_ptr(), cache.desc(),
+          table.data_ptr(), cols, lens.data_ptr(), None if n_new is None else n_new.data_ptr(),
+          _ALL_KEYS if window is None else int(window), int(sinks), float(scale), float(decay),
+          None if mass is None else mass.data_ptr(), out.data_ptr(), M)
+    return out
+
+
+def cache_keep(mass: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.Tensor,
+               budget: int, sinks: int = 0, recent: int = 0
+               ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Which tokens of each head a ``budget`` keeps (vecattn_cache_keep): the first ``sinks``, the
+    last ``recent``, and the heaviest by ``mass`` (float32 [B, heads, M]).  Returns idx (int32 [B,
+    heads, budget], ascending, -1 padded) and kept (int32 [B]), how many each sequence has."""
+    dev = _cache_args(cache, table, lens, mass.shape[0])
+    if mass.dim() != 3:
+        raise ValueError("mass must be [B, heads, M]")
+    B, M = mass.shape[0], mass.shape[2]
+    _fp32_on(mass, (B, cache.heads, M), dev, "mass")
+    idx = mass.new_empty((B, cache.heads, int(budget)), dtype=torch.int32)
+    kept = mass.new_empty((B,), dtype=torch.int32)
+    _call(dev, "cache_keep", load().vecattn_cache_keep,
+          mass.data_ptr(), M, B, cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(),
+          int(budget), int(sinks), int(recent), idx.data_ptr(), kept.data_ptr())
+    return idx, kept
+
+
+def cache_gather(cache: Cache, table: torch.Tensor, idx: torch.Tensor, kept: torch.Tensor,
+                 to_table: torch.Tensor, to: Optional[Cache] = None,
+                 mass: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Moves tokens ``idx`` (int32 [B, heads, budget], kept[b] of them) of each head into the pages
+    of ``to_table``, which no page of ``table`` may be among (vecattn_cache_gather); of the same
+    cache or of ``to``.  With ``mass`` (float32 [B, heads, M]) returns theirs ([B, heads, budget],
+    0 past kept)."""
+    if idx.dim() != 3:
+        raise ValueError("idx must be [B, heads, budget]")
+    to = cache if to is None else to
+    B, budget = idx.shape[0], idx.shape[2]
+    dev = _cache_args(cache, table, kept, B)
+    _cache_args(to, to_table, kept, B)
+    _int32_on(idx, (B, cache.heads, budget), dev, "idx")
+    out, M = None, 0
+    if mass is not None:
+        M = mass.shape[-1]
+        _fp32_on(mass, (B, cache.heads, M), dev, "mass")
+        out = mass.new_zeros((B, cache.heads, budget))
+    _call(dev, "cache_gather", load().vecattn_cache_gather,
+          cache.desc(), table.data_ptr(), table.shape[1], B, idx.data_ptr(), kept.data_ptr(),
+          budget, to.desc(), to_table.data_ptr(), to_table.shape[1],
+          None if mass is None else mass.data_ptr(), M, None if out is None else out.data_ptr())
+    return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _cross_workspace(q_shape, k_shape) -> int:
+    if len(q_shape) != 4 or len(k_shape) != 4:
+        raise ValueError("expected [B, H, N, D] tensors")
+    n = ctypes.c_size_t(0)
+    qd, kd = TDesc(*q_shape, 0, 0, q_shape[3]), TDesc(*k_shape, 0, 0, k_shape[3])
+    _check(load().vecattn_cross_attn_workspace_size(ctypes.byref(qd), ctypes.byref(kd),
+                                                    ctypes.byref(n)), "cross_attn_workspace_size")
+    return n.value
+
+
+def cross_attn_workspace_bytes(q: torch.Tensor, k: torch.Tensor) -> int:
+    """Workspace bytes of cross_attn for these shapes."""
+    return _cross_workspace(q.shape, k.shape)
+
+
+def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+               lens: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+               n_q: Optional[torch.Tensor] = None, scale: float = 0.0,
+               out: Optional[torch.Tensor] = None, return_lse: bool = False,
+               workspace: Optional[torch.Tensor] = None):
+    """Attention of q [B, Hq, Nq, D] over another sequence's k, v [B, Hkv, Nk, D]
+    (vecattn_cross_attn): the keys below ``lens`` (int32 [B]) that ``mask`` (bool or uint8 [B, Nk],
+    true: seen) leaves.  ``n_q`` (int32 [B]): the rows of each sequence that exist; padded rows of a
+    given ``out`` are left as they were (0 in an ``out`` made here)."""
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _bf16_cuda(t, n)
+    dev = q.device
+    new = q.new_empty if n_q is None else q.new_zeros
+    if out is None:
+        out = new(q.shape)
+    _bf16_cuda(out, "out")
+    _same_device(dev, k=k, v=v, out=out, mask=mask, workspace=workspace)
+    need = cross_attn_workspace_bytes(q, k)
+    B, Nk = k.shape[0], k.shape[2]
+    if lens is not None:
+        _int32_on(lens, q.shape[:1], dev, "lens")
+    if n_q is not None:
+        _int32_on(n_q, q.shape[:1], dev, "n_q")
+    mask_sB = 0
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8) or mask.shape != (B, Nk) \
+                or (Nk > 1 and mask.stride(1) != 1):
+            raise ValueError("mask must be a bool or uint8 [B, Nk] tensor with contiguous rows")
+        mask_sB = mask.stride(0) if B > 1 else 0
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    lse = new(q.shape[:3], dtype=torch.float32) if return_lse else None
+    _call(dev, "cross_attn", load().vecattn_cross_attn,
+          q.data_ptr(), _tdesc(q.shape, q.stride()), k.data_ptr(), _tdesc(k.shape, k.stride()),
+          v.data_ptr(), _tdesc(v.shape, v.stride()), None if lens is None else lens.data_ptr(),
+          None if mask is None else mask.data_ptr(), mask_sB,
+          None if n_q is None else n_q.data_ptr(), float(scale), out.data_ptr(),
+          _tdesc(out.shape, out.stride()), None if lse is None else lse.data_ptr(),
+          None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel() * workspace.element_size())
+    return (out, lse) if return_lse else out
+
+
+_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROPE_SCALINGS = {None: 0, "linear": 1, "ntk": 2, "parts": 3, "bands": 4}
+
+
+@dataclass(frozen=True)
+class Rope:
+    """How rows are turned by their positions (vecattn_rope_spec): ``freq`` in radians per
+    position, one per pair, ``axis`` the position that turns each pair, ``factor`` of the turned
+    values."""
+    layout: str
+    freq: Tuple[float, ...]
+    axis: Tuple[int, ...]
+    factor: float = 1.0
+
+    def __post_init__(self):
+        n = len(self.freq)
+        if self.layout not in _ROPE_LAYOUTS:
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        if n < 1 or len(self.axis) != n:
+            raise ValueError("freq and axis need an entry per pair")
+        specs = []
+        freq, axis = (ctypes.c_double * n)(*self.freq), (ctypes.c_int32 * n)(*self.axis)
+        for transposed in (0, 1):
+            specs.append(RopeSpec(2 * n, _ROPE_LAYOUTS[self.layout], max(self.axis) + 1, transposed,
+                                  float(self.factor), freq, axis))
+        object.__setattr__(self, "_specs", tuple(specs))
+
+    @property
+    def axes(self) -> int:
+        return max(self.axis) + 1
+
+
+def rope_ladder(rot: int, base: float = 10000.0, scaling: Optional[str] = None,
+                factor: float = 1.0, context: float = 0.0, fast: float = 32.0, slow: float = 1.0):
+    """Frequencies of rot / 2 pairs and the factor of the turned values (vecattn_rope_ladder);
+    ``scaling`` for contexts ``factor`` times longer: None, "linear", "ntk", "parts" or "bands"."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {list(_ROPE_SCALINGS)}")
+    freq, m = (ctypes.c_double * max(1, int(rot) // 2))(), ctypes.c_double(0.0)
+    _check(load().vecattn_rope_ladder(int(rot), float(base), _ROPE_SCALINGS[scaling], float(factor),
+                                      float(context), float(fast), float(slow), freq,
+                                      ctypes.byref(m)), "rope_ladder")
+    return tuple(freq), m.value
+
+
+def rope_plan(rot: int, base: float = 10000.0, layout: str = "half", scaling: Optional[str] = None,
+              factor: float = 1.0, context: float = 0.0, fast: float = 32.0, slow: float = 1.0,
+              sections=None, own_ladders: bool = False) -> Rope:
+    """The turn of the first ``rot`` values of a head, for rope().  ``sections``: pairs that each
+    axis of position takes, in order (their sum is rot / 2); they share one ladder of frequencies,
+    or with ``own_ladders`` each has one of its own length.  The rest as for rope_ladder."""
+    rot = int(rot)
+    sections = [rot // 2] if sections is None else [int(n) for n in sections]
+    if rot % 2 or sum(sections) * 2 != rot or min(sections) < 1:
+        raise ValueError("sections must be positive and add up to rot / 2")
+    if own_ladders:
+        parts = [rope_ladder(2 * n, base, scaling, factor, context, fast, slow) for n in sections]
+        freq, m = sum((p[0] for p in parts), ()), parts[0][1]
+    else:
+        freq, m = rope_ladder(rot, base, scaling, factor, context, fast, slow)
+    axis = sum(((a,) * n for a, n in enumerate(sections)), ())
+    return Rope(layout, freq, axis, m)
+
+
+def rope(plan: Rope, q: torch.Tensor, k: Optional[torch.Tensor] = None,
+         pos: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None,
+         n_new: Optional[torch.Tensor] = None, start: int = 0, transpose: bool = False, out=None):
+    """Rows of q [B, Hq, N, D], and of k [B, Hkv, N, D] if given, turned by their positions
+    (vecattn_rope): ``pos`` (int32 [B, N], or [axes, B, N]), or ``lens`` (int32 [B]; the last rows
+    of each sequence, as cache_write places them), or ``start`` + row.  ``n_new`` (int32 [B]): the
+    rows of each sequence that exist.  ``transpose``: the gradient of the turn (and, where the
+    plan's factor is 1, its inverse).  ``out``: what takes the results, q or the pair (q, k) itself
+    to turn in place; padded rows of it are left as they were, and are 0 in one made here.  Returns
+    the turned q, or the pair."""
+    _bf16_cuda(q, "q")
+    dev = q.device
+    if k is not None:
+        _bf16_cuda(k, "k")
+    new = q.new_empty if n_new is None else q.new_zeros
+    if out is None:
+        qo, ko = new(q.shape), None if k is None else new(k.shape)
+    else:
+        qo, ko = (out, None) if k is None else out
+    _bf16_cuda(qo, "out")
+    if ko is not None:
+        _bf16_cuda(ko, "out")
+    _same_device(dev, k=k, qo=qo, ko=ko)
+    B, _, N, _ = q.shape
+    sA = sB = 0
+    if pos is not None:
+        if pos.dim() == 2 and plan.axes == 1:
+            pos = pos[None]
+        if pos.dtype is not torch.int32 or pos.shape != (plan.axes, B, N) or pos.device != dev \
+                or (N > 1 and pos.stride(2) != 1):
+            raise ValueError(f"pos must be an int32 [{plan.axes}, B, N] tensor on {dev} with "
+                             "contiguous rows")
+        sA, sB = pos.stride(0) if plan.axes > 1 else 0, pos.stride(1) if B > 1 else 0
+    if lens is not None:
+        _int32_on(lens, (B,), dev, "lens")
+    if n_new is not None:
+        _int32_on(n_new, (B,), dev, "n_new")
+    _call(dev, "rope", load().vecattn_rope,
+          q.data_ptr(), _tdesc(q.shape, q.stride()), None if k is None else k.data_ptr(),
+          None if k is None else _tdesc(k.shape, k.stride()),
+          ctypes.byref(plan._specs[1 if transpose else 0]),
+          None if pos is None else pos.data_ptr(), sA, sB,
+          None if lens is None else lens.data_ptr(), None if n_new is None else n_new.data_ptr(),
+          int(start), qo.data_ptr(), _tdesc(qo.shape, qo.stride()),
+          None if k is None else ko.data_ptr(),
+          None if k is None else _tdesc(ko.shape, ko.stride()))
+    return qo if k is None else (qo, ko)

@@ -15,7 +15,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["vecattn_api.cpp", "plan.cpp", "pool.hip", "sparse_attn.hip", "select.hip",
            "select_short.hip", "check.hip", "stats.hip", "noalloc.hip", "attn_order.hip",
-           "window_attn.hip", "cache.hip", "cache_attn.hip", "cache_chunk.hip"]
+           "window_attn.hip", "cache.hip", "cache_attn.hip", "cache_chunk.hip",
+           "cache_mass.hip", "cache_keep.hip", "cross_attn.hip", "rope.hip"]
 
 # Packed fp32 VALU instructions are disabled for all device code.
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -119,6 +119,28 @@ __device__ __forceinline__ uint32_t quantise32(const u32x4 (&w)[4], uint32_t (&b
   return (both & 0xFFFFu) | (sbits << 16);
 }
 
+// Dword x of the codes of eight tokens, for four head-dim values: c[e] holds the four
+// values' codes of the token in slot e, a byte each.
+template <int BITS>
+__device__ __forceinline__ void transpose_codes(const uint32_t (&c)[8], int x, uint32_t (&out)[4]) {
+  uint32_t p[4];   // byte i of the dwords to come, of four values
+  if constexpr (BITS == 4) {   // nibbles 2 i and 2 i + 1
+    p[0] = c[0] | c[2] << 4, p[1] = c[4] | c[6] << 4;
+    p[2] = c[1] | c[3] << 4, p[3] = c[5] | c[7] << 4;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = c[4 * x + i];
+  }
+  const uint32_t a0 = __builtin_amdgcn_perm(p[1], p[0], 0x05010400u);   // values 0, 1: bytes 0, 1
+  const uint32_t a1 = __builtin_amdgcn_perm(p[1], p[0], 0x07030602u);   // values 2, 3
+  const uint32_t b0 = __builtin_amdgcn_perm(p[3], p[2], 0x05010400u);
+  const uint32_t b1 = __builtin_amdgcn_perm(p[3], p[2], 0x07030602u);
+  out[0] = __builtin_amdgcn_perm(b0, a0, 0x05040100u);
+  out[1] = __builtin_amdgcn_perm(b0, a0, 0x07060302u);
+  out[2] = __builtin_amdgcn_perm(b1, a1, 0x05040100u);
+  out[3] = __builtin_amdgcn_perm(b1, a1, 0x07060302u);
+}
+
 // Half of a workgroup's threads take K, half V, each half a group of a token.  A whole
 // block is put together in LDS and stored 16 bytes a lane; of a part of one only the
 // new tokens' codes are stored, V's within the dwords they share with others.
@@ -190,22 +212,8 @@ __global__ __launch_bounds__(2 * D) void k_cache_write(
     }
 #pragma unroll
     for (int x = 0; x < L::kDw; ++x) {
-      uint32_t p[4];   // byte i of the dwords to come, of four values
-      if constexpr (BITS == 4) {   // nibbles 2 i and 2 i + 1
-        p[0] = c[0] | c[2] << 4, p[1] = c[4] | c[6] << 4;
-        p[2] = c[1] | c[3] << 4, p[3] = c[5] | c[7] << 4;
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = c[4 * x + i];
-      }
-      const uint32_t a0 = __builtin_amdgcn_perm(p[1], p[0], 0x05010400u);   // values 0, 1: bytes 0, 1
-      const uint32_t a1 = __builtin_amdgcn_perm(p[1], p[0], 0x07030602u);   // values 2, 3
-      const uint32_t b0 = __builtin_amdgcn_perm(p[3], p[2], 0x05010400u);
-      const uint32_t b1 = __builtin_amdgcn_perm(p[3], p[2], 0x07030602u);
-      const uint32_t out[4] = {__builtin_amdgcn_perm(b0, a0, 0x05040100u),
-                               __builtin_amdgcn_perm(b0, a0, 0x07060302u),
-                               __builtin_amdgcn_perm(b1, a1, 0x05040100u),
-                               __builtin_amdgcn_perm(b1, a1, 0x07060302u)};
+      uint32_t out[4];
+      transpose_codes<BITS>(c, x, out);
       auto byte_of = [&](int i) __attribute__((always_inline)) {
         return L::kHalf + code_byte((d + i) / 16 * L::kDw + x, g * 16 + (d + i) % 16);
       };
@@ -310,6 +318,128 @@ __global__ __launch_bounds__(256) void k_cache_read(
   }
 }
 
+// Chosen tokens of a head into pages of their own: slot i takes the codes and (m, s) of
+// token idx[i] as they are.  A workgroup puts one block of 32 slots together in LDS and
+// stores it whole.  Of K a token's codes lie in four runs; of V, whose dwords eight
+// tokens share, its codes are picked out to bytes and put together anew.  What it reads
+// of V is what bounds it: eight tokens' codes for each one kept (a sixteenth of the
+// tokens kept at random reads half of them).
+struct GatherTo {
+  uint8_t* data;
+  const int32_t* table;
+  int64_t cols, pages;
+  int32_t page_shift;
+};
+
+template <int D, int BITS>
+__global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
+                                                      const int32_t* __restrict__ idx,
+                                                      const int32_t* __restrict__ kept,
+                                                      int64_t budget,
+                                                      const float* __restrict__ mass, int64_t M,
+                                                      float* __restrict__ mass_out) {
+  using L = CacheLayout<D, BITS>;
+  constexpr int RUN = D / 32 * L::kDw;   // dwords of a token's codes of K on a lane
+  const int64_t b = blockIdx.z;
+  const int h = blockIdx.y;
+  const int64_t n = min(max(static_cast<int64_t>(kept[b]), int64_t(0)), budget);
+  const int64_t jb = blockIdx.x, j0 = jb * kCacheBlock;
+  if (j0 >= n) return;
+  const int count = static_cast<int>(min<int64_t>(n - j0, kCacheBlock));
+  const PageMap dst_map{to.data, to.table, to.cols, to.pages, map.H, to.page_shift};
+  uint8_t* dst = block_ptr<L::kBytes>(dst_map, b, h, jb);
+
+  __shared__ __align__(16) uint8_t image[L::kBytes];
+  __shared__ __align__(16) uint32_t codes[kCacheBlock][D / 4 + 4];   // V's, a byte each
+  __shared__ const uint8_t* s_blk[kCacheBlock];                      // NULL: no such token
+  __shared__ int s_token[kCacheBlock];                               // within its block
+  const int64_t bh = b * map.H + h;
+  if (threadIdx.x < kCacheBlock) {
+    const int slot = threadIdx.x;
+    const uint8_t* blk = nullptr;
+    int64_t j = -1;
+    if (slot < count) {
+      j = idx[bh * budget + j0 + slot];
+      if (j >= 0) blk = block_ptr<L::kBytes>(map, b, h, j >> 5);
+      if (mass_out)
+        mass_out[bh * budget + j0 + slot] =
+            j >= 0 && j < M ? mass[bh * M + j] : __builtin_nanf("");
+    }
+    s_blk[slot] = blk;
+    s_token[slot] = static_cast<int>(j & 31);
+  }
+  if (!dst) return;   // the same for all threads
+  __syncthreads();
+  // K's codes, and the groups of both.
+  for (int i = threadIdx.x; i < kCacheBlock * 4; i += 256) {
+    const int slot = i & 31, g = i >> 5;
+    const uint8_t* blk = s_blk[slot];
+    const int from = s_token[slot];
+    const int a = (from >> 4) * RUN, c = (slot >> 4) * RUN;
+#pragma unroll
+    for (int x = 0; x < RUN; ++x) {
+      const uint32_t w = blk ? *reinterpret_cast<const uint32_t*>(
+                                   blk + code_byte(a + x, g * 16 + (from & 15)))
+                             : 0u;
+      *reinterpret_cast<uint32_t*>(image + code_byte(c + x, g * 16 + (slot & 15))) = w;
+    }
+  }
+  for (int i = threadIdx.x; i < kCacheBlock * 2 * L::kG; i += 256) {
+    const int slot = i / L::kG % kCacheBlock, half = i / (L::kG * kCacheBlock), gi = i % L::kG;
+    const uint8_t* blk = s_blk[slot];
+    const int at = half * L::kHalf + L::kCodes;
+    reinterpret_cast<uint32_t*>(image + at)[slot * L::kG + gi] =
+        blk ? reinterpret_cast<const uint32_t*>(blk + at)[s_token[slot] * L::kG + gi] : 0x7FC07FC0u;
+  }
+  // V: sixteen lanes a token, 16 bytes at a time; a dword is of one head-dim value (4 bits)
+  // or of half its tokens (8 bits).
+  uint8_t* bytes = reinterpret_cast<uint8_t*>(codes);
+  constexpr int kRow = 4 * (D / 4 + 4);
+#pragma unroll
+  for (int i0 = 0; i0 < kCacheBlock * 16; i0 += 256) {
+    const int i = i0 + threadIdx.x, slot = i >> 4, ln = i & 15;
+    const uint8_t* blk = s_blk[slot];
+    const int token = s_token[slot];
+    // token = 16 (e / 4) + 4 g + e % 4
+    const int g = (token >> 2) & 3, e = (token >> 4) * 4 + (token & 3);
+#pragma unroll
+    for (int c = 0; c < L::kRun / 4; ++c) {
+      u32x4 w = {0, 0, 0, 0};
+      if (blk) w = *reinterpret_cast<const u32x4*>(blk + L::kHalf + code_byte(4 * c, g * 16 + ln));
+      if constexpr (BITS == 4) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          bytes[slot * kRow + 16 * (4 * c + y) + ln] =
+              static_cast<uint8_t>(w[y] >> (4 * nibble_of(e)) & 0xFu);
+      } else {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          bytes[slot * kRow + 16 * (2 * c + y) + ln] =
+              static_cast<uint8_t>((e >> 2 ? w[2 * y + 1] : w[2 * y]) >> (8 * (e & 3)));
+      }
+    }
+  }
+  __syncthreads();
+  for (int it = threadIdx.x; it < D; it += 256) {
+    const int d = it % (D / 4) * 4, g = it / (D / 4);
+    uint32_t c[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = codes[(e >> 2) * 16 + 4 * g + (e & 3)][d / 4];
+#pragma unroll
+    for (int x = 0; x < L::kDw; ++x) {
+      uint32_t out[4];
+      transpose_codes<BITS>(c, x, out);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<uint32_t*>(
+            image + L::kHalf + code_byte((d + i) / 16 * L::kDw + x, g * 16 + (d + i) % 16)) = out[i];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < L::kBytes / 16; i += 256)
+    *reinterpret_cast<u32x4*>(dst + 16 * i) = *reinterpret_cast<const u32x4*>(image + 16 * i);
+}
+
 PageMap page_map(const CacheArgs& c) {
   return PageMap{static_cast<uint8_t*>(c.data), c.table, c.cols, c.pages, c.H,
                  __builtin_ctz(static_cast<unsigned>(c.page))};
@@ -345,6 +475,22 @@ hipError_t launch_cache_read(const CacheArgs& c, int64_t start, const Tensor4& k
   };
   if (c.D == 128) c.bits == 4 ? run(k_cache_read<128, 4>) : run(k_cache_read<128, 8>);
   else c.bits == 4 ? run(k_cache_read<64, 4>) : run(k_cache_read<64, 8>);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_gather(const CacheArgs& c, const CacheArgs& to, int64_t B,
+                               const int32_t* idx, const int32_t* kept, int64_t budget,
+                               const float* mass, int64_t M, float* mass_out, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((budget + kCacheBlock - 1) / kCacheBlock),
+                  static_cast<unsigned>(c.H), static_cast<unsigned>(B));
+  const GatherTo g{static_cast<uint8_t*>(to.data), to.table, to.cols, to.pages,
+                   __builtin_ctz(static_cast<unsigned>(to.page))};
+  auto run = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, page_map(c), g, idx, kept, budget, mass, M,
+                       mass_out);
+  };
+  if (c.D == 128) c.bits == 4 ? run(k_cache_gather<128, 4>) : run(k_cache_gather<128, 8>);
+  else c.bits == 4 ? run(k_cache_gather<64, 4>) : run(k_cache_gather<64, 8>);
   return hipGetLastError();
 }
 

@@ -1,0 +1,442 @@
+// What new tokens' attention puts on each cached token: for token j of a key/value
+// head, the sum over the rows (new tokens and query heads that share the head) of
+// exp(scale q . k_j - lse), added to the sum that the token has collected before.
+//
+// A key is m + s u per group of 64 values (cache_common.h), q . k = sum_G s_G (q_G . u_G)
+// + m_G sum(q_G): the codes go into the matrix instructions as small fp16 numbers,
+// exactly, and rows of q as fp16 times a power of two, so that only fp32 sums round.
+// A token belongs to one wave, which adds its rows in one order: no atomics.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "cache_rows.h"
+
+namespace vecattn {
+namespace {
+
+struct MassParams {
+  const uint16_t* q;
+  int64_t q_sB, q_sH, q_sN;
+  const float* lse;
+  const uint8_t* data;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* n_new;
+  const float* mass;   // NULL: nothing collected before
+  float* out;
+  int64_t M;           // entries per sequence and head
+  int32_t cols, pages, page_shift;
+  int32_t H, n, group, window, sinks;
+  int32_t in_place;    // what no row sees stays as it is
+  float scale_log2, decay;
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Where a sequence's tokens and rows are.
+struct Place {
+  int32_t p_first, rows, end;   // position of row 0, rows of all heads, tokens with an entry
+};
+__device__ __forceinline__ Place place_of(const MassParams& a, int64_t b) {
+  const int len = min(max(a.lens[b], 0), 1 << 30);
+  const int nb = a.n_new ? min(max(a.n_new[b], 0), a.n) : a.n;
+  return Place{len - nb, nb * a.group, static_cast<int>(min<int64_t>(len, a.M))};
+}
+
+// Base of a block of a head's keys, or NULL where no page is held.
+template <int BYTES>
+__device__ __forceinline__ const uint8_t* keys_of(const MassParams& a, int64_t b, int h, int jb) {
+  const int sh = a.page_shift - 5;
+  const int col = jb >> sh;
+  if (col >= a.cols) return nullptr;
+  const int64_t page = ((ScalarInts)(a.table + b * a.cols))[col];
+  if (page < 0 || page >= a.pages) return nullptr;
+  return a.data + (((page * a.H + h) << sh) + (jb & ((1 << sh) - 1))) * BYTES;
+}
+
+// x summed over 16 lanes, on each of them.
+__device__ __forceinline__ float row_sum(float x) {
+  auto turn = [&](auto ctl) __attribute__((always_inline)) {
+    const int y = __builtin_bit_cast(int, x);
+    x += __builtin_bit_cast(
+        float, __builtin_amdgcn_update_dpp(y, y, decltype(ctl)::value, 0xf, 0xf, false));
+  };
+  turn(std::integral_constant<int, 0x128>{});   // row_ror:8
+  turn(std::integral_constant<int, 0x124>{});
+  turn(std::integral_constant<int, 0x122>{});
+  turn(std::integral_constant<int, 0x121>{});
+  return x;
+}
+
+// Token j's sum: what it had before (a new token: nothing) and w.
+__device__ __forceinline__ void collect(const MassParams& a, const Place& s, int64_t bh, int j,
+                                        float w) {
+  const int64_t at = bh * a.M + j;
+  if (a.mass && j < s.p_first) w = __builtin_fmaf(a.decay, a.mass[at], w);
+  a.out[at] = w;
+}
+
+// Sixteen rows at most: waves take blocks of 32 tokens in turn.
+template <int D, int BITS>
+__global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
+  using L = CacheLayout<D, BITS>;
+  constexpr int G = L::kG, DW = L::kDw, ST = D / 32;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.y;
+  const int64_t b = blockIdx.z, bh = b * a.H + h;
+  const Place s = place_of(a, b);
+  const int blocks = (s.end + kCacheBlock - 1) / kCacheBlock;
+  const int step = gridDim.x * 4;
+  int jb = blockIdx.x * 4 + wave;
+  if (jb >= blocks) return;
+
+  const int tok = n / a.group, hq = h * a.group + n % a.group;
+  bool have = n < s.rows;
+  float lse = have ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
+  have = have && lse != kNegInf;
+  Rows<D, BITS> rows;
+  rows.load(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN, have, g);
+  const float to_log2 = a.scale_log2 * rows.unscale;
+  const float off = have ? lse * kLog2e : INFINITY;   // a row that is not there weighs 0
+  const int pos = have ? s.p_first + tok : -1;
+  const int p_lo = s.p_first, p_hi = s.p_first + (s.rows - 1) / a.group;
+
+  auto seen = [&](int i) __attribute__((always_inline)) {   // by some row
+    const int j0 = i * kCacheBlock;
+    return s.rows > 0 && j0 <= p_hi && (j0 + 31 > p_lo - a.window || j0 < a.sinks);
+  };
+  struct Keys {
+    uint32_t c[L::kRun], p[2][4 * G];
+  };
+  auto load = [&](Keys& x, int i) __attribute__((always_inline)) {
+    const uint8_t* blk = i < blocks && seen(i) ? keys_of<L::kBytes>(a, b, h, i) : nullptr;
+    if (!blk) return false;
+#pragma unroll
+    for (int c = 0; c < L::kRun / 4; ++c)
+      *reinterpret_cast<u32x4*>(x.c + 4 * c) =
+          *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
+#pragma unroll
+    for (int tl = 0; tl < 2; ++tl)
+#pragma unroll
+      for (int c = 0; c < G; ++c)
+        *reinterpret_cast<u32x4*>(x.p[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
+            blk + L::kCodes + (16 * tl + 4 * g) * G * 4 + 16 * c);
+    return true;
+  };
+  auto work = [&](const Keys& x, bool held, int i) __attribute__((always_inline)) {
+    const int j0 = i * kCacheBlock;
+    // The lane's token in what is written: of tile n / 4, element n % 4.
+    const int j = j0 + 16 * ((n >> 2) & 1) + 4 * g + (n & 3);
+    float w = 0.0f;
+    if (held) {
+      const bool masked = j0 + 31 > p_lo || (j0 <= p_hi - a.window && j0 + 31 >= a.sinks);
+      float p[2][4];
+#pragma unroll
+      for (int tl = 0; tl < 2; ++tl) {
+        f32x4 acc[G];
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) acc[gi] = f32x4{};
+#pragma unroll
+        for (int st = 0; st < ST; ++st)
+          acc[st / 2] = rows.dot(x.c + (tl * ST + st) * DW, st, acc[st / 2]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float y = 0.0f;
+#pragma unroll
+          for (int gi = 0; gi < G; ++gi) {
+            y = __builtin_fmaf(high_of(x.p[tl][e * G + gi]), acc[gi][e], y);
+            y = __builtin_fmaf(low_of(x.p[tl][e * G + gi]), rows.sum[gi], y);
+          }
+          y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
+          if (masked) {
+            const int jt = j0 + 16 * tl + 4 * g + e;
+            y = jt <= pos && (jt > pos - a.window || jt < a.sinks) ? y : 0.0f;
+          }
+          p[tl][e] = row_sum(y);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w = (n & 7) == e ? p[e / 4][e % 4] : w;
+    }
+    if (n < 8 && j < s.end && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, w);
+  };
+  Keys cur, nxt;
+  bool held = load(cur, jb);
+  while (jb < blocks) {
+    const bool more = load(nxt, jb + step);
+    work(cur, held, jb);
+    jb += step;
+    if (jb >= blocks) break;
+    held = load(cur, jb + step);
+    work(nxt, more, jb);
+    jb += step;
+  }
+}
+
+// More rows: NB blocks of 32 tokens per wave stay in registers as fp16 codes, and the
+// rows pass by in tiles of 32, put into LDS by the workgroup's four waves, one tile
+// ahead.  v_mfma_f32_32x32x16 (lane l = 32 g + n): A: token n, head-dim values 16 st +
+// 8 g + 0..7; B: row n, the same; C: row n, tokens 8 (e / 4) + 4 g + e % 4.  The m_G
+// sum(q_G) terms start the sums: m_G is bf16 as it is, and sum(q_G) goes in as three
+// bf16 numbers that add up to it.
+template <int D, int BITS, int NB>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_mass_many(
+    const MassParams a) {
+  using L = CacheLayout<D, BITS>;
+  constexpr int G = L::kG, DW = L::kDw, ST = D / 16, SW = D / 32;
+  constexpr int kRowBytes = 2 * D + 16;      // rows 16 bytes apart in the banks
+  struct Tile {
+    uint8_t q[32 * kRowBytes];
+    u32x4 sums[32];                          // 2 x 3 bf16, 0
+    float to_log2[32], off[32];
+  };
+  __shared__ __align__(16) Tile tiles[2];
+  const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.y;
+  const int64_t b = blockIdx.z, bh = b * a.H + h;
+  const Place s = place_of(a, b);
+  const int blocks = (s.end + kCacheBlock - 1) / kCacheBlock;
+  const int first = blockIdx.x * 4 * NB;   // of the workgroup
+  if (first >= blocks) return;
+  const int jb0 = first + wave * NB;
+
+  bool held[NB];
+  bf16x8 low[NB];
+  f16x8 codes[NB][ST];
+  float step_of[NB][G][16], w[NB][16];
+#pragma unroll
+  for (int x = 0; x < NB; ++x) {
+    const uint8_t* blk = jb0 + x < blocks ? keys_of<L::kBytes>(a, b, h, jb0 + x) : nullptr;
+    held[x] = blk != nullptr;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) w[x][e] = 0.0f;
+    low[x] = bf16x8{};
+#pragma unroll
+    for (int st = 0; st < ST; ++st) codes[x][st] = f16x8{};
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) step_of[x][gi][e] = 0.0f;
+    if (!blk) continue;
+#pragma unroll
+    for (int st = 0; st < ST; ++st) {
+      // Token n = 16 t + n % 16, values 16 st + 8 g on: run dword (t D / 32 + st / 2) kDw
+      // of lane 16 (2 (st % 2) + g) + n % 16.
+      const int w0 = ((n >> 4) * SW + st / 2) * DW, from = (2 * (st & 1) + g) * 16 + (n & 15);
+      uint32_t u[DW];
+#pragma unroll
+      for (int y = 0; y < DW; ++y)
+        u[y] = *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + y, from));
+      codes[x][st] = __builtin_bit_cast(f16x8, codes_f16<BITS>(u));
+    }
+    const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + L::kCodes);
+    if (g == 0) {
+      const uint32_t m0 = par[n * G] & 0xFFFFu, m1 = G > 1 ? par[n * G + G - 1] & 0xFFFFu : 0u;
+      low[x] = __builtin_bit_cast(bf16x8, u32x4{m0 | m0 << 16, m0 | m1 << 16, m1 | m1 << 16, 0u});
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi)
+        step_of[x][gi][e] = high_of(par[(8 * (e / 4) + 4 * g + e % 4) * G + gi]);
+  }
+
+  // Row tiles [t0, t1) that may see one of the workgroup's tokens.
+  const int ntiles = (s.rows + 31) / 32;
+  int t0 = 0;
+  {
+    const int j_first = first * kCacheBlock;      // rows before it see none of them
+    const int r = max(0, j_first - s.p_first) * a.group;
+    t0 = j_first > s.p_first ? r / 32 : 0;
+  }
+  // Eight threads a row, 16 bytes at a time.
+  constexpr int C = D / 64;   // 16-byte chunks per thread
+  const int sr = threadIdx.x >> 3, sc = threadIdx.x & 7;
+  u32x4 raw[C];
+  float raw_lse = kNegInf;
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    const int row = 32 * t + sr;
+    const bool have = row < s.rows;
+    const int tok = row / a.group, hq = h * a.group + row % a.group;
+    raw_lse = have ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      raw[c] = u32x4{0, 0, 0, 0};
+      if (have && raw_lse != kNegInf)
+        raw[c] = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN +
+                                                 8 * (c * 8 + sc));
+    }
+  };
+  auto stage = [&](Tile& to) __attribute__((always_inline)) {
+    float top = 0x1p-100f, sum[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      sum[c] = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = low_of(raw[c][e]), hi = high_of(raw[c][e]);
+        top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
+        sum[c] += lo + hi;
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      top = fmaxf(top, __shfl_xor(top, o));
+#pragma unroll
+      for (int c = 0; c < C; ++c) sum[c] += __shfl_xor(sum[c], o);   // chunks c hold group c
+    }
+    // The largest value between 2^14 and 2^15 (cache_rows.h).
+    const int k = 15 - __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      u32x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        y[e] = to_f16(__builtin_amdgcn_ldexpf(low_of(raw[c][e]), k),
+                      __builtin_amdgcn_ldexpf(high_of(raw[c][e]), k));
+      *reinterpret_cast<u32x4*>(to.q + sr * kRowBytes + 16 * (c * 8 + sc)) = y;
+    }
+    if (sc == 0) {
+      uint32_t part[6] = {};
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float x = __builtin_amdgcn_ldexpf(sum[c], k - kCodeExp<BITS>);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const uint32_t bits = __float_as_uint(x) & 0xFFFF0000u;   // eight leading bits
+          part[3 * c + i] = bits >> 16;
+          x = (bits & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float(bits);
+        }
+      }
+      to.sums[sr] = u32x4{part[0] | part[1] << 16, part[2] | part[3] << 16, part[4] | part[5] << 16,
+                          0u};
+      to.to_log2[sr] = a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, kCodeExp<BITS> - k);
+      to.off[sr] = raw_lse == kNegInf ? INFINITY : raw_lse * kLog2e;
+    }
+  };
+  if (t0 < ntiles) {
+    fetch(t0);
+    stage(tiles[t0 & 1]);
+  }
+  __syncthreads();
+  for (int t = t0; t < ntiles; ++t) {
+    if (t + 1 < ntiles) fetch(t + 1);
+    const Tile& tile = tiles[t & 1];
+    const int r1 = min(32 * t + 31, s.rows - 1);
+    const int p_lo = s.p_first + 32 * t / a.group, p_hi = s.p_first + r1 / a.group;
+    const u32x4 sums = g == 0 ? tile.sums[n] : u32x4{0, 0, 0, 0};
+    const float to_log2 = tile.to_log2[n], off = tile.off[n];
+    const int pos = off == INFINITY ? -1 : s.p_first + (32 * t + n) / a.group;
+    const uint8_t* qrow = tile.q + n * kRowBytes + 16 * g;
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+      const int j0 = (jb0 + x) * kCacheBlock;
+      if (!held[x] || j0 > p_hi || (j0 + 31 <= p_lo - a.window && j0 >= a.sinks)) continue;
+      const f32x16 start = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          low[x], __builtin_bit_cast(bf16x8, sums), f32x16{}, 0, 0, 0);
+      f32x16 acc[G];
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi) acc[gi] = f32x16{};
+#pragma unroll
+      for (int st = 0; st < ST; ++st)
+        acc[st / 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+            codes[x][st],
+            __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(qrow + 32 * st)),
+            acc[st / 4], 0, 0, 0);
+      const bool masked = j0 + 31 > p_lo || (j0 <= p_hi - a.window && j0 + 31 >= a.sinks);
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float y = start[e];
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) y = __builtin_fmaf(step_of[x][gi][e], acc[gi][e], y);
+        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + 8 * (e / 4) + 4 * g + e % 4;
+          p[e] = j <= pos && (j > pos - a.window || j < a.sinks) ? p[e] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) w[x][e] += p[e];
+    }
+    if (t + 1 < ntiles) stage(tiles[(t + 1) & 1]);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int x = 0; x < NB; ++x) {
+    float mine = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float y = row_sum(w[x][e]);
+      const float all = y + __shfl_xor(y, 16);
+      mine = (n & 15) == e ? all : mine;
+    }
+    const int j = (jb0 + x) * kCacheBlock + 8 * ((n & 15) / 4) + 4 * g + (n & 3);
+    if (n < 16 && jb0 + x < blocks && j < s.end) collect(a, s, bh, j, mine);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
+  const CacheArgs& c = x.cache;
+  MassParams a;
+  a.q = static_cast<const uint16_t*>(x.q.ptr);
+  a.q_sB = x.q.sB, a.q_sH = x.q.sH, a.q_sN = x.q.sN;
+  a.lse = x.lse;
+  a.data = static_cast<const uint8_t*>(c.data);
+  a.table = c.table;
+  a.lens = c.lens;
+  a.n_new = x.n_new;
+  a.mass = x.mass;
+  a.out = x.out;
+  a.M = x.M;
+  a.cols = static_cast<int32_t>(c.cols);
+  a.pages = static_cast<int32_t>(std::min<int64_t>(c.pages, INT32_MAX));
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(c.page));
+  a.H = c.H;
+  a.n = static_cast<int32_t>(x.q.N);
+  a.group = static_cast<int32_t>(x.q.H / c.H);
+  a.window = static_cast<int32_t>(x.window);
+  a.sinks = static_cast<int32_t>(x.sinks);
+  a.in_place = x.mass == x.out && x.decay == 1.0f;
+  const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(c.D));
+  a.scale_log2 = scale * kLog2e;
+  a.decay = x.decay;
+  const int64_t rows = static_cast<int64_t>(a.n) * a.group;
+  const int64_t blocks = (std::min(x.M, c.cols * c.page) + kCacheBlock - 1) / kCacheBlock;
+  const int64_t heads = x.q.B * c.H;
+  auto launch = [&](auto kernel, int64_t groups) {
+    hipLaunchKernelGGL(kernel,
+                       dim3(static_cast<unsigned>(groups), static_cast<unsigned>(c.H),
+                            static_cast<unsigned>(x.q.B)),
+                       dim3(256), 0, stream, a);
+  };
+  auto pick = [&](auto dim, auto bits) {
+    constexpr int D = decltype(dim)::value, BITS = decltype(bits)::value;
+    if (rows <= 16) {
+      const int64_t fill = std::max<int64_t>(1, 4096 / heads);
+      launch(k_mass_few<D, BITS>, std::min((blocks + 3) / 4, fill));
+    } else if (heads * blocks >= 4096) {
+      launch(k_mass_many<D, BITS, 2>, (blocks + 7) / 8);
+    } else {
+      launch(k_mass_many<D, BITS, 1>, (blocks + 3) / 4);
+    }
+  };
+  using std::integral_constant;
+  if (c.D == 128)
+    c.bits == 4 ? pick(integral_constant<int, 128>{}, integral_constant<int, 4>{})
+                : pick(integral_constant<int, 128>{}, integral_constant<int, 8>{});
+  else
+    c.bits == 4 ? pick(integral_constant<int, 64>{}, integral_constant<int, 4>{})
+                : pick(integral_constant<int, 64>{}, integral_constant<int, 8>{});
+  return hipGetLastError();
+}
+
+}  // namespace vecattn

@@ -167,6 +167,67 @@ bool cache_attn_grid_ok(const CacheAttnShape& s);
 size_t cache_attn_workspace_bytes(const CacheAttnShape& s);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, hipStream_t stream);
 
+// The attention weight that rows of q put on cached tokens, added up per token, and
+// eviction by it: which tokens a budget keeps, and these into other pages.
+struct CacheMassArgs {
+  Tensor4 q;
+  const float* lse;
+  CacheArgs cache;
+  const int32_t* n_new;
+  int64_t window, sinks;
+  float scale, decay;
+  const float* mass;   // [B, H, M], or NULL
+  float* out;          // [B, H, M]
+  int64_t M;
+};
+hipError_t launch_cache_mass(const CacheMassArgs& a, hipStream_t stream);
+hipError_t launch_cache_keep(const CacheArgs& c, int64_t B, const float* mass, int64_t M,
+                             int64_t budget, int64_t sinks, int64_t recent, int32_t* idx,
+                             int32_t* kept, hipStream_t stream);
+hipError_t launch_cache_gather(const CacheArgs& c, const CacheArgs& to, int64_t B,
+                               const int32_t* idx, const int32_t* kept, int64_t budget,
+                               const float* mass, int64_t M, float* mass_out, hipStream_t stream);
+
+// Attention over an encoder's states.  How the work is dealt out, and so the
+// workspace, follows from the shape.
+struct CrossArgs {
+  Tensor4 q, k, v;
+  void* o;
+  int64_t o_sB, o_sH, o_sN;
+  float* lse;
+  const int32_t* lens;
+  const uint8_t* mask;
+  int64_t mask_sB;
+  const int32_t* n_q;
+  float scale;
+  void* workspace;
+};
+constexpr int32_t kCrossRows = 128;   // rows per workgroup, where there are many
+bool cross_attn_grid_ok(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D);
+size_t cross_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk,
+                                  int64_t D);
+hipError_t launch_cross_attn(const CrossArgs& a, hipStream_t stream);
+
+// Rotary positions of q and, where k.ptr is not NULL, of k.
+constexpr int32_t kRopeMaxPairs = 64;
+struct RopeArgs {
+  Tensor4 q, k, qo, ko;
+  int32_t rot;
+  bool half, transposed;
+  double factor;
+  const double* freq;    // host, [rot / 2], radians per position
+  const int32_t* axis;   // host, [rot / 2], or NULL: axis 0
+  const int32_t* pos;    // positions, or NULL: from lens, or start + row
+  int64_t pos_sA, pos_sB;
+  const int32_t *lens, *n_new;
+  int64_t start;
+};
+hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
+
+// Host: a ladder of frequencies, also of the forms for long contexts.
+void rope_ladder(int32_t rot, double base, int32_t scaling, double factor, double context,
+                 double fast, double slow, double* freq, double* mfactor);
+
 // Host: per-head filter ratios by dynamic programming (Eq. 5).  Returns 0, or
 // 1 when no choice reaches the target.
 int plan_filter_ratios(int32_t H, int32_t C, const double* sp, const double* perf, double target,

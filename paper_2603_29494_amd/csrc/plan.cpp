@@ -1,3 +1,5 @@
+// Host code that plans: rotary frequencies, and per-head filter ratios.
+//
 // Per-head filter ratios (paper Sec. 3.1.2, Eq. 5): choose one candidate filter
 // ratio per head so that the heads' mean sparsity reaches a target and the
 // summed per-head performance is largest.  Host code; the tables sp_h and
@@ -11,12 +13,14 @@
 //   best_0(0) = 0, best_0(S > 0) = -inf,  q_{h,c} = round(sp_h(c) * grid),
 // and the answer is best_H(ceil(target * H * grid)).  Ties go to the lower
 // candidate index.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <limits>
 #include <vector>
 
 #include "launch.h"
+#include "vecattn.h"
 
 namespace vecattn {
 
@@ -61,6 +65,34 @@ int plan_filter_ratios(int32_t H, int32_t C, const double* sp, const double* per
     S = rest > 0 ? rest : 0;
   }
   return 0;
+}
+
+void rope_ladder(int32_t rot, double base, int32_t scaling, double factor, double context,
+                 double fast, double slow, double* freq, double* mfactor) {
+  const double two_pi = 6.283185307179586477;
+  const int32_t half = rot / 2;
+  // Stretched base: the lowest frequency comes out divided by factor, the highest as it is.
+  if (scaling == VECATTN_ROPE_NTK && half > 1) base *= std::pow(factor, half / (half - 1.0));
+  // The pair (a real number) that makes so many turns over the context.
+  auto pair_at = [&](double turns) {
+    return half * std::log(context / (turns * two_pi)) / std::log(base);
+  };
+  double low = 0.0, high = 0.0;
+  if (scaling == VECATTN_ROPE_PARTS) {
+    low = std::min(std::max(std::floor(pair_at(fast)), 0.0), half - 1.0);
+    high = std::min(std::max(std::ceil(pair_at(slow)), 0.0), half - 1.0);
+  }
+  for (int32_t i = 0; i < half; ++i) {
+    const double f = std::pow(base, -static_cast<double>(i) / half);
+    double kept = 1.0;   // share of f that is not divided by factor
+    if (scaling == VECATTN_ROPE_LINEAR) kept = 0.0;
+    if (scaling == VECATTN_ROPE_PARTS)
+      kept = 1.0 - std::min(std::max((i - low) / std::max(high - low, 0.001), 0.0), 1.0);
+    if (scaling == VECATTN_ROPE_BANDS)
+      kept = std::min(std::max((context * f / two_pi - slow) / (fast - slow), 0.0), 1.0);
+    freq[i] = kept * f + (1.0 - kept) * (f / factor);
+  }
+  *mfactor = scaling == VECATTN_ROPE_PARTS ? 0.1 * std::log(factor) + 1.0 : 1.0;
 }
 
 }  // namespace vecattn

@@ -397,6 +397,25 @@ bool same_shape(const vecattn_tdesc* a, const vecattn_tdesc* b) {
   return a->B == b->B && a->H == b->H && a->N == b->N && a->D == b->D;
 }
 
+// Strides of dimensions of size 1 address nothing.
+bool same_strides(const vecattn_tdesc* a, const vecattn_tdesc* b) {
+  return (a->B == 1 || a->sB == b->sB) && (a->H == 1 || a->sH == b->sH) &&
+         (a->N == 1 || a->sN == b->sN);
+}
+
+// What the workspace of the attention over an encoder's states, and the call, need of
+// the shapes.
+vecattn_status check_cross(const vecattn_tdesc* qd, const vecattn_tdesc* kd) {
+  if (!qd || !kd || qd->B < 1 || qd->H < 1 || qd->N < 1 || kd->H < 1 || kd->N < 1 ||
+      qd->N > kMaxN || kd->N > kMaxN)
+    return VECATTN_ERR_INVALID_ARG;
+  if (kd->B != qd->B || kd->D != qd->D || qd->H % kd->H != 0) return VECATTN_ERR_INVALID_ARG;
+  if ((qd->D != 64 && qd->D != 128) ||
+      !vecattn::cross_attn_grid_ok(qd->B, qd->H, kd->H, qd->N, kd->N, qd->D))
+    return VECATTN_ERR_UNSUPPORTED;
+  return VECATTN_OK;
+}
+
 size_t cache_page_bytes(const vecattn_cache* c) {
   const size_t token = static_cast<size_t>(c->D) * c->bits / 8 + static_cast<size_t>(c->D) / 64 * 4;
   return 2 * token * static_cast<size_t>(c->page) * static_cast<size_t>(c->H);
@@ -621,6 +640,168 @@ vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
   vecattn::CacheAttnArgs a{s, to_tensor(q, qd), to_cache(cache, table, cols, lens), n_new, o,
                            od->sB, od->sH, od->sN, lse, scale, workspace};
   hipError_t e = vecattn::launch_cache_attn(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const float* lse,
+                                  const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, const int32_t* n_new, int64_t window,
+                                  int64_t sinks, float scale, float decay, const float* mass,
+                                  float* out, int64_t M, void* stream) {
+  vecattn_status st;
+  if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
+  vecattn::CacheAttnShape s;
+  if ((st = check_cache_attn(qd, cache, true, cols, window, sinks, &s)) != VECATTN_OK) return st;
+  if (!lse || !table || !lens || !out || M < 1 || M > kMaxN) return VECATTN_ERR_INVALID_ARG;
+  if (!std::isfinite(scale) || scale < 0.0f || !std::isfinite(decay) || decay < 0.0f)
+    return VECATTN_ERR_INVALID_ARG;
+  vecattn::CacheMassArgs a{to_tensor(q, qd), lse, to_cache(cache, table, cols, lens), n_new,
+                           s.window, s.sinks, scale, decay, mass, out, M};
+  hipError_t e = vecattn::launch_cache_mass(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
+                                  const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, int64_t budget, int64_t sinks,
+                                  int64_t recent, int32_t* idx, int32_t* kept, void* stream) {
+  const vecattn_status st = check_cache(cache, true);
+  if (st != VECATTN_OK) return st;
+  if (!mass || !table || !lens || !idx || !kept || B < 1 || M < 1 || M > kMaxN)
+    return VECATTN_ERR_INVALID_ARG;
+  if (!cols_ok(cols, cache->page) || budget < 1 || budget > kMaxN || sinks < 0 || recent < 0 ||
+      sinks > budget || recent > budget - sinks)
+    return VECATTN_ERR_INVALID_ARG;
+  if (B > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
+  hipError_t e = vecattn::launch_cache_keep(to_cache(cache, table, cols, lens), B, mass, M, budget,
+                                            sinks, recent, idx, kept,
+                                            static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                    int64_t B, const int32_t* idx, const int32_t* kept,
+                                    int64_t budget, const vecattn_cache* to,
+                                    const int32_t* to_table, int64_t to_cols, const float* mass,
+                                    int64_t M, float* mass_out, void* stream) {
+  vecattn_status st;
+  if ((st = check_cache(cache, true)) != VECATTN_OK) return st;
+  if ((st = check_cache(to, true)) != VECATTN_OK) return st;
+  if (to->H != cache->H || to->D != cache->D || to->bits != cache->bits)
+    return VECATTN_ERR_INVALID_ARG;
+  if (!table || !idx || !kept || !to_table || B < 1 || budget < 1 || budget > kMaxN)
+    return VECATTN_ERR_INVALID_ARG;
+  if (!cols_ok(cols, cache->page) || !cols_ok(to_cols, to->page)) return VECATTN_ERR_INVALID_ARG;
+  if ((mass == nullptr) != (mass_out == nullptr) || (mass && (M < 1 || M > kMaxN)))
+    return VECATTN_ERR_INVALID_ARG;
+  if (B > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
+  hipError_t e = vecattn::launch_cache_gather(
+      to_cache(cache, table, cols, nullptr), to_cache(to, to_table, to_cols, nullptr), B, idx, kept,
+      budget, mass, M, mass_out, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cross_attn_workspace_size(const vecattn_tdesc* qd, const vecattn_tdesc* kd,
+                                                 size_t* bytes) {
+  if (!bytes) return VECATTN_ERR_INVALID_ARG;
+  const vecattn_status st = check_cross(qd, kd);
+  if (st != VECATTN_OK) return st;
+  *bytes = vecattn::cross_attn_workspace_bytes(qd->B, qd->H, kd->H, qd->N, kd->N, qd->D);
+  return VECATTN_OK;
+}
+
+vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const void* k,
+                                  const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,
+                                  const int32_t* lens, const uint8_t* mask, int64_t mask_sB,
+                                  const int32_t* n_q, float scale, void* o,
+                                  const vecattn_tdesc* od, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  vecattn_status st;
+  if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
+  if ((st = check_desc(k, kd)) != VECATTN_OK) return st;
+  if ((st = check_desc(v, vd)) != VECATTN_OK) return st;
+  if ((st = check_desc(o, od)) != VECATTN_OK) return st;
+  if ((st = check_cross(qd, kd)) != VECATTN_OK) return st;
+  if (!same_shape(vd, kd) || !same_shape(od, qd)) return VECATTN_ERR_INVALID_ARG;
+  if (mask_sB < 0 || !std::isfinite(scale) || scale < 0.0f) return VECATTN_ERR_INVALID_ARG;
+  // A tile's 64 rows are addressed with 32-bit byte offsets.
+  if (kd->N > 1 && (kd->sN >= (int64_t(1) << 24) || vd->sN >= (int64_t(1) << 24)))
+    return VECATTN_ERR_UNSUPPORTED;
+  const size_t need = vecattn::cross_attn_workspace_bytes(qd->B, qd->H, kd->H, qd->N, kd->N, qd->D);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return VECATTN_ERR_CAPACITY;
+  if (workspace && !aligned16(workspace)) return VECATTN_ERR_INVALID_ARG;
+  vecattn::CrossArgs a{to_tensor(q, qd), to_tensor(k, kd), to_tensor(v, vd), o, od->sB, od->sH,
+                       od->sN, lse, lens, mask, mask_sB, n_q, scale, workspace};
+  hipError_t e = vecattn::launch_cross_attn(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_rope_ladder(int32_t rot, double base, int32_t scaling, double factor,
+                                   double context, double fast, double slow, double* freq,
+                                   double* mfactor) {
+  if (!freq || !mfactor || rot < 2 || rot > 2 * vecattn::kRopeMaxPairs || rot % 2 != 0)
+    return VECATTN_ERR_INVALID_ARG;
+  if (scaling < VECATTN_ROPE_NONE || scaling > VECATTN_ROPE_BANDS || !std::isfinite(base) ||
+      base <= 1.0)
+    return VECATTN_ERR_INVALID_ARG;
+  if (scaling != VECATTN_ROPE_NONE && (!std::isfinite(factor) || factor < 1.0))
+    return VECATTN_ERR_INVALID_ARG;
+  if ((scaling == VECATTN_ROPE_PARTS || scaling == VECATTN_ROPE_BANDS) &&
+      (!std::isfinite(context) || context <= 0.0 || !std::isfinite(slow) || slow <= 0.0 ||
+       !std::isfinite(fast) || fast <= slow))
+    return VECATTN_ERR_INVALID_ARG;
+  vecattn::rope_ladder(rot, base, scaling, factor, context, fast, slow, freq, mfactor);
+  return VECATTN_OK;
+}
+
+vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* k,
+                            const vecattn_tdesc* kd, const vecattn_rope_spec* spec,
+                            const int32_t* pos, int64_t pos_sA, int64_t pos_sB,
+                            const int32_t* lens, const int32_t* n_new, int64_t start, void* qo,
+                            const vecattn_tdesc* qod, void* ko, const vecattn_tdesc* kod,
+                            void* stream) {
+  vecattn_status st;
+  if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
+  if ((st = check_desc(qo, qod)) != VECATTN_OK) return st;
+  if (!same_shape(qod, qd) || (q == qo && !same_strides(qod, qd))) return VECATTN_ERR_INVALID_ARG;
+  const bool with_k = k || kd || ko || kod;
+  if (with_k) {
+    if ((st = check_desc(k, kd)) != VECATTN_OK) return st;
+    if ((st = check_desc(ko, kod)) != VECATTN_OK) return st;
+    if (!same_shape(kod, kd) || (k == ko && !same_strides(kod, kd))) return VECATTN_ERR_INVALID_ARG;
+    if (kd->B != qd->B || kd->N != qd->N || kd->D != qd->D) return VECATTN_ERR_INVALID_ARG;
+  }
+  if (!spec || spec->rot < 2 || spec->rot > qd->D || spec->rot % 2 != 0 || !spec->freq ||
+      (spec->layout != VECATTN_ROPE_HALF && spec->layout != VECATTN_ROPE_INTERLEAVED) ||
+      spec->axes < 1 || spec->axes > 4 || (spec->transposed != 0 && spec->transposed != 1) ||
+      !std::isfinite(spec->factor))
+    return VECATTN_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < spec->rot / 2; ++i) {
+    if (!(std::fabs(spec->freq[i]) <= 1024.0)) return VECATTN_ERR_INVALID_ARG;
+    if (spec->axis && (spec->axis[i] < 0 || spec->axis[i] >= spec->axes))
+      return VECATTN_ERR_INVALID_ARG;
+  }
+  if ((pos && lens) || pos_sA < 0 || pos_sB < 0 || start > kMaxN || start < -kMaxN)
+    return VECATTN_ERR_INVALID_ARG;
+  if (qd->H + (with_k ? kd->H : 0) > kMaxGridYZ || qd->B > kMaxN / qd->N)
+    return VECATTN_ERR_UNSUPPORTED;
+  vecattn::RopeArgs a{to_tensor(q, qd),
+                      with_k ? to_tensor(k, kd) : Tensor4{},
+                      to_tensor(qo, qod),
+                      with_k ? to_tensor(ko, kod) : Tensor4{},
+                      spec->rot,
+                      spec->layout == VECATTN_ROPE_HALF,
+                      spec->transposed != 0,
+                      spec->factor,
+                      spec->freq,
+                      spec->axis,
+                      pos,
+                      pos_sA,
+                      pos_sB,
+                      lens,
+                      n_new,
+                      start};
+  hipError_t e = vecattn::launch_rope(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 
