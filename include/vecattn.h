@@ -86,6 +86,11 @@ typedef enum vecattn_sel_mode {
                                first C entries): with a large cap (threshold
                                modes, cap = N) this saves writing the padding */
 
+/* Of the `flags` of entry points that have them: the rows (or entries) of an output that
+ * belong to no row (or token) of their sequence are written as 0 instead of being left as
+ * they were. */
+#define VECATTN_CLEAR_PADDING 8
+
 typedef struct vecattn_tdesc {
   int64_t B, H, N, D; /* logical sizes */
   int64_t sB, sH, sN; /* element strides of the B, H and N dimensions */
@@ -554,19 +559,28 @@ vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
  *   out[b,h,j] = w                            for the new ones (mass is not read),
  * j < lens[b].  A row whose lse is -inf adds nothing; a token that no page holds gets
  * w = 0.  Entries at or past lens[b] are left as they were.
+ *   flags : 0 or VECATTN_CLEAR_PADDING
  *   q, table, cols, lens, n_new, window, sinks, scale : as for vecattn_cache_attn
  *   lse  : fp32 [B, Hq, n] contiguous
  *   mass : optional fp32 [B, H, M] contiguous; NULL: 0.  May be out itself.
  *   out  : fp32 [B, H, M] contiguous; tokens at or past M have no entry
- * Sums are fp32, of one order (no atomics).  Asynchronous, one launch.
- * Errors: as vecattn_cache_attn; INVALID_ARG for M < 1 or > 2^30, or a decay that is
- * negative or not finite.
+ *   workspace : device memory (16-byte aligned) of at least
+ *          vecattn_cache_mass_workspace_size bytes for the same qd and cache (0, with up to
+ *          16 rows n * Hq / H: may be NULL); contents need not be initialised.  Calls that
+ *          may overlap need one each.
+ * Sums are fp32, of one order (no atomics).  What a call does follows lens, n_new and table
+ * on the device, so that a captured call can be replayed as they change.
+ * Errors: as vecattn_cache_attn; INVALID_ARG for M < 1 or > 2^30, a decay that is negative
+ * or not finite, or other flags.
  */
+vecattn_status vecattn_cache_mass_workspace_size(const vecattn_tdesc* qd,
+                                                 const vecattn_cache* cache, size_t* bytes);
 vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const float* lse,
                                   const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                   const int32_t* lens, const int32_t* n_new, int64_t window,
                                   int64_t sinks, float scale, float decay, const float* mass,
-                                  float* out, int64_t M, void* stream);
+                                  float* out, int64_t M, int32_t flags, void* workspace, size_t workspace_bytes,
+                                  void* stream);
 
 /*
  * Which tokens of each sequence and head a budget keeps.  Candidates are the tokens
@@ -578,15 +592,22 @@ vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const 
  *   idx  : int32 [B, H, budget] output, ascending, -1 past the kept ones
  *   kept : int32 [B] output, how many (the same for every head): lens of the pages
  *          that vecattn_cache_gather fills
- * Asynchronous, one launch.
+ *   workspace : device memory (16-byte aligned) of at least
+ *          vecattn_cache_keep_workspace_size bytes for the same cache, cols, B and M (0 for
+ *          up to 8192 tokens: may be NULL); contents need not be initialised.  Calls that
+ *          may overlap need one each.
+ * Asynchronous; one launch for up to 8192 tokens (M, or cols * page), six for more.
  * Errors: INVALID_ARG (null pointer, B < 1, M or budget < 1 or > 2^30, sinks or recent
- * < 0, sinks + recent > budget, a bad cache, cols < 1 or cols * page > 2^30); UNSUPPORTED
- * (more than 65535 sequences or heads).
+ * < 0, sinks + recent > budget, a bad cache, cols < 1 or cols * page > 2^30, misalignment);
+ * CAPACITY (workspace too small); UNSUPPORTED (more than 65535 sequences or heads).
  */
+vecattn_status vecattn_cache_keep_workspace_size(const vecattn_cache* cache, int64_t cols,
+                                                 int64_t B, int64_t M, size_t* bytes);
 vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
                                   const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                   const int32_t* lens, int64_t budget, int64_t sinks,
-                                  int64_t recent, int32_t* idx, int32_t* kept, void* stream);
+                                  int64_t recent, int32_t* idx, int32_t* kept, void* workspace,
+                                  size_t workspace_bytes, void* stream);
 
 /*
  * Moves chosen tokens, per head, into other pages: slot i < kept[b] of sequence b and
@@ -603,8 +624,9 @@ vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
  *   mass : optional fp32 [B, H, M] contiguous; with mass_out, fp32 [B, H, budget]
  *          contiguous: mass_out[b,h,i] = mass[b,h,idx[b,h,i]] for i < kept[b] (NaN for an
  *          index outside [0, M)), the rest left as it was.  Both or neither.
+ *   flags : 0 or VECATTN_CLEAR_PADDING (of mass_out)
  * Asynchronous, one launch.
- * Errors: INVALID_ARG (null pointer, one of mass and mass_out alone, B < 1, budget or M
+ * Errors: INVALID_ARG (null pointer, other flags, one of mass and mass_out alone, B < 1, budget or M
  * < 1 or > 2^30, caches of other heads, D or bits, a bad cache, cols or to_cols < 1 or
  * more than 2^30 tokens); UNSUPPORTED (more than 65535 sequences or heads).
  */
@@ -612,7 +634,7 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
                                     int64_t B, const int32_t* idx, const int32_t* kept,
                                     int64_t budget, const vecattn_cache* to,
                                     const int32_t* to_table, int64_t to_cols, const float* mass,
-                                    int64_t M, float* mass_out, void* stream);
+                                    int64_t M, float* mass_out, int32_t flags, void* stream);
 
 /*
  * Attention of rows over another sequence's keys, such as an encoder's states (encoded
@@ -626,6 +648,7 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
  *          (0: one for all); what a masked key holds, NaN and infinities too, reaches no row
  *   n_q  : optional int32 [B] device memory (clamped to [0, Nq]): the rows of sequence b
  *          that exist; those past it are left as they were.  NULL: all Nq.
+ *   flags : 0 or VECATTN_CLEAR_PADDING
  *   scale : 0 means 1 / sqrt(D)
  *   lse  : optional fp32 [B, Hq, Nq] contiguous output, may be NULL
  *   workspace : device memory (16-byte aligned) of at least
@@ -635,7 +658,7 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
  * depend on the order of execution (no atomics).  What a call does follows lens, mask and
  * n_q on the device, so that a captured call can be replayed as they change.
  * Errors: INVALID_ARG (null pointer, shape mismatch, Hq % Hkv != 0, mask_sB < 0, a bad
- * scale, misalignment); CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128},
+ * scale, other flags, misalignment); CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128},
  * Nq * Hq / Hkv > 2^30, more than 2^24 sequences times Hkv, about 2^23 workgroups, a K or
  * V row stride of 2^24 elements or more).
  */
@@ -644,7 +667,7 @@ vecattn_status vecattn_cross_attn_workspace_size(const vecattn_tdesc* qd, const 
 vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const void* k,
                                   const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,
                                   const int32_t* lens, const uint8_t* mask, int64_t mask_sB,
-                                  const int32_t* n_q, float scale, void* o,
+                                  const int32_t* n_q, int32_t flags, float scale, void* o,
                                   const vecattn_tdesc* od, float* lse, void* workspace,
                                   size_t workspace_bytes, void* stream);
 
@@ -655,6 +678,8 @@ vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const 
  * transposed, t is -t (with the same factor: the gradient of the turn, and with factor 1
  * its inverse).  Values past rot stay as they are, bit for bit.
  */
+#define VECATTN_ROPE_TRANSPOSED 1
+
 typedef enum vecattn_rope_layout {
   VECATTN_ROPE_HALF = 0,       /* pair i is values i and i + rot / 2 */
   VECATTN_ROPE_INTERLEAVED = 1 /* pair i is values 2 i and 2 i + 1 */
@@ -676,7 +701,7 @@ typedef struct vecattn_rope_spec {
   int32_t rot;         /* values turned: even, 2 to D */
   int32_t layout;      /* vecattn_rope_layout */
   int32_t axes;        /* positions per token, 1 to 4 (e.g. time, height, width) */
-  int32_t transposed;  /* 0 or 1 */
+  int32_t flags;       /* VECATTN_ROPE_TRANSPOSED and VECATTN_CLEAR_PADDING bits */
   double factor;
   const double* freq;  /* host memory, rot / 2 frequencies in radians per position */
   const int32_t* axis; /* host memory, rot / 2: which position turns each pair; NULL: the

@@ -19,6 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libvecattn.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_CAPACITY, ERR_DEVICE = range(5)
+CLEAR_PADDING, ROPE_TRANSPOSED = 8, 1
 CAUSAL, KEEP_DIAG, UNPADDED = 1, 2, 4  # bits of the selection entry points' `causal` argument
 SEL_TOPK, SEL_TOPP, SEL_MINS, SEL_MINS_TILED = 0, 1, 2, 3
 _MODES = {"topk": SEL_TOPK, "topp": SEL_TOPP, "mins": SEL_MINS, "mins_tiled": SEL_MINS_TILED}
@@ -43,7 +44,7 @@ class CacheDesc(ctypes.Structure):
 
 class RopeSpec(ctypes.Structure):
     _fields_ = [("rot", ctypes.c_int32), ("layout", ctypes.c_int32), ("axes", ctypes.c_int32),
-                ("transposed", ctypes.c_int32), ("factor", ctypes.c_double),
+                ("flags", ctypes.c_int32), ("factor", ctypes.c_double),
                 ("freq", ctypes.POINTER(ctypes.c_double)),
                 ("axis", ctypes.POINTER(ctypes.c_int32))]
 
@@ -100,11 +101,17 @@ def load() -> ctypes.CDLL:
                                                       ctypes.POINTER(ctypes.c_size_t)]
     lib.vecattn_cache_attn.argtypes = [P, D, C, P, i64, P, P, i64, i64, f32, P, D, P, P,
                                        ctypes.c_size_t, P]
-    lib.vecattn_cache_mass.argtypes = [P, D, P, C, P, i64, P, P, i64, i64, f32, f32, P, P, i64, P]
-    lib.vecattn_cache_keep.argtypes = [P, i64, i64, C, P, i64, P, i64, i64, i64, P, P, P]
-    lib.vecattn_cache_gather.argtypes = [C, P, i64, i64, P, P, i64, C, P, i64, P, i64, P, P]
+    lib.vecattn_cache_mass_workspace_size.argtypes = [D, C, ctypes.POINTER(ctypes.c_size_t)]
+    lib.vecattn_cache_mass.argtypes = [P, D, P, C, P, i64, P, P, i64, i64, f32, f32, P, P, i64, i32,
+                                       P,
+                                       ctypes.c_size_t, P]
+    lib.vecattn_cache_keep_workspace_size.argtypes = [C, i64, i64, i64,
+                                                      ctypes.POINTER(ctypes.c_size_t)]
+    lib.vecattn_cache_keep.argtypes = [P, i64, i64, C, P, i64, P, i64, i64, i64, P, P, P,
+                                       ctypes.c_size_t, P]
+    lib.vecattn_cache_gather.argtypes = [C, P, i64, i64, P, P, i64, C, P, i64, P, i64, P, i32, P]
     lib.vecattn_cross_attn_workspace_size.argtypes = [D, D, ctypes.POINTER(ctypes.c_size_t)]
-    lib.vecattn_cross_attn.argtypes = [P, D, P, D, P, D, P, P, i64, P, f32, P, D, P, P,
+    lib.vecattn_cross_attn.argtypes = [P, D, P, D, P, D, P, P, i64, P, i32, f32, P, D, P, P,
                                        ctypes.c_size_t, P]
     lib.vecattn_rope_ladder.argtypes = [i32, f64, i32, f64, f64, f64, f64, P, ctypes.POINTER(f64)]
     lib.vecattn_rope.argtypes = [P, D, P, D, ctypes.POINTER(RopeSpec), P, i64, i64, P, P, i64, P, D,
@@ -117,7 +124,8 @@ def load() -> ctypes.CDLL:
                  "vecattn_sparse_attn_ordered", "vecattn_attn_order", "vecattn_window_attn",
                  "vecattn_cache_size", "vecattn_cache_write", "vecattn_cache_read",
                  "vecattn_cache_attn_workspace_size", "vecattn_cache_attn",
-                 "vecattn_cache_mass", "vecattn_cache_keep", "vecattn_cache_gather",
+                 "vecattn_cache_mass_workspace_size", "vecattn_cache_mass",
+                 "vecattn_cache_keep_workspace_size", "vecattn_cache_keep", "vecattn_cache_gather",
                  "vecattn_cross_attn_workspace_size", "vecattn_cross_attn",
                  "vecattn_rope_ladder", "vecattn_rope"):
         getattr(lib, name).restype = ctypes.c_int
@@ -729,11 +737,26 @@ def _fp32_on(t: torch.Tensor, shape, device, name: str):
         raise ValueError(f"{name} must be a contiguous float32 {list(shape)} tensor on {device}")
 
 
+@functools.lru_cache(maxsize=4096)
+def _mass_workspace(shape, pages, heads, dim, page, bits) -> int:
+    n = ctypes.c_size_t(0)
+    B, H, N, Dd = shape
+    qd, cd = TDesc(B, H, N, Dd, 0, 0, Dd), CacheDesc(None, pages, heads, dim, page, bits)
+    _check(load().vecattn_cache_mass_workspace_size(ctypes.byref(qd), ctypes.byref(cd),
+                                                    ctypes.byref(n)), "cache_mass_workspace_size")
+    return n.value
+
+
+def cache_mass_workspace_bytes(q: torch.Tensor, cache: Cache) -> int:
+    """Workspace bytes of cache_mass for these shapes."""
+    return _mass_workspace(q.shape, cache.pages, cache.heads, cache.dim, cache.page, cache.bits)
+
+
 def cache_mass(q: torch.Tensor, lse: torch.Tensor, cache: Cache, table: torch.Tensor,
                lens: torch.Tensor, mass: Optional[torch.Tensor] = None,
                n_new: Optional[torch.Tensor] = None, window: Optional[int] = None, sinks: int = 0,
-               scale: float = 0.0, decay: float = 1.0, out: Optional[torch.Tensor] = None
-               ) -> torch.Tensor:
+               scale: float = 0.0, decay: float = 1.0, out: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The attention weight that the new tokens of q [B, Hq, n, dim] put on each cached token, per
     key/value head (vecattn_cache_mass), added to ``decay`` times ``mass`` (float32 [B, heads, M];
     0 when not given, M then the table's tokens).  ``lse``: what cache_attn returned for the same
@@ -746,9 +769,15 @@ def cache_mass(q: torch.Tensor, lse: torch.Tensor, cache: Cache, table: torch.Te
     given = out if out is not None else mass
     M = cols * cache.page if given is None or given.dim() != 3 else given.shape[2]
     shape = (B, cache.heads, M)
+    flags = 0
     if out is None:
-        out = q.new_zeros(shape, dtype=torch.float32)
-    _same_device(dev, q=q)
+        out, flags = q.new_empty(shape, dtype=torch.float32), CLEAR_PADDING
+    _same_device(dev, q=q, workspace=workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    need = cache_mass_workspace_bytes(q, cache)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _fp32_on(lse, q.shape[:3], dev, "lse")
     _fp32_on(out, shape, dev, "out")
     if mass is not None:
@@ -757,26 +786,52 @@ def cache_mass(q: torch.Tensor, lse: torch.Tensor, cache: Cache, table: torch.Te
           q.data_ptr(), _tdesc(q.shape, q.stride()), lse.data_ptr(), cache.desc(),
           table.data_ptr(), cols, lens.data_ptr(), None if n_new is None else n_new.data_ptr(),
           _ALL_KEYS if window is None else int(window), int(sinks), float(scale), float(decay),
-          None if mass is None else mass.data_ptr(), out.data_ptr(), M)
+          None if mass is None else mass.data_ptr(), out.data_ptr(), M, flags,
+          None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel() * workspace.element_size())
     return out
 
 
+@functools.lru_cache(maxsize=4096)
+def _keep_workspace(pages, heads, dim, page, bits, cols, B, M) -> int:
+    n = ctypes.c_size_t(0)
+    cd = CacheDesc(None, pages, heads, dim, page, bits)
+    _check(load().vecattn_cache_keep_workspace_size(ctypes.byref(cd), cols, B, M, ctypes.byref(n)),
+           "cache_keep_workspace_size")
+    return n.value
+
+
+def cache_keep_workspace_bytes(mass: torch.Tensor, cache: Cache, cols: int) -> int:
+    """Workspace bytes of cache_keep for these shapes (a table of ``cols`` columns)."""
+    return _keep_workspace(cache.pages, cache.heads, cache.dim, cache.page, cache.bits, int(cols),
+                           mass.shape[0], mass.shape[2])
+
+
 def cache_keep(mass: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torch.Tensor,
-               budget: int, sinks: int = 0, recent: int = 0
-               ) -> Tuple[torch.Tensor, torch.Tensor]:
+               budget: int, sinks: int = 0, recent: int = 0,
+               workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Which tokens of each head a ``budget`` keeps (vecattn_cache_keep): the first ``sinks``, the
     last ``recent``, and the heaviest by ``mass`` (float32 [B, heads, M]).  Returns idx (int32 [B,
     heads, budget], ascending, -1 padded) and kept (int32 [B]), how many each sequence has."""
-    dev = _cache_args(cache, table, lens, mass.shape[0])
     if mass.dim() != 3:
         raise ValueError("mass must be [B, heads, M]")
     B, M = mass.shape[0], mass.shape[2]
+    dev = _cache_args(cache, table, lens, B)
     _fp32_on(mass, (B, cache.heads, M), dev, "mass")
+    _same_device(dev, workspace=workspace)
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    cols = table.shape[1]
+    need = cache_keep_workspace_bytes(mass, cache, cols)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     idx = mass.new_empty((B, cache.heads, int(budget)), dtype=torch.int32)
     kept = mass.new_empty((B,), dtype=torch.int32)
     _call(dev, "cache_keep", load().vecattn_cache_keep,
-          mass.data_ptr(), M, B, cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(),
-          int(budget), int(sinks), int(recent), idx.data_ptr(), kept.data_ptr())
+          mass.data_ptr(), M, B, cache.desc(), table.data_ptr(), cols, lens.data_ptr(),
+          int(budget), int(sinks), int(recent), idx.data_ptr(), kept.data_ptr(),
+          None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel() * workspace.element_size())
     return idx, kept
 
 
@@ -798,11 +853,12 @@ def cache_gather(cache: Cache, table: torch.Tensor, idx: torch.Tensor, kept: tor
     if mass is not None:
         M = mass.shape[-1]
         _fp32_on(mass, (B, cache.heads, M), dev, "mass")
-        out = mass.new_zeros((B, cache.heads, budget))
+        out = mass.new_empty((B, cache.heads, budget))
     _call(dev, "cache_gather", load().vecattn_cache_gather,
           cache.desc(), table.data_ptr(), table.shape[1], B, idx.data_ptr(), kept.data_ptr(),
           budget, to.desc(), to_table.data_ptr(), to_table.shape[1],
-          None if mass is None else mass.data_ptr(), M, None if out is None else out.data_ptr())
+          None if mass is None else mass.data_ptr(), M, None if out is None else out.data_ptr(),
+          CLEAR_PADDING)
     return out
 
 
@@ -834,9 +890,9 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     for t, n in ((q, "q"), (k, "k"), (v, "v")):
         _bf16_cuda(t, n)
     dev = q.device
-    new = q.new_empty if n_q is None else q.new_zeros
+    flags = 0
     if out is None:
-        out = new(q.shape)
+        out, flags = q.new_empty(q.shape), CLEAR_PADDING
     _bf16_cuda(out, "out")
     _same_device(dev, k=k, v=v, out=out, mask=mask, workspace=workspace)
     need = cross_attn_workspace_bytes(q, k)
@@ -855,12 +911,15 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
         raise ValueError("workspace must be contiguous")
     if workspace is None and need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    lse = new(q.shape[:3], dtype=torch.float32) if return_lse else None
+    lse = None
+    if return_lse:   # 0 for padded rows as well
+        new = q.new_empty if n_q is None or flags else q.new_zeros
+        lse = new(q.shape[:3], dtype=torch.float32)
     _call(dev, "cross_attn", load().vecattn_cross_attn,
           q.data_ptr(), _tdesc(q.shape, q.stride()), k.data_ptr(), _tdesc(k.shape, k.stride()),
           v.data_ptr(), _tdesc(v.shape, v.stride()), None if lens is None else lens.data_ptr(),
           None if mask is None else mask.data_ptr(), mask_sB,
-          None if n_q is None else n_q.data_ptr(), float(scale), out.data_ptr(),
+          None if n_q is None else n_q.data_ptr(), flags, float(scale), out.data_ptr(),
           _tdesc(out.shape, out.stride()), None if lse is None else lse.data_ptr(),
           None if workspace is None else workspace.data_ptr(),
           0 if workspace is None else workspace.numel() * workspace.element_size())
@@ -889,9 +948,11 @@ class Rope:
             raise ValueError("freq and axis need an entry per pair")
         specs = []
         freq, axis = (ctypes.c_double * n)(*self.freq), (ctypes.c_int32 * n)(*self.axis)
-        for transposed in (0, 1):
-            specs.append(RopeSpec(2 * n, _ROPE_LAYOUTS[self.layout], max(self.axis) + 1, transposed,
-                                  float(self.factor), freq, axis))
+        for clear in (0, CLEAR_PADDING):
+            for transposed in (0, ROPE_TRANSPOSED):
+                specs.append(ctypes.byref(RopeSpec(
+                    2 * n, _ROPE_LAYOUTS[self.layout], max(self.axis) + 1, clear | transposed,
+                    float(self.factor), freq, axis)))
         object.__setattr__(self, "_specs", tuple(specs))
 
     @property
@@ -945,9 +1006,9 @@ def rope(plan: Rope, q: torch.Tensor, k: Optional[torch.Tensor] = None,
     dev = q.device
     if k is not None:
         _bf16_cuda(k, "k")
-    new = q.new_empty if n_new is None else q.new_zeros
-    if out is None:
-        qo, ko = new(q.shape), None if k is None else new(k.shape)
+    clear = out is None
+    if clear:
+        qo, ko = q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)
     else:
         qo, ko = (out, None) if k is None else out
     _bf16_cuda(qo, "out")
@@ -971,7 +1032,7 @@ def rope(plan: Rope, q: torch.Tensor, k: Optional[torch.Tensor] = None,
     _call(dev, "rope", load().vecattn_rope,
           q.data_ptr(), _tdesc(q.shape, q.stride()), None if k is None else k.data_ptr(),
           None if k is None else _tdesc(k.shape, k.stride()),
-          ctypes.byref(plan._specs[1 if transpose else 0]),
+          plan._specs[(2 if clear else 0) + (1 if transpose else 0)],
           None if pos is None else pos.data_ptr(), sA, sB,
           None if lens is None else lens.data_ptr(), None if n_new is None else n_new.data_ptr(),
           int(start), qo.data_ptr(), _tdesc(qo.shape, qo.stride()),

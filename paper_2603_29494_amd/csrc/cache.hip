@@ -319,11 +319,10 @@ __global__ __launch_bounds__(256) void k_cache_read(
 }
 
 // Chosen tokens of a head into pages of their own: slot i takes the codes and (m, s) of
-// token idx[i] as they are.  A workgroup puts one block of 32 slots together in LDS and
-// stores it whole.  Of K a token's codes lie in four runs; of V, whose dwords eight
-// tokens share, its codes are picked out to bytes and put together anew.  What it reads
-// of V is what bounds it: eight tokens' codes for each one kept (a sixteenth of the
-// tokens kept at random reads half of them).
+// token idx[i] as they are.  A workgroup puts two blocks of 32 slots together in LDS and
+// stores them whole.  Of K a token's codes lie in four runs; of V, whose dwords eight
+// tokens share, its codes are picked out to bytes and put together anew.  The chain of
+// loads index, table, codes bounds it, with as many of them under way as a CU takes.
 struct GatherTo {
   uint8_t* data;
   const int32_t* table;
@@ -337,24 +336,28 @@ __global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
                                                       const int32_t* __restrict__ kept,
                                                       int64_t budget,
                                                       const float* __restrict__ mass, int64_t M,
-                                                      float* __restrict__ mass_out) {
+                                                      float* __restrict__ mass_out, bool clear) {
   using L = CacheLayout<D, BITS>;
   constexpr int RUN = D / 32 * L::kDw;   // dwords of a token's codes of K on a lane
+  constexpr int NB = 2, SLOTS = NB * kCacheBlock;
   const int64_t b = blockIdx.z;
   const int h = blockIdx.y;
   const int64_t n = min(max(static_cast<int64_t>(kept[b]), int64_t(0)), budget);
-  const int64_t jb = blockIdx.x, j0 = jb * kCacheBlock;
+  const int64_t jb = static_cast<int64_t>(blockIdx.x) * NB, j0 = jb * kCacheBlock;
+  if (mass_out && clear && threadIdx.x < SLOTS) {
+    const int64_t i = j0 + threadIdx.x;
+    if (i >= n && i < budget) mass_out[(b * map.H + h) * budget + i] = 0.0f;
+  }
   if (j0 >= n) return;
-  const int count = static_cast<int>(min<int64_t>(n - j0, kCacheBlock));
+  const int count = static_cast<int>(min<int64_t>(n - j0, SLOTS));
   const PageMap dst_map{to.data, to.table, to.cols, to.pages, map.H, to.page_shift};
-  uint8_t* dst = block_ptr<L::kBytes>(dst_map, b, h, jb);
 
-  __shared__ __align__(16) uint8_t image[L::kBytes];
-  __shared__ __align__(16) uint32_t codes[kCacheBlock][D / 4 + 4];   // V's, a byte each
-  __shared__ const uint8_t* s_blk[kCacheBlock];                      // NULL: no such token
-  __shared__ int s_token[kCacheBlock];                               // within its block
+  __shared__ __align__(16) uint8_t image[NB][L::kBytes];
+  __shared__ __align__(16) uint32_t codes[SLOTS][D / 4 + 4];   // V's, a byte each
+  __shared__ const uint8_t* s_blk[SLOTS];                      // NULL: no such token
+  __shared__ int s_token[SLOTS];                               // within its block
   const int64_t bh = b * map.H + h;
-  if (threadIdx.x < kCacheBlock) {
+  if (threadIdx.x < SLOTS) {
     const int slot = threadIdx.x;
     const uint8_t* blk = nullptr;
     int64_t j = -1;
@@ -368,76 +371,97 @@ __global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
     s_blk[slot] = blk;
     s_token[slot] = static_cast<int>(j & 31);
   }
-  if (!dst) return;   // the same for all threads
-  __syncthreads();
-  // K's codes, and the groups of both.
-  for (int i = threadIdx.x; i < kCacheBlock * 4; i += 256) {
-    const int slot = i & 31, g = i >> 5;
-    const uint8_t* blk = s_blk[slot];
-    const int from = s_token[slot];
-    const int a = (from >> 4) * RUN, c = (slot >> 4) * RUN;
+  uint8_t* dst[NB];
 #pragma unroll
-    for (int x = 0; x < RUN; ++x) {
-      const uint32_t w = blk ? *reinterpret_cast<const uint32_t*>(
-                                   blk + code_byte(a + x, g * 16 + (from & 15)))
-                             : 0u;
-      *reinterpret_cast<uint32_t*>(image + code_byte(c + x, g * 16 + (slot & 15))) = w;
-    }
+  for (int x = 0; x < NB; ++x)
+    dst[x] = x * kCacheBlock < count ? block_ptr<L::kBytes>(dst_map, b, h, jb + x) : nullptr;
+  __syncthreads();
+  // All loads first: K's codes, the groups of both, and V, sixteen lanes a token, 16 bytes
+  // at a time.
+  static_assert(SLOTS * 4 == 256 && SLOTS * 2 * L::kG <= 256, "one item per thread");
+  uint32_t k_run[RUN], par = 0x7FC07FC0u;
+  const int ks = threadIdx.x & (SLOTS - 1), kg = threadIdx.x / SLOTS;
+  {
+    const uint8_t* blk = s_blk[ks];
+    const int from = s_token[ks], a = (from >> 4) * RUN;
+#pragma unroll
+    for (int x = 0; x < RUN; ++x)
+      k_run[x] = blk ? *reinterpret_cast<const uint32_t*>(blk + code_byte(a + x, kg * 16 + (from & 15)))
+                     : 0u;
   }
-  for (int i = threadIdx.x; i < kCacheBlock * 2 * L::kG; i += 256) {
-    const int slot = i / L::kG % kCacheBlock, half = i / (L::kG * kCacheBlock), gi = i % L::kG;
+  const int ps = threadIdx.x / L::kG % SLOTS, gi = threadIdx.x % L::kG;
+  const int group_at = (threadIdx.x / (L::kG * SLOTS) ? L::kHalf : 0) + L::kCodes;
+  const bool has_par = threadIdx.x < SLOTS * 2 * L::kG;
+  if (has_par && s_blk[ps])
+    par = reinterpret_cast<const uint32_t*>(s_blk[ps] + group_at)[s_token[ps] * L::kG + gi];
+  constexpr int VI = SLOTS * 16 / 256, VC = L::kRun / 4;
+  const int ln = threadIdx.x & 15;
+  u32x4 v[VI][VC];
+#pragma unroll
+  for (int i = 0; i < VI; ++i) {
+    const int slot = 16 * i + (threadIdx.x >> 4);
     const uint8_t* blk = s_blk[slot];
-    const int at = half * L::kHalf + L::kCodes;
-    reinterpret_cast<uint32_t*>(image + at)[slot * L::kG + gi] =
-        blk ? reinterpret_cast<const uint32_t*>(blk + at)[s_token[slot] * L::kG + gi] : 0x7FC07FC0u;
+    const int g = (s_token[slot] >> 2) & 3;   // token = 16 (e / 4) + 4 g + e % 4
+#pragma unroll
+    for (int c = 0; c < VC; ++c)
+      v[i][c] = blk ? *reinterpret_cast<const u32x4*>(blk + L::kHalf + code_byte(4 * c, g * 16 + ln))
+                    : u32x4{0, 0, 0, 0};
   }
-  // V: sixteen lanes a token, 16 bytes at a time; a dword is of one head-dim value (4 bits)
-  // or of half its tokens (8 bits).
+  {
+    const int slot = ks & 31, c = (slot >> 4) * RUN;
+#pragma unroll
+    for (int x = 0; x < RUN; ++x)
+      *reinterpret_cast<uint32_t*>(image[ks >> 5] + code_byte(c + x, kg * 16 + (slot & 15))) = k_run[x];
+  }
+  if (has_par)
+    reinterpret_cast<uint32_t*>(image[ps >> 5] + group_at)[(ps & 31) * L::kG + gi] = par;
+  // Of V a dword is of one head-dim value (4 bits) or of half its tokens (8 bits).
   uint8_t* bytes = reinterpret_cast<uint8_t*>(codes);
   constexpr int kRow = 4 * (D / 4 + 4);
 #pragma unroll
-  for (int i0 = 0; i0 < kCacheBlock * 16; i0 += 256) {
-    const int i = i0 + threadIdx.x, slot = i >> 4, ln = i & 15;
-    const uint8_t* blk = s_blk[slot];
-    const int token = s_token[slot];
-    // token = 16 (e / 4) + 4 g + e % 4
-    const int g = (token >> 2) & 3, e = (token >> 4) * 4 + (token & 3);
+  for (int i = 0; i < VI; ++i) {
+    const int slot = 16 * i + (threadIdx.x >> 4), token = s_token[slot];
+    const int e = (token >> 4) * 4 + (token & 3);
 #pragma unroll
-    for (int c = 0; c < L::kRun / 4; ++c) {
-      u32x4 w = {0, 0, 0, 0};
-      if (blk) w = *reinterpret_cast<const u32x4*>(blk + L::kHalf + code_byte(4 * c, g * 16 + ln));
+    for (int c = 0; c < VC; ++c) {
       if constexpr (BITS == 4) {
 #pragma unroll
         for (int y = 0; y < 4; ++y)
           bytes[slot * kRow + 16 * (4 * c + y) + ln] =
-              static_cast<uint8_t>(w[y] >> (4 * nibble_of(e)) & 0xFu);
+              static_cast<uint8_t>(v[i][c][y] >> (4 * nibble_of(e)) & 0xFu);
       } else {
 #pragma unroll
         for (int y = 0; y < 2; ++y)
           bytes[slot * kRow + 16 * (2 * c + y) + ln] =
-              static_cast<uint8_t>((e >> 2 ? w[2 * y + 1] : w[2 * y]) >> (8 * (e & 3)));
+              static_cast<uint8_t>((e >> 2 ? v[i][c][2 * y + 1] : v[i][c][2 * y]) >> (8 * (e & 3)));
       }
     }
   }
   __syncthreads();
-  for (int it = threadIdx.x; it < D; it += 256) {
-    const int d = it % (D / 4) * 4, g = it / (D / 4);
+  for (int it = threadIdx.x; it < NB * D; it += 256) {
+    const int x0 = it / D, d = it % (D / 4) * 4, g = it % D / (D / 4);
     uint32_t c[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = codes[(e >> 2) * 16 + 4 * g + (e & 3)][d / 4];
+    for (int e = 0; e < 8; ++e)
+      c[e] = codes[x0 * kCacheBlock + (e >> 2) * 16 + 4 * g + (e & 3)][d / 4];
 #pragma unroll
     for (int x = 0; x < L::kDw; ++x) {
       uint32_t out[4];
       transpose_codes<BITS>(c, x, out);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<uint32_t*>(
-            image + L::kHalf + code_byte((d + i) / 16 * L::kDw + x, g * 16 + (d + i) % 16)) = out[i];
+        *reinterpret_cast<uint32_t*>(image[x0] + L::kHalf +
+                                     code_byte((d + i) / 16 * L::kDw + x, g * 16 + (d + i) % 16)) =
+            out[i];
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < L::kBytes / 16; i += 256)
-    *reinterpret_cast<u32x4*>(dst + 16 * i) = *reinterpret_cast<const u32x4*>(image + 16 * i);
+#pragma unroll
+  for (int x = 0; x < NB; ++x)
+    if (dst[x])
+      for (int i = threadIdx.x; i < L::kBytes / 16; i += 256)
+        *reinterpret_cast<u32x4*>(dst[x] + 16 * i) =
+            *reinterpret_cast<const u32x4*>(image[x] + 16 * i);
 }
 
 PageMap page_map(const CacheArgs& c) {
@@ -480,14 +504,15 @@ hipError_t launch_cache_read(const CacheArgs& c, int64_t start, const Tensor4& k
 
 hipError_t launch_cache_gather(const CacheArgs& c, const CacheArgs& to, int64_t B,
                                const int32_t* idx, const int32_t* kept, int64_t budget,
-                               const float* mass, int64_t M, float* mass_out, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>((budget + kCacheBlock - 1) / kCacheBlock),
+                               const float* mass, int64_t M, float* mass_out, bool clear,
+                               hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((budget + 2 * kCacheBlock - 1) / (2 * kCacheBlock)),
                   static_cast<unsigned>(c.H), static_cast<unsigned>(B));
   const GatherTo g{static_cast<uint8_t*>(to.data), to.table, to.cols, to.pages,
                    __builtin_ctz(static_cast<unsigned>(to.page))};
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, page_map(c), g, idx, kept, budget, mass, M,
-                       mass_out);
+                       mass_out, clear);
   };
   if (c.D == 128) c.bits == 4 ? run(k_cache_gather<128, 4>) : run(k_cache_gather<128, 8>);
   else c.bits == 4 ? run(k_cache_gather<64, 4>) : run(k_cache_gather<64, 8>);

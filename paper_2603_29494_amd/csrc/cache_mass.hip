@@ -29,6 +29,7 @@ struct MassParams {
   int32_t cols, pages, page_shift;
   int32_t H, n, group, window, sinks;
   int32_t in_place;    // what no row sees stays as it is
+  int32_t clear;       // entries past a sequence's tokens become 0
   float scale_log2, decay;
 };
 
@@ -69,10 +70,19 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
+// Blocks that a (sequence, head) has entries to write in.
+__device__ __forceinline__ int blocks_of(const MassParams& a, const Place& s) {
+  return static_cast<int>(((a.clear ? a.M : s.end) + kCacheBlock - 1) / kCacheBlock);
+}
+
 // Token j's sum: what it had before (a new token: nothing) and w.
 __device__ __forceinline__ void collect(const MassParams& a, const Place& s, int64_t bh, int j,
                                         float w) {
   const int64_t at = bh * a.M + j;
+  if (j >= s.end) {
+    if (a.clear && j < a.M) a.out[at] = 0.0f;
+    return;
+  }
   if (a.mass && j < s.p_first) w = __builtin_fmaf(a.decay, a.mass[at], w);
   a.out[at] = w;
 }
@@ -87,7 +97,7 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   const int h = blockIdx.y;
   const int64_t b = blockIdx.z, bh = b * a.H + h;
   const Place s = place_of(a, b);
-  const int blocks = (s.end + kCacheBlock - 1) / kCacheBlock;
+  const int blocks = blocks_of(a, s);
   const int step = gridDim.x * 4;
   int jb = blockIdx.x * 4 + wave;
   if (jb >= blocks) return;
@@ -160,7 +170,7 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) w = (n & 7) == e ? p[e / 4][e % 4] : w;
     }
-    if (n < 8 && j < s.end && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, w);
+    if (n < 8 && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, w);
   };
   Keys cur, nxt;
   bool held = load(cur, jb);
@@ -175,214 +185,231 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   }
 }
 
-// More rows: NB blocks of 32 tokens per wave stay in registers as fp16 codes, and the
-// rows pass by in tiles of 32, put into LDS by the workgroup's four waves, one tile
-// ahead.  v_mfma_f32_32x32x16 (lane l = 32 g + n): A: token n, head-dim values 16 st +
-// 8 g + 0..7; B: row n, the same; C: row n, tokens 8 (e / 4) + 4 g + e % 4.  The m_G
-// sum(q_G) terms start the sums: m_G is bf16 as it is, and sum(q_G) goes in as three
-// bf16 numbers that add up to it.
-template <int D, int BITS, int NB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_mass_many(
-    const MassParams a) {
+// More rows, in tiles of 32, brought once into the form in which the products take them:
+// fp16 times a power of two, the sums over each group's values, and what takes a product
+// to a weight.
+template <int D>
+struct RowTile {
+  static constexpr int kRowBytes = 2 * D + 16;   // rows 16 bytes apart in the banks
+  uint8_t q[32 * kRowBytes];
+  u32x4 sums[32];                // of each group as three bf16 that add up to it; 0, 0
+  float to_log2[32], off[32];    // off: the row's lse, in log2 units; inf where it weighs nothing
+};
+
+// One tile per workgroup, eight threads a row.
+template <int D, int BITS>
+__global__ __launch_bounds__(256) void k_mass_rows(const MassParams a, RowTile<D>* out) {
+  constexpr int C = D / 64;   // 16-byte chunks per thread
+  const int h = blockIdx.y;
+  const int64_t b = blockIdx.z;
+  const Place s = place_of(a, b);
+  const int t = blockIdx.x;
+  if (32 * t >= s.rows) return;
+  RowTile<D>& to = out[(b * a.H + h) * gridDim.x + t];
+  const int sr = threadIdx.x >> 3, sc = threadIdx.x & 7;
+  const int row = 32 * t + sr;
+  const int tok = row / a.group, hq = h * a.group + row % a.group;
+  const float lse = row < s.rows ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
+  const bool have = lse != kNegInf;
+  u32x4 raw[C];
+  float top = 0x1p-100f, sum[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    raw[c] = u32x4{0, 0, 0, 0};
+    if (have)
+      raw[c] = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN +
+                                               8 * (c * 8 + sc));
+    sum[c] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float lo = low_of(raw[c][e]), hi = high_of(raw[c][e]);
+      top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
+      sum[c] += lo + hi;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) {
+    top = fmaxf(top, __shfl_xor(top, o));
+#pragma unroll
+    for (int c = 0; c < C; ++c) sum[c] += __shfl_xor(sum[c], o);   // chunks c hold group c
+  }
+  // The largest value between 2^14 and 2^15 (cache_rows.h).
+  const int k = 15 - __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    u32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = to_f16(__builtin_amdgcn_ldexpf(low_of(raw[c][e]), k),
+                    __builtin_amdgcn_ldexpf(high_of(raw[c][e]), k));
+    *reinterpret_cast<u32x4*>(to.q + sr * RowTile<D>::kRowBytes + 16 * (c * 8 + sc)) = y;
+  }
+  if (sc > 0) return;
+  uint32_t part[6] = {};
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    float x = __builtin_amdgcn_ldexpf(sum[c], k - kCodeExp<BITS>);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const uint32_t bits = __float_as_uint(x) & 0xFFFF0000u;   // eight leading bits
+      part[3 * c + i] = bits >> 16;
+      x = (bits & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float(bits);
+    }
+  }
+  to.sums[sr] = u32x4{part[0] | part[1] << 16, part[2] | part[3] << 16, part[4] | part[5] << 16, 0u};
+  to.to_log2[sr] = a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, kCodeExp<BITS> - k);
+  to.off[sr] = have ? lse * kLog2e : INFINITY;
+}
+
+// A block of 32 tokens per wave stays in registers as fp16 codes, and the row tiles pass by
+// in LDS, fetched two ahead by the workgroup's four waves.  v_mfma_f32_32x32x16 (lane l =
+// 32 g + n): A: token n, head-dim values 16 st + 8 g + 0..7; B: row n, the same; C: row n,
+// tokens 8 (e / 4) + 4 g + e % 4.  The m_G sum(q_G) terms start the sums, m_G being bf16 as
+// it is.  Row tiles that see all of the workgroup's tokens, most of them, pass without
+// masks, in a loop of their own.
+template <int D, int BITS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k_mass_many(
+    const MassParams a, const RowTile<D>* row_tiles, int32_t tiles_held) {
   using L = CacheLayout<D, BITS>;
+  using Tile = RowTile<D>;
   constexpr int G = L::kG, DW = L::kDw, ST = D / 16, SW = D / 32;
-  constexpr int kRowBytes = 2 * D + 16;      // rows 16 bytes apart in the banks
-  struct Tile {
-    uint8_t q[32 * kRowBytes];
-    u32x4 sums[32];                          // 2 x 3 bf16, 0
-    float to_log2[32], off[32];
-  };
-  __shared__ __align__(16) Tile tiles[2];
+  constexpr int U = (sizeof(Tile) + 4095) / 4096;   // direct loads per wave and tile
+  __shared__ __align__(16) uint8_t ring[3][U * 4096];
   const int lane = threadIdx.x & 63, n = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.y;
   const int64_t b = blockIdx.z, bh = b * a.H + h;
   const Place s = place_of(a, b);
-  const int blocks = (s.end + kCacheBlock - 1) / kCacheBlock;
-  const int first = blockIdx.x * 4 * NB;   // of the workgroup
+  const int blocks = blocks_of(a, s);
+  const int first = blockIdx.x * 4;   // the workgroup's blocks
   if (first >= blocks) return;
-  const int jb0 = first + wave * NB;
+  const int jb = first + wave, j0 = jb * kCacheBlock;
 
-  bool held[NB];
-  bf16x8 low[NB];
-  f16x8 codes[NB][ST];
-  float step_of[NB][G][16], w[NB][16];
-#pragma unroll
-  for (int x = 0; x < NB; ++x) {
-    const uint8_t* blk = jb0 + x < blocks ? keys_of<L::kBytes>(a, b, h, jb0 + x) : nullptr;
-    held[x] = blk != nullptr;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) w[x][e] = 0.0f;
-    low[x] = bf16x8{};
-#pragma unroll
-    for (int st = 0; st < ST; ++st) codes[x][st] = f16x8{};
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) step_of[x][gi][e] = 0.0f;
-    if (!blk) continue;
-#pragma unroll
-    for (int st = 0; st < ST; ++st) {
-      // Token n = 16 t + n % 16, values 16 st + 8 g on: run dword (t D / 32 + st / 2) kDw
-      // of lane 16 (2 (st % 2) + g) + n % 16.
-      const int w0 = ((n >> 4) * SW + st / 2) * DW, from = (2 * (st & 1) + g) * 16 + (n & 15);
-      uint32_t u[DW];
-#pragma unroll
-      for (int y = 0; y < DW; ++y)
-        u[y] = *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + y, from));
-      codes[x][st] = __builtin_bit_cast(f16x8, codes_f16<BITS>(u));
-    }
-    const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + L::kCodes);
-    if (g == 0) {
-      const uint32_t m0 = par[n * G] & 0xFFFFu, m1 = G > 1 ? par[n * G + G - 1] & 0xFFFFu : 0u;
-      low[x] = __builtin_bit_cast(bf16x8, u32x4{m0 | m0 << 16, m0 | m1 << 16, m1 | m1 << 16, 0u});
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-#pragma unroll
-      for (int gi = 0; gi < G; ++gi)
-        step_of[x][gi][e] = high_of(par[(8 * (e / 4) + 4 * g + e % 4) * G + gi]);
-  }
-
-  // Row tiles [t0, t1) that may see one of the workgroup's tokens.
-  const int ntiles = (s.rows + 31) / 32;
-  int t0 = 0;
-  {
-    const int j_first = first * kCacheBlock;      // rows before it see none of them
-    const int r = max(0, j_first - s.p_first) * a.group;
-    t0 = j_first > s.p_first ? r / 32 : 0;
-  }
-  // Eight threads a row, 16 bytes at a time.
-  constexpr int C = D / 64;   // 16-byte chunks per thread
-  const int sr = threadIdx.x >> 3, sc = threadIdx.x & 7;
-  u32x4 raw[C];
-  float raw_lse = kNegInf;
-  auto fetch = [&](int t) __attribute__((always_inline)) {
-    const int row = 32 * t + sr;
-    const bool have = row < s.rows;
-    const int tok = row / a.group, hq = h * a.group + row % a.group;
-    raw_lse = have ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      raw[c] = u32x4{0, 0, 0, 0};
-      if (have && raw_lse != kNegInf)
-        raw[c] = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN +
-                                                 8 * (c * 8 + sc));
-    }
+  // Row tiles: [t0, c0) and [c1, ntiles) with masks, [c0, c1) whole; those before t0 see
+  // none of the workgroup's tokens [j_lo, j_hi].
+  const int ntiles = first * kCacheBlock < s.end ? (s.rows + 31) / 32 : 0;
+  const int j_lo = first * kCacheBlock, j_hi = min(j_lo + 4 * kCacheBlock, s.end) - 1;
+  auto tile_at = [&](int64_t row) __attribute__((always_inline)) {
+    const int64_t t = row < 0 ? 0 : row >> 5;
+    return t < ntiles ? static_cast<int>(t) : ntiles;
   };
-  auto stage = [&](Tile& to) __attribute__((always_inline)) {
-    float top = 0x1p-100f, sum[C];
+  const int64_t off_lo = int64_t(j_lo) - s.p_first, off_hi = int64_t(j_hi) - s.p_first;
+  const int t0 = tile_at(off_lo * a.group);
+  const int c0 = max(t0, tile_at(off_hi * a.group + 31));
+  const int c1 = j_hi < a.sinks ? ntiles : max(c0, tile_at((off_lo + a.window) * a.group));
+
+  const Tile* tiles = row_tiles + bh * tiles_held;
+  auto fetch = [&](int t, int st) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<Tile*>(tiles + t), 0, sizeof(Tile), 0x00020000);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      sum[c] = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float lo = low_of(raw[c][e]), hi = high_of(raw[c][e]);
-        top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
-        sum[c] += lo + hi;
-      }
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      top = fmaxf(top, __shfl_xor(top, o));
-#pragma unroll
-      for (int c = 0; c < C; ++c) sum[c] += __shfl_xor(sum[c], o);   // chunks c hold group c
-    }
-    // The largest value between 2^14 and 2^15 (cache_rows.h).
-    const int k = 15 - __builtin_amdgcn_frexp_expf(top);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      u32x4 y;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        y[e] = to_f16(__builtin_amdgcn_ldexpf(low_of(raw[c][e]), k),
-                      __builtin_amdgcn_ldexpf(high_of(raw[c][e]), k));
-      *reinterpret_cast<u32x4*>(to.q + sr * kRowBytes + 16 * (c * 8 + sc)) = y;
-    }
-    if (sc == 0) {
-      uint32_t part[6] = {};
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float x = __builtin_amdgcn_ldexpf(sum[c], k - kCodeExp<BITS>);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-          const uint32_t bits = __float_as_uint(x) & 0xFFFF0000u;   // eight leading bits
-          part[3 * c + i] = bits >> 16;
-          x = (bits & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float(bits);
-        }
-      }
-      to.sums[sr] = u32x4{part[0] | part[1] << 16, part[2] | part[3] << 16, part[4] | part[5] << 16,
-                          0u};
-      to.to_log2[sr] = a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, kCodeExp<BITS> - k);
-      to.off[sr] = raw_lse == kNegInf ? INFINITY : raw_lse * kLog2e;
+    for (int u = 0; u < U; ++u) {
+      const int at = (wave * U + u) * 1024;
+      gather16_to_lds(rs, at + 16 * lane, ring[st] + at);
     }
   };
   if (t0 < ntiles) {
-    fetch(t0);
-    stage(tiles[t0 & 1]);
+    fetch(t0, 0);
+    fetch(min(t0 + 1, ntiles - 1), 1);
   }
-  __syncthreads();
-  for (int t = t0; t < ntiles; ++t) {
-    if (t + 1 < ntiles) fetch(t + 1);
-    const Tile& tile = tiles[t & 1];
-    const int r1 = min(32 * t + 31, s.rows - 1);
-    const int p_lo = s.p_first + 32 * t / a.group, p_hi = s.p_first + r1 / a.group;
-    const u32x4 sums = g == 0 ? tile.sums[n] : u32x4{0, 0, 0, 0};
+
+  // A block that no page holds passes as zeros, and its sums are left out at the end.
+  const uint8_t* blk = j0 < s.end ? keys_of<L::kBytes>(a, b, h, jb) : nullptr;
+  bf16x8 low = {};
+  f16x8 codes[ST];
+  float step_of[G][16], w[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) w[e] = 0.0f;
+#pragma unroll
+  for (int st = 0; st < ST; ++st) {
+    // Token n = 16 t + n % 16, values 16 st + 8 g on: run dword (t D / 32 + st / 2) kDw
+    // of lane 16 (2 (st % 2) + g) + n % 16.
+    const int w0 = ((n >> 4) * SW + st / 2) * DW, from = (2 * (st & 1) + g) * 16 + (n & 15);
+    uint32_t u[DW];
+#pragma unroll
+    for (int y = 0; y < DW; ++y)
+      u[y] = blk ? *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + y, from)) : 0u;
+    codes[st] = __builtin_bit_cast(f16x8, codes_f16<BITS>(u));
+  }
+  const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + L::kCodes);
+  if (blk && g == 0) {
+    const uint32_t m0 = par[n * G] & 0xFFFFu, m1 = G > 1 ? par[n * G + G - 1] & 0xFFFFu : 0u;
+    low = __builtin_bit_cast(bf16x8, u32x4{m0 | m0 << 16, m0 | m1 << 16, m1 | m1 << 16, 0u});
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi)
+      step_of[gi][e] = blk ? high_of(par[(8 * (e / 4) + 4 * g + e % 4) * G + gi]) : 0.0f;
+
+  int st = 0;
+  auto turn = [&](int t, auto masked_tag) __attribute__((always_inline)) {
+    wait_vmcnt<U>();   // of the tile after it
+    __builtin_amdgcn_s_barrier();
+    // Past the last tile that one is fetched again (into a stage that nothing reads).
+    fetch(min(t + 2, ntiles - 1), st == 0 ? 2 : st - 1);
+    const Tile& tile = *reinterpret_cast<const Tile*>(ring[st]);
+    st = st == 2 ? 0 : st + 1;
+    const u32x4 sums = tile.sums[n];   // the low half of A's slots is 0 for g = 1
     const float to_log2 = tile.to_log2[n], off = tile.off[n];
+    const uint8_t* qrow = tile.q + n * Tile::kRowBytes + 16 * g;
+    const f32x16 start = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        low, __builtin_bit_cast(bf16x8, sums), f32x16{}, 0, 0, 0);
+    f32x16 acc[G];
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) acc[gi] = f32x16{};
+#pragma unroll
+    for (int st = 0; st < ST; ++st)
+      acc[st / 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+          codes[st], __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(qrow + 32 * st)),
+          acc[st / 4], 0, 0, 0);
     const int pos = off == INFINITY ? -1 : s.p_first + (32 * t + n) / a.group;
-    const uint8_t* qrow = tile.q + n * kRowBytes + 16 * g;
-#pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      const int j0 = (jb0 + x) * kCacheBlock;
-      if (!held[x] || j0 > p_hi || (j0 + 31 <= p_lo - a.window && j0 >= a.sinks)) continue;
-      const f32x16 start = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          low[x], __builtin_bit_cast(bf16x8, sums), f32x16{}, 0, 0, 0);
-      f32x16 acc[G];
-#pragma unroll
-      for (int gi = 0; gi < G; ++gi) acc[gi] = f32x16{};
-#pragma unroll
-      for (int st = 0; st < ST; ++st)
-        acc[st / 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-            codes[x][st],
-            __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(qrow + 32 * st)),
-            acc[st / 4], 0, 0, 0);
-      const bool masked = j0 + 31 > p_lo || (j0 <= p_hi - a.window && j0 + 31 >= a.sinks);
-      float p[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float y = start[e];
-#pragma unroll
-        for (int gi = 0; gi < G; ++gi) y = __builtin_fmaf(step_of[x][gi][e], acc[gi][e], y);
-        p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
-      }
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = j0 + 8 * (e / 4) + 4 * g + e % 4;
-          p[e] = j <= pos && (j > pos - a.window || j < a.sinks) ? p[e] : 0.0f;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) w[x][e] += p[e];
-    }
-    if (t + 1 < ntiles) stage(tiles[(t + 1) & 1]);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int x = 0; x < NB; ++x) {
-    float mine = 0.0f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float y = row_sum(w[x][e]);
-      const float all = y + __shfl_xor(y, 16);
-      mine = (n & 15) == e ? all : mine;
+      float y = start[e];
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi) y = __builtin_fmaf(step_of[gi][e], acc[gi][e], y);
+      y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
+      if constexpr (decltype(masked_tag)::value) {
+        const int j = j0 + 8 * (e / 4) + 4 * g + e % 4;
+        y = j <= pos && (j > pos - a.window || j < a.sinks) ? y : 0.0f;
+      }
+      w[e] += y;
     }
-    const int j = (jb0 + x) * kCacheBlock + 8 * ((n & 15) / 4) + 4 * g + (n & 3);
-    if (n < 16 && jb0 + x < blocks && j < s.end) collect(a, s, bh, j, mine);
+  };
+#pragma unroll 1
+  for (int t = t0; t < c0; ++t) turn(t, std::true_type{});
+#pragma unroll 1
+  for (int t = c0; t < c1; ++t) turn(t, std::false_type{});
+#pragma unroll 1
+  for (int t = c1; t < ntiles; ++t) turn(t, std::true_type{});
+  wait_all();
+
+  float mine = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float y = row_sum(w[e]);
+    const float all = y + __shfl_xor(y, 16);
+    mine = (n & 15) == e ? all : mine;
   }
+  const int j = j0 + 8 * ((n & 15) / 4) + 4 * g + (n & 3);
+  if (n < 16 && jb < blocks) collect(a, s, bh, j, blk ? mine : 0.0f);
 }
 
+template <int D>
+size_t row_tiles_bytes(int64_t heads, int64_t rows) {
+  return static_cast<size_t>(heads) * ((rows + 31) / 32) * sizeof(RowTile<D>);
+}
+
+constexpr int kFewRows = 16;   // that one tile of columns takes as they come
+
 }  // namespace
+
+size_t cache_mass_workspace_bytes(const CacheAttnShape& s) {
+  const int64_t rows = s.n * (s.Hq / s.H);
+  if (rows <= kFewRows) return 0;
+  return s.D == 128 ? row_tiles_bytes<128>(s.B * s.H, rows) : row_tiles_bytes<64>(s.B * s.H, rows);
+}
 
 hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
   const CacheArgs& c = x.cache;
@@ -406,27 +433,32 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
   a.window = static_cast<int32_t>(x.window);
   a.sinks = static_cast<int32_t>(x.sinks);
   a.in_place = x.mass == x.out && x.decay == 1.0f;
+  a.clear = x.clear;
   const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(c.D));
   a.scale_log2 = scale * kLog2e;
   a.decay = x.decay;
   const int64_t rows = static_cast<int64_t>(a.n) * a.group;
-  const int64_t blocks = (std::min(x.M, c.cols * c.page) + kCacheBlock - 1) / kCacheBlock;
+  const int64_t entries = x.clear ? x.M : std::min(x.M, c.cols * c.page);
+  const int64_t blocks = (entries + kCacheBlock - 1) / kCacheBlock;
   const int64_t heads = x.q.B * c.H;
-  auto launch = [&](auto kernel, int64_t groups) {
+  auto launch = [&](auto kernel, int64_t groups, auto... more) {
     hipLaunchKernelGGL(kernel,
                        dim3(static_cast<unsigned>(groups), static_cast<unsigned>(c.H),
                             static_cast<unsigned>(x.q.B)),
-                       dim3(256), 0, stream, a);
+                       dim3(256), 0, stream, a, more...);
   };
   auto pick = [&](auto dim, auto bits) {
     constexpr int D = decltype(dim)::value, BITS = decltype(bits)::value;
-    if (rows <= 16) {
-      const int64_t fill = std::max<int64_t>(1, 4096 / heads);
+    if (rows <= kFewRows) {
+      // Two workgroups per place on the CUs, so that unequal lengths even out (4 x 131072
+      // tokens, 4 heads: 46 us; 45 with half of them, 49 with twice as many).
+      const int64_t fill = std::max<int64_t>(1, 2048 / heads);
       launch(k_mass_few<D, BITS>, std::min((blocks + 3) / 4, fill));
-    } else if (heads * blocks >= 4096) {
-      launch(k_mass_many<D, BITS, 2>, (blocks + 7) / 8);
     } else {
-      launch(k_mass_many<D, BITS, 1>, (blocks + 3) / 4);
+      RowTile<D>* prepared = static_cast<RowTile<D>*>(x.workspace);
+      const int64_t tiles = (rows + 31) / 32;
+      launch(k_mass_rows<D, BITS>, tiles, prepared);
+      launch(k_mass_many<D, BITS>, (blocks + 3) / 4, prepared, static_cast<int32_t>(tiles));
     }
   };
   using std::integral_constant;

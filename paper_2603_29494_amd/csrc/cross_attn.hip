@@ -38,11 +38,14 @@ struct CrossParams {
   const uint8_t* mask;
   int64_t mask_sB;
   const int32_t* n_q;
+  int32_t clear;       // rows past n_q become 0
   float* part;         // [item][rows of a tile][D] sums, then [item][rows of a tile] (m, l)
-  int32_t Hkv, group, Nq, Nk, row_tiles, chunks, chunk, run;
-  int64_t items;
+  int32_t Hkv, group, Nq, Nk, row_tiles, chunks, chunk, near_heads;
+  uint32_t items, per_xcd;   // per_xcd: consecutive items of an XCD, which share keys in its L2
   float scale_log2;
 };
+
+typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 struct Item {
   int64_t b, index;
@@ -53,26 +56,27 @@ __device__ __forceinline__ int chunks_of(const CrossParams& a, int len) {
   return max(1, (len + a.chunk - 1) / a.chunk);
 }
 __device__ __forceinline__ int keys_of(const CrossParams& a, int64_t b) {
-  return a.lens ? min(max(a.lens[b], 0), a.Nk) : a.Nk;
+  return a.lens ? min(max(((ScalarInts)a.lens)[b], 0), a.Nk) : a.Nk;
 }
 __device__ __forceinline__ int rows_of(const CrossParams& a, int64_t b) {
-  return (a.n_q ? min(max(a.n_q[b], 0), a.Nq) : a.Nq) * a.group;
+  return (a.n_q ? min(max(((ScalarInts)a.n_q)[b], 0), a.Nq) : a.Nq) * a.group;
 }
 
-// Sequence and key/value head, then row tile, then chunk.  The hardware deals workgroup x
-// to XCD x % 8; an XCD takes `run` consecutive items at a time, which share keys, so that
-// it finds them in its own L2.
-__device__ __forceinline__ bool find_item(const CrossParams& a, int tile_rows, Item& s) {
-  const int64_t slot = blockIdx.x >> 3;
-  int64_t i = (slot / a.run * 8 + (blockIdx.x & 7)) * a.run + slot % a.run;
-  if (i >= a.items) return false;
-  s.index = i;
-  s.c = static_cast<int>(i % a.chunks);
-  i /= a.chunks;
-  s.rt = static_cast<int>(i % a.row_tiles);
-  i /= a.row_tiles;
-  s.hk = static_cast<int>(i % a.Hkv);
-  s.b = i / a.Hkv;
+// Item i: sequence and near_heads heads, then row tile, then head among these, then chunk.
+// Rows of heads beside each other lie beside each other in memory where tensors are
+// token-major, and one head's alone would meet few of an L2's channels.  False where the
+// item has no rows or no keys to take.
+__device__ __forceinline__ bool decode(const CrossParams& a, int tile_rows, uint32_t i, Item& s) {
+  uint32_t rest = i / static_cast<uint32_t>(a.chunks);
+  s.c = static_cast<int>(i - rest * a.chunks);
+  const uint32_t near = rest / static_cast<uint32_t>(a.near_heads);
+  const uint32_t lo = rest - near * a.near_heads;
+  rest = near / static_cast<uint32_t>(a.row_tiles);
+  s.rt = static_cast<int>(near - rest * a.row_tiles);
+  const uint32_t bh = rest * a.near_heads + lo, b = bh / static_cast<uint32_t>(a.Hkv);
+  s.hk = static_cast<int>(bh - b * a.Hkv);
+  s.b = b;
+  s.index = (static_cast<int64_t>(bh) * a.row_tiles + s.rt) * a.chunks + s.c;
   s.len = keys_of(a, s.b);
   s.rows = rows_of(a, s.b);
   s.count = chunks_of(a, s.len);
@@ -95,57 +99,84 @@ __device__ __forceinline__ void put_lse(const CrossParams& a, int64_t b, int hk,
       l == 0.0f ? kNegInf : (m + __builtin_log2f(l)) * kLn2;
 }
 
-// Bit r: key j0 + r exists and the mask leaves it.
+// The rows of an item's tile that do not exist, where they become 0.
+template <int D>
+__device__ __forceinline__ void clear_rows(const CrossParams& a, const Item& s, int tile_rows) {
+  if (!a.clear || s.c > 0) return;
+  const int first = max(s.rows, s.rt * tile_rows);
+  const int count = min((s.rt + 1) * tile_rows, a.Nq * a.group) - first;
+  for (int i = threadIdx.x; i < count * (D / 8); i += blockDim.x) {
+    const int row = first + i / (D / 8);
+    reinterpret_cast<u32x4*>(o_row(a, s.b, s.hk, row))[i % (D / 8)] = u32x4{0, 0, 0, 0};
+    if (a.lse && i % (D / 8) == 0) {
+      const int tok = row / a.group, h = s.hk * a.group + row % a.group;
+      a.lse[(s.b * a.Hkv * a.group + h) * a.Nq + tok] = 0.0f;
+    }
+  }
+}
+
+// Bit r: key j0 + r, of `keys`, exists and the mask leaves it.
 template <int KEYS>
-__device__ __forceinline__ uint64_t visible(const CrossParams& a, const Item& s, int j0, int lane) {
-  bool see = lane < KEYS && j0 + lane < s.len;
-  if (a.mask && see) see = a.mask[s.b * a.mask_sB + j0 + lane] != 0;
+__device__ __forceinline__ uint64_t visible(const uint8_t* mask, int keys, int j0, int lane) {
+  bool see = lane < KEYS && j0 + lane < keys;
+  if (mask && see) see = mask[j0 + lane] != 0;
   return __ballot(see);
 }
 
-// Direct-to-LDS instruction u of a tile of KEYS rows (16 bytes a lane).  HIDE: rows that
-// are not visible read 0; rows at or past len do so always.
-template <int D, int KEYS, bool HIDE>
-__device__ __forceinline__ void gather(const uint16_t* base, int64_t sN, int j0, int len, int u,
-                                       int lane, uint64_t see, uint16_t* dst) {
+// Direct-to-LDS instruction u of a tile of KEYS rows from row j0 on (16 bytes a lane).  HIDE:
+// rows that are not visible read 0; rows past `keys` do so always.
+// col: 16 times the lane's chunk, swizzled for the instruction's first row; row: its row of the
+// instruction's times rowb.
+template <int D>
+__device__ __forceinline__ uint32_t gather_col(int lane) {
   constexpr int CH = D / 8;
-  const uint32_t rowb = static_cast<uint32_t>(sN) * 2u;
+  return 16u * ((lane % CH) ^ swz<D>(lane / CH));
+}
+template <int D, int KEYS, bool HIDE>
+__device__ __forceinline__ void gather(const uint16_t* base, uint32_t rowb, int j0, int keys, int u,
+                                       int lane, uint32_t col, uint32_t row, uint64_t see,
+                                       uint16_t* dst) {
+  constexpr int CH = D / 8, R = 64 / CH;   // rows of an instruction
+  const int n = min(KEYS, keys - j0);
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t*>(base + j0 * sN), 0, max(min(KEYS, len - j0) - 1, 0) * rowb + 2 * D,
-      0x00020000);
-  const int i = u * 64 + lane, r = i / CH;
-  uint32_t at = r * rowb + 16u * ((i % CH) ^ swz<D>(r));
-  if constexpr (HIDE) at = see >> r & 1 ? at : 0x80000000u;
+      const_cast<char*>(reinterpret_cast<const char*>(base) + static_cast<int64_t>(j0) * rowb), 0,
+      n > 0 ? (n - 1) * rowb + 2 * D : 0, 0x00020000);
+  // Row u R + lane / CH, whose swizzle is its parts' exclusive or.
+  uint32_t at = (col ^ (16u * swz<D>(u * R))) + row + u * R * rowb;
+  if constexpr (HIDE) at = static_cast<uint32_t>(see >> (u * R)) >> (lane / CH) & 1 ? at : 0x80000000u;
   gather16_to_lds(rs, at, dst + u * 64 * 8);
 }
 
-// One wave's 32 rows against tiles of keys.  KEYS: of a tile, 32 or 64.
-template <int D, int KEYS>
+// x, not known to be the same as before: what follows from it is computed where it is used.
+// Held over the walk, the operands' addresses would not fit the registers.
+__device__ __forceinline__ uint32_t fresh(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// One wave's 32 rows against 32 keys at a time.
+template <int D>
 struct Wave {
-  static constexpr int DS = D / 16, DB = D / 32, RB = 2 * D, HF = KEYS / 32;
+  static constexpr int DS = D / 16, DB = D / 32, RB = 2 * D;
   bf16x8 qf[DS];
   f32x16 oacc[DB];
   float m_run, l_run;
-  uint32_t koff[DS], voff[DB][2];
+  uint32_t kat, vat;   // where the lane's operands lie: of K's first values, of V's first keys
   int g, ln;
 
-  __device__ __forceinline__ void start(int lane) {
-    g = lane >> 5, ln = lane & 31;
+  __device__ __forceinline__ void clear() {
     m_run = kUnseen;
     l_run = 0.0f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db] = f32x16{};
-#pragma unroll
-    for (int s = 0; s < DS; ++s) koff[s] = ln * RB + 16 * ((2 * s + g) ^ swz<D>(ln));
+  }
+  __device__ __forceinline__ void start(int lane) {
+    g = lane >> 5, ln = lane & 31;
+    clear();
+    kat = ln * RB + 16 * (g ^ swz<D>(ln));
     const int j16 = lane & 15, tq = j16 >> 2, tp = j16 & 3, vhalf = (lane >> 4) & 1;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {
-        const int d = 32 * db + 16 * vhalf + 4 * tp;
-        const int k0 = 4 * g + tq + 8 * hi;
-        voff[db][hi] = k0 * RB + 16 * ((d >> 3) ^ swz<D>(k0)) + 8 * ((d >> 2) & 1);
-      }
+    const int k0 = 4 * g + tq;
+    vat = k0 * RB + 16 * ((2 * vhalf + (tp >> 1)) ^ swz<D>(k0)) + 8 * (tp & 1);
   }
   __device__ __forceinline__ void load(const uint16_t* row, bool have) {
 #pragma unroll
@@ -155,90 +186,106 @@ struct Wave {
       qf[s] = __builtin_bit_cast(bf16x8, t);
     }
   }
-  __device__ __forceinline__ void score(f32x16 (&s)[HF], const uint16_t* k) {
-    const char* kb = reinterpret_cast<const char*>(k);
-#pragma unroll
-    for (int hf = 0; hf < HF; ++hf) {
-      s[hf] = f32x16{};
-#pragma unroll
-      for (int i = 0; i < DS; ++i)
-        s[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            __builtin_bit_cast(bf16x8,
-                               *reinterpret_cast<const u32x4*>(kb + hf * 32 * RB + koff[i])),
-            qf[i], s[hf], 0, 0, 0);
-    }
+  // Values 16 i .. + 15 of K (its chunk 2 i + g, swizzled).
+  __device__ __forceinline__ i16x8 kread(int i, const uint16_t* k, uint32_t at) {
+    return *reinterpret_cast<const i16x8*>(reinterpret_cast<const char*>(k) + (at ^ (32 * i)));
   }
-  __device__ __forceinline__ void hide(f32x16 (&s)[HF], uint64_t see) {
+  // Operands are read kAhead instructions ahead of their use, in a fixed order: the
+  // compiler would read all of them first, which the registers have no room for.
+  static constexpr int kAhead = 3;
+  __device__ __forceinline__ void score(f32x16& s, const uint16_t* k) {
+    const uint32_t at = kat;
+    i16x8 ring[kAhead];
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf) {
-      const uint32_t bits = static_cast<uint32_t>(see >> (32 * hf)) >> (4 * g);
+    for (int i = 0; i < kAhead; ++i) ring[i] = kread(i, k, at);
+    s = f32x16{};
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[hf][e] = bits >> (8 * (e / 4) + e % 4) & 1u ? s[hf][e] : kNegInf;
+    for (int i = 0; i < DS; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ring[i % kAhead]), qf[i],
+                                                  s, 0, 0, 0);
+      if (i + kAhead < DS) ring[i % kAhead] = kread(i + kAhead, k, at);
     }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  __device__ __forceinline__ void hide(f32x16& s, uint32_t see) {
+    const uint32_t bits = see >> (4 * g);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = bits >> (8 * (e / 4) + e % 4) & 1u ? s[e] : kNegInf;
+  }
+  static __device__ __forceinline__ float largest(const f32x16& s) {
+    float top = kNegInf;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[e]);
+    return top;
+  }
+  // The sums times alpha.  In place by force: of products of its own on a rare branch the
+  // compiler makes a second set of registers for O, and copies one to the other on the
+  // common way.  It does not see what the instructions read and write: they wait for the
+  // matrix instructions before them, and those after them wait for them, by themselves
+  // (a 32x32x16 product's result can be read after 18 cycles).
+  __device__ __forceinline__ void rescale(float alpha) {
+    l_run *= alpha;
+    asm volatile("s_nop 15\n\ts_nop 15");
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float x = oacc[db][e];
+        asm volatile("v_mul_f32_e32 %0, %1, %0" : "+v"(x) : "v"(alpha));
+        oacc[db][e] = x;
+      }
+    asm volatile("s_nop 7");
   }
   // The weights against the reference as it is; a row whose sum is past 256 on one of its
-  // lanes (one that had none among them) moves its reference to its maximum first.
-  __device__ __forceinline__ void weigh(const f32x16 (&s)[HF], float scale_log2,
-                                        bf16x8 (&pb)[2 * HF]) {
-    float p[HF][16], sum;
+  // lanes moves its reference first.
+  __device__ __forceinline__ void weigh(const f32x16& s, float scale_log2, bf16x8 (&pb)[2]) {
+    float sum;
     auto weights = [&]() __attribute__((always_inline)) {
-      float part[2 * HF];
-#pragma unroll
-      for (int hf = 0; hf < HF; ++hf) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          p[hf][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[hf][e], scale_log2, -m_run));
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float* y = p[hf] + 8 * x;
-          part[2 * hf + x] = ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
-        }
-      }
-      sum = part[0] + part[1];
-      if constexpr (HF == 2) sum += part[2] + part[3];
-    };
-    weights();
-    if (__any(sum > 256.0f)) {
-      float top = kNegInf;
-#pragma unroll
-      for (int hf = 0; hf < HF; ++hf)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[hf][e]);
-      const bool up = wave_max_xor32(sum) > 256.0f;   // no row depends on its neighbours
-      const float m_new = up ? fmaxf(m_run, wave_max_xor32(top) * scale_log2) : m_run;
-      const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
-      m_run = m_new;
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
-      weights();
-    }
-    l_run += sum;
-#pragma unroll
-    for (int hf = 0; hf < HF; ++hf)
+      float part[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         f32x8 y;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = p[hf][8 * x + e];
-        pb[2 * hf + x] = __builtin_convertvector(y, bf16x8);
+        for (int e = 0; e < 8; ++e)
+          y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * x + e], scale_log2, -m_run));
+        part[x] = ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+        pb[x] = __builtin_convertvector(y, bf16x8);
       }
+      sum = part[0] + part[1];
+    };
+    weights();
+    if (__any(sum > 256.0f)) {
+      const bool up = wave_max_xor32(sum) > 256.0f;   // no row depends on its neighbours
+      const float m_new = up ? fmaxf(m_run, wave_max_xor32(largest(s)) * scale_log2) : m_run;
+      rescale(__builtin_amdgcn_exp2f(m_run - m_new));
+      m_run = m_new;
+      weights();
+    }
+    l_run += sum;
   }
-  __device__ __forceinline__ void add(const bf16x8 (&pb)[2 * HF], const uint16_t* v) {
-    const char* vb = reinterpret_cast<const char*>(v);
+  // Values 32 db .. + 31 of keys 16 ks .. + 15 of V, transposed.
+  __device__ __forceinline__ i16x8 vread(int ks, int db, const uint16_t* v, uint32_t at) {
+    const char* vb = reinterpret_cast<const char*>(v) + 16 * ks * RB;  // the swizzle repeats
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(i16x4, vb + (at ^ (64 * db))));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        LDS_PTR(i16x4, vb + (at ^ (64 * db + 32)) + 8 * RB));   // eight keys on
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  __device__ __forceinline__ void add(const bf16x8 (&pb)[2], const uint16_t* v) {
+    const uint32_t at = vat;
+    constexpr int N = 2 * DB;
+    i16x8 ring[kAhead];
 #pragma unroll
-    for (int ks = 0; ks < 2 * HF; ++ks)
+    for (int i = 0; i < kAhead; ++i) ring[i] = vread(i / DB, i % DB, v, at);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        // The swizzle repeats every 16 rows.
-        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            LDS_PTR(i16x4, vb + voff[db][0] + 16 * ks * RB));
-        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            LDS_PTR(i16x4, vb + voff[db][1] + 16 * ks * RB));
-        const i16x8 x = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), pb[ks],
-                                                           oacc[db], 0, 0, 0);
-      }
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_barrier(0);
+      oacc[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8, ring[i % kAhead]), pb[i / DB], oacc[i % DB], 0, 0, 0);
+      if (i + kAhead < N) ring[i % kAhead] = vread((i + kAhead) / DB, (i + kAhead) % DB, v, at);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 };
 
@@ -250,78 +297,108 @@ __device__ __forceinline__ void put_part(const CrossParams& a, const Item& s, in
 }
 template <int D>
 __device__ __forceinline__ float* part_ml(const CrossParams& a, int64_t index, int tile_rows, int r) {
-  return a.part + a.items * tile_rows * D + (index * tile_rows + r) * 2;
+  return a.part + static_cast<int64_t>(a.items) * tile_rows * D + (index * tile_rows + r) * 2;
 }
 
-template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_cross_many(
+// Many rows.  Tiles of 32 keys in three stages, one barrier each: a tile is fetched while
+// the two before it are worked on.
+template <int D, bool MASK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 3 : 4))) void k_cross_many(
     const CrossParams a) {
-  constexpr int KEYS = 64, U = KEYS * (D / 8) / 256;
-  using W = Wave<D, KEYS>;
+  constexpr int KEYS = 32, U = KEYS * (D / 8) / 256;   // direct loads per wave and matrix
+  using W = Wave<D>;
+  constexpr int DB = W::DB;
   __shared__ __align__(16) uint16_t k_s0[KEYS * D];
   __shared__ __align__(16) uint16_t k_s1[KEYS * D];
+  __shared__ __align__(16) uint16_t k_s2[KEYS * D];
   __shared__ __align__(16) uint16_t v_s0[KEYS * D];
   __shared__ __align__(16) uint16_t v_s1[KEYS * D];
+  __shared__ __align__(16) uint16_t v_s2[KEYS * D];
   Item s;
-  if (!find_item(a, kCrossRows, s)) return;
+  const uint32_t i = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+  if (blockIdx.x >> 3 >= a.per_xcd || i >= a.items) return;
+  const bool some = decode(a, kCrossRows, i, s);
+  clear_rows<D>(a, s, kCrossRows);
+  if (!some) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint16_t* kh = a.k + s.b * a.k_sB + s.hk * a.k_sH;
-  const uint16_t* vh = a.v + s.b * a.v_sB + s.hk * a.v_sH;
-  const int first = s.c * a.chunk, last = min(s.len, first + a.chunk);
-  const int ntiles = (last - first + KEYS - 1) / KEYS;
+  const int first = s.c * a.chunk, keys = min(s.len - first, a.chunk);
+  const uint16_t* kh = a.k + s.b * a.k_sB + s.hk * a.k_sH + first * a.k_sN;
+  const uint16_t* vh = a.v + s.b * a.v_sB + s.hk * a.v_sH + first * a.v_sN;
+  const uint32_t k_rowb = static_cast<uint32_t>(a.k_sN) * 2u;
+  const uint32_t v_rowb = static_cast<uint32_t>(a.v_sN) * 2u;
+  const uint32_t col = gather_col<D>(lane), k_row = lane / (D / 8) * k_rowb,
+                 v_row = lane / (D / 8) * v_rowb;
+  const uint8_t* mask = MASK ? a.mask + s.b * a.mask_sB + first : nullptr;
+  const int ntiles = (keys + KEYS - 1) / KEYS;
+
+  auto fetch = [&](int t, uint32_t see, uint16_t* k, uint16_t* v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      gather<D, KEYS, false>(kh, k_rowb, t * KEYS, keys, wave * U + u, lane, col, k_row, see, k);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      gather<D, KEYS, MASK>(vh, v_rowb, t * KEYS, keys, wave * U + u, lane, col, v_row, see, v);
+  };
+  // Visible keys of a tile; with a mask from its bytes, fetched a tile earlier.
+  auto key_byte = [&](int t) __attribute__((always_inline)) {
+    const int j = t * KEYS + (lane & 31);
+    return MASK && j < keys ? mask[j] : 0;
+  };
+  auto visible = [&](int t, int byte) __attribute__((always_inline)) {
+    if constexpr (MASK) return static_cast<uint32_t>(__ballot(byte != 0));
+    const int n = keys - t * KEYS;
+    return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+  };
   const int row = s.rt * kCrossRows + 32 * wave + (lane & 31);
   const bool have = row < s.rows;
   W w;
   w.start(lane);
-  w.load(q_row(a, s, have ? row : 0), have);
-
-  auto fetch = [&](int t, uint64_t see, uint16_t* k, uint16_t* v) __attribute__((always_inline)) {
-    const int j0 = first + t * KEYS;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      gather<D, KEYS, false>(kh, a.k_sN, j0, s.len, wave * U + u, lane, see, k);
-    if (a.mask) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        gather<D, KEYS, true>(vh, a.v_sN, j0, s.len, wave * U + u, lane, see, v);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        gather<D, KEYS, false>(vh, a.v_sN, j0, s.len, wave * U + u, lane, see, v);
-    }
-  };
-  uint64_t see = 0, see_next = 0;
+  // Visible keys of the tile that is worked on and the two after it, the last as it came.
+  uint32_t see = 0, see1 = 0;
+  int byte2 = 0;
   if (ntiles > 0) {
-    see = visible<KEYS>(a, s, first, lane);
+    const int b0 = key_byte(0), b1 = key_byte(1);
+    byte2 = key_byte(2);
+    see = visible(0, b0), see1 = visible(1, b1);
     fetch(0, see, k_s0, v_s0);
+    w.load(q_row(a, s, have ? row : 0), have);
+    if (ntiles > 1) fetch(1, see1, k_s1, v_s1);
   }
-  auto turn = [&](int t, const uint16_t* k, const uint16_t* v, uint16_t* k1, uint16_t* v1)
+  bool settled = false;
+  auto turn = [&](int t, const uint16_t* k, const uint16_t* v, uint16_t* k2, uint16_t* v2)
                   __attribute__((always_inline)) {
-    if (t + 1 < ntiles) see_next = visible<KEYS>(a, s, first + (t + 1) * KEYS, lane);
-    wait_all();
+    // Tile t is there, and every wave is through with the one whose stage is filled again.
+    if (t + 1 < ntiles) wait_vmcnt<2 * U>();
+    else wait_all();
     __builtin_amdgcn_s_barrier();
-    if (t + 1 < ntiles) fetch(t + 1, see_next, k1, v1);
-    f32x16 x[2];
-    bf16x8 pb[4];
+    const uint32_t see2 = visible(t + 2, byte2);
+    byte2 = key_byte(t + 3);
+    if (t + 2 < ntiles) fetch(t + 2, see2, k2, v2);
+    f32x16 x;
+    bf16x8 pb[2];
     w.score(x, k);
-    if (see != ~uint64_t(0)) w.hide(x, see);
+    if (see != ~0u) w.hide(x, see);
+    if (!settled) {   // the first keys of which one is visible, the same for all rows
+      w.m_run = fmaxf(w.m_run, wave_max_xor32(W::largest(x)) * a.scale_log2);
+      settled = see != 0;
+    }
     w.weigh(x, a.scale_log2, pb);
     w.add(pb, v);
-    see = see_next;
+    see = see1, see1 = see2;
   };
-  for (int t = 0; t < ntiles; t += 2) {
-    turn(t, k_s0, v_s0, k_s1, v_s1);
+  for (int t = 0; t < ntiles; t += 3) {
+    turn(t, k_s0, v_s0, k_s2, v_s2);
     if (t + 1 < ntiles) turn(t + 1, k_s1, v_s1, k_s0, v_s0);
+    if (t + 2 < ntiles) turn(t + 2, k_s2, v_s2, k_s1, v_s1);
   }
 
-  float l = w.l_run;
-  l += __shfl_xor(l, 32);
-  if (!have) return;
+  const float l = w.l_run + __shfl_xor(w.l_run, 32);
   if (s.count > 1) {
+    if (!have) return;
     const int r = 32 * wave + w.ln;
 #pragma unroll
-    for (int db = 0; db < W::DB; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int vq = 0; vq < 4; ++vq) {
         f32x4 y;
@@ -336,17 +413,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     return;
   }
   const float inv = l > 0.0f ? 1.0f / l : l;   // no key: 0; NaN stays
-  if (w.g == 0) put_lse(a, s.b, s.hk, row, w.m_run, l);
-  uint16_t* orow = o_row(a, s.b, s.hk, row);
+  if (have && w.g == 0) put_lse(a, s.b, s.hk, row, w.m_run, l);
+  uint16_t* orow = o_row(a, s.b, s.hk, have ? row : 0);
 #pragma unroll
-  for (int db = 0; db < W::DB; ++db)
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int vq = 0; vq < 4; ++vq) {
-      f32x4 y;
+    for (int x = 0; x < 2; ++x) {
+      // A lane of a row holds four values of every eight: after a swap, eight of every
+      // sixteen.
+      u32x2 y[2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = w.oacc[db][4 * vq + e] * inv;
-      *reinterpret_cast<bf16x4*>(orow + 32 * db + 8 * vq + 4 * w.g) =
-          __builtin_convertvector(y, bf16x4);
+      for (int vq = 0; vq < 2; ++vq) {
+        f32x4 z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = w.oacc[db][8 * x + 4 * vq + e] * inv;
+        y[vq] = __builtin_bit_cast(u32x2, __builtin_convertvector(z, bf16x4));
+      }
+      const auto lo = __builtin_amdgcn_permlane32_swap(y[0][0], y[1][0], false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(y[0][1], y[1][1], false, false);
+      if (have)
+        *reinterpret_cast<u32x4*>(orow + 32 * db + 16 * x + 8 * w.g) =
+            u32x4{lo[0], hi[0], lo[1], hi[1]};
     }
 }
 
@@ -354,20 +441,29 @@ template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_cross_few(
     const CrossParams a) {
   constexpr int KEYS = 32, U = KEYS * (D / 8) / 64, ROWS = 32;
-  using W = Wave<D, KEYS>;
+  using W = Wave<D>;
   __shared__ __align__(16) uint16_t k_s0[4][KEYS * D];
   __shared__ __align__(16) uint16_t k_s1[4][KEYS * D];
   __shared__ __align__(16) uint16_t v_s0[4][KEYS * D];
   __shared__ __align__(16) uint16_t v_s1[4][KEYS * D];
   __shared__ float s_m[4][ROWS], s_l[4][ROWS];
   Item s;
-  if (!find_item(a, ROWS, s)) return;
+  const uint32_t i = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+  if (blockIdx.x >> 3 >= a.per_xcd || i >= a.items) return;
+  const bool some = decode(a, ROWS, i, s);
+  clear_rows<D>(a, s, ROWS);
+  if (!some) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint16_t* kh = a.k + s.b * a.k_sB + s.hk * a.k_sH;
-  const uint16_t* vh = a.v + s.b * a.v_sB + s.hk * a.v_sH;
-  const int first = s.c * a.chunk, last = min(s.len, first + a.chunk);
-  const int ntiles = (last - first + KEYS - 1) / KEYS;
+  const int first = s.c * a.chunk, keys = min(s.len - first, a.chunk);
+  const uint16_t* kh = a.k + s.b * a.k_sB + s.hk * a.k_sH + first * a.k_sN;
+  const uint16_t* vh = a.v + s.b * a.v_sB + s.hk * a.v_sH + first * a.v_sN;
+  const uint32_t k_rowb = static_cast<uint32_t>(a.k_sN) * 2u;
+  const uint32_t v_rowb = static_cast<uint32_t>(a.v_sN) * 2u;
+  const uint32_t col = gather_col<D>(lane), k_row = lane / (D / 8) * k_rowb,
+                 v_row = lane / (D / 8) * v_rowb;
+  const uint8_t* mask = a.mask ? a.mask + s.b * a.mask_sB + first : nullptr;
+  const int ntiles = (keys + KEYS - 1) / KEYS;
   const int row = s.rt * ROWS + (lane & 31);
   const bool have = row < s.rows;
   W w;
@@ -375,11 +471,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   w.load(q_row(a, s, have ? row : 0), have);
 
   auto fetch = [&](int t, uint64_t see, uint16_t* k, uint16_t* v) __attribute__((always_inline)) {
-    const int j0 = first + t * KEYS;
+    const int j0 = t * KEYS;
 #pragma unroll
-    for (int u = 0; u < U; ++u) gather<D, KEYS, false>(kh, a.k_sN, j0, s.len, u, lane, see, k);
+    for (int u = 0; u < U; ++u) gather<D, KEYS, false>(kh, k_rowb, j0, keys, u, lane, col, k_row, see, k);
 #pragma unroll
-    for (int u = 0; u < U; ++u) gather<D, KEYS, true>(vh, a.v_sN, j0, s.len, u, lane, see, v);
+    for (int u = 0; u < U; ++u) gather<D, KEYS, true>(vh, v_rowb, j0, keys, u, lane, col, v_row, see, v);
   };
   // A tile is worked on while the wave's next is fetched; past the last one the fetch
   // goes to the last again (into a buffer that nothing reads).
@@ -387,23 +483,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   int t = wave;
   uint64_t see = 0, see1 = 0;
   if (t < ntiles) {
-    see = visible<KEYS>(a, s, first + t * KEYS, lane);
+    see = visible<KEYS>(mask, keys, t * KEYS, lane);
     fetch(t, see, k_s0[wave], v_s0[wave]);
-    see1 = visible<KEYS>(a, s, first + tile(t + 4) * KEYS, lane);
+    see1 = visible<KEYS>(mask, keys, tile(t + 4) * KEYS, lane);
   }
   auto turn = [&](const uint16_t* k, const uint16_t* v, uint16_t* k1, uint16_t* v1)
                   __attribute__((always_inline)) {
     fetch(tile(t + 4), see1, k1, v1);
     wait_vmcnt<2 * U>();
-    f32x16 x[1];
+    f32x16 x;
     bf16x8 pb[2];
     w.score(x, k);
-    if (see != 0xFFFFFFFFu) w.hide(x, see);
+    if (see != 0xFFFFFFFFu) w.hide(x, static_cast<uint32_t>(see));
     w.weigh(x, a.scale_log2, pb);
     w.add(pb, v);
     see = see1;
     t += 4;
-    see1 = visible<KEYS>(a, s, first + tile(t + 4) * KEYS, lane);
+    see1 = visible<KEYS>(mask, keys, tile(t + 4) * KEYS, lane);
   };
   while (t < ntiles) {
     turn(k_s0[wave], v_s0[wave], k_s1[wave], v_s1[wave]);
@@ -531,7 +627,7 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
   const int64_t units = B * Hkv * d.tiles;
   // Workgroups that run at a time, and the fewest keys that pay for a chunk.
   const int64_t slots = d.few && D == 128 ? 256 : 512;
-  const int64_t least = 256;
+  const int64_t least = 512;
   int64_t chunks = std::min((Nk + least - 1) / least, std::max<int64_t>(1, 2 * slots / units));
   d.chunk = static_cast<int32_t>(((Nk + chunks - 1) / chunks + 127) / 128 * 128);
   d.chunks = static_cast<int32_t>((Nk + d.chunk - 1) / d.chunk);
@@ -567,21 +663,27 @@ hipError_t launch_cross_attn(const CrossArgs& x, hipStream_t stream) {
   a.lens = x.lens;
   a.mask = x.mask, a.mask_sB = x.mask_sB;
   a.n_q = x.n_q;
+  a.clear = x.clear && x.n_q;
   a.part = static_cast<float*>(x.workspace);
   a.Hkv = static_cast<int32_t>(x.k.H);
   a.group = static_cast<int32_t>(x.q.H / x.k.H);
   a.Nq = static_cast<int32_t>(x.q.N), a.Nk = static_cast<int32_t>(x.k.N);
   a.row_tiles = d.tiles, a.chunks = d.chunks, a.chunk = d.chunk;
-  a.items = d.items;
+  a.items = static_cast<uint32_t>(d.items);
   const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(x.q.D));
   a.scale_log2 = std::max(scale * 1.4426950408889634f, 0x1p-126f);   // -inf * 0 is no mask
-  a.run = static_cast<int32_t>(std::min<int64_t>(64, std::max<int64_t>(1, a.items / 32)));
-  const int64_t rounds = (a.items + 8 * a.run - 1) / (8 * a.run);
-  const dim3 grid(static_cast<unsigned>(rounds * 8 * a.run));
+  // Heads side by side whose keys and values fit half of an XCD's 4 MB of L2.
+  a.near_heads = 1;
+  for (int32_t n = 2; n <= a.Hkv; ++n)
+    if (a.Hkv % n == 0 && n * x.k.N * x.k.D * 4 <= (2 << 20)) a.near_heads = n;
+  // XCD x (workgroups x, x + 8, ..) takes items [x per_xcd, (x + 1) per_xcd).
+  a.per_xcd = (a.items + 7) / 8;
+  const dim3 grid(8 * a.per_xcd);
   auto pick = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     if (d.few) hipLaunchKernelGGL(k_cross_few<D>, grid, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL(k_cross_many<D>, grid, dim3(256), 0, stream, a);
+    else if (a.mask) hipLaunchKernelGGL((k_cross_many<D, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((k_cross_many<D, false>), grid, dim3(256), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.chunks == 1) return e;
     const int64_t total = x.q.B * x.q.H * x.q.N;

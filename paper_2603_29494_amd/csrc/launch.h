@@ -179,14 +179,19 @@ struct CacheMassArgs {
   const float* mass;   // [B, H, M], or NULL
   float* out;          // [B, H, M]
   int64_t M;
+  bool clear;          // entries past a sequence's tokens become 0
+  void* workspace;
 };
+size_t cache_mass_workspace_bytes(const CacheAttnShape& s);
 hipError_t launch_cache_mass(const CacheMassArgs& a, hipStream_t stream);
+size_t cache_keep_workspace_bytes(const CacheArgs& c, int64_t B, int64_t M);
 hipError_t launch_cache_keep(const CacheArgs& c, int64_t B, const float* mass, int64_t M,
                              int64_t budget, int64_t sinks, int64_t recent, int32_t* idx,
-                             int32_t* kept, hipStream_t stream);
+                             int32_t* kept, void* workspace, hipStream_t stream);
 hipError_t launch_cache_gather(const CacheArgs& c, const CacheArgs& to, int64_t B,
                                const int32_t* idx, const int32_t* kept, int64_t budget,
-                               const float* mass, int64_t M, float* mass_out, hipStream_t stream);
+                               const float* mass, int64_t M, float* mass_out, bool clear,
+                               hipStream_t stream);
 
 // Attention over an encoder's states.  How the work is dealt out, and so the
 // workspace, follows from the shape.
@@ -199,6 +204,7 @@ struct CrossArgs {
   const uint8_t* mask;
   int64_t mask_sB;
   const int32_t* n_q;
+  bool clear;      // rows past n_q become 0
   float scale;
   void* workspace;
 };
@@ -213,7 +219,7 @@ constexpr int32_t kRopeMaxPairs = 64;
 struct RopeArgs {
   Tensor4 q, k, qo, ko;
   int32_t rot;
-  bool half, transposed;
+  bool half, transposed, clear;   // clear: rows past n_new become 0
   double factor;
   const double* freq;    // host, [rot / 2], radians per position
   const int32_t* axis;   // host, [rot / 2], or NULL: axis 0

@@ -40,7 +40,7 @@ struct RopeParams {
   int32_t Hq, heads;  // q's heads, and k's with them
   int32_t token_log2; // a wave's rows are 1 << token_log2 tokens by the rest in heads
   int32_t split;      // waves that share a run's heads
-  int32_t rot, in_place;
+  int32_t rot, in_place, clear;
   float factor;       // negated sines for the transposed turn
   float sine;
   double turns[kRopeMaxPairs];
@@ -94,7 +94,8 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
   const int tokens = 1 << a.token_log2, heads = ROWS >> a.token_log2;
   const int64_t n = (unit % a.runs) * tokens + (r & (tokens - 1));
   const int64_t rows = a.n_new ? min(max(static_cast<int64_t>(a.n_new[b]), int64_t(0)), a.N) : a.N;
-  if (n >= rows) return;
+  const bool gone = n >= rows;
+  if (n >= a.N || (gone && !a.clear)) return;
 
   // Chunks (of eight values) that this thread holds.
   const int half = a.rot >> 1;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
     if (j >= pairs8) c0 = 2 * j, c1 = 2 * j + 1;   // behind the turned values
   }
   const bool turned0 = 8 * c0 < a.rot, turned1 = 8 * c1 < a.rot;
-  const bool store0 = turned0 || !a.in_place, store1 = turned1 || !a.in_place;
+  const bool store0 = turned0 || gone || !a.in_place, store1 = turned1 || gone || !a.in_place;
   // Values of chunk 0 or 1 belong to pair index:
   Turn t[PAIRS];
   if (turned0 || turned1) {
@@ -185,6 +186,7 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
       }
       __builtin_amdgcn_wave_barrier();
     }
+    if (gone) x0 = x1 = u32x4{0, 0, 0, 0};
     if (store0) reinterpret_cast<u32x4*>(dst)[c0] = x0;
     if (store1) reinterpret_cast<u32x4*>(dst)[c1] = x1;
   }
@@ -212,6 +214,7 @@ hipError_t launch_rope(const RopeArgs& x, hipStream_t stream) {
   a.rot = x.rot;
   // Values behind the turned ones stay where they are if both tensors do.
   a.in_place = x.q.ptr == x.qo.ptr && (!with_k || x.k.ptr == x.ko.ptr);
+  a.clear = x.clear;
   a.factor = static_cast<float>(x.factor);
   a.sine = x.transposed ? -a.factor : a.factor;
   for (int i = 0; i < x.rot / 2; ++i) {

@@ -397,6 +397,8 @@ bool same_shape(const vecattn_tdesc* a, const vecattn_tdesc* b) {
   return a->B == b->B && a->H == b->H && a->N == b->N && a->D == b->D;
 }
 
+bool flags_ok(int32_t flags) { return flags == 0 || flags == VECATTN_CLEAR_PADDING; }
+
 // Strides of dimensions of size 1 address nothing.
 bool same_strides(const vecattn_tdesc* a, const vecattn_tdesc* b) {
   return (a->B == 1 || a->sB == b->sB) && (a->H == 1 || a->sH == b->sH) &&
@@ -464,6 +466,14 @@ vecattn_status check_cache_attn(const vecattn_tdesc* qd, const vecattn_cache* c,
   *s = vecattn::CacheAttnShape{qd->B, qd->H, c->H, qd->N, qd->D, cols, c->page,
                                std::min(window, kMaxN), std::min(sinks, kMaxN)};
   return vecattn::cache_attn_grid_ok(*s) ? VECATTN_OK : VECATTN_ERR_UNSUPPORTED;
+}
+
+vecattn_status check_keep(const vecattn_cache* c, bool with_data, int64_t cols, int64_t B,
+                          int64_t M) {
+  const vecattn_status st = check_cache(c, with_data);
+  if (st != VECATTN_OK) return st;
+  if (!cols_ok(cols, c->page) || B < 1 || M < 1 || M > kMaxN) return VECATTN_ERR_INVALID_ARG;
+  return B > kMaxGridYZ ? VECATTN_ERR_UNSUPPORTED : VECATTN_OK;
 }
 
 vecattn::CacheArgs to_cache(const vecattn_cache* c, const int32_t* table, int64_t cols,
@@ -643,39 +653,65 @@ vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 
+vecattn_status vecattn_cache_mass_workspace_size(const vecattn_tdesc* qd,
+                                                 const vecattn_cache* cache, size_t* bytes) {
+  if (!bytes) return VECATTN_ERR_INVALID_ARG;
+  vecattn::CacheAttnShape s;
+  const vecattn_status st = check_cache_attn(qd, cache, false, 1, 1, 0, &s);
+  if (st != VECATTN_OK) return st;
+  *bytes = vecattn::cache_mass_workspace_bytes(s);
+  return VECATTN_OK;
+}
+
 vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const float* lse,
                                   const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                   const int32_t* lens, const int32_t* n_new, int64_t window,
                                   int64_t sinks, float scale, float decay, const float* mass,
-                                  float* out, int64_t M, void* stream) {
+                                  float* out, int64_t M, int32_t flags, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
   vecattn_status st;
   if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
   vecattn::CacheAttnShape s;
   if ((st = check_cache_attn(qd, cache, true, cols, window, sinks, &s)) != VECATTN_OK) return st;
   if (!lse || !table || !lens || !out || M < 1 || M > kMaxN) return VECATTN_ERR_INVALID_ARG;
-  if (!std::isfinite(scale) || scale < 0.0f || !std::isfinite(decay) || decay < 0.0f)
+  if (!std::isfinite(scale) || scale < 0.0f || !std::isfinite(decay) || decay < 0.0f ||
+      !flags_ok(flags))
     return VECATTN_ERR_INVALID_ARG;
+  const size_t need = vecattn::cache_mass_workspace_bytes(s);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return VECATTN_ERR_CAPACITY;
+  if (workspace && !aligned16(workspace)) return VECATTN_ERR_INVALID_ARG;
   vecattn::CacheMassArgs a{to_tensor(q, qd), lse, to_cache(cache, table, cols, lens), n_new,
-                           s.window, s.sinks, scale, decay, mass, out, M};
+                           s.window, s.sinks, scale, decay, mass, out, M, flags != 0, workspace};
   hipError_t e = vecattn::launch_cache_mass(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_keep_workspace_size(const vecattn_cache* cache, int64_t cols,
+                                                 int64_t B, int64_t M, size_t* bytes) {
+  if (!bytes) return VECATTN_ERR_INVALID_ARG;
+  const vecattn_status st = check_keep(cache, false, cols, B, M);
+  if (st != VECATTN_OK) return st;
+  *bytes = vecattn::cache_keep_workspace_bytes(to_cache(cache, nullptr, cols, nullptr), B, M);
+  return VECATTN_OK;
 }
 
 vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
                                   const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                   const int32_t* lens, int64_t budget, int64_t sinks,
-                                  int64_t recent, int32_t* idx, int32_t* kept, void* stream) {
-  const vecattn_status st = check_cache(cache, true);
+                                  int64_t recent, int32_t* idx, int32_t* kept, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  const vecattn_status st = check_keep(cache, true, cols, B, M);
   if (st != VECATTN_OK) return st;
-  if (!mass || !table || !lens || !idx || !kept || B < 1 || M < 1 || M > kMaxN)
+  if (!mass || !table || !lens || !idx || !kept) return VECATTN_ERR_INVALID_ARG;
+  if (budget < 1 || budget > kMaxN || sinks < 0 || recent < 0 || sinks > budget ||
+      recent > budget - sinks)
     return VECATTN_ERR_INVALID_ARG;
-  if (!cols_ok(cols, cache->page) || budget < 1 || budget > kMaxN || sinks < 0 || recent < 0 ||
-      sinks > budget || recent > budget - sinks)
-    return VECATTN_ERR_INVALID_ARG;
-  if (B > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
-  hipError_t e = vecattn::launch_cache_keep(to_cache(cache, table, cols, lens), B, mass, M, budget,
-                                            sinks, recent, idx, kept,
-                                            static_cast<hipStream_t>(stream));
+  const vecattn::CacheArgs c = to_cache(cache, table, cols, lens);
+  const size_t need = vecattn::cache_keep_workspace_bytes(c, B, M);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return VECATTN_ERR_CAPACITY;
+  if (workspace && !aligned16(workspace)) return VECATTN_ERR_INVALID_ARG;
+  hipError_t e = vecattn::launch_cache_keep(c, B, mass, M, budget, sinks, recent, idx, kept,
+                                            workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 
@@ -683,7 +719,7 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
                                     int64_t B, const int32_t* idx, const int32_t* kept,
                                     int64_t budget, const vecattn_cache* to,
                                     const int32_t* to_table, int64_t to_cols, const float* mass,
-                                    int64_t M, float* mass_out, void* stream) {
+                                    int64_t M, float* mass_out, int32_t flags, void* stream) {
   vecattn_status st;
   if ((st = check_cache(cache, true)) != VECATTN_OK) return st;
   if ((st = check_cache(to, true)) != VECATTN_OK) return st;
@@ -692,12 +728,13 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
   if (!table || !idx || !kept || !to_table || B < 1 || budget < 1 || budget > kMaxN)
     return VECATTN_ERR_INVALID_ARG;
   if (!cols_ok(cols, cache->page) || !cols_ok(to_cols, to->page)) return VECATTN_ERR_INVALID_ARG;
-  if ((mass == nullptr) != (mass_out == nullptr) || (mass && (M < 1 || M > kMaxN)))
+  if ((mass == nullptr) != (mass_out == nullptr) || (mass && (M < 1 || M > kMaxN)) ||
+      !flags_ok(flags))
     return VECATTN_ERR_INVALID_ARG;
   if (B > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
   hipError_t e = vecattn::launch_cache_gather(
       to_cache(cache, table, cols, nullptr), to_cache(to, to_table, to_cols, nullptr), B, idx, kept,
-      budget, mass, M, mass_out, static_cast<hipStream_t>(stream));
+      budget, mass, M, mass_out, flags != 0, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 
@@ -713,7 +750,7 @@ vecattn_status vecattn_cross_attn_workspace_size(const vecattn_tdesc* qd, const 
 vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const void* k,
                                   const vecattn_tdesc* kd, const void* v, const vecattn_tdesc* vd,
                                   const int32_t* lens, const uint8_t* mask, int64_t mask_sB,
-                                  const int32_t* n_q, float scale, void* o,
+                                  const int32_t* n_q, int32_t flags, float scale, void* o,
                                   const vecattn_tdesc* od, float* lse, void* workspace,
                                   size_t workspace_bytes, void* stream) {
   vecattn_status st;
@@ -723,7 +760,8 @@ vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const 
   if ((st = check_desc(o, od)) != VECATTN_OK) return st;
   if ((st = check_cross(qd, kd)) != VECATTN_OK) return st;
   if (!same_shape(vd, kd) || !same_shape(od, qd)) return VECATTN_ERR_INVALID_ARG;
-  if (mask_sB < 0 || !std::isfinite(scale) || scale < 0.0f) return VECATTN_ERR_INVALID_ARG;
+  if (mask_sB < 0 || !std::isfinite(scale) || scale < 0.0f || !flags_ok(flags))
+    return VECATTN_ERR_INVALID_ARG;
   // A tile's 64 rows are addressed with 32-bit byte offsets.
   if (kd->N > 1 && (kd->sN >= (int64_t(1) << 24) || vd->sN >= (int64_t(1) << 24)))
     return VECATTN_ERR_UNSUPPORTED;
@@ -731,7 +769,7 @@ vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const 
   if (need > 0 && (!workspace || workspace_bytes < need)) return VECATTN_ERR_CAPACITY;
   if (workspace && !aligned16(workspace)) return VECATTN_ERR_INVALID_ARG;
   vecattn::CrossArgs a{to_tensor(q, qd), to_tensor(k, kd), to_tensor(v, vd), o, od->sB, od->sH,
-                       od->sN, lse, lens, mask, mask_sB, n_q, scale, workspace};
+                       od->sN, lse, lens, mask, mask_sB, n_q, flags != 0, scale, workspace};
   hipError_t e = vecattn::launch_cross_attn(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
@@ -773,7 +811,7 @@ vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* 
   }
   if (!spec || spec->rot < 2 || spec->rot > qd->D || spec->rot % 2 != 0 || !spec->freq ||
       (spec->layout != VECATTN_ROPE_HALF && spec->layout != VECATTN_ROPE_INTERLEAVED) ||
-      spec->axes < 1 || spec->axes > 4 || (spec->transposed != 0 && spec->transposed != 1) ||
+      spec->axes < 1 || spec->axes > 4 || (spec->flags & ~(VECATTN_ROPE_TRANSPOSED | VECATTN_CLEAR_PADDING)) != 0 ||
       !std::isfinite(spec->factor))
     return VECATTN_ERR_INVALID_ARG;
   for (int32_t i = 0; i < spec->rot / 2; ++i) {
@@ -791,7 +829,8 @@ vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* 
                       with_k ? to_tensor(ko, kod) : Tensor4{},
                       spec->rot,
                       spec->layout == VECATTN_ROPE_HALF,
-                      spec->transposed != 0,
+                      (spec->flags & VECATTN_ROPE_TRANSPOSED) != 0,
+                      (spec->flags & VECATTN_CLEAR_PADDING) != 0,
                       spec->factor,
                       spec->freq,
                       spec->axis,

@@ -23,11 +23,11 @@ def cache(data=FAKE, pages=8, H=2, D=128, page=64, bits=4):
     return _lib.CacheDesc(data, pages, H, D, page, bits)
 
 
-def spec(rot=8, layout=0, axes=1, transposed=0, factor=1.0, freq=None, axis=None):
+def spec(rot=8, layout=0, axes=1, flags=0, factor=1.0, freq=None, axis=None):
     n = max(1, rot // 2)
     f = (ctypes.c_double * n)(*(freq or [1.0] * n))
     a = None if axis is None else (ctypes.c_int32 * n)(*axis)
-    s = _lib.RopeSpec(rot, layout, axes, transposed, factor, f, a)
+    s = _lib.RopeSpec(rot, layout, axes, flags, factor, f, a)
     s.keep = (f, a)
     return s
 
@@ -57,7 +57,7 @@ def test_rope_rejects_bad_arguments():
     assert rope(start=0, pos=FAKE, sA=-1) == INVALID and rope(start=0, pos=FAKE, sB=-1) == INVALID
     assert rope(start=-(1 << 30) - 1) == INVALID and rope(start=(1 << 30) + 1) == INVALID
     for bad in (dict(rot=0), dict(rot=7), dict(rot=130), dict(layout=2), dict(layout=-1),
-                dict(axes=0), dict(axes=5), dict(transposed=2), dict(factor=math.inf),
+                dict(axes=0), dict(axes=5), dict(flags=2), dict(flags=4), dict(factor=math.inf),
                 dict(factor=math.nan), dict(freq=[1.0, math.nan, 1.0, 1.0]),
                 dict(freq=[1.0, 1.0, 1.0, 1025.0]), dict(axis=[0, 0, 0, 1]),
                 dict(axis=[0, -1, 0, 0])):
@@ -135,31 +135,44 @@ def test_cache_mass_rejects_bad_arguments():
     lib = _lib.load()
 
     def mass(q=FAKE, qd=None, lse=FAKE, c=None, table=FAKE, cols=4, lens=FAKE, window=8, sinks=0,
-             scale=0.0, decay=-1.0, out=FAKE, M=256):
+             scale=0.0, decay=-1.0, out=FAKE, M=256, flags=0, ws=None,
+             nws=0):
         # decay = -1 is refused as well
         return lib.vecattn_cache_mass(q, REF(qd or desc(2, 4, 1, 128)), lse, REF(c or cache()), table,
                                       cols, lens, None, window, sinks, scale, decay, None, out, M,
-                                      None)
+                                      flags, ws, nws, None)
     assert mass() == INVALID
     for name in ("q", "lse", "table", "lens", "out"):
         assert mass(decay=1.0, **{name: None}) == INVALID, name
     assert mass(decay=math.nan) == INVALID and mass(decay=math.inf) == INVALID
     for bad in (dict(q=FAKE + 8), dict(window=0), dict(sinks=-1), dict(scale=-1.0), dict(M=0),
                 dict(scale=math.nan), dict(M=(1 << 30) + 1), dict(cols=0), dict(c=cache(data=None)),
+                dict(flags=1),
                 dict(c=cache(D=64)), dict(qd=desc(2, 3, 1, 128)), dict(c=cache(bits=2))):
         assert mass(decay=1.0, **bad) == INVALID, bad
     assert mass(decay=1.0, qd=desc(2, 4, 1, 80)) == UNSUPPORTED
     assert mass(decay=1.0, qd=desc(1, 4, 1 << 28, 128)) == UNSUPPORTED
+    # more than 16 rows need a workspace
+    n, many = ctypes.c_size_t(9), desc(2, 4, 9, 128)
+    assert lib.vecattn_cache_mass_workspace_size(REF(desc(2, 4, 8, 128)), REF(cache()), REF(n)) == OK
+    assert n.value == 0
+    assert lib.vecattn_cache_mass_workspace_size(REF(many), REF(cache()), REF(n)) == OK
+    assert n.value > 0
+    assert mass(decay=1.0, qd=many) == CAPACITY
+    assert mass(decay=1.0, qd=many, ws=FAKE, nws=n.value - 1) == CAPACITY
+    assert mass(decay=1.0, qd=many, ws=FAKE + 8, nws=n.value) == INVALID
+    assert lib.vecattn_cache_mass_workspace_size(REF(many), REF(cache()), None) == INVALID
+    assert lib.vecattn_cache_mass_workspace_size(REF(many), REF(cache(H=3)), REF(n)) == INVALID
 
 
 def test_cache_keep_and_gather_reject_bad_arguments():
     lib = _lib.load()
 
     def keep(mass=FAKE, M=256, B=2, c=None, table=FAKE, cols=4, lens=FAKE, budget=8, sinks=0,
-             recent=9, idx=FAKE, kept=FAKE):
+             recent=9, idx=FAKE, kept=FAKE, ws=None, nws=0):
         # recent = 9 is more than the budget
         return lib.vecattn_cache_keep(mass, M, B, REF(c or cache()), table, cols, lens, budget, sinks,
-                                      recent, idx, kept, None)
+                                      recent, idx, kept, ws, nws, None)
     assert keep() == INVALID
     for name in ("mass", "table", "lens", "idx", "kept"):
         assert keep(recent=0, **{name: None}) == INVALID, name
@@ -170,19 +183,32 @@ def test_cache_keep_and_gather_reject_bad_arguments():
         assert keep(**dict(dict(recent=0), **bad)) == INVALID, bad
     assert keep(recent=0, B=70000) == UNSUPPORTED
     assert keep(recent=0, c=cache(D=96)) == UNSUPPORTED
+    # more than 8192 tokens need a workspace
+    n = ctypes.c_size_t(9)
+    size = lib.vecattn_cache_keep_workspace_size
+    assert size(REF(cache()), 128, 2, 1 << 20, REF(n)) == OK and n.value == 0
+    assert size(REF(cache()), 129, 2, 1 << 20, REF(n)) == OK and n.value > 0
+    long = dict(recent=0, cols=129, M=1 << 20)
+    assert keep(**long) == CAPACITY and keep(ws=FAKE, nws=n.value - 1, **long) == CAPACITY
+    assert keep(ws=FAKE + 8, nws=n.value, **long) == INVALID
+    assert size(REF(cache()), 0, 2, 64, REF(n)) == INVALID
+    assert size(REF(cache()), 4, 0, 64, REF(n)) == INVALID
+    assert size(REF(cache()), 4, 2, 0, REF(n)) == INVALID
+    assert size(REF(cache()), 4, 2, 64, None) == INVALID
+    assert size(REF(cache()), 4, 70000, 64, REF(n)) == UNSUPPORTED
 
     def gather(c=None, table=FAKE, cols=4, B=2, idx=FAKE, kept=FAKE, budget=8, to=None,
-               to_table=FAKE, to_cols=0, mass=FAKE, M=256, mass_out=FAKE):
+               to_table=FAKE, to_cols=0, mass=FAKE, M=256, mass_out=FAKE, flags=0):
         # to_cols = 0 is refused as well
         return lib.vecattn_cache_gather(REF(c or cache()), table, cols, B, idx, kept, budget,
                                         REF(to or cache()), to_table, to_cols, mass, M, mass_out,
-                                        None)
+                                        flags, None)
     assert gather() == INVALID
     for name in ("table", "idx", "kept", "to_table", "mass", "mass_out"):
         assert gather(to_cols=4, **{name: None}) == INVALID, name
     for bad in (dict(cols=0), dict(B=0), dict(budget=0), dict(M=0), dict(to=cache(H=3)),
                 dict(to=cache(D=64)), dict(to=cache(bits=8)), dict(to=cache(data=None)),
-                dict(c=cache(data=FAKE + 4)), dict(to_cols=1 << 25)):
+                dict(c=cache(data=FAKE + 4)), dict(to_cols=1 << 25), dict(flags=2)):
         assert gather(**dict(dict(to_cols=4), **bad)) == INVALID, bad
     assert gather(to_cols=4, B=70000) == UNSUPPORTED
 
@@ -191,16 +217,16 @@ def test_cross_attn_rejects_bad_arguments():
     lib = _lib.load()
 
     def cross(q=FAKE, k=FAKE, v=FAKE, o=FAKE, qd=None, kd=None, vd=None, od=None, mask=None, sB=0,
-              scale=-1.0, ws=None, nws=0):
+              scale=-1.0, flags=0, ws=None, nws=0):
         # scale = -1 is refused as well
         qd, kd = qd or desc(1, 4, 64, 128), kd or desc(1, 2, 77, 128)
         return lib.vecattn_cross_attn(q, REF(qd), k, REF(kd), v, REF(vd or kd), None, mask, sB, None,
-                                      scale, o, REF(od or qd), None, ws, nws, None)
+                                      flags, scale, o, REF(od or qd), None, ws, nws, None)
     assert cross() == INVALID
     for name in "qkvo":
         assert cross(scale=0.0, **{name: None}) == INVALID
         assert cross(scale=0.0, **{name: FAKE + 8}) == INVALID
-    for bad in (dict(scale=math.nan), dict(sB=-1), dict(qd=desc(1, 3, 64, 128)),
+    for bad in (dict(scale=math.nan), dict(sB=-1), dict(flags=1), dict(qd=desc(1, 3, 64, 128)),
                 dict(kd=desc(2, 2, 77, 128)), dict(kd=desc(1, 2, 77, 64)),
                 dict(vd=desc(1, 2, 78, 128)), dict(od=desc(1, 4, 63, 128)), dict(ws=FAKE + 8, nws=64)):
         assert cross(**dict(dict(scale=0.0), **bad)) == INVALID, bad
