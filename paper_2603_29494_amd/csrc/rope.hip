@@ -9,10 +9,10 @@
 // swapped and signed by the quarter.  Products and their sum are fp32, rounded
 // to bf16 once.
 //
-// A wave takes a token and walks over its heads, q's and then k's, so that the angles
-// are computed once for all of them; where rows of a head lie beside each other
-// (head-major tensors) its rows are consecutive tokens of one head instead.  A
-// thread holds 32 bytes of a row: 16-byte chunks c and c + half of the turned values,
+// A wave takes a token and walks over its heads, q's and then k's; a lane computes the
+// angle of one pair, and the others read it from LDS.  Where rows of a head lie beside
+// each other (head-major tensors) its rows are consecutive tokens of one head instead, and
+// every thread computes the angles that it needs, for all heads.  A thread holds 32 bytes of a row: 16-byte chunks c and c + half of the turned values,
 // which are partners in the half layout.
 #include <algorithm>
 #include <cmath>
@@ -54,9 +54,10 @@ struct Turn {
 // Cosine and sine of 2 pi (pos x turns), times f and fs.
 __device__ __forceinline__ Turn turn_of(double pos, double turns, float f, float fs) {
   const double quarters = 4.0 * turns;   // exact
-  const double n = __builtin_rint(pos * quarters);
+  // Beside 2^52 a sum is an integer, in its low bits too (here below 2^41).
+  const double big = __builtin_fma(pos, quarters, 0x1.8p52), n = big - 0x1.8p52;
   const float r = static_cast<float>(__builtin_fma(pos, quarters, -n));   // quarter turns, |r| <= 1/2
-  const int quad = static_cast<int>(static_cast<int64_t>(n)) & 3;
+  const int quad = static_cast<int>(__double_as_longlong(big)) & 3;
   const float x = r * 1.57079632679489662f;   // pi / 2
   const float x2 = x * x;
   float s = __builtin_fmaf(x2, 1.0f / 362880.0f, -1.0f / 5040.0f);
@@ -109,10 +110,19 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
   const bool store0 = turned0 || gone || !a.in_place, store1 = turned1 || gone || !a.in_place;
   // Values of chunk 0 or 1 belong to pair index:
   Turn t[PAIRS];
+  const double p0 = a.pos ? 0.0
+                          : static_cast<double>(a.lens ? static_cast<int64_t>(a.lens[b]) - rows + n
+                                                       : a.start + n);
+  auto angle = [&](int pair) __attribute__((always_inline)) {
+    double p = p0;
+    if (a.pos) p = a.pos[a.axis[pair] * a.pos_sA + b * a.pos_sB + n];
+    return turn_of(p, a.turns[pair], a.factor, a.sine);
+  };
+  __shared__ Turn table[4][kRopeMaxPairs];
+  Turn* shared = table[threadIdx.x >> 6];
+  if (a.token_log2 == 0 && lane < half) shared[lane] = angle(lane);
+  __builtin_amdgcn_wave_barrier();   // a wave's LDS accesses keep their order
   if (turned0 || turned1) {
-    const double p0 = a.pos ? 0.0
-                            : static_cast<double>(a.lens ? static_cast<int64_t>(a.lens[b]) - rows + n
-                                                         : a.start + n);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) {
       int pair;
@@ -122,13 +132,8 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
         const int d = 8 * (i < 8 ? c0 : c1) + (i & 7);
         pair = d < half ? d : d - half;
       }
-      if (pair < half) {
-        double p = p0;
-        if (a.pos) p = a.pos[a.axis[pair] * a.pos_sA + b * a.pos_sB + n];
-        t[i] = turn_of(p, a.turns[pair], a.factor, a.sine);
-      } else {
-        t[i] = Turn{1.0f, 0.0f};   // not used
-      }
+      pair = min(pair, half - 1);   // of those past the turned values nothing is used
+      t[i] = a.token_log2 == 0 ? shared[pair] : angle(pair);
     }
   }
   for (int h = part * heads + (r >> a.token_log2); h < a.heads; h += a.split * heads) {
