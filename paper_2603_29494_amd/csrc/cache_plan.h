@@ -4,6 +4,7 @@
 #pragma once
 
 #include "cache_common.h"
+#include "wave_scan.h"
 
 namespace vecattn {
 
@@ -32,21 +33,6 @@ struct AttnParams {
   int32_t least;     // blocks of a chunk at least
   float scale_log2;
 };
-
-// Inclusive prefix sum over the wave with DPP moves (see select_common.h), and its
-// last value.
-__device__ __forceinline__ int wave_incl_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr:1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
-  return x;
-}
-__device__ __forceinline__ int wave_total(int x) {
-  return __builtin_amdgcn_readlane(wave_incl_scan(x), 63);
-}
 
 // What one row tile sees, in blocks of 32 tokens: the first `ns` blocks (sinks),
 // then blocks nb0 ..; `total` of both.

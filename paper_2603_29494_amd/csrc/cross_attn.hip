@@ -21,6 +21,7 @@
 
 #include "device_common.h"
 #include "launch.h"
+#include "wave_scan.h"
 
 namespace vecattn {
 namespace {
@@ -40,7 +41,8 @@ struct CrossParams {
   const int32_t* n_q;
   int32_t clear;       // rows past n_q become 0
   float* part;         // [item][rows of a tile][D] sums, then [item][rows of a tile] (m, l)
-  int32_t Hkv, group, Nq, Nk, row_tiles, chunks, chunk, near_heads;
+  int32_t Hkv, group, Nq, Nk, row_tiles, chunks, chunk, near_heads, batch;
+  int32_t target, least;     // of few rows: most chunks, of all heads (0: one each); their tiles
   uint32_t items, per_xcd;   // per_xcd: consecutive items of an XCD, which share keys in its L2
   float scale_log2;
 };
@@ -83,6 +85,64 @@ __device__ __forceinline__ bool decode(const CrossParams& a, int tile_rows, uint
   return s.rt * tile_rows < s.rows && s.c < s.count;
 }
 
+// Few rows: the chunks, of `tiles` tiles of kFewKeys, that a sequence's keys are cut into.
+constexpr int kFewKeys = 32, kMaxDealt = 256;   // sequences that are dealt out by their lengths
+struct Share {
+  int b, first, count, tiles;
+};
+
+// The share that chunk `index` belongs to; b < 0 if there is none.  Every wave of every
+// workgroup computes the same from the lengths: chunks of a size that makes at most
+// `target` of them for all heads.
+__device__ __forceinline__ Share find_share(const CrossParams& a, int index) {
+  if (a.target == 0) return Share{index < a.batch ? index : -1, index, 1, a.Nk};
+  constexpr int kPasses = kMaxDealt / 64;
+  const int lane = threadIdx.x & 63;
+  int total[kPasses], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int b = 64 * i + lane;
+    total[i] = 64 * i < a.batch && b < a.batch ? (keys_of(a, b) + kFewKeys - 1) / kFewKeys : 0;
+    sum += (total[i] + 7) >> 3;   // 256 x 2^25 tiles, in units of 8
+  }
+  const int64_t tiles = static_cast<int64_t>(wave_total(sum)) * 8 * a.Hkv;
+  // Chunks of a multiple of four tiles, one for each wave at a time.
+  auto size_for = [&](int parts) __attribute__((always_inline)) {
+    return (max(static_cast<int>((tiles + parts - 1) / parts), a.least) + 3) & ~3;
+  };
+  auto count_of = [&](int i, int size) __attribute__((always_inline)) {
+    return 64 * i + lane < a.batch ? max(1, (total[i] + size - 1) / size) : 0;
+  };
+  // As many tiles per chunk as fill `target`, unless the sequences' last chunks make more of
+  // them; the second size cannot (each sequence adds less than one).
+  int size = size_for(a.target), chunks = 0;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) chunks += count_of(i, size);
+  if (static_cast<int64_t>(wave_total(chunks)) * a.Hkv > a.target)
+    size = size_for(a.target - a.batch * a.Hkv);
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    if (64 * i >= a.batch) break;
+    const int count = count_of(i, size), incl = wave_incl_scan(count);
+    const int first = before + incl - count;
+    const uint64_t at = __ballot(index >= first && index < first + count);
+    if (at) {
+      const int l = __builtin_ctzll(at);
+      return Share{64 * i + l, __builtin_amdgcn_readlane(first, l),
+                   __builtin_amdgcn_readlane(count, l), size};
+    }
+    before += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return Share{-1, 0, 0, 0};
+}
+
+// Where a sequence's share is left for the join, behind the parts.
+template <int D>
+__device__ __forceinline__ int2* shares_of(const CrossParams& a) {
+  return reinterpret_cast<int2*>(a.part + static_cast<int64_t>(a.items) * 32 * (D + 2));
+}
+
 __device__ __forceinline__ const uint16_t* q_row(const CrossParams& a, const Item& s, int row) {
   const int tok = row / a.group, h = s.hk * a.group + row % a.group;
   return a.q + s.b * a.q_sB + h * a.q_sH + tok * a.q_sN;
@@ -113,14 +173,6 @@ __device__ __forceinline__ void clear_rows(const CrossParams& a, const Item& s, 
       a.lse[(s.b * a.Hkv * a.group + h) * a.Nq + tok] = 0.0f;
     }
   }
-}
-
-// Bit r: key j0 + r, of `keys`, exists and the mask leaves it.
-template <int KEYS>
-__device__ __forceinline__ uint64_t visible(const uint8_t* mask, int keys, int j0, int lane) {
-  bool see = lane < KEYS && j0 + lane < keys;
-  if (mask && see) see = mask[j0 + lane] != 0;
-  return __ballot(see);
 }
 
 // Direct-to-LDS instruction u of a tile of KEYS rows from row j0 on (16 bytes a lane).  HIDE:
@@ -346,7 +398,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     return MASK && j < keys ? mask[j] : 0;
   };
   auto visible = [&](int t, int byte) __attribute__((always_inline)) {
-    if constexpr (MASK) return static_cast<uint32_t>(__ballot(byte != 0));
+    if constexpr (MASK) {
+      asm volatile("" : "+v"(byte));   // compared here, not where it is fetched
+      return static_cast<uint32_t>(__ballot(byte != 0));
+    }
     const int n = keys - t * KEYS;
     return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
   };
@@ -440,22 +495,33 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
 template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_cross_few(
     const CrossParams a) {
-  constexpr int KEYS = 32, U = KEYS * (D / 8) / 64, ROWS = 32;
+  constexpr int KEYS = kFewKeys, U = KEYS * (D / 8) / 64, ROWS = 32;
   using W = Wave<D>;
   __shared__ __align__(16) uint16_t k_s0[4][KEYS * D];
   __shared__ __align__(16) uint16_t k_s1[4][KEYS * D];
   __shared__ __align__(16) uint16_t v_s0[4][KEYS * D];
   __shared__ __align__(16) uint16_t v_s1[4][KEYS * D];
   __shared__ float s_m[4][ROWS], s_l[4][ROWS];
+  const uint32_t chunk = blockIdx.x / static_cast<uint32_t>(a.Hkv);
+  const Share share = find_share(a, static_cast<int>(chunk));
+  if (share.b < 0) return;
   Item s;
-  const uint32_t i = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
-  if (blockIdx.x >> 3 >= a.per_xcd || i >= a.items) return;
-  const bool some = decode(a, ROWS, i, s);
+  s.index = blockIdx.x;
+  s.b = share.b;
+  s.hk = static_cast<int>(blockIdx.x - chunk * a.Hkv);
+  s.rt = 0;
+  s.c = static_cast<int>(chunk) - share.first;
+  s.count = share.count;
+  s.len = keys_of(a, s.b);
+  s.rows = rows_of(a, s.b);
+  if (a.target && s.c == 0 && s.hk == 0 && threadIdx.x == 0)
+    shares_of<D>(a)[s.b] = int2{share.first, share.count};
   clear_rows<D>(a, s, ROWS);
-  if (!some) return;
+  if (s.rows == 0) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int first = s.c * a.chunk, keys = min(s.len - first, a.chunk);
+  const int first = s.count > 1 ? s.c * share.tiles * KEYS : 0;
+  const int keys = s.count > 1 ? min(s.len - first, share.tiles * KEYS) : s.len;
   const uint16_t* kh = a.k + s.b * a.k_sB + s.hk * a.k_sH + first * a.k_sN;
   const uint16_t* vh = a.v + s.b * a.v_sB + s.hk * a.v_sH + first * a.v_sN;
   const uint32_t k_rowb = static_cast<uint32_t>(a.k_sN) * 2u;
@@ -480,26 +546,36 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   // A tile is worked on while the wave's next is fetched; past the last one the fetch
   // goes to the last again (into a buffer that nothing reads).
   auto tile = [&](int t) __attribute__((always_inline)) { return min(t, ntiles - 1); };
+  // Visible keys of the tile that is worked on and of the next; of the one after that the
+  // lane's byte, fetched before the next tile's keys, so that it does not wait for them.
+  auto key_byte = [&](int t) __attribute__((always_inline)) {
+    const int j = t * KEYS + (lane & 31);
+    return j < keys ? (mask ? mask[j] : 1) : 0;
+  };
+  auto bits = [&](int byte) __attribute__((always_inline)) {
+    asm volatile("" : "+v"(byte));   // compared here, not where it is fetched
+    return static_cast<uint32_t>(__ballot(byte != 0));
+  };
   int t = wave;
-  uint64_t see = 0, see1 = 0;
+  uint32_t see = 0, see1 = 0;
   if (t < ntiles) {
-    see = visible<KEYS>(mask, keys, t * KEYS, lane);
+    const int b0 = key_byte(t), b1 = key_byte(tile(t + 4));
+    see = bits(b0), see1 = bits(b1);
     fetch(t, see, k_s0[wave], v_s0[wave]);
-    see1 = visible<KEYS>(mask, keys, tile(t + 4) * KEYS, lane);
   }
   auto turn = [&](const uint16_t* k, const uint16_t* v, uint16_t* k1, uint16_t* v1)
                   __attribute__((always_inline)) {
+    const int byte2 = key_byte(tile(t + 8));
     fetch(tile(t + 4), see1, k1, v1);
     wait_vmcnt<2 * U>();
     f32x16 x;
     bf16x8 pb[2];
     w.score(x, k);
-    if (see != 0xFFFFFFFFu) w.hide(x, static_cast<uint32_t>(see));
+    if (see != ~0u) w.hide(x, see);
     w.weigh(x, a.scale_log2, pb);
     w.add(pb, v);
-    see = see1;
+    see = see1, see1 = bits(byte2);
     t += 4;
-    see1 = visible<KEYS>(mask, keys, tile(t + 4) * KEYS, lane);
   };
   while (t < ntiles) {
     turn(k_s0[wave], v_s0[wave], k_s1[wave], v_s1[wave]);
@@ -572,7 +648,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 }
 
 // Joins the chunks of a row, a wave per row, a lane D / 64 values.
-template <int D>
+template <int D, bool FEW>
 __global__ __launch_bounds__(256) void k_cross_merge(const CrossParams a, int32_t tile_rows,
                                                      int64_t total) {
   constexpr int V = D / 64;
@@ -584,13 +660,23 @@ __global__ __launch_bounds__(256) void k_cross_merge(const CrossParams a, int32_
   const int64_t bh = id / rows_all;
   const int hk = static_cast<int>(bh % a.Hkv);
   const int64_t b = bh / a.Hkv;
-  const int count = chunks_of(a, keys_of(a, b));
+  // The row's parts: every `step`-th row of them from the first on.
+  int count;
+  int64_t at, step;
+  if constexpr (FEW) {
+    const int2 share = shares_of<D>(a)[b];   // first, count
+    count = share.y;
+    at = static_cast<int64_t>(share.x) * a.Hkv + hk;
+    step = static_cast<int64_t>(a.Hkv) * tile_rows;
+  } else {
+    count = chunks_of(a, keys_of(a, b));
+    at = (bh * a.row_tiles + row / tile_rows) * a.chunks;
+    step = tile_rows;
+  }
   if (count <= 1 || row >= rows_of(a, b)) return;
-  const int64_t at = (bh * a.row_tiles + row / tile_rows) * a.chunks;
   const int r = row % tile_rows;
   const float* ml = part_ml<D>(a, at, tile_rows, r);
   const float* src = a.part + (at * tile_rows + r) * D + V * lane;
-  const int64_t step = static_cast<int64_t>(tile_rows);
   float m = kUnseen;
   for (int i = lane; i < count; i += 64) m = fmaxf(m, ml[i * step * 2]);
 #pragma unroll
@@ -614,7 +700,7 @@ __global__ __launch_bounds__(256) void k_cross_merge(const CrossParams a, int32_
 // the launch agree.
 struct Deal {
   bool few;
-  int32_t rows, tiles, chunks, chunk;
+  int32_t rows, tiles, chunks, chunk, target, least;
   int64_t items;
 };
 
@@ -628,6 +714,20 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
   // Workgroups that run at a time, and the fewest keys that pay for a chunk.
   const int64_t slots = d.few && D == 128 ? 256 : 512;
   const int64_t least = 512;
+  d.target = d.least = 0;
+  if (d.few) {
+    // Cut by the lengths on the device; never into fewer than two chunks per head.
+    const int64_t most = (Nk + least - 1) / least;
+    d.chunks = most > 1 && B <= kMaxDealt ? 2 : 1;   // or more
+    d.chunk = 0;
+    d.items = units;
+    if (d.chunks > 1) {
+      d.target = static_cast<int32_t>(std::max(slots, 2 * units));
+      d.least = static_cast<int32_t>(least / kFewKeys);
+      d.items = std::min<int64_t>(d.target, units * most);
+    }
+    return d;
+  }
   int64_t chunks = std::min((Nk + least - 1) / least, std::max<int64_t>(1, 2 * slots / units));
   d.chunk = static_cast<int32_t>(((Nk + chunks - 1) / chunks + 127) / 128 * 128);
   d.chunks = static_cast<int32_t>((Nk + d.chunk - 1) / d.chunk);
@@ -640,7 +740,9 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
 size_t cross_attn_workspace_bytes(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk,
                                   int64_t D) {
   const Deal d = deal(B, Hq, Hkv, Nq, Nk, D);
-  return d.chunks > 1 ? static_cast<size_t>(d.items) * d.rows * (D + 2) * sizeof(float) : 0;
+  return d.chunks > 1 ? static_cast<size_t>(d.items) * d.rows * (D + 2) * sizeof(float) +
+                            (d.few ? static_cast<size_t>(B) * 2 * sizeof(int32_t) : 0)
+                      : 0;
 }
 
 bool cross_attn_grid_ok(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D) {
@@ -669,6 +771,7 @@ hipError_t launch_cross_attn(const CrossArgs& x, hipStream_t stream) {
   a.group = static_cast<int32_t>(x.q.H / x.k.H);
   a.Nq = static_cast<int32_t>(x.q.N), a.Nk = static_cast<int32_t>(x.k.N);
   a.row_tiles = d.tiles, a.chunks = d.chunks, a.chunk = d.chunk;
+  a.batch = static_cast<int32_t>(x.q.B), a.target = d.target, a.least = d.least;
   a.items = static_cast<uint32_t>(d.items);
   const float scale = x.scale != 0.0f ? x.scale : 1.0f / sqrtf(static_cast<float>(x.q.D));
   a.scale_log2 = std::max(scale * 1.4426950408889634f, 0x1p-126f);   // -inf * 0 is no mask
@@ -678,7 +781,7 @@ hipError_t launch_cross_attn(const CrossArgs& x, hipStream_t stream) {
     if (a.Hkv % n == 0 && n * x.k.N * x.k.D * 4 <= (2 << 20)) a.near_heads = n;
   // XCD x (workgroups x, x + 8, ..) takes items [x per_xcd, (x + 1) per_xcd).
   a.per_xcd = (a.items + 7) / 8;
-  const dim3 grid(8 * a.per_xcd);
+  const dim3 grid(d.few ? a.items : 8 * a.per_xcd);
   auto pick = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     if (d.few) hipLaunchKernelGGL(k_cross_few<D>, grid, dim3(256), 0, stream, a);
@@ -687,8 +790,9 @@ hipError_t launch_cross_attn(const CrossArgs& x, hipStream_t stream) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || d.chunks == 1) return e;
     const int64_t total = x.q.B * x.q.H * x.q.N;
-    hipLaunchKernelGGL(k_cross_merge<D>, dim3(static_cast<unsigned>((total + 3) / 4)), dim3(256), 0,
-                       stream, a, d.rows, total);
+    const dim3 joins(static_cast<unsigned>((total + 3) / 4));
+    if (d.few) hipLaunchKernelGGL((k_cross_merge<D, true>), joins, dim3(256), 0, stream, a, d.rows, total);
+    else hipLaunchKernelGGL((k_cross_merge<D, false>), joins, dim3(256), 0, stream, a, d.rows, total);
     return hipGetLastError();
   };
   return x.q.D == 128 ? pick(std::integral_constant<int, 128>{})

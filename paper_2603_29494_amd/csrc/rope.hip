@@ -16,6 +16,7 @@
 // which are partners in the half layout.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.h"
 #include "launch.h"
@@ -81,7 +82,21 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, bf16x2));
 }
 
-template <int D, int LAYOUT>
+// A 16-byte chunk; STREAM: past the caches.
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load_chunk(const uint16_t* row, int c) {
+  const u32x4* at = reinterpret_cast<const u32x4*>(row) + c;
+  if constexpr (STREAM) return __builtin_nontemporal_load(at);
+  return *at;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_chunk(uint16_t* row, int c, u32x4 x) {
+  u32x4* at = reinterpret_cast<u32x4*>(row) + c;
+  if constexpr (STREAM) __builtin_nontemporal_store(x, at);
+  else *at = x;
+}
+
+template <int D, int LAYOUT, bool STREAM>
 __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
   constexpr int TH = D / 16;          // threads per row
   constexpr int ROWS = 64 / TH;       // rows of a wave
@@ -144,8 +159,8 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
     uint16_t* dst = is_q ? a.qo + b * a.qo_sB + hh * a.qo_sH + n * a.qo_sN
                          : a.ko + b * a.ko_sB + hh * a.ko_sH + n * a.ko_sN;
     u32x4 x0 = {}, x1 = {};
-    if (store0) x0 = reinterpret_cast<const u32x4*>(src)[c0];
-    if (store1) x1 = reinterpret_cast<const u32x4*>(src)[c1];
+    if (store0) x0 = load_chunk<STREAM>(src, c0);
+    if (store1) x1 = load_chunk<STREAM>(src, c1);
     if constexpr (LAYOUT == kInterleaved) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -192,8 +207,8 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
       __builtin_amdgcn_wave_barrier();
     }
     if (gone) x0 = x1 = u32x4{0, 0, 0, 0};
-    if (store0) reinterpret_cast<u32x4*>(dst)[c0] = x0;
-    if (store1) reinterpret_cast<u32x4*>(dst)[c1] = x1;
+    if (store0) store_chunk<STREAM>(dst, c0, x0);
+    if (store1) store_chunk<STREAM>(dst, c1, x1);
   }
 }
 
@@ -237,15 +252,24 @@ hipError_t launch_rope(const RopeArgs& x, hipStream_t stream) {
   a.split = static_cast<int32_t>(std::min(passes, std::max<int64_t>(1, 8192 / a.units)));
   const dim3 grid(static_cast<unsigned>((a.units * a.split + 3) / 4));
   const int layout = !x.half ? kInterleaved : x.rot % 16 == 0 ? kHalfChunks : kHalfAny;
+  // What is turned, in and out, is past 256 MB: no cache holds it until it is read (131072
+  // tokens of 32 heads: 399 us through the caches, 377 past them).
+  const bool stream_past = 4 * x.q.B * x.q.N * a.heads * x.q.D > (int64_t(256) << 20);
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
+  auto pick = [&](auto dim, auto past) {
+    constexpr int D = decltype(dim)::value;
+    constexpr bool PAST = decltype(past)::value;
+    if (layout == kInterleaved) run(k_rope<D, kInterleaved, PAST>);
+    else if (layout == kHalfChunks) run(k_rope<D, kHalfChunks, PAST>);
+    else run(k_rope<D, kHalfAny, PAST>);
+  };
+  using std::integral_constant;
   if (x.q.D == 128)
-    layout == kInterleaved ? run(k_rope<128, kInterleaved>)
-                           : layout == kHalfChunks ? run(k_rope<128, kHalfChunks>)
-                                                   : run(k_rope<128, kHalfAny>);
+    stream_past ? pick(integral_constant<int, 128>{}, std::true_type{})
+                : pick(integral_constant<int, 128>{}, std::false_type{});
   else
-    layout == kInterleaved ? run(k_rope<64, kInterleaved>)
-                           : layout == kHalfChunks ? run(k_rope<64, kHalfChunks>)
-                                                   : run(k_rope<64, kHalfAny>);
+    stream_past ? pick(integral_constant<int, 64>{}, std::true_type{})
+                : pick(integral_constant<int, 64>{}, std::false_type{});
   return hipGetLastError();
 }
 
