@@ -260,10 +260,17 @@ struct Wave {
     }
     __builtin_amdgcn_sched_barrier(0);
   }
+  // Element e of a lane is key 8 (e / 4) + 4 g + e % 4: a bit of either half of the wave, put
+  // together on the scalar side.
   __device__ __forceinline__ void hide(f32x16& s, uint32_t see) {
-    const uint32_t bits = see >> (4 * g);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = bits >> (8 * (e / 4) + e % 4) & 1u ? s[e] : kNegInf;
+    for (int e = 0; e < 16; ++e) {
+      const int j = 8 * (e / 4) + e % 4;
+      const uint32_t lo = static_cast<int32_t>(see << (31 - j)) >> 31;
+      const uint32_t hi = static_cast<int32_t>(see << (27 - j)) >> 31;
+      const bool there = __builtin_amdgcn_inverse_ballot_w64(uint64_t(hi) << 32 | lo);
+      s[e] = there ? s[e] : kNegInf;
+    }
   }
   static __device__ __forceinline__ float largest(const f32x16& s) {
     float top = kNegInf;
@@ -711,12 +718,13 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
   d.rows = d.few ? 32 : kCrossRows;
   d.tiles = static_cast<int32_t>((rows + d.rows - 1) / d.rows);
   const int64_t units = B * Hkv * d.tiles;
-  // Workgroups that run at a time, and the fewest keys that pay for a chunk.
-  const int64_t slots = d.few && D == 128 ? 256 : 512;
-  const int64_t least = 512;
   d.target = d.least = 0;
   if (d.few) {
-    // Cut by the lengths on the device; never into fewer than two chunks per head.
+    // Cut by the lengths on the device into as many chunks as workgroups run at a time (one
+    // of 128 values per CU, two of 64; 16 sequences of 0 to 16384 keys: 45 us, 62 in chunks of
+    // 2048), never into fewer than two per head, nor into ones of fewer keys than pay for a
+    // chunk.
+    const int64_t slots = D == 128 ? 256 : 512, least = 512;
     const int64_t most = (Nk + least - 1) / least;
     d.chunks = most > 1 && B <= kMaxDealt ? 2 : 1;   // or more
     d.chunk = 0;
@@ -728,7 +736,11 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
     }
     return d;
   }
-  int64_t chunks = std::min((Nk + least - 1) / least, std::max<int64_t>(1, 2 * slots / units));
+  // Many rows: parts and their join cost about as much as 512 keys, so the keys are cut only
+  // where row tiles leave half of the CUs without one (8 tiles over 16384 keys: 24 us in 32
+  // chunks, 324 in one; 200 tiles over 1200: 31 in one, 44 in two; 512 over 4096: 150 and
+  // 178).
+  const int64_t chunks = units > 128 ? 1 : std::max<int64_t>(1, std::min(Nk / 512, 512 / units));
   d.chunk = static_cast<int32_t>(((Nk + chunks - 1) / chunks + 127) / 128 * 128);
   d.chunks = static_cast<int32_t>((Nk + d.chunk - 1) / d.chunk);
   d.items = units * d.chunks;
