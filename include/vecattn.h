@@ -658,7 +658,7 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
  * depend on the order of execution (no atomics).  What a call does follows lens, mask and
  * n_q on the device, so that a captured call can be replayed as they change.
  * Errors: INVALID_ARG (null pointer, shape mismatch, Hq % Hkv != 0, mask_sB < 0, a bad
- * scale, other flags, misalignment); CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128},
+ * scale, other flags, an output whose sequences or heads share memory, misalignment); CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128},
  * Nq * Hq / Hkv > 2^30, more than 2^24 sequences times Hkv, about 2^23 workgroups, a K or
  * V row stride of 2^24 elements or more).
  */
@@ -738,8 +738,8 @@ vecattn_status vecattn_rope_ladder(int32_t rot, double base, int32_t scaling, do
  * any position, and a result is rounded to bf16 once.  Asynchronous, one launch.
  * Errors: INVALID_ARG (null pointer, shape mismatch, both pos and lens, |start| > 2^30,
  * a bad stride, a spec outside what its comments allow, a factor or frequency that is not
- * finite, |frequency| > 1024, an output that is its input with other strides,
- * misalignment); UNSUPPORTED (D not in {64, 128}, more than 65535 heads in all, B * N >
+ * finite, |frequency| > 1024, an output that is its input with other strides or whose
+ * sequences or heads share memory (a stride of 0), misalignment); UNSUPPORTED (D not in {64, 128}, more than 65535 heads in all, B * N >
  * 2^30).
  */
 vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* k,

@@ -405,6 +405,11 @@ bool same_strides(const vecattn_tdesc* a, const vecattn_tdesc* b) {
          (a->N == 1 || a->sN == b->sN);
 }
 
+// An output whose sequences or heads share memory would be written several times.
+bool shares_rows(const vecattn_tdesc* d) {
+  return (d->B > 1 && d->sB == 0) || (d->H > 1 && d->sH == 0);
+}
+
 // What the workspace of the attention over an encoder's states, and the call, need of
 // the shapes.
 vecattn_status check_cross(const vecattn_tdesc* qd, const vecattn_tdesc* kd) {
@@ -759,7 +764,7 @@ vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const 
   if ((st = check_desc(v, vd)) != VECATTN_OK) return st;
   if ((st = check_desc(o, od)) != VECATTN_OK) return st;
   if ((st = check_cross(qd, kd)) != VECATTN_OK) return st;
-  if (!same_shape(vd, kd) || !same_shape(od, qd)) return VECATTN_ERR_INVALID_ARG;
+  if (!same_shape(vd, kd) || !same_shape(od, qd) || shares_rows(od)) return VECATTN_ERR_INVALID_ARG;
   if (mask_sB < 0 || !std::isfinite(scale) || scale < 0.0f || !flags_ok(flags))
     return VECATTN_ERR_INVALID_ARG;
   // A tile's 64 rows are addressed with 32-bit byte offsets.
@@ -801,12 +806,14 @@ vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* 
   vecattn_status st;
   if ((st = check_desc(q, qd)) != VECATTN_OK) return st;
   if ((st = check_desc(qo, qod)) != VECATTN_OK) return st;
-  if (!same_shape(qod, qd) || (q == qo && !same_strides(qod, qd))) return VECATTN_ERR_INVALID_ARG;
+  if (!same_shape(qod, qd) || shares_rows(qod) || (q == qo && !same_strides(qod, qd)))
+    return VECATTN_ERR_INVALID_ARG;
   const bool with_k = k || kd || ko || kod;
   if (with_k) {
     if ((st = check_desc(k, kd)) != VECATTN_OK) return st;
     if ((st = check_desc(ko, kod)) != VECATTN_OK) return st;
-    if (!same_shape(kod, kd) || (k == ko && !same_strides(kod, kd))) return VECATTN_ERR_INVALID_ARG;
+    if (!same_shape(kod, kd) || shares_rows(kod) || (k == ko && !same_strides(kod, kd)))
+      return VECATTN_ERR_INVALID_ARG;
     if (kd->B != qd->B || kd->N != qd->N || kd->D != qd->D) return VECATTN_ERR_INVALID_ARG;
   }
   if (!spec || spec->rot < 2 || spec->rot > qd->D || spec->rot % 2 != 0 || !spec->freq ||

@@ -88,12 +88,29 @@ def test_lengths_masks_and_padding(gpu, D, Hq, Hkv, Nq, Nk):
         for b in range(B):
             n = min(n_q[b], Nq)
             assert (o[b, :, n:] == 9.0).all() and (lse[b, :, n:] == 0).all()
+    # an output made by the call: its padding is 0
+    o, lse = va.cross_attn(q, k, v, lens=int32(lens), mask=mask.cuda(), n_q=int32(n_q),
+                           return_lse=True)
+    ref.check(o, lse, cross64(q, k, v, lens, mask, n_q))
+    for b in range(B):
+        n = min(n_q[b], Nq)
+        assert (o[b, :, n:] == 0).all() and (lse[b, :, n:] == 0).all()
     # lengths alone: only what is past them hides
     for b in range(B):
         k[b, :, :min(lens[b], Nk)], v[b, :, :min(lens[b], Nk)] = (
             rows(7 + b, Hkv, min(lens[b], Nk), D), rows(17 + b, Hkv, min(lens[b], Nk), D))
     o, lse = va.cross_attn(q, k, v, lens=int32(lens), return_lse=True)
     ref.check(o, lse, cross64(q, k, v, lens))
+
+
+def test_many_sequences_and_uneven_lengths(gpu):
+    """More sequences than are dealt out by their lengths, and as many with lengths far apart."""
+    for B, Nk in ((300, 600), (256, 1100), (33, 3000)):
+        q, k, v = rows(1, B, 2, 1, 64), rows(2, B, 1, Nk, 64), rows(3, B, 1, Nk, 64)
+        lens = (torch.rand(B, generator=torch.Generator().manual_seed(B)) ** 4 * (Nk + 1)).int()
+        lens[0], lens[-1] = Nk, 0
+        o, lse = va.cross_attn(q, k, v, lens=lens.cuda(), return_lse=True)
+        ref.check(o, lse, cross64(q, k, v, lens=lens.tolist()))
 
 
 @pytest.mark.parametrize("Nq", [1, 90])

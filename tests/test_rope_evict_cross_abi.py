@@ -53,6 +53,12 @@ def test_rope_rejects_bad_arguments():
     # in place with other strides
     assert rope(start=0, qo=FAKE, qod=desc(1, 4, 8, 128, sN=256)) == INVALID
     assert rope(start=0, ko=FAKE, kod=desc(1, 2, 8, 128, sN=256)) == INVALID
+    # outputs whose sequences or heads lie on each other, in place or not
+    for z in (_lib.TDesc(2, 4, 8, 128, 0, 1024, 128), _lib.TDesc(2, 4, 8, 128, 4096, 0, 128)):
+        two = desc(2, 2, 8, 128)
+        assert rope(start=0, qd=z, qod=z, kd=two) == INVALID
+        assert rope(start=0, qd=z, qo=FAKE, qod=z, kd=two) == INVALID
+        assert rope(start=0, qd=desc(2, 4, 8, 128), kd=z, kod=z) == INVALID
     assert rope(start=0, pos=FAKE, lens=FAKE) == INVALID
     assert rope(start=0, pos=FAKE, sA=-1) == INVALID and rope(start=0, pos=FAKE, sB=-1) == INVALID
     assert rope(start=-(1 << 30) - 1) == INVALID and rope(start=(1 << 30) + 1) == INVALID
@@ -230,6 +236,8 @@ def test_cross_attn_rejects_bad_arguments():
                 dict(kd=desc(2, 2, 77, 128)), dict(kd=desc(1, 2, 77, 64)),
                 dict(vd=desc(1, 2, 78, 128)), dict(od=desc(1, 4, 63, 128)), dict(ws=FAKE + 8, nws=64)):
         assert cross(**dict(dict(scale=0.0), **bad)) == INVALID, bad
+    for z in (_lib.TDesc(2, 4, 64, 128, 0, 8192, 128), _lib.TDesc(2, 4, 64, 128, 32768, 0, 128)):
+        assert cross(scale=0.0, qd=desc(2, 4, 64, 128), od=z, kd=desc(2, 2, 77, 128)) == INVALID
     assert cross(scale=0.0, qd=desc(1, 4, 64, 80)) == UNSUPPORTED
     assert cross(scale=0.0, kd=desc(1, 2, 77, 128, sN=1 << 24)) == UNSUPPORTED
     assert cross(scale=0.0, vd=desc(1, 2, 77, 128, sN=1 << 24)) == UNSUPPORTED
