@@ -45,24 +45,32 @@ __device__ __forceinline__ Place place_of(const MassParams& a, int64_t b) {
   return Place{len - nb, nb * a.group, static_cast<int>(min<int64_t>(len, a.M))};
 }
 
-// Base of a block of a head's keys, or NULL where no page is held.
+// The page that holds a block (past the table: some page), and the base of a head's keys of
+// the block, or NULL where no page is held.
+__device__ __forceinline__ int page_of(const MassParams& a, int64_t b, int jb) {
+  return ((ScalarInts)(a.table + b * a.cols))[min(jb >> (a.page_shift - 5), a.cols - 1)];
+}
 template <int BYTES>
-__device__ __forceinline__ const uint8_t* keys_of(const MassParams& a, int64_t b, int h, int jb) {
+__device__ __forceinline__ const uint8_t* keys_of(const MassParams& a, int64_t page, int h, int jb) {
   const int sh = a.page_shift - 5;
-  const int col = jb >> sh;
-  if (col >= a.cols) return nullptr;
-  const int64_t page = ((ScalarInts)(a.table + b * a.cols))[col];
-  if (page < 0 || page >= a.pages) return nullptr;
+  if (jb >> sh >= a.cols || page < 0 || page >= a.pages) return nullptr;
   return a.data + (((page * a.H + h) << sh) + (jb & ((1 << sh) - 1))) * BYTES;
 }
 
-// x summed over 16 lanes, on each of them.
+// x summed over 16 lanes (or each half of them), on each of them.
+template <bool HALF = false>
 __device__ __forceinline__ float row_sum(float x) {
   auto turn = [&](auto ctl) __attribute__((always_inline)) {
     const int y = __builtin_bit_cast(int, x);
     x += __builtin_bit_cast(
         float, __builtin_amdgcn_update_dpp(y, y, decltype(ctl)::value, 0xf, 0xf, false));
   };
+  if constexpr (HALF) {
+    turn(std::integral_constant<int, 0xB1>{});    // quad_perm [1, 0, 3, 2]
+    turn(std::integral_constant<int, 0x4E>{});    // quad_perm [2, 3, 0, 1]
+    turn(std::integral_constant<int, 0x141>{});   // row_half_mirror
+    return x;
+  }
   turn(std::integral_constant<int, 0x128>{});   // row_ror:8
   turn(std::integral_constant<int, 0x124>{});
   turn(std::integral_constant<int, 0x122>{});
@@ -75,23 +83,30 @@ __device__ __forceinline__ int blocks_of(const MassParams& a, const Place& s) {
   return static_cast<int>(((a.clear ? a.M : s.end) + kCacheBlock - 1) / kCacheBlock);
 }
 
-// Token j's sum: what it had before (a new token: nothing) and w.
+// What token j has collected before (a new token: nothing).
+__device__ __forceinline__ float before(const MassParams& a, const Place& s, int64_t bh, int j) {
+  return a.mass && j < s.p_first && j < s.end ? a.mass[bh * a.M + j] : 0.0f;
+}
+
+// Token j's sum.
 __device__ __forceinline__ void collect(const MassParams& a, const Place& s, int64_t bh, int j,
-                                        float w) {
+                                        float old, float w) {
   const int64_t at = bh * a.M + j;
   if (j >= s.end) {
     if (a.clear && j < a.M) a.out[at] = 0.0f;
     return;
   }
-  if (a.mass && j < s.p_first) w = __builtin_fmaf(a.decay, a.mass[at], w);
-  a.out[at] = w;
+  a.out[at] = __builtin_fmaf(a.decay, old, w);
 }
 
-// Sixteen rows at most: waves take blocks of 32 tokens in turn.
-template <int D, int BITS>
+// Sixteen rows at most: waves take blocks of 32 tokens in turn.  HALF, up to eight rows: the
+// 16 columns of the matrix instructions hold them twice, once for either 16 tokens of a
+// block, which halves the work per score.
+template <int D, int BITS, bool HALF>
 __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, ST = D / 32;
+  constexpr int NT = HALF ? 1 : 2;   // groups of four tokens whose scores a lane holds
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.y;
@@ -102,8 +117,10 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   int jb = blockIdx.x * 4 + wave;
   if (jb >= blocks) return;
 
-  const int tok = n / a.group, hq = h * a.group + n % a.group;
-  bool have = n < s.rows;
+  const int row = HALF ? n & 7 : n;
+  const bool second = HALF && (n & 8);   // the lane's columns are for the block's last 16 tokens
+  const int tok = row / a.group, hq = h * a.group + row % a.group;
+  bool have = row < s.rows;
   float lse = have ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
   have = have && lse != kNegInf;
   Rows<D, BITS> rows;
@@ -118,68 +135,80 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
     return s.rows > 0 && j0 <= p_hi && (j0 + 31 > p_lo - a.window || j0 < a.sinks);
   };
   struct Keys {
-    uint32_t c[L::kRun], p[2][4 * G];
+    uint32_t c[L::kRun], p[NT][4 * G];
+    float old;
   };
-  auto load = [&](Keys& x, int i) __attribute__((always_inline)) {
-    const uint8_t* blk = i < blocks && seen(i) ? keys_of<L::kBytes>(a, b, h, i) : nullptr;
+  // The lane's token in what is written of a block, element n % 4 of one of its tiles; half
+  // of the lanes write one.
+  const bool writes = HALF ? (n & 4) == 0 : n < 8;
+  auto token = [&](int i) __attribute__((always_inline)) {
+    return i * kCacheBlock + 2 * (HALF ? n & 8 : 2 * (n & 4)) + 4 * g + (n & 3);
+  };
+  auto load = [&](Keys& x, int i, int page) __attribute__((always_inline)) {
+    x.old = i < blocks && writes ? before(a, s, bh, token(i)) : 0.0f;
+    const uint8_t* blk = i < blocks && seen(i) ? keys_of<L::kBytes>(a, page, h, i) : nullptr;
     if (!blk) return false;
 #pragma unroll
     for (int c = 0; c < L::kRun / 4; ++c)
       *reinterpret_cast<u32x4*>(x.c + 4 * c) =
           *reinterpret_cast<const u32x4*>(blk + (c * 64 + lane) * 16);
 #pragma unroll
-    for (int tl = 0; tl < 2; ++tl)
+    for (int tl = 0; tl < NT; ++tl)
 #pragma unroll
       for (int c = 0; c < G; ++c)
         *reinterpret_cast<u32x4*>(x.p[tl] + 4 * c) = *reinterpret_cast<const u32x4*>(
-            blk + L::kCodes + (16 * tl + 4 * g) * G * 4 + 16 * c);
+            blk + L::kCodes + (16 * (HALF ? n >> 3 : tl) + 4 * g) * G * 4 + 16 * c);
     return true;
   };
   auto work = [&](const Keys& x, bool held, int i) __attribute__((always_inline)) {
-    const int j0 = i * kCacheBlock;
-    // The lane's token in what is written: of tile n / 4, element n % 4.
-    const int j = j0 + 16 * ((n >> 2) & 1) + 4 * g + (n & 3);
+    const int j0 = i * kCacheBlock, j = token(i);
     float w = 0.0f;
     if (held) {
       const bool masked = j0 + 31 > p_lo || (j0 <= p_hi - a.window && j0 + 31 >= a.sinks);
-      float p[2][4];
+      f32x4 acc[2][G];
 #pragma unroll
       for (int tl = 0; tl < 2; ++tl) {
-        f32x4 acc[G];
 #pragma unroll
-        for (int gi = 0; gi < G; ++gi) acc[gi] = f32x4{};
+        for (int gi = 0; gi < G; ++gi) acc[tl][gi] = f32x4{};
 #pragma unroll
         for (int st = 0; st < ST; ++st)
-          acc[st / 2] = rows.dot(x.c + (tl * ST + st) * DW, st, acc[st / 2]);
+          acc[tl][st / 2] = rows.dot(x.c + (tl * ST + st) * DW, st, acc[tl][st / 2]);
+      }
+#pragma unroll
+      for (int tl = 0; tl < NT; ++tl)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float y = 0.0f;
 #pragma unroll
           for (int gi = 0; gi < G; ++gi) {
-            y = __builtin_fmaf(high_of(x.p[tl][e * G + gi]), acc[gi][e], y);
+            const float c = HALF ? (second ? acc[1][gi][e] : acc[0][gi][e]) : acc[tl][gi][e];
+            y = __builtin_fmaf(high_of(x.p[tl][e * G + gi]), c, y);
             y = __builtin_fmaf(low_of(x.p[tl][e * G + gi]), rows.sum[gi], y);
           }
           y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
           if (masked) {
-            const int jt = j0 + 16 * tl + 4 * g + e;
+            const int jt = j0 + (HALF ? 2 * (n & 8) : 16 * tl) + 4 * g + e;
             y = jt <= pos && (jt > pos - a.window || jt < a.sinks) ? y : 0.0f;
           }
-          p[tl][e] = row_sum(y);
+          const float sum = row_sum<HALF>(y);
+          w = (HALF ? n & 3 : n & 7) == 4 * tl + e ? sum : w;
         }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w = (n & 7) == e ? p[e / 4][e % 4] : w;
     }
-    if (n < 8 && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, w);
+    if (writes && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, x.old, w);
   };
+  // Each block is fetched while the one before is worked on, its page's entry one block
+  // earlier still.
   Keys cur, nxt;
-  bool held = load(cur, jb);
+  int page = page_of(a, b, jb + step);
+  bool held = load(cur, jb, page_of(a, b, jb));
   while (jb < blocks) {
-    const bool more = load(nxt, jb + step);
+    const bool more = load(nxt, jb + step, page);
+    page = page_of(a, b, jb + 2 * step);
     work(cur, held, jb);
     jb += step;
     if (jb >= blocks) break;
-    held = load(cur, jb + step);
+    held = load(cur, jb + step, page);
+    page = page_of(a, b, jb + 2 * step);
     work(nxt, more, jb);
     jb += step;
   }
@@ -314,7 +343,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   }
 
   // A block that no page holds passes as zeros, and its sums are left out at the end.
-  const uint8_t* blk = j0 < s.end ? keys_of<L::kBytes>(a, b, h, jb) : nullptr;
+  const uint8_t* blk =
+      j0 < s.end ? keys_of<L::kBytes>(a, page_of(a, b, jb), h, jb) : nullptr;
   bf16x8 low = {};
   f16x8 codes[ST];
   float step_of[G][16], w[16];
@@ -393,7 +423,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
     mine = (n & 15) == e ? all : mine;
   }
   const int j = j0 + 8 * ((n & 15) / 4) + 4 * g + (n & 3);
-  if (n < 16 && jb < blocks) collect(a, s, bh, j, blk ? mine : 0.0f);
+  if (n < 16 && jb < blocks) collect(a, s, bh, j, before(a, s, bh, j), blk ? mine : 0.0f);
 }
 
 template <int D>
@@ -453,7 +483,9 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
       // Two workgroups per place on the CUs, so that unequal lengths even out (4 x 131072
       // tokens, 4 heads: 46 us; 45 with half of them, 49 with twice as many).
       const int64_t fill = std::max<int64_t>(1, 2048 / heads);
-      launch(k_mass_few<D, BITS>, std::min((blocks + 3) / 4, fill));
+      const int64_t groups = std::min((blocks + 3) / 4, fill);
+      if (rows <= 8) launch(k_mass_few<D, BITS, true>, groups);
+      else launch(k_mass_few<D, BITS, false>, groups);
     } else {
       RowTile<D>* prepared = static_cast<RowTile<D>*>(x.workspace);
       const int64_t tiles = (rows + 31) / 32;
