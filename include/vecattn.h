@@ -509,6 +509,12 @@ vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* tab
                                   const int32_t* lens, int64_t start, void* k,
                                   const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
                                   void* stream);
+/* vecattn_cache_read with every row of k and v written: 0 for tokens at or past lens[b]
+ * and for those that no page holds. */
+vecattn_status vecattn_cache_read_whole(const vecattn_cache* cache, const int32_t* table,
+                                        int64_t cols, const int32_t* lens, int64_t start, void* k,
+                                        const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
+                                        void* stream);
 
 /*
  * Attention of the last n tokens of each sequence over its cached tokens: one

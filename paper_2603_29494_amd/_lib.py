@@ -97,6 +97,7 @@ def load() -> ctypes.CDLL:
     lib.vecattn_cache_size.argtypes = [C, ctypes.POINTER(ctypes.c_size_t)]
     lib.vecattn_cache_write.argtypes = [P, D, P, D, C, P, i64, P, P, P]
     lib.vecattn_cache_read.argtypes = [C, P, i64, P, i64, P, D, P, D, P]
+    lib.vecattn_cache_read_whole.argtypes = [C, P, i64, P, i64, P, D, P, D, P]
     lib.vecattn_cache_attn_workspace_size.argtypes = [D, C, i64, i64, i64,
                                                       ctypes.POINTER(ctypes.c_size_t)]
     lib.vecattn_cache_attn.argtypes = [P, D, C, P, i64, P, P, i64, i64, f32, P, D, P, P,
@@ -123,6 +124,7 @@ def load() -> ctypes.CDLL:
                  "vecattn_head_sparsity", "vecattn_recall", "vecattn_select_noalloc",
                  "vecattn_sparse_attn_ordered", "vecattn_attn_order", "vecattn_window_attn",
                  "vecattn_cache_size", "vecattn_cache_write", "vecattn_cache_read",
+                 "vecattn_cache_read_whole",
                  "vecattn_cache_attn_workspace_size", "vecattn_cache_attn",
                  "vecattn_cache_mass_workspace_size", "vecattn_cache_mass",
                  "vecattn_cache_keep_workspace_size", "vecattn_cache_keep", "vecattn_cache_gather",
@@ -667,15 +669,17 @@ def cache_read(cache: Cache, table: torch.Tensor, lens: torch.Tensor, n: int, st
     B = table.shape[0]
     dev = _cache_args(cache, table, lens, B)
     shape = (B, cache.heads, n, cache.dim)
+    read = load().vecattn_cache_read
     if out is None:
-        out = tuple(torch.zeros(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
+        out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=dev) for _ in range(2))
+        read = load().vecattn_cache_read_whole
     k, v = out
     for t, name in ((k, "k"), (v, "v")):
         _bf16_cuda(t, name)
         if t.shape != shape:
             raise ValueError("out must be a pair of [B, heads, n, dim] tensors")
     _same_device(dev, k=k, v=v)
-    _call(dev, "cache_read", load().vecattn_cache_read,
+    _call(dev, "cache_read", read,
           cache.desc(), table.data_ptr(), table.shape[1], lens.data_ptr(), int(start),
           k.data_ptr(), _tdesc(k.shape, k.stride()), v.data_ptr(), _tdesc(v.shape, v.stride()))
     return k, v

@@ -269,7 +269,7 @@ template <int D, int BITS>
 __global__ __launch_bounds__(256) void k_cache_read(
     PageMap map, const int32_t* __restrict__ lens, int64_t start, int64_t n,
     uint16_t* __restrict__ k, int64_t k_sB, int64_t k_sH, int64_t k_sN, uint16_t* __restrict__ v,
-    int64_t v_sB, int64_t v_sH, int64_t v_sN) {
+    int64_t v_sB, int64_t v_sH, int64_t v_sN, bool clear) {
   using L = CacheLayout<D, BITS>;
   constexpr int CH = D / 8;
   constexpr int RPP = 256 / CH;
@@ -278,8 +278,22 @@ __global__ __launch_bounds__(256) void k_cache_read(
   const int64_t len = min(max(lens[b], 0), 1 << 30);
   const int64_t jb = (start >> 5) + blockIdx.x;
   const int64_t j0 = jb * kCacheBlock;
-  if (j0 >= len) return;
-  const uint8_t* blk = block_ptr<L::kBytes>(map, b, h, jb);
+  const int c = threadIdx.x % CH;
+  auto k_row = [&](int64_t r) __attribute__((always_inline)) {
+    return reinterpret_cast<u32x4*>(k + b * k_sB + h * k_sH + r * k_sN + 8 * c);
+  };
+  auto v_row = [&](int64_t r) __attribute__((always_inline)) {
+    return reinterpret_cast<u32x4*>(v + b * v_sB + h * v_sH + r * v_sN + 8 * c);
+  };
+  const uint8_t* blk = j0 < len ? block_ptr<L::kBytes>(map, b, h, jb) : nullptr;
+  if (clear) {   // rows of tokens that are not held
+#pragma unroll
+    for (int pass = 0; pass < kCacheBlock / RPP; ++pass) {
+      const int64_t j = j0 + pass * RPP + threadIdx.x / CH, r = j - start;
+      if (r < 0 || r >= n || (blk && j < len)) continue;
+      *k_row(r) = *v_row(r) = u32x4{0, 0, 0, 0};
+    }
+  }
   if (!blk) return;
   __shared__ uint8_t codes[kCacheBlock][D];  // V's, token-major
   for (int it = threadIdx.x; it < 4 * D; it += 256) {
@@ -295,7 +309,6 @@ __global__ __launch_bounds__(256) void k_cache_read(
     for (int e = 0; e < 8; ++e) codes[(e >> 2) * 16 + 4 * g + (e & 3)][d] = static_cast<uint8_t>(u[e]);
   }
   __syncthreads();
-  const int c = threadIdx.x % CH;
 #pragma unroll
   for (int pass = 0; pass < kCacheBlock / RPP; ++pass) {
     const int key = pass * RPP + threadIdx.x / CH;
@@ -309,11 +322,11 @@ __global__ __launch_bounds__(256) void k_cache_read(
       dw[x] = *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + x, l));
     unpack8<BITS>(dw, u);
     const int gi = key * L::kG + c / 8;
-    *reinterpret_cast<u32x4*>(k + b * k_sB + h * k_sH + r * k_sN + 8 * c) =
+    *k_row(r) =
         values8(reinterpret_cast<const uint32_t*>(blk + L::kCodes)[gi], u);
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] = codes[key][8 * c + e];
-    *reinterpret_cast<u32x4*>(v + b * v_sB + h * v_sH + r * v_sN + 8 * c) =
+    *v_row(r) =
         values8(reinterpret_cast<const uint32_t*>(blk + L::kHalf + L::kCodes)[gi], u);
   }
 }
@@ -488,14 +501,14 @@ hipError_t launch_cache_write(const Tensor4& k, const Tensor4& v, const CacheArg
 }
 
 hipError_t launch_cache_read(const CacheArgs& c, int64_t start, const Tensor4& k, const Tensor4& v,
-                             hipStream_t stream) {
+                             bool clear, hipStream_t stream) {
   const int64_t blocks = (start + k.N + kCacheBlock - 1) / kCacheBlock - start / kCacheBlock;
   const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(k.H),
                   static_cast<unsigned>(k.B));
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, page_map(c), c.lens, start, k.N,
                        static_cast<uint16_t*>(const_cast<void*>(k.ptr)), k.sB, k.sH, k.sN,
-                       static_cast<uint16_t*>(const_cast<void*>(v.ptr)), v.sB, v.sH, v.sN);
+                       static_cast<uint16_t*>(const_cast<void*>(v.ptr)), v.sB, v.sH, v.sN, clear);
   };
   if (c.D == 128) c.bits == 4 ? run(k_cache_read<128, 4>) : run(k_cache_read<128, 8>);
   else c.bits == 4 ? run(k_cache_read<64, 4>) : run(k_cache_read<64, 8>);

@@ -143,8 +143,9 @@ struct CacheArgs {
 };
 hipError_t launch_cache_write(const Tensor4& k, const Tensor4& v, const CacheArgs& c,
                               const int32_t* n_new, hipStream_t stream);
+// clear: rows of tokens that are not held become 0.
 hipError_t launch_cache_read(const CacheArgs& c, int64_t start, const Tensor4& k, const Tensor4& v,
-                             hipStream_t stream);
+                             bool clear, hipStream_t stream);
 
 // Attention over the cache.  How the work is dealt out, and so the workspace,
 // follows from the shape.

@@ -612,17 +612,31 @@ vecattn_status vecattn_cache_write(const void* k, const vecattn_tdesc* kd, const
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 
-vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* table, int64_t cols,
-                                  const int32_t* lens, int64_t start, void* k,
-                                  const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
-                                  void* stream) {
+static vecattn_status read_cache(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                 const int32_t* lens, int64_t start, void* k,
+                                 const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
+                                 bool clear, void* stream) {
   vecattn_status st = check_cache_rows(k, kd, v, vd, cache, table, cols, lens);
   if (st != VECATTN_OK) return st;
   if (start < 0 || start > kMaxN) return VECATTN_ERR_INVALID_ARG;
   hipError_t e = vecattn::launch_cache_read(to_cache(cache, table, cols, lens), start,
-                                            to_tensor(k, kd), to_tensor(v, vd),
+                                            to_tensor(k, kd), to_tensor(v, vd), clear,
                                             static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_read(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                  const int32_t* lens, int64_t start, void* k,
+                                  const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
+                                  void* stream) {
+  return read_cache(cache, table, cols, lens, start, k, kd, v, vd, false, stream);
+}
+
+vecattn_status vecattn_cache_read_whole(const vecattn_cache* cache, const int32_t* table,
+                                        int64_t cols, const int32_t* lens, int64_t start, void* k,
+                                        const vecattn_tdesc* kd, void* v, const vecattn_tdesc* vd,
+                                        void* stream) {
+  return read_cache(cache, table, cols, lens, start, k, kd, v, vd, true, stream);
 }
 
 vecattn_status vecattn_cache_attn_workspace_size(const vecattn_tdesc* qd,

@@ -348,6 +348,25 @@ def test_a_layer_with_eviction(gpu):
         assert torch.equal(o1, got) and torch.equal(state, weights)
 
 
+@pytest.mark.parametrize("D,bits,page", [(128, 4, 64), (64, 8, 32)])
+@pytest.mark.parametrize("start", [0, 5, 70])
+def test_reading_back_whole(gpu, D, bits, page, start):
+    """Outputs that the call makes are 0 wherever no token is held, whatever memory they get."""
+    lens = [100, 1, 0, 193]
+    k = rows(1, 4, 2, 193, D)
+    table, pages = paged(lens, page)
+    cache = fresh_cache(pages, 2, D, page, bits)
+    va.cache_write(cache, k, k, table, int32(lens), n_new=int32(lens))
+    table[3, 1] = -1
+    for n in (1, 33, 250):
+        want = [torch.zeros(4, 2, n, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        va.cache_read(cache, table, int32(lens), n, start=start, out=tuple(want))
+        junk = [torch.full_like(want[0], 7.0) for _ in range(2)]
+        del junk
+        for a, b in zip(va.cache_read(cache, table, int32(lens), n, start=start), want):
+            assert torch.equal(a, b)
+
+
 def test_calls_at_once_give_what_they_give_alone(gpu):
     ks, cache, table, q, lse = setup(128, 4, 64, [9000, 3000], 4, 7, 1)
     lens = int32([9000, 3000])
