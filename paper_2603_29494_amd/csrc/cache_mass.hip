@@ -4,8 +4,17 @@
 //
 // A key is m + s u per group of 64 values (cache_common.h), q . k = sum_G s_G (q_G . u_G)
 // + m_G sum(q_G): the codes go into the matrix instructions as small fp16 numbers,
-// exactly, and rows of q as fp16 times a power of two, so that only fp32 sums round.
-// A token belongs to one wave, which adds its rows in one order: no atomics.
+// exactly, and rows of q as fp16 times a power of two (many rows: both as bf16), so that
+// only fp32 sums round.  A token belongs to one wave, which adds its rows in one order: no
+// atomics.
+//
+// Few rows are bound by reading K's half of the cache: four sequences of 131072 tokens in 4
+// bits, 4 heads of 128, 7 rows each: 35 us, 4.8 TB/s.  Many rows by the matrix products and
+// the exponentials, whose times add: 512 tokens of 28 heads over 33280 in 8 bits, 4 heads:
+// 178 us, 690 TFLOP/s (190 with rows of q in fp16 and their powers of two applied to every
+// score).  How many workgroups there are counts there, three fit a CU at a time: 1040 take
+// 178 us, 768 take 127.  Rows split among three workgroups, with a launch that joins their
+// sums, took 185 us against 190 for these and 77 against 92 for 8192 tokens.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -214,15 +223,15 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   }
 }
 
-// More rows, in tiles of 32, brought once into the form in which the products take them:
-// fp16 times a power of two, the sums over each group's values, and what takes a product
-// to a weight.
+// More rows, in tiles of 32, brought once into the form in which the products take them: as
+// they are, and with what starts their scores (in log2 units), the sums over each group's
+// values and less the lse.  bf16 is their own type and holds codes of 8 bits exactly.
 template <int D>
 struct RowTile {
   static constexpr int kRowBytes = 2 * D + 16;   // rows 16 bytes apart in the banks
   uint8_t q[32 * kRowBytes];
-  u32x4 sums[32];                // of each group as three bf16 that add up to it; 0, 0
-  float to_log2[32], off[32];    // off: the row's lse, in log2 units; inf where it weighs nothing
+  u32x4 start[2][32];   // as three bf16 that add up to them: each group's sum; less the lse
+  float off[32];        // the lse; inf where the row weighs nothing
 };
 
 // One tile per workgroup, eight threads a row.
@@ -240,61 +249,47 @@ __global__ __launch_bounds__(256) void k_mass_rows(const MassParams a, RowTile<D
   const int tok = row / a.group, hq = h * a.group + row % a.group;
   const float lse = row < s.rows ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
   const bool have = lse != kNegInf;
-  u32x4 raw[C];
-  float top = 0x1p-100f, sum[C];
+  float sum[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    raw[c] = u32x4{0, 0, 0, 0};
+    u32x4 x = {0, 0, 0, 0};
     if (have)
-      raw[c] = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN +
-                                               8 * (c * 8 + sc));
+      x = *reinterpret_cast<const u32x4*>(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN +
+                                          8 * (c * 8 + sc));
+    *reinterpret_cast<u32x4*>(to.q + sr * RowTile<D>::kRowBytes + 16 * (c * 8 + sc)) = x;
     sum[c] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float lo = low_of(raw[c][e]), hi = high_of(raw[c][e]);
-      top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
-      sum[c] += lo + hi;
-    }
+    for (int e = 0; e < 4; ++e) sum[c] += low_of(x[e]) + high_of(x[e]);
   }
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) {
-    top = fmaxf(top, __shfl_xor(top, o));
+  for (int o = 1; o < 8; o <<= 1)
 #pragma unroll
     for (int c = 0; c < C; ++c) sum[c] += __shfl_xor(sum[c], o);   // chunks c hold group c
-  }
-  // The largest value between 2^14 and 2^15 (cache_rows.h).
-  const int k = 15 - __builtin_amdgcn_frexp_expf(top);
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    u32x4 y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      y[e] = to_f16(__builtin_amdgcn_ldexpf(low_of(raw[c][e]), k),
-                    __builtin_amdgcn_ldexpf(high_of(raw[c][e]), k));
-    *reinterpret_cast<u32x4*>(to.q + sr * RowTile<D>::kRowBytes + 16 * (c * 8 + sc)) = y;
-  }
   if (sc > 0) return;
-  uint32_t part[6] = {};
-#pragma unroll
-  for (int c = 0; c < C; ++c) {
-    float x = __builtin_amdgcn_ldexpf(sum[c], k - kCodeExp<BITS>);
+  const float off = have ? lse * kLog2e : INFINITY;
+  uint32_t part[9] = {};
+  auto cut = [&](float x, int at) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       const uint32_t bits = __float_as_uint(x) & 0xFFFF0000u;   // eight leading bits
-      part[3 * c + i] = bits >> 16;
+      part[at + i] = bits >> 16;
       x = (bits & 0x7F800000u) == 0x7F800000u ? 0.0f : x - __uint_as_float(bits);
     }
-  }
-  to.sums[sr] = u32x4{part[0] | part[1] << 16, part[2] | part[3] << 16, part[4] | part[5] << 16, 0u};
-  to.to_log2[sr] = a.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, kCodeExp<BITS> - k);
-  to.off[sr] = have ? lse * kLog2e : INFINITY;
+  };
+#pragma unroll
+  for (int c = 0; c < C; ++c) cut(sum[c] * a.scale_log2, 3 * c);
+  cut(-off, 6);
+  to.start[0][sr] = u32x4{part[0] | part[1] << 16, part[2] | part[3] << 16, part[4] | part[5] << 16, 0u};
+  to.start[1][sr] = u32x4{part[6] | part[7] << 16, part[8], 0u, 0u};
+  to.off[sr] = off;
 }
 
-// A block of 32 tokens per wave stays in registers as fp16 codes, and the row tiles pass by
+// A block of 32 tokens per wave stays in registers as bf16 codes, and the row tiles pass by
 // in LDS, fetched two ahead by the workgroup's four waves.  v_mfma_f32_32x32x16 (lane l =
 // 32 g + n): A: token n, head-dim values 16 st + 8 g + 0..7; B: row n, the same; C: row n,
-// tokens 8 (e / 4) + 4 g + e % 4.  The m_G sum(q_G) terms start the sums, m_G being bf16 as
-// it is.  Row tiles that see all of the workgroup's tokens, most of them, pass without
+// tokens 8 (e / 4) + 4 g + e % 4.  The m_G sum(q_G) terms and the lse start the sums, m_G
+// being bf16 as it is; what is left per score is a product and sum for each group, an exp2
+// and its sum.  Row tiles that see all of the workgroup's tokens, most of them, pass without
 // masks, in a loop of their own.
 template <int D, int BITS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k_mass_many(
@@ -345,8 +340,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   // A block that no page holds passes as zeros, and its sums are left out at the end.
   const uint8_t* blk =
       j0 < s.end ? keys_of<L::kBytes>(a, page_of(a, b, jb), h, jb) : nullptr;
-  bf16x8 low = {};
-  f16x8 codes[ST];
+  bf16x8 low = {}, codes[ST];
   float step_of[G][16], w[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) w[e] = 0.0f;
@@ -359,10 +353,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
 #pragma unroll
     for (int y = 0; y < DW; ++y)
       u[y] = blk ? *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + y, from)) : 0u;
-    codes[st] = __builtin_bit_cast(f16x8, codes_f16<BITS>(u));
+    u32x4 x = codes_16<BITS>(u);
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      x[y] = __float_as_uint(static_cast<float>(x[y] & 0xFFu)) >> 16 |
+             (__float_as_uint(static_cast<float>(x[y] >> 16)) & 0xFFFF0000u);
+    codes[st] = __builtin_bit_cast(bf16x8, x);
   }
   const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + L::kCodes);
-  if (blk && g == 0) {
+  if (blk && g == 1) {
+    low = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F80u, 0u, 0u});   // 1, 1, 1
+  } else if (blk) {
     const uint32_t m0 = par[n * G] & 0xFFFFu, m1 = G > 1 ? par[n * G + G - 1] & 0xFFFFu : 0u;
     low = __builtin_bit_cast(bf16x8, u32x4{m0 | m0 << 16, m0 | m1 << 16, m1 | m1 << 16, 0u});
   }
@@ -370,7 +371,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   for (int e = 0; e < 16; ++e)
 #pragma unroll
     for (int gi = 0; gi < G; ++gi)
-      step_of[gi][e] = blk ? high_of(par[(8 * (e / 4) + 4 * g + e % 4) * G + gi]) : 0.0f;
+      step_of[gi][e] = blk ? a.scale_log2 * high_of(par[(8 * (e / 4) + 4 * g + e % 4) * G + gi]) : 0.0f;
 
   int st = 0;
   auto turn = [&](int t, auto masked_tag) __attribute__((always_inline)) {
@@ -380,26 +381,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
     fetch(min(t + 2, ntiles - 1), st == 0 ? 2 : st - 1);
     const Tile& tile = *reinterpret_cast<const Tile*>(ring[st]);
     st = st == 2 ? 0 : st + 1;
-    const u32x4 sums = tile.sums[n];   // the low half of A's slots is 0 for g = 1
-    const float to_log2 = tile.to_log2[n], off = tile.off[n];
+    const u32x4 first_terms = tile.start[g][n];
     const uint8_t* qrow = tile.q + n * Tile::kRowBytes + 16 * g;
     const f32x16 start = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-        low, __builtin_bit_cast(bf16x8, sums), f32x16{}, 0, 0, 0);
+        low, __builtin_bit_cast(bf16x8, first_terms), f32x16{}, 0, 0, 0);
     f32x16 acc[G];
 #pragma unroll
     for (int gi = 0; gi < G; ++gi) acc[gi] = f32x16{};
 #pragma unroll
     for (int st = 0; st < ST; ++st)
-      acc[st / 4] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-          codes[st], __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4*>(qrow + 32 * st)),
+      acc[st / 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          codes[st], __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(qrow + 32 * st)),
           acc[st / 4], 0, 0, 0);
-    const int pos = off == INFINITY ? -1 : s.p_first + (32 * t + n) / a.group;
+    const int pos = tile.off[n] == INFINITY ? -1 : s.p_first + (32 * t + n) / a.group;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       float y = start[e];
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) y = __builtin_fmaf(step_of[gi][e], acc[gi][e], y);
-      y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
+      y = __builtin_amdgcn_exp2f(y);
       if constexpr (decltype(masked_tag)::value) {
         const int j = j0 + 8 * (e / 4) + 4 * g + e % 4;
         y = j <= pos && (j > pos - a.window || j < a.sinks) ? y : 0.0f;
@@ -481,7 +481,7 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
     constexpr int D = decltype(dim)::value, BITS = decltype(bits)::value;
     if (rows <= kFewRows) {
       // Two workgroups per place on the CUs, so that unequal lengths even out (4 x 131072
-      // tokens, 4 heads: 46 us; 45 with half of them, 49 with twice as many).
+      // tokens, 4 heads: 35 us, also with half of them; 38 with twice as many).
       const int64_t fill = std::max<int64_t>(1, 2048 / heads);
       const int64_t groups = std::min((blocks + 3) / 4, fill);
       if (rows <= 8) launch(k_mass_few<D, BITS, true>, groups);
