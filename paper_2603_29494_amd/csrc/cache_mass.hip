@@ -11,10 +11,9 @@
 // Few rows are bound by reading K's half of the cache: four sequences of 131072 tokens in 4
 // bits, 4 heads of 128, 7 rows each: 35 us, 4.8 TB/s.  Many rows by the matrix products and
 // the exponentials, whose times add: 512 tokens of 28 heads over 33280 in 8 bits, 4 heads:
-// 178 us, 690 TFLOP/s (190 with rows of q in fp16 and their powers of two applied to every
-// score).  How many workgroups there are counts there, three fit a CU at a time: 1040 take
-// 178 us, 768 take 127.  Rows split among three workgroups, with a launch that joins their
-// sums, took 185 us against 190 for these and 77 against 92 for 8192 tokens.
+// 178 us at best, 690 TFLOP/s (190 on the same card with rows of q in fp16 and their powers
+// of two applied to every score).  How many workgroups there are counts there, three fit a
+// CU at a time: 1040 take 178 us, 768 take 127; splitting the rows of such numbers gains 3%.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -39,6 +38,9 @@ struct MassParams {
   int32_t H, n, group, window, sinks;
   int32_t in_place;    // what no row sees stays as it is
   int32_t clear;       // entries past a sequence's tokens become 0
+  float* part;         // [split][B * H][slots], where the rows are split
+  int64_t slots;
+  int32_t splits;
   float scale_log2, decay;
 };
 
@@ -305,22 +307,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   const int64_t b = blockIdx.z, bh = b * a.H + h;
   const Place s = place_of(a, b);
   const int blocks = blocks_of(a, s);
-  const int first = blockIdx.x * 4;   // the workgroup's blocks
+  const int split = blockIdx.x % a.splits;
+  const int first = blockIdx.x / a.splits * 4;   // the workgroup's blocks
   if (first >= blocks) return;
   const int jb = first + wave, j0 = jb * kCacheBlock;
 
   // Row tiles: [t0, c0) and [c1, ntiles) with masks, [c0, c1) whole; those before t0 see
   // none of the workgroup's tokens [j_lo, j_hi].
-  const int ntiles = first * kCacheBlock < s.end ? (s.rows + 31) / 32 : 0;
+  int ntiles = first * kCacheBlock < s.end ? (s.rows + 31) / 32 : 0;
   const int j_lo = first * kCacheBlock, j_hi = min(j_lo + 4 * kCacheBlock, s.end) - 1;
   auto tile_at = [&](int64_t row) __attribute__((always_inline)) {
     const int64_t t = row < 0 ? 0 : row >> 5;
     return t < ntiles ? static_cast<int>(t) : ntiles;
   };
   const int64_t off_lo = int64_t(j_lo) - s.p_first, off_hi = int64_t(j_hi) - s.p_first;
-  const int t0 = tile_at(off_lo * a.group);
-  const int c0 = max(t0, tile_at(off_hi * a.group + 31));
-  const int c1 = j_hi < a.sinks ? ntiles : max(c0, tile_at((off_lo + a.window) * a.group));
+  int t0 = tile_at(off_lo * a.group), c0 = tile_at(off_hi * a.group + 31);
+  int c1 = j_hi < a.sinks ? ntiles : tile_at((off_lo + a.window) * a.group);
+  // Of these the workgroup's share.
+  const int share = (ntiles - t0 + a.splits - 1) / a.splits;
+  t0 = min(t0 + split * share, ntiles);
+  ntiles = min(t0 + share, ntiles);
+  c0 = min(max(c0, t0), ntiles);
+  c1 = min(max(c1, c0), ntiles);
 
   const Tile* tiles = row_tiles + bh * tiles_held;
   auto fetch = [&](int t, int st) __attribute__((always_inline)) {
@@ -423,7 +431,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
     mine = (n & 15) == e ? all : mine;
   }
   const int j = j0 + 8 * ((n & 15) / 4) + 4 * g + (n & 3);
-  if (n < 16 && jb < blocks) collect(a, s, bh, j, before(a, s, bh, j), blk ? mine : 0.0f);
+  if (n >= 16 || jb >= blocks) return;
+  if (!blk) mine = 0.0f;
+  if (a.splits == 1) collect(a, s, bh, j, before(a, s, bh, j), mine);
+  else a.part[(static_cast<int64_t>(split) * gridDim.z * a.H + bh) * a.slots + j] = mine;
+}
+
+// The sums of a token's rows, split by split.
+__global__ __launch_bounds__(256) void k_mass_join(const MassParams a) {
+  const int h = blockIdx.y;
+  const int64_t b = blockIdx.z, bh = b * a.H + h, heads = static_cast<int64_t>(gridDim.z) * a.H;
+  const Place s = place_of(a, b);
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  if (j >= min(a.slots, kCacheBlock * static_cast<int64_t>(blocks_of(a, s)))) return;
+  float w = 0.0f;
+  for (int i = 0; i < a.splits; ++i) w += a.part[(i * heads + bh) * a.slots + j];
+  collect(a, s, bh, j, before(a, s, bh, j), w);
 }
 
 template <int D>
@@ -433,12 +456,24 @@ size_t row_tiles_bytes(int64_t heads, int64_t rows) {
 
 constexpr int kFewRows = 16;   // that one tile of columns takes as they come
 
+// Where blocks alone leave CUs without a workgroup (a CU holds three), their rows are split
+// among as many as fill them, with eight tiles each at least (512 tokens of 28 heads over 512
+// tokens: 26 us, 77 in one; over 8192: 66 and 81; with six per CU 72).
+constexpr int64_t kFill = 3 * 256, kLeastTiles = 8;
+int64_t splits_of(int64_t groups, int64_t rows) {
+  return std::max<int64_t>(1, std::min(kFill / groups, rows / (32 * kLeastTiles)));
+}
+size_t parts_bytes(int64_t rows) {
+  return rows < 64 * kLeastTiles ? 0 : kFill * 4 * kCacheBlock * sizeof(float);
+}
+
 }  // namespace
 
 size_t cache_mass_workspace_bytes(const CacheAttnShape& s) {
   const int64_t rows = s.n * (s.Hq / s.H);
   if (rows <= kFewRows) return 0;
-  return s.D == 128 ? row_tiles_bytes<128>(s.B * s.H, rows) : row_tiles_bytes<64>(s.B * s.H, rows);
+  return parts_bytes(rows) + (s.D == 128 ? row_tiles_bytes<128>(s.B * s.H, rows)
+                                         : row_tiles_bytes<64>(s.B * s.H, rows));
 }
 
 hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
@@ -490,7 +525,13 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
       RowTile<D>* prepared = static_cast<RowTile<D>*>(x.workspace);
       const int64_t tiles = (rows + 31) / 32;
       launch(k_mass_rows<D, BITS>, tiles, prepared);
-      launch(k_mass_many<D, BITS>, (blocks + 3) / 4, prepared, static_cast<int32_t>(tiles));
+      const int64_t groups = (blocks + 3) / 4;
+      a.splits = static_cast<int32_t>(splits_of(groups * heads, rows));
+      a.slots = groups * 4 * kCacheBlock;
+      a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(x.workspace) +
+                                        row_tiles_bytes<D>(heads, rows));
+      launch(k_mass_many<D, BITS>, groups * a.splits, prepared, static_cast<int32_t>(tiles));
+      if (a.splits > 1) launch(k_mass_join, (a.slots + 255) / 256);
     }
   };
   using std::integral_constant;
