@@ -12,8 +12,13 @@
 // A wave takes a token and walks over its heads, q's and then k's; a lane computes the
 // angle of one pair, and the others read it from LDS.  Where rows of a head lie beside
 // each other (head-major tensors) its rows are consecutive tokens of one head instead, and
-// every thread computes the angles that it needs, for all heads.  A thread holds 32 bytes of a row: 16-byte chunks c and c + half of the turned values,
-// which are partners in the half layout.
+// every thread computes the angles that it needs, for all heads.  A thread holds 32 bytes
+// of a row: 16-byte chunks c and c + half of the turned values, which are partners in the
+// half layout.
+//
+// Bound by memory, 131072 tokens of 28 + 4 heads of 128: 377 us, 5.7 TB/s; 75600 of 40 + 40:
+// 606 us, 5.1 TB/s.  With each thread computing the angles of its own pairs these took 487
+// and 650.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
