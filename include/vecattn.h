@@ -585,8 +585,8 @@ vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const 
                                   const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                   const int32_t* lens, const int32_t* n_new, int64_t window,
                                   int64_t sinks, float scale, float decay, const float* mass,
-                                  float* out, int64_t M, int32_t flags, void* workspace, size_t workspace_bytes,
-                                  void* stream);
+                                  float* out, int64_t M, int32_t flags, void* workspace,
+                                  size_t workspace_bytes, void* stream);
 
 /*
  * Which tokens of each sequence and head a budget keeps.  Candidates are the tokens
@@ -632,9 +632,9 @@ vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
  *          index outside [0, M)), the rest left as it was.  Both or neither.
  *   flags : 0 or VECATTN_CLEAR_PADDING (of mass_out)
  * Asynchronous, one launch.
- * Errors: INVALID_ARG (null pointer, other flags, one of mass and mass_out alone, B < 1, budget or M
- * < 1 or > 2^30, caches of other heads, D or bits, a bad cache, cols or to_cols < 1 or
- * more than 2^30 tokens); UNSUPPORTED (more than 65535 sequences or heads).
+ * Errors: INVALID_ARG (null pointer, other flags, one of mass and mass_out alone, B < 1,
+ * budget or M < 1 or > 2^30, caches of other heads, D or bits, a bad cache, cols or to_cols
+ * < 1 or more than 2^30 tokens); UNSUPPORTED (more than 65535 sequences or heads).
  */
 vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                     int64_t B, const int32_t* idx, const int32_t* kept,
@@ -664,9 +664,10 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
  * depend on the order of execution (no atomics).  What a call does follows lens, mask and
  * n_q on the device, so that a captured call can be replayed as they change.
  * Errors: INVALID_ARG (null pointer, shape mismatch, Hq % Hkv != 0, mask_sB < 0, a bad
- * scale, other flags, an output whose sequences or heads share memory, misalignment); CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128},
- * Nq * Hq / Hkv > 2^30, more than 2^24 sequences times Hkv, about 2^23 workgroups, a K or
- * V row stride of 2^24 elements or more).
+ * scale, other flags, an output whose sequences or heads share memory, misalignment);
+ * CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128}, Nq * Hq / Hkv > 2^30, more
+ * than 2^24 sequences times Hkv, about 2^23 workgroups, a K or V row stride of 2^24 elements
+ * or more).
  */
 vecattn_status vecattn_cross_attn_workspace_size(const vecattn_tdesc* qd, const vecattn_tdesc* kd,
                                                  size_t* bytes);
@@ -745,8 +746,8 @@ vecattn_status vecattn_rope_ladder(int32_t rot, double base, int32_t scaling, do
  * Errors: INVALID_ARG (null pointer, shape mismatch, both pos and lens, |start| > 2^30,
  * a bad stride, a spec outside what its comments allow, a factor or frequency that is not
  * finite, |frequency| > 1024, an output that is its input with other strides or whose
- * sequences or heads share memory (a stride of 0), misalignment); UNSUPPORTED (D not in {64, 128}, more than 65535 heads in all, B * N >
- * 2^30).
+ * sequences or heads share memory (a stride of 0), misalignment); UNSUPPORTED (D not in
+ * {64, 128}, more than 65535 heads in all, B * N > 2^30).
  */
 vecattn_status vecattn_rope(const void* q, const vecattn_tdesc* qd, const void* k,
                             const vecattn_tdesc* kd, const vecattn_rope_spec* spec,
