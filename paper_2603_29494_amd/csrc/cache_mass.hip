@@ -503,8 +503,7 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
   a.scale_log2 = scale * kLog2e;
   a.decay = x.decay;
   const int64_t rows = static_cast<int64_t>(a.n) * a.group;
-  const int64_t entries = x.clear ? x.M : std::min(x.M, c.cols * c.page);
-  const int64_t blocks = (entries + kCacheBlock - 1) / kCacheBlock;
+  const int64_t blocks = (x.M + kCacheBlock - 1) / kCacheBlock;
   const int64_t heads = x.q.B * c.H;
   auto launch = [&](auto kernel, int64_t groups, auto... more) {
     hipLaunchKernelGGL(kernel,

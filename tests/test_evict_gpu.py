@@ -134,6 +134,24 @@ def test_mass_window_padding_and_missing_pages(gpu, group, n, window, sinks):
             assert torch.equal(got[b, :, L:], (old if inplace else torch.full_like(old, -7.0))[b, :, L:])
 
 
+@pytest.mark.parametrize("group,n", [(3, 2), (3, 40), (8, 160)])
+def test_mass_of_tokens_past_the_table(gpu, group, n):
+    """Tokens that the table has no column for are held nowhere: what they had collected decays."""
+    lens, held = [500, 700], 256
+    ks, cache, table, _, _ = setup(64, 8, 32, lens, 2, group, n, 7)
+    table = table[:, :held // 32].contiguous()
+    q = rows(11, 2, 2 * group, n, 64)
+    _, lse = va.cache_attn(q, cache, table, int32(lens), return_lse=True)
+    hidden = [torch.arange(L) >= held for L in lens]
+    old = torch.rand(2, 2, 640, generator=torch.Generator().manual_seed(3)).cuda()
+    out = torch.full_like(old, -7.0)
+    va.cache_mass(q, lse, cache, table, int32(lens), mass=old, decay=0.5, out=out)
+    full = torch.cat([old.cpu(), torch.zeros(2, 2, 60)], 2)
+    refs = mass64(q, lse, ks, 8, lens, full, decay=0.5, hidden=hidden)
+    check_mass(out, [(b, h, min(L, 640), t[:640], e[:640]) for b, h, L, t, e in refs])
+    assert (out[0, :, 500:] == -7.0).all()
+
+
 def test_mass_adds_up_to_the_rows(gpu):
     """A row's weights sum to one: over all tokens the sums are the number of rows."""
     lens, n, group = [5000, 800], 20, 4
