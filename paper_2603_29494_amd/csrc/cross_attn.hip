@@ -741,9 +741,12 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
   }
   // Many rows: parts and their join cost about as much as 512 keys, so the keys are cut only
   // where row tiles leave half of the CUs without one (8 tiles over 16384 keys: 24 us in 32
-  // chunks, 324 in one; 200 tiles over 1200: 31 in one, 44 in two; 512 over 4096: 150 and
-  // 178).
-  const int64_t chunks = units > 128 ? 1 : std::max<int64_t>(1, std::min(Nk / 512, 512 / units));
+  // chunks, 324 in one), or, of many keys, all CUs without a second (in three chunks; 130
+  // tiles over 4096 keys: 60 us, 84 in one; 256 over 16384: 351 and 412; but 200 over 4096: 94
+  // and 90, 320 over 4096: 143 and 138).
+  const int64_t chunks = units <= 128   ? std::max<int64_t>(1, std::min(Nk / 512, 512 / units))
+                         : units <= 256 ? (Nk >= 24 * units ? 3 : 1)
+                                        : 1;
   d.chunk = static_cast<int32_t>(((Nk + chunks - 1) / chunks + 127) / 128 * 128);
   d.chunks = static_cast<int32_t>((Nk + d.chunk - 1) / d.chunk);
   d.items = units * d.chunks;

@@ -583,7 +583,7 @@ vecattn_status vecattn_window_attn(const void* q, const vecattn_tdesc* qd, const
   if (qd->B > kMaxGridYZ || qd->H > kMaxGridYZ ||
       qd->B * qd->H * num_blocks(qd->N, vecattn::kWindowRows) > (int64_t(1) << 23))
     return VECATTN_ERR_UNSUPPORTED;
-  // A tile's 64 rows are addressed with 32-bit byte offsets.
+  // A tile's rows are addressed with 32-bit byte offsets.
   if (kd->N > 1 && (kd->sN >= (int64_t(1) << 24) || vd->sN >= (int64_t(1) << 24)))
     return VECATTN_ERR_UNSUPPORTED;
   vecattn::WindowArgs a{to_tensor(q, qd), to_tensor(k, kd), to_tensor(v, vd), o, od->sB, od->sH,
@@ -781,7 +781,7 @@ vecattn_status vecattn_cross_attn(const void* q, const vecattn_tdesc* qd, const 
   if (!same_shape(vd, kd) || !same_shape(od, qd) || shares_rows(od)) return VECATTN_ERR_INVALID_ARG;
   if (mask_sB < 0 || !std::isfinite(scale) || scale < 0.0f || !flags_ok(flags))
     return VECATTN_ERR_INVALID_ARG;
-  // A tile's 64 rows are addressed with 32-bit byte offsets.
+  // A tile's rows are addressed with 32-bit byte offsets.
   if (kd->N > 1 && (kd->sN >= (int64_t(1) << 24) || vd->sN >= (int64_t(1) << 24)))
     return VECATTN_ERR_UNSUPPORTED;
   const size_t need = vecattn::cross_attn_workspace_bytes(qd->B, qd->H, kd->H, qd->N, kd->N, qd->D);

@@ -61,6 +61,17 @@ def test_against_the_formula(gpu, D, Hq, Hkv, Nq, Nk):
     ref.check(o, lse, cross64(q, k, v))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_row_tiles_over_many_keys(gpu, D):
+    """More row tiles than half of the CUs and keys enough to be cut, some lengths within the first
+    piece."""
+    B, H, Nq, Nk = 16, 9, 37, 3500
+    q, k, v = rows(21, B, H, Nq, D), rows(22, B, H, Nk, D), rows(23, B, H, Nk, D)
+    lens = [3500, 0, 1, 3499, 1167, 1280, 1281, 2560, 2561, 3000] + [3500] * 6
+    o, lse = va.cross_attn(q, k, v, lens=int32(lens), return_lse=True)
+    ref.check(o, lse, cross64(q, k, v, lens=lens))
+
+
 @pytest.mark.parametrize("D,Hq,Hkv", [(64, 4, 4), (128, 6, 2)])
 @pytest.mark.parametrize("Nq", [1, 7, 50, 200])
 @pytest.mark.parametrize("Nk", [45, 700, 2100])
