@@ -110,10 +110,10 @@ __device__ __forceinline__ void collect(const MassParams& a, const Place& s, int
   a.out[at] = __builtin_fmaf(a.decay, old, w);
 }
 
-// Sixteen rows at most: waves take blocks of 32 tokens in turn.  HALF, up to eight rows: the
-// 16 columns of the matrix instructions hold them twice, once for either 16 tokens of a
-// block, which halves the work per score.
-template <int D, int BITS, bool HALF>
+// Few rows, T times 16 at most: waves take blocks of 32 tokens in turn.  HALF, up to eight
+// rows: the 16 columns of the matrix instructions hold them twice, once for either 16 tokens
+// of a block, which halves the work per score.
+template <int D, int BITS, bool HALF, int T>
 __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   using L = CacheLayout<D, BITS>;
   constexpr int G = L::kG, DW = L::kDw, ST = D / 32;
@@ -128,17 +128,23 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
   int jb = blockIdx.x * 4 + wave;
   if (jb >= blocks) return;
 
-  const int row = HALF ? n & 7 : n;
+  static_assert(!HALF || T == 1);
   const bool second = HALF && (n & 8);   // the lane's columns are for the block's last 16 tokens
-  const int tok = row / a.group, hq = h * a.group + row % a.group;
-  bool have = row < s.rows;
-  float lse = have ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
-  have = have && lse != kNegInf;
-  Rows<D, BITS> rows;
-  rows.load(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN, have, g);
-  const float to_log2 = a.scale_log2 * rows.unscale;
-  const float off = have ? lse * kLog2e : INFINITY;   // a row that is not there weighs 0
-  const int pos = have ? s.p_first + tok : -1;
+  Rows<D, BITS> rows[T];
+  float to_log2[T], off[T];
+  int pos[T];
+#pragma unroll
+  for (int t = 0; t < T; ++t) {
+    const int row = 16 * t + (HALF ? n & 7 : n);
+    const int tok = row / a.group, hq = h * a.group + row % a.group;
+    bool have = row < s.rows;
+    const float lse = have ? a.lse[(b * a.H * a.group + hq) * a.n + tok] : kNegInf;
+    have = have && lse != kNegInf;
+    rows[t].load(a.q + b * a.q_sB + hq * a.q_sH + tok * a.q_sN, have, g);
+    to_log2[t] = a.scale_log2 * rows[t].unscale;
+    off[t] = have ? lse * kLog2e : INFINITY;   // a row that is not there weighs 0
+    pos[t] = have ? s.p_first + tok : -1;
+  }
   const int p_lo = s.p_first, p_hi = s.p_first + (s.rows - 1) / a.group;
 
   auto seen = [&](int i) __attribute__((always_inline)) {   // by some row
@@ -176,34 +182,46 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
     float w = 0.0f;
     if (held) {
       const bool masked = j0 + 31 > p_lo || (j0 <= p_hi - a.window && j0 + 31 >= a.sinks);
-      f32x4 acc[2][G];
+      f32x4 acc[2][T][G];
+      auto multiply = [&](int tl) __attribute__((always_inline)) {
 #pragma unroll
-      for (int tl = 0; tl < 2; ++tl) {
+        for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int gi = 0; gi < G; ++gi) acc[tl][gi] = f32x4{};
+          for (int gi = 0; gi < G; ++gi) acc[tl][t][gi] = f32x4{};
 #pragma unroll
         for (int st = 0; st < ST; ++st)
-          acc[tl][st / 2] = rows.dot(x.c + (tl * ST + st) * DW, st, acc[tl][st / 2]);
-      }
 #pragma unroll
-      for (int tl = 0; tl < NT; ++tl)
+          for (int t = 0; t < T; ++t)
+            acc[tl][t][st / 2] = rows[t].dot(x.c + (tl * ST + st) * DW, st, acc[tl][t][st / 2]);
+      };
+      multiply(0);
+      if constexpr (HALF) multiply(1);
+#pragma unroll
+      for (int tl = 0; tl < NT; ++tl) {
+        if (tl > 0) multiply(tl);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float y = 0.0f;
+          float all = 0.0f;
 #pragma unroll
-          for (int gi = 0; gi < G; ++gi) {
-            const float c = HALF ? (second ? acc[1][gi][e] : acc[0][gi][e]) : acc[tl][gi][e];
-            y = __builtin_fmaf(high_of(x.p[tl][e * G + gi]), c, y);
-            y = __builtin_fmaf(low_of(x.p[tl][e * G + gi]), rows.sum[gi], y);
+          for (int t = 0; t < T; ++t) {
+            float y = 0.0f;
+#pragma unroll
+            for (int gi = 0; gi < G; ++gi) {
+              const float c = HALF && second ? acc[1][t][gi][e] : acc[tl][t][gi][e];
+              y = __builtin_fmaf(high_of(x.p[tl][e * G + gi]), c, y);
+              y = __builtin_fmaf(low_of(x.p[tl][e * G + gi]), rows[t].sum[gi], y);
+            }
+            y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2[t], -off[t]));
+            if (masked) {
+              const int jt = j0 + (HALF ? 2 * (n & 8) : 16 * tl) + 4 * g + e;
+              y = jt <= pos[t] && (jt > pos[t] - a.window || jt < a.sinks) ? y : 0.0f;
+            }
+            all = t == 0 ? y : all + y;
           }
-          y = __builtin_amdgcn_exp2f(__builtin_fmaf(y, to_log2, -off));
-          if (masked) {
-            const int jt = j0 + (HALF ? 2 * (n & 8) : 16 * tl) + 4 * g + e;
-            y = jt <= pos && (jt > pos - a.window || jt < a.sinks) ? y : 0.0f;
-          }
-          const float sum = row_sum<HALF>(y);
+          const float sum = row_sum<HALF>(all);
           w = (HALF ? n & 3 : n & 7) == 4 * tl + e ? sum : w;
         }
+      }
     }
     if (writes && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, x.old, w);
   };
@@ -454,7 +472,10 @@ size_t row_tiles_bytes(int64_t heads, int64_t rows) {
   return static_cast<size_t>(heads) * ((rows + 31) / 32) * sizeof(RowTile<D>);
 }
 
-constexpr int kFewRows = 16;   // that one tile of columns takes as they come
+// Rows whose columns the waves of k_mass_few hold: sixteen to a register tile, five of those
+// (4 x 131072 tokens, 4 heads of 128 in 4 bits: 35 us for 7 rows, 46 for 14, 65 for 28, 107 for
+// 56, 118 for 77, where k_mass_many takes 160 to 184; six tiles 228 for 84 rows, 184 there).
+constexpr int kFewRows = 80;
 
 // Where blocks alone leave CUs without a workgroup (a CU holds three), their rows are split
 // among as many as fill them, with eight tiles each at least (512 tokens of 28 heads over 512
@@ -518,8 +539,12 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
       // tokens, 4 heads: 35 us, also with half of them; 38 with twice as many).
       const int64_t fill = std::max<int64_t>(1, 2048 / heads);
       const int64_t groups = std::min((blocks + 3) / 4, fill);
-      if (rows <= 8) launch(k_mass_few<D, BITS, true>, groups);
-      else launch(k_mass_few<D, BITS, false>, groups);
+      if (rows <= 8) launch(k_mass_few<D, BITS, true, 1>, groups);
+      else if (rows <= 16) launch(k_mass_few<D, BITS, false, 1>, groups);
+      else if (rows <= 32) launch(k_mass_few<D, BITS, false, 2>, groups);
+      else if (rows <= 48) launch(k_mass_few<D, BITS, false, 3>, groups);
+      else if (rows <= 64) launch(k_mass_few<D, BITS, false, 4>, groups);
+      else launch(k_mass_few<D, BITS, false, 5>, groups);
     } else {
       RowTile<D>* prepared = static_cast<RowTile<D>*>(x.workspace);
       const int64_t tiles = (rows + 31) / 32;

@@ -87,7 +87,7 @@ def setup(D, bits, page, lens, Hkv, group, n, seed=0, n_new=None, window=None, s
 
 @pytest.mark.parametrize("D,bits,page", [(128, 4, 64), (64, 4, 32), (128, 8, 32), (64, 8, 128)])
 @pytest.mark.parametrize("group,n", [(1, 1), (7, 1), (4, 4), (5, 5), (1, 33), (7, 40), (2, 300),
-                                     (8, 260)])
+                                     (8, 260), (5, 9), (16, 4), (1, 79), (9, 9)])
 def test_mass(gpu, D, bits, page, group, n):
     lens = [max(n, L) for L in (1, 33, 700)]
     ks, cache, table, q, lse = setup(D, bits, page, lens, 2, group, n)
@@ -107,7 +107,8 @@ def test_mass(gpu, D, bits, page, group, n):
         assert torch.equal(again[b, :, L:], old[b, :, L:])
 
 
-@pytest.mark.parametrize("group,n", [(7, 1), (4, 3), (3, 70), (8, 200)])
+@pytest.mark.parametrize("group,n", [(7, 1), (4, 3), (3, 70), (8, 200), (3, 9), (13, 5),
+                                     (5, 16)])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (33, 5), (100, 64)])
 def test_mass_window_padding_and_missing_pages(gpu, group, n, window, sinks):
     lens, n_new = [n + 400, n + 3, 2, 300], int32([n, 1, n + 9, 0])
