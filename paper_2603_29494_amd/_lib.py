@@ -540,6 +540,10 @@ def _tdesc(shape, strides):
                               Dd if N == 1 else sN))
 
 
+def _contiguous_like(t: torch.Tensor) -> torch.Tensor:   # sooner than t.new_empty(t.shape)
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _int32_on(t: torch.Tensor, shape, device, name: str):
     if t.dtype is not torch.int32 or t.shape != shape or t.device != device \
             or not t.is_contiguous():
@@ -896,7 +900,7 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     dev = q.device
     flags = 0
     if out is None:
-        out, flags = q.new_empty(q.shape), CLEAR_PADDING
+        out, flags = _contiguous_like(q), CLEAR_PADDING
     _bf16_cuda(out, "out")
     _same_device(dev, k=k, v=v, out=out, mask=mask, workspace=workspace)
     need = cross_attn_workspace_bytes(q, k)
@@ -1012,7 +1016,7 @@ def rope(plan: Rope, q: torch.Tensor, k: Optional[torch.Tensor] = None,
         _bf16_cuda(k, "k")
     clear = out is None
     if clear:
-        qo, ko = q.new_empty(q.shape), None if k is None else k.new_empty(k.shape)
+        qo, ko = _contiguous_like(q), None if k is None else _contiguous_like(k)
     else:
         qo, ko = (out, None) if k is None else out
     _bf16_cuda(qo, "out")

@@ -741,12 +741,14 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
   }
   // Many rows: parts and their join cost about as much as 512 keys, so the keys are cut only
   // where row tiles leave half of the CUs without one (8 tiles over 16384 keys: 24 us in 32
-  // chunks, 324 in one), or, of many keys, all CUs without a second (in three chunks; 130
-  // tiles over 4096 keys: 60 us, 84 in one; 256 over 16384: 351 and 412; but 200 over 4096: 94
-  // and 90, 320 over 4096: 143 and 138).
-  const int64_t chunks = units <= 128   ? std::max<int64_t>(1, std::min(Nk / 512, 512 / units))
-                         : units <= 256 ? (Nk >= 24 * units ? 3 : 1)
-                                        : 1;
+  // chunks, 324 in one), or, of many keys, where CUs have very different numbers of them: in
+  // three up to one each (130 tiles over 4096 keys: 60 us, 84 in one; 256 over 16384: 351 and
+  // 412; but 200 over 4096: 94 and 90), in four up to three for every two CUs (288 over 8192:
+  // 170 and 230, 384: 208 and 224; 448: 241 and 239).
+  const int64_t balanced = units <= 256 ? 3 : units <= 384 ? 4 : 1;
+  const int64_t chunks = units <= 128       ? std::max<int64_t>(1, std::min(Nk / 512, 512 / units))
+                         : Nk >= 24 * units ? balanced
+                                            : 1;
   d.chunk = static_cast<int32_t>(((Nk + chunks - 1) / chunks + 127) / 128 * 128);
   d.chunks = static_cast<int32_t>((Nk + d.chunk - 1) / d.chunk);
   d.items = units * d.chunks;

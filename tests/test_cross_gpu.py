@@ -61,13 +61,13 @@ def test_against_the_formula(gpu, D, Hq, Hkv, Nq, Nk):
     ref.check(o, lse, cross64(q, k, v))
 
 
-@pytest.mark.parametrize("D", [64, 128])
-def test_many_row_tiles_over_many_keys(gpu, D):
-    """More row tiles than half of the CUs and keys enough to be cut, some lengths within the first
-    piece."""
-    B, H, Nq, Nk = 16, 9, 37, 3500
+@pytest.mark.parametrize("D,H,Nq,Nk", [(64, 9, 37, 3500), (128, 9, 37, 3500), (64, 17, 33, 6600)])
+def test_many_row_tiles_over_many_keys(gpu, D, H, Nq, Nk):
+    """More row tiles than half of the CUs, and than all, and keys enough to be cut, some lengths
+    within the first piece."""
+    B = 16
     q, k, v = rows(21, B, H, Nq, D), rows(22, B, H, Nk, D), rows(23, B, H, Nk, D)
-    lens = [3500, 0, 1, 3499, 1167, 1280, 1281, 2560, 2561, 3000] + [3500] * 6
+    lens = [Nk, 0, 1, Nk - 1, 1167, 1280, 1281, 2560, 2561, 3000] + [Nk] * 6
     o, lse = va.cross_attn(q, k, v, lens=int32(lens), return_lse=True)
     ref.check(o, lse, cross64(q, k, v, lens=lens))
 
