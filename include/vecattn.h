@@ -600,9 +600,9 @@ vecattn_status vecattn_cache_mass(const void* q, const vecattn_tdesc* qd, const 
  *          that vecattn_cache_gather fills
  *   workspace : device memory (16-byte aligned) of at least
  *          vecattn_cache_keep_workspace_size bytes for the same cache, cols, B and M (0 for
- *          up to 8192 tokens: may be NULL); contents need not be initialised.  Calls that
+ *          up to 32768 tokens: may be NULL); contents need not be initialised.  Calls that
  *          may overlap need one each.
- * Asynchronous; one launch for up to 8192 tokens (M, or cols * page), six for more.
+ * Asynchronous; one launch for up to 32768 tokens (M, or cols * page), six for more.
  * Errors: INVALID_ARG (null pointer, B < 1, M or budget < 1 or > 2^30, sinks or recent
  * < 0, sinks + recent > budget, a bad cache, cols < 1 or cols * page > 2^30, misalignment);
  * CAPACITY (workspace too small); UNSUPPORTED (more than 65535 sequences or heads).

@@ -3,17 +3,18 @@
 // collected, the lower index first among equals.
 //
 // Weights become 32-bit keys of the same order (a protected token the largest, NaN the
-// smallest), and three rounds over 11, 11 and 10 bits of them find the key of the last
-// token that is kept: integer counts, so that nothing depends on their order.  The tokens
-// above it, and the first of those equal to it, are then written in ascending order, each
-// wave its own range.
+// smallest, 0 no token), and three rounds over 11, 11 and 10 bits of them find the key of the
+// last token that is kept: integer counts, so that nothing depends on their order.  The
+// tokens above it, and the first of those equal to it, are then written in ascending order,
+// each wave its own range.
 //
-// A row (a sequence and key/value head) of up to 8192 tokens is one workgroup's, its keys
-// in registers (512 rows of up to 8192 tokens: 25 us).  Longer ones are cut into segments
-// of as many, a workgroup each, with a launch per round, and counts that meet in the
-// workspace: 16 rows of 131072 tokens take 51 us in six launches of 5 to 12 us each, against
-// 330 us for a CU alone per row.  What bounds either is the chain of rounds, each a load,
-// counts in LDS and a scan over its bins.
+// A row (a sequence and key/value head) of up to 32768 tokens is one workgroup's, its keys
+// in registers: 9 us for 700 tokens, 14 for 8192, 36 for 32768 (in six launches the same, and
+// 242 instead of 85 for 512 such rows).  Longer ones are cut into segments of 8192, a
+// workgroup each, with a launch per round, and counts that meet in the workspace: 16 rows of
+// 131072 tokens take 51 us in six launches of 5 to 12 us each, against 330 us for a CU alone
+// per row.  What bounds either is the chain of rounds, each a load, counts in LDS and a scan
+// over its bins.
 #include <algorithm>
 
 #include "device_common.h"
@@ -50,39 +51,37 @@ __device__ __forceinline__ int wave_sum(int x) {   // on every lane
 
 // A workgroup's tokens, up to kSegment from `base` on: wave w takes [span w, span (w + 1))
 // of them.
+template <int ITEMS>
 struct Keys {
-  uint32_t key[kItems];
-  uint64_t held[kItems];
+  uint32_t key[ITEMS];   // 0: no token that a page holds
   int from, rounds;
 
   __device__ __forceinline__ void load(const KeepParams& a, int64_t b, int64_t bh, int base, int end,
                                        int len, int lane, int wave) {
-    rounds = (min(end - base, kSegment) + kThreads - 1) / kThreads;
+    rounds = (min(end - base, ITEMS * kThreads) + kThreads - 1) / kThreads;
     from = base + wave * 64 * rounds;
     const float* mass = a.mass + bh * a.M;
     const int32_t* table = a.table + b * a.cols;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < ITEMS; ++i) {
       const int j = from + 64 * i + lane;
-      bool is = false;
       uint32_t k = 0;
       if (i < rounds && j < end) {
         const float x = mass[j] + 0.0f;   // one zero
         const int64_t page = table[j >> a.page_shift];
-        is = page >= 0 && page < a.pages;
         const uint32_t bits = __float_as_uint(x);
-        k = x != x ? 0u : bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+        k = x != x ? 1u : bits & 0x80000000u ? ~bits : bits | 0x80000000u;
         if (j < a.sinks || j >= len - a.recent) k = 0xFFFFFFFFu;
+        if (page < 0 || page >= a.pages) k = 0;
       }
       key[i] = k;
-      held[i] = __ballot(is);
     }
   }
   template <typename F>
-  __device__ __forceinline__ void each(int lane, F&& f) const {
+  __device__ __forceinline__ void each(F&& f) const {
 #pragma unroll
-    for (int i = 0; i < kItems; ++i)
-      if (i < rounds) f(i, key[i], (held[i] >> lane & 1) != 0);
+    for (int i = 0; i < ITEMS; ++i)
+      if (i < rounds) f(i, key[i], key[i] != 0);
   }
 };
 
@@ -109,11 +108,12 @@ struct Shared {
 };
 
 // Counts, into hist, the held keys whose bits above the round's are `last`.
-__device__ __forceinline__ void count_bins(const Keys& k, Shared& s, int round, uint32_t last) {
-  const int lane = threadIdx.x & 63, shift = shift_of(round), take = bits_of(round);
+template <int ITEMS>
+__device__ __forceinline__ void count_bins(const Keys<ITEMS>& k, Shared& s, int round, uint32_t last) {
+  const int shift = shift_of(round), take = bits_of(round);
   for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist[i] = 0;
   __syncthreads();
-  k.each(lane, [&](int, uint32_t key, bool is) {
+  k.each([&](int, uint32_t key, bool is) {
     if (is && (round == 0 || key >> (shift + take) == last))
       atomicAdd(&s.hist[key >> shift & ((1u << take) - 1u)], 1);
   });
@@ -153,10 +153,11 @@ __device__ __forceinline__ void find_bin(Shared& s, int round, uint32_t& last, i
 struct Before {
   int more, same, all_more, all_same;
 };
-__device__ __forceinline__ Before count_kept(const Keys& k, Shared& s, uint32_t last) {
+template <int ITEMS>
+__device__ __forceinline__ Before count_kept(const Keys<ITEMS>& k, Shared& s, uint32_t last) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int more = 0, same = 0;
-  k.each(lane, [&](int, uint32_t key, bool is) {
+  k.each([&](int, uint32_t key, bool is) {
     more += is && key > last ? 1 : 0;
     same += is && key == last ? 1 : 0;
   });
@@ -174,12 +175,13 @@ __device__ __forceinline__ Before count_kept(const Keys& k, Shared& s, uint32_t 
 }
 
 // Writes the kept ones of a wave; more and same: kept and equal ones before them.
-__device__ __forceinline__ void write_kept(const Keys& k, int32_t* idx, uint32_t last, int need,
+template <int ITEMS>
+__device__ __forceinline__ void write_kept(const Keys<ITEMS>& k, int32_t* idx, uint32_t last, int need,
                                            int more, int same) {
   const int lane = threadIdx.x & 63;
   const uint64_t below = (uint64_t(1) << lane) - 1;
   int at = more + min(same, need);
-  k.each(lane, [&](int i, uint32_t key, bool is) {
+  k.each([&](int i, uint32_t key, bool is) {
     const bool tie = is && key == last;
     const uint64_t ties = __ballot(tie);
     const bool keep = (is && key > last) || (tie && same + __builtin_popcountll(ties & below) < need);
@@ -190,11 +192,12 @@ __device__ __forceinline__ void write_kept(const Keys& k, int32_t* idx, uint32_t
   });
 }
 
-__device__ __forceinline__ int count_held(const Keys& k, Shared& s) {
+template <int ITEMS>
+__device__ __forceinline__ int count_held(const Keys<ITEMS>& k, Shared& s) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   int mine = 0;
 #pragma unroll
-  for (int i = 0; i < kItems; ++i) mine += __builtin_popcountll(k.held[i]);
+  for (int i = 0; i < ITEMS; ++i) mine += __builtin_popcountll(__ballot(k.key[i] != 0));
   if (lane == 0) s.wave[wave] = mine;
   __syncthreads();
   int sum = 0;
@@ -204,14 +207,16 @@ __device__ __forceinline__ int count_held(const Keys& k, Shared& s) {
   return sum;
 }
 
-// Rows of one segment.
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(8))) void k_keep_row(const KeepParams a) {
+// Rows of one workgroup.
+template <int ITEMS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(ITEMS > 8 ? 4 : 8)))
+void k_keep_row(const KeepParams a) {
   __shared__ Shared s;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Row r = row_of(a, blockIdx.y, blockIdx.x);
   int32_t* idx = a.idx + r.bh * a.budget;
-  Keys k;
+  Keys<ITEMS> k;
   k.load(a, r.b, r.bh, 0, r.end, r.len, lane, wave);
   const int n = static_cast<int>(min<int64_t>(count_held(k, s), a.budget));
   if (blockIdx.x == 0 && threadIdx.x == 0) a.kept[r.b] = n;
@@ -269,7 +274,7 @@ __global__ __launch_bounds__(kThreads) void k_keep_round(const KeepParams a) {
       work[kState + 2 * (ROUND - 1) + 1] = need;
     }
   }
-  Keys k;
+  Keys<kItems> k;
   k.load(a, b, r.bh, base, r.end, r.len, lane, wave);
   if constexpr (ROUND < 3) {
     if constexpr (ROUND == 0) {
@@ -306,15 +311,17 @@ __global__ __launch_bounds__(kThreads) void k_keep_round(const KeepParams a) {
   }
 }
 
+int64_t tokens_of(int64_t M, const CacheArgs& c) { return std::min(M, c.cols * c.page); }
+constexpr int64_t kWholeRow = 4 * kSegment;   // tokens that one workgroup takes
 int64_t segments_of(int64_t M, const CacheArgs& c) {
-  return (std::min(M, c.cols * c.page) + kSegment - 1) / kSegment;
+  return (tokens_of(M, c) + kSegment - 1) / kSegment;
 }
 
 }  // namespace
 
 size_t cache_keep_workspace_bytes(const CacheArgs& c, int64_t B, int64_t M) {
+  if (tokens_of(M, c) <= kWholeRow) return 0;
   const int64_t segments = segments_of(M, c);
-  if (segments <= 1) return 0;
   return static_cast<size_t>(B) * c.H * (kSegments + 2 * segments) * sizeof(int32_t);
 }
 
@@ -335,8 +342,12 @@ hipError_t launch_cache_keep(const CacheArgs& c, int64_t B, const float* mass, i
   a.work = static_cast<int32_t*>(workspace);
   a.work_size = kSegments + 2 * segments;
   const dim3 rows(static_cast<unsigned>(c.H), static_cast<unsigned>(B));
-  if (segments <= 1) {
-    hipLaunchKernelGGL(k_keep_row, rows, dim3(kThreads), 0, stream, a);
+  const int64_t tokens = tokens_of(M, c);
+  if (tokens <= kWholeRow) {
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, rows, dim3(kThreads), 0, stream, a); };
+    if (tokens <= kSegment) run(k_keep_row<8>);
+    else if (tokens <= 2 * kSegment) run(k_keep_row<16>);
+    else run(k_keep_row<32>);
     return hipGetLastError();
   }
   const dim3 grid(static_cast<unsigned>(segments), static_cast<unsigned>(c.H),

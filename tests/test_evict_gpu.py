@@ -199,7 +199,8 @@ def keep_ref(mass, held, length, budget, sinks, recent):
 @pytest.mark.parametrize("M,lens,budget,sinks,recent", [
     (64, [0, 1, 64], 1, 0, 0), (64, [5, 63, 64], 64, 3, 7), (100, [99, 100, 150], 40, 10, 30),
     (2000, [17, 1999, 900], 500, 0, 0), (9000, [8999, 1025, 70], 1000, 64, 128),
-    (30000, [30000, 24577, 1], 7001, 4, 0)])
+    (30000, [30000, 24577, 1], 7001, 4, 0), (16000, [16000, 8193, 15999], 4000, 0, 9),
+    (70000, [70000, 40961, 1], 9001, 4, 70)])
 @pytest.mark.parametrize("kind", ["spread", "ties", "special"])
 def test_keep(gpu, M, lens, budget, sinks, recent, kind):
     H, page = 2, 32

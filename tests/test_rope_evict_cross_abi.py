@@ -189,12 +189,12 @@ def test_cache_keep_and_gather_reject_bad_arguments():
         assert keep(**dict(dict(recent=0), **bad)) == INVALID, bad
     assert keep(recent=0, B=70000) == UNSUPPORTED
     assert keep(recent=0, c=cache(D=96)) == UNSUPPORTED
-    # more than 8192 tokens need a workspace
+    # more than 32768 tokens need a workspace
     n = ctypes.c_size_t(9)
     size = lib.vecattn_cache_keep_workspace_size
-    assert size(REF(cache()), 128, 2, 1 << 20, REF(n)) == OK and n.value == 0
-    assert size(REF(cache()), 129, 2, 1 << 20, REF(n)) == OK and n.value > 0
-    long = dict(recent=0, cols=129, M=1 << 20)
+    assert size(REF(cache()), 512, 2, 1 << 20, REF(n)) == OK and n.value == 0
+    assert size(REF(cache()), 513, 2, 1 << 20, REF(n)) == OK and n.value > 0
+    long = dict(recent=0, cols=513, M=1 << 20)
     assert keep(**long) == CAPACITY and keep(ws=FAKE, nws=n.value - 1, **long) == CAPACITY
     assert keep(ws=FAKE + 8, nws=n.value, **long) == INVALID
     assert size(REF(cache()), 0, 2, 64, REF(n)) == INVALID
