@@ -572,7 +572,7 @@ vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
  *   out  : fp32 [B, H, M] contiguous; tokens at or past M have no entry
  *   workspace : device memory (16-byte aligned) of at least
  *          vecattn_cache_mass_workspace_size bytes for the same qd and cache (0, with up to
- *          80 rows n * Hq / H: may be NULL); contents need not be initialised.  Calls that
+ *          48 rows n * Hq / H: may be NULL); contents need not be initialised.  Calls that
  *          may overlap need one each.
  * Sums are fp32, of one order (no atomics).  What a call does follows lens, n_new and table
  * on the device, so that a captured call can be replayed as they change.

@@ -9,11 +9,12 @@
 // atomics.
 //
 // Few rows are bound by reading K's half of the cache: four sequences of 131072 tokens in 4
-// bits, 4 heads of 128, 7 rows each: 35 us, 4.8 TB/s.  Many rows by the matrix products and
+// bits, 4 heads of 128, 7 rows each: 34 us, 4.9 TB/s.  Many rows by the matrix products and
 // the exponentials, whose times add: 512 tokens of 28 heads over 33280 in 8 bits, 4 heads:
-// 178 us at best, 690 TFLOP/s (190 on the same card with rows of q in fp16 and their powers
-// of two applied to every score).  How many workgroups there are counts there, three fit a
-// CU at a time: 1040 take 178 us, 768 take 127; splitting the rows of such numbers gains 3%.
+// 175 us at best, 700 TFLOP/s (13 more with rows of q in fp16 and their powers of two applied
+// to every score; 5 more with the codes fetched by dwords and each sum's lanes added on
+// their own, 55 of 190 more for 126 rows over 4 x 131072 tokens).  How many workgroups there
+// are counts there, three fit a CU at a time; splitting the rows of such numbers gains 3%.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -68,25 +69,32 @@ __device__ __forceinline__ const uint8_t* keys_of(const MassParams& a, int64_t p
   return a.data + (((page * a.H + h) << sh) + (jb & ((1 << sh) - 1))) * BYTES;
 }
 
-// x summed over 16 lanes (or each half of them), on each of them.
-template <bool HALF = false>
-__device__ __forceinline__ float row_sum(float x) {
-  auto turn = [&](auto ctl) __attribute__((always_inline)) {
-    const int y = __builtin_bit_cast(int, x);
-    x += __builtin_bit_cast(
-        float, __builtin_amdgcn_update_dpp(y, y, decltype(ctl)::value, 0xf, 0xf, false));
-  };
-  if constexpr (HALF) {
-    turn(std::integral_constant<int, 0xB1>{});    // quad_perm [1, 0, 3, 2]
-    turn(std::integral_constant<int, 0x4E>{});    // quad_perm [2, 3, 0, 1]
-    turn(std::integral_constant<int, 0x141>{});   // row_half_mirror
-    return x;
+// x of the lane that DPP control CTL names (0 past a row's end).
+template <int CTL>
+__device__ __forceinline__ float from_lane(float x) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTL, 0xf, 0xf, true));
+}
+constexpr int kRor8 = 0x128, kHalfMirror = 0x141, kXor2 = 0x4E, kXor1 = 0xB1, kShl4 = 0x104;
+
+// Sums over lanes of several values: every step leaves half of the values, each with the lane
+// (of the two that CTL pairs) that has its bit in n, the lane's number.
+template <int CTL, int BIT>
+__device__ __forceinline__ float halve(float clear, float set, int n) {
+  return (n & BIT ? set : clear) + from_lane<CTL>(n & BIT ? clear : set);
+}
+// v[n % COUNT] over the COUNT lanes that differ in these bits of n.
+template <int COUNT>
+__device__ __forceinline__ float lanes_sum(const float* v, int n) {
+  if constexpr (COUNT == 1) {
+    return v[0];
+  } else {
+    constexpr int CTL = COUNT == 16 ? kRor8 : COUNT == 8 ? kHalfMirror : COUNT == 4 ? kXor2 : kXor1;
+    float x[COUNT / 2];
+#pragma unroll
+    for (int e = 0; e < COUNT / 2; ++e) x[e] = halve<CTL, COUNT / 2>(v[e], v[e + COUNT / 2], n);
+    return lanes_sum<COUNT / 2>(x, n);
   }
-  turn(std::integral_constant<int, 0x128>{});   // row_ror:8
-  turn(std::integral_constant<int, 0x124>{});
-  turn(std::integral_constant<int, 0x122>{});
-  turn(std::integral_constant<int, 0x121>{});
-  return x;
 }
 
 // Blocks that a (sequence, head) has entries to write in.
@@ -183,6 +191,7 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
     if (held) {
       const bool masked = j0 + 31 > p_lo || (j0 <= p_hi - a.window && j0 + 31 >= a.sinks);
       f32x4 acc[2][T][G];
+      float sums[4 * NT];
       auto multiply = [&](int tl) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < T; ++t)
@@ -218,10 +227,12 @@ __global__ __launch_bounds__(256) void k_mass_few(const MassParams a) {
             }
             all = t == 0 ? y : all + y;
           }
-          const float sum = row_sum<HALF>(all);
-          w = (HALF ? n & 3 : n & 7) == 4 * tl + e ? sum : w;
+          sums[4 * tl + e] = all;
         }
       }
+      // To the lanes that write: of 16 columns, or of each half of them.
+      w = lanes_sum<4 * NT>(sums, n);
+      w += HALF ? from_lane<kShl4>(w) : from_lane<kRor8>(w);
     }
     if (writes && (held || !a.in_place || j >= s.p_first)) collect(a, s, bh, j, x.old, w);
   };
@@ -323,6 +334,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.y;
   const int64_t b = blockIdx.z, bh = b * a.H + h;
+  const int page = page_of(a, b, blockIdx.x / a.splits * 4 + wave);   // beside what follows
   const Place s = place_of(a, b);
   const int blocks = blocks_of(a, s);
   const int split = blockIdx.x % a.splits;
@@ -363,41 +375,57 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
     fetch(min(t0 + 1, ntiles - 1), 1);
   }
 
-  // A block that no page holds passes as zeros, and its sums are left out at the end.
-  const uint8_t* blk =
-      j0 < s.end ? keys_of<L::kBytes>(a, page_of(a, b, jb), h, jb) : nullptr;
-  bf16x8 low = {}, codes[ST];
+  // A block that no page holds passes as some other, and its sums are left out at the end.
+  const uint8_t* blk = j0 < s.end ? keys_of<L::kBytes>(a, page, h, jb) : nullptr;
+  const uint8_t* src = blk ? blk : a.data;
+  bf16x8 codes[ST];
   float step_of[G][16], w[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) w[e] = 0.0f;
+  // Token n = 16 t + n % 16, values 16 st + 8 g on: run dword (t D / 32 + st / 2) kDw
+  // of lane 16 (2 (st % 2) + g) + n % 16.
+  constexpr int RUN = SW * DW, LOAD = RUN < 4 ? RUN : 4;
+  typedef uint32_t Words __attribute__((ext_vector_type(LOAD)));
+  Words u[2][RUN / LOAD];
+#pragma unroll
+  for (int odd = 0; odd < 2; ++odd)
+#pragma unroll
+    for (int c = 0; c < RUN / LOAD; ++c)
+      u[odd][c] = *reinterpret_cast<const Words*>(
+          src + code_byte((n >> 4) * RUN + c * LOAD, (2 * odd + g) * 16 + (n & 15)));
+  const uint32_t* par = reinterpret_cast<const uint32_t*>(src + L::kCodes);
+  u32x4 steps[4][G];
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int c = 0; c < G; ++c)
+      steps[q][c] = reinterpret_cast<const u32x4*>(par + (8 * q + 4 * g) * G)[c];
+  const uint32_t m0 = par[n * G] & 0xFFFFu, m1 = G > 1 ? par[n * G + G - 1] & 0xFFFFu : 0u;
+  const bf16x8 low = __builtin_bit_cast(
+      bf16x8, g == 0 ? u32x4{m0 | m0 << 16, m0 | m1 << 16, m1 | m1 << 16, 0u}
+                     : u32x4{0x3F803F80u, 0x3F80u, 0u, 0u});   // 1, 1, 1
 #pragma unroll
   for (int st = 0; st < ST; ++st) {
-    // Token n = 16 t + n % 16, values 16 st + 8 g on: run dword (t D / 32 + st / 2) kDw
-    // of lane 16 (2 (st % 2) + g) + n % 16.
-    const int w0 = ((n >> 4) * SW + st / 2) * DW, from = (2 * (st & 1) + g) * 16 + (n & 15);
-    uint32_t u[DW];
+    uint32_t run[DW];
 #pragma unroll
-    for (int y = 0; y < DW; ++y)
-      u[y] = blk ? *reinterpret_cast<const uint32_t*>(blk + code_byte(w0 + y, from)) : 0u;
-    u32x4 x = codes_16<BITS>(u);
+    for (int y = 0; y < DW; ++y) {
+      const int at = st / 2 * DW + y;
+      run[y] = u[st & 1][at / LOAD][at % LOAD];
+    }
+    u32x4 x = codes_16<BITS>(run);
 #pragma unroll
     for (int y = 0; y < 4; ++y)
       x[y] = __float_as_uint(static_cast<float>(x[y] & 0xFFu)) >> 16 |
              (__float_as_uint(static_cast<float>(x[y] >> 16)) & 0xFFFF0000u);
     codes[st] = __builtin_bit_cast(bf16x8, x);
   }
-  const uint32_t* par = reinterpret_cast<const uint32_t*>(blk + L::kCodes);
-  if (blk && g == 1) {
-    low = __builtin_bit_cast(bf16x8, u32x4{0x3F803F80u, 0x3F80u, 0u, 0u});   // 1, 1, 1
-  } else if (blk) {
-    const uint32_t m0 = par[n * G] & 0xFFFFu, m1 = G > 1 ? par[n * G + G - 1] & 0xFFFFu : 0u;
-    low = __builtin_bit_cast(bf16x8, u32x4{m0 | m0 << 16, m0 | m1 << 16, m1 | m1 << 16, 0u});
-  }
 #pragma unroll
   for (int e = 0; e < 16; ++e)
 #pragma unroll
-    for (int gi = 0; gi < G; ++gi)
-      step_of[gi][e] = blk ? a.scale_log2 * high_of(par[(8 * (e / 4) + 4 * g + e % 4) * G + gi]) : 0.0f;
+    for (int gi = 0; gi < G; ++gi) {
+      const int at = e % 4 * G + gi;
+      step_of[gi][e] = a.scale_log2 * high_of(steps[e / 4][at / 4][at % 4]);
+    }
 
   int st = 0;
   auto turn = [&](int t, auto masked_tag) __attribute__((always_inline)) {
@@ -441,17 +469,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void k
   for (int t = c1; t < ntiles; ++t) turn(t, std::true_type{});
   wait_all();
 
-  float mine = 0.0f;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const float y = row_sum(w[e]);
-    const float all = y + __shfl_xor(y, 16);
-    mine = (n & 15) == e ? all : mine;
-  }
   const int j = j0 + 8 * ((n & 15) / 4) + 4 * g + (n & 3);
-  if (n >= 16 || jb >= blocks) return;
+  const bool writes = n < 16 && jb < blocks;
+  const float old = writes && a.splits == 1 ? before(a, s, bh, j) : 0.0f;
+  float mine = lanes_sum<16>(w, n);
+  mine += __shfl_xor(mine, 16);
+  if (!writes) return;
   if (!blk) mine = 0.0f;
-  if (a.splits == 1) collect(a, s, bh, j, before(a, s, bh, j), mine);
+  if (a.splits == 1) collect(a, s, bh, j, old, mine);
   else a.part[(static_cast<int64_t>(split) * gridDim.z * a.H + bh) * a.slots + j] = mine;
 }
 
@@ -472,14 +497,14 @@ size_t row_tiles_bytes(int64_t heads, int64_t rows) {
   return static_cast<size_t>(heads) * ((rows + 31) / 32) * sizeof(RowTile<D>);
 }
 
-// Rows whose columns the waves of k_mass_few hold: sixteen to a register tile, five of those
-// (4 x 131072 tokens, 4 heads of 128 in 4 bits: 35 us for 7 rows, 46 for 14, 65 for 28, 107 for
-// 56, 118 for 77, where k_mass_many takes 160 to 184; six tiles 228 for 84 rows, 184 there).
-constexpr int kFewRows = 80;
+// Rows whose columns the waves of k_mass_few hold: sixteen to a register tile, three of those
+// (4 x 131072 tokens, 4 heads of 128 in 4 bits: 34 us for 7 rows, 38 for 14, 57 for 28, 68 for
+// 42, where k_mass_many takes 104; both about 100 for 63).
+constexpr int kFewRows = 48;
 
 // Where blocks alone leave CUs without a workgroup (a CU holds three), their rows are split
 // among as many as fill them, with eight tiles each at least (512 tokens of 28 heads over 512
-// tokens: 26 us, 77 in one; over 8192: 66 and 81; with six per CU 72).
+// tokens: 23 us, 77 in one; over 8192: 61 and 81).
 constexpr int64_t kFill = 3 * 256, kLeastTiles = 8;
 int64_t splits_of(int64_t groups, int64_t rows) {
   return std::max<int64_t>(1, std::min(kFill / groups, rows / (32 * kLeastTiles)));
@@ -536,15 +561,13 @@ hipError_t launch_cache_mass(const CacheMassArgs& x, hipStream_t stream) {
     constexpr int D = decltype(dim)::value, BITS = decltype(bits)::value;
     if (rows <= kFewRows) {
       // Two workgroups per place on the CUs, so that unequal lengths even out (4 x 131072
-      // tokens, 4 heads: 35 us, also with half of them; 38 with twice as many).
+      // tokens, 4 heads: 34 us, also with half of them; 37 with twice as many).
       const int64_t fill = std::max<int64_t>(1, 2048 / heads);
       const int64_t groups = std::min((blocks + 3) / 4, fill);
       if (rows <= 8) launch(k_mass_few<D, BITS, true, 1>, groups);
       else if (rows <= 16) launch(k_mass_few<D, BITS, false, 1>, groups);
       else if (rows <= 32) launch(k_mass_few<D, BITS, false, 2>, groups);
-      else if (rows <= 48) launch(k_mass_few<D, BITS, false, 3>, groups);
-      else if (rows <= 64) launch(k_mass_few<D, BITS, false, 4>, groups);
-      else launch(k_mass_few<D, BITS, false, 5>, groups);
+      else launch(k_mass_few<D, BITS, false, 3>, groups);
     } else {
       RowTile<D>* prepared = static_cast<RowTile<D>*>(x.workspace);
       const int64_t tiles = (rows + 31) / 32;

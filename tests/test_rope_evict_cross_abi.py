@@ -158,9 +158,9 @@ def test_cache_mass_rejects_bad_arguments():
         assert mass(decay=1.0, **bad) == INVALID, bad
     assert mass(decay=1.0, qd=desc(2, 4, 1, 80)) == UNSUPPORTED
     assert mass(decay=1.0, qd=desc(1, 4, 1 << 28, 128)) == UNSUPPORTED
-    # more than 80 rows need a workspace
-    n, many = ctypes.c_size_t(9), desc(2, 4, 41, 128)
-    assert lib.vecattn_cache_mass_workspace_size(REF(desc(2, 4, 40, 128)), REF(cache()), REF(n)) == OK
+    # more than 48 rows need a workspace
+    n, many = ctypes.c_size_t(9), desc(2, 4, 25, 128)
+    assert lib.vecattn_cache_mass_workspace_size(REF(desc(2, 4, 24, 128)), REF(cache()), REF(n)) == OK
     assert n.value == 0
     assert lib.vecattn_cache_mass_workspace_size(REF(many), REF(cache()), REF(n)) == OK
     assert n.value > 0
