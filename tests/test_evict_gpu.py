@@ -403,3 +403,51 @@ def test_calls_at_once_give_what_they_give_alone(gpu):
     torch.cuda.synchronize()
     for m, i, n in outs:
         assert torch.equal(m, mass) and torch.equal(i, idx) and torch.equal(n, kept)
+
+
+def test_replayed_chunks_and_long_rows(gpu):
+    """Graphs that share a workspace, of calls of several launches, follow the lengths on the
+    device; between the replays the same calls run eagerly."""
+    ks, cache, table, q, _ = setup(64, 4, 32, [700, 300], 2, 4, 160)
+    other = rows(77, *q.shape)
+    lens, n_new = int32([700, 300]), int32([160, 160])
+    lse = torch.full(q.shape[:3], 6.0, device="cuda")
+    M = 40960
+    long = fresh_cache(2 * M // 64, 1, 64, 64, 4)
+    pages = torch.randperm(2 * M // 64, generator=torch.Generator().manual_seed(5))
+    pages = pages.to(torch.int32).view(2, -1).cuda()
+    mass = torch.rand(2, 1, M, generator=torch.Generator().manual_seed(6)).cuda()
+    held = int32([M, 33000])
+    need = max(va.cache_mass_workspace_bytes(q, cache),
+               va.cache_keep_workspace_bytes(mass, long, pages.shape[1]))
+    assert va.cache_keep_workspace_bytes(mass, long, pages.shape[1]) > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros(2, 2, table.shape[1] * 32, device="cuda") for _ in range(2)]
+
+    def weights(x, out):
+        return va.cache_mass(x, lse, cache, table, lens, n_new=n_new, out=out, workspace=ws)
+    graphs, kept = [], []
+    for x, out in zip((q, other), outs):
+        weights(x, out)
+        va.cache_keep(mass, long, pages, held, 500, 4, 64, workspace=ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            weights(x, out)
+            kept.append(va.cache_keep(mass, long, pages, held, 500, 4, 64, workspace=ws))
+    for a, b, long_lens in (((700, 300), (160, 160), (M, 33000)), ((161, 0), (160, 0), (0, 1)),
+                            ((500, 299), (3, 160), (40000, 501)), ((700, 300), (160, 160), (M, M))):
+        lens.copy_(int32(a)), n_new.copy_(int32(b)), held.copy_(int32(long_lens))
+        for i, x in enumerate((q, other)):
+            outs[i].fill_(-3.0)
+            want = weights(x, torch.full_like(outs[i], -3.0))
+            idx, n = va.cache_keep(mass, long, pages, held, 500, 4, 64, workspace=ws)
+            torch.cuda.synchronize()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want)
+            assert torch.equal(kept[i][0], idx) and torch.equal(kept[i][1], n)
+            assert n.tolist() == [min(500, L) for L in long_lens]
+            for s in range(2):
+                ref_idx = keep_ref(mass[s, 0].tolist(), range(long_lens[s]), long_lens[s], 500, 4, 64)
+                assert idx[s, 0, :len(ref_idx)].tolist() == ref_idx
