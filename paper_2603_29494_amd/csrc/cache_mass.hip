@@ -13,8 +13,9 @@
 // the exponentials, whose times add: 512 tokens of 28 heads over 33280 in 8 bits, 4 heads:
 // 175 us at best, 700 TFLOP/s (13 more with rows of q in fp16 and their powers of two applied
 // to every score; 5 more with the codes fetched by dwords and each sum's lanes added on
-// their own, 55 of 190 more for 126 rows over 4 x 131072 tokens).  How many workgroups there
-// are counts there, three fit a CU at a time; splitting the rows of such numbers gains 3%.
+// their own, which also takes 207 us instead of 128 for 126 rows over 4 x 131072 tokens).
+// Three workgroups fit a CU at a time, and 1040 come out uneven there; splitting their rows
+// gains 3%.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
