@@ -726,9 +726,13 @@ Deal deal(int64_t B, int64_t Hq, int64_t Hkv, int64_t Nq, int64_t Nk, int64_t D)
     // Cut by the lengths on the device into as many chunks as workgroups run at a time (one
     // of 128 values per CU, two of 64; 16 sequences of 0 to 16384 keys: 45 us, 62 in chunks of
     // 2048), never into fewer than two per head, nor into ones of fewer keys than pay for a
-    // chunk.
+    // chunk.  Up to 1024 keys, or 4096 where heads alone fill the chip, none are cut: the join
+    // and what it reads cost more (four heads over 1000 keys: 13 us, 14 cut; 512 over 577
+    // of 64 values: 16 and 24; 256 over 4000: 95 and 102; but 64 over 2000 of uneven lengths:
+    // 20 and 17).
     const int64_t slots = D == 128 ? 256 : 512, least = 512;
-    const int64_t most = (Nk + least - 1) / least;
+    const int64_t whole = std::min<int64_t>(std::max<int64_t>(16 * units, 1024), 4096);
+    const int64_t most = Nk <= whole ? 1 : (Nk + least - 1) / least;
     d.chunks = most > 1 && B <= kMaxDealt ? 2 : 1;   // or more
     d.chunk = 0;
     d.items = units;

@@ -116,7 +116,7 @@ def test_lengths_masks_and_padding(gpu, D, Hq, Hkv, Nq, Nk):
 
 def test_many_sequences_and_uneven_lengths(gpu):
     """More sequences than are dealt out by their lengths, and as many with lengths far apart."""
-    for B, Nk in ((300, 600), (256, 1100), (33, 3000)):
+    for B, Nk in ((300, 600), (256, 1100), (33, 3000), (256, 4200), (130, 5000)):
         q, k, v = rows(1, B, 2, 1, 64), rows(2, B, 1, Nk, 64), rows(3, B, 1, Nk, 64)
         lens = (torch.rand(B, generator=torch.Generator().manual_seed(B)) ** 4 * (Nk + 1)).int()
         lens[0], lens[-1] = Nk, 0
