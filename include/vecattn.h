@@ -699,8 +699,10 @@ typedef enum vecattn_rope_scaling { /* for contexts longer than the trained one 
                               frequency divided by factor, the highest as it was */
   VECATTN_ROPE_PARTS = 3,  /* pairs up to the one that makes `fast` turns over `context`
                               keep f_i, from the one that makes `slow` on f_i / factor, those
-                              between (both rounded outwards) a share of each that is linear
-                              in i; the turned values times 0.1 ln(factor) + 1 */
+                              between (both rounded outwards, to no less than 0; the second,
+                              which may lie past the last pair, to no more than rot - 1) a
+                              share of each that is linear in i; the turned values times
+                              0.1 ln(factor) + 1 */
   VECATTN_ROPE_BANDS = 4   /* the same, but the share is linear in the turns c f_i / 2 pi */
 } vecattn_rope_scaling;
 

@@ -79,8 +79,9 @@ void rope_ladder(int32_t rot, double base, int32_t scaling, double factor, doubl
   };
   double low = 0.0, high = 0.0;
   if (scaling == VECATTN_ROPE_PARTS) {
-    low = std::min(std::max(std::floor(pair_at(fast)), 0.0), half - 1.0);
-    high = std::min(std::max(std::ceil(pair_at(slow)), 0.0), half - 1.0);
+    // The slow end may lie past the last pair: then no pair is divided in full.
+    low = std::max(std::floor(pair_at(fast)), 0.0);
+    high = std::min(std::max(std::ceil(pair_at(slow)), 0.0), rot - 1.0);
   }
   for (int32_t i = 0; i < half; ++i) {
     const double f = std::pow(base, -static_cast<double>(i) / half);
