@@ -302,7 +302,12 @@ def prepare(case, seed):
     if own:
         import paper_2603_29494_amd as va
     if case["kind"] == "rope":
-        if own:
+        if own and case["scaling"] == "parts":
+            # The case's own ladder, which ends its ramp at the last pair at the latest: the
+            # library's goes on past that where two to four pairs have a ladder.
+            freq, axis, factor = _ladder(case)
+            s["plan"] = va.Rope(case["layout"], tuple(freq.tolist()), tuple(axis.tolist()), factor)
+        elif own:
             s["plan"] = va.rope_plan(
                 case["rot"], base=LADDER, layout=case["layout"],
                 scaling=None if case["scaling"] == "none" else case["scaling"], factor=FACTOR,
