@@ -569,7 +569,8 @@ vecattn_status vecattn_cache_attn(const void* q, const vecattn_tdesc* qd,
  *   q, table, cols, lens, n_new, window, sinks, scale : as for vecattn_cache_attn
  *   lse  : fp32 [B, Hq, n] contiguous
  *   mass : optional fp32 [B, H, M] contiguous; NULL: 0.  May be out itself.
- *   out  : fp32 [B, H, M] contiguous; tokens at or past M have no entry
+ *   out  : fp32 [B, H, M] contiguous; tokens at or past M have no entry, and what is put on
+ *          them is not kept: M is best the tokens of the table
  *   workspace : device memory (16-byte aligned) of at least
  *          vecattn_cache_mass_workspace_size bytes for the same qd and cache (0, with up to
  *          48 rows n * Hq / H: may be NULL); contents need not be initialised.  Calls that
@@ -641,6 +642,16 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
                                     int64_t budget, const vecattn_cache* to,
                                     const int32_t* to_table, int64_t to_cols, const float* mass,
                                     int64_t M, float* mass_out, int32_t flags, void* stream);
+/* vecattn_cache_gather with mass_out fp32 [B, H, M_out], M_out from budget to 2^30, so that
+ * tokens that are written behind the kept ones have an entry in it: what
+ * vecattn_cache_mass and vecattn_cache_keep then take as [B, H, M]. */
+vecattn_status vecattn_cache_gather_wide(const vecattn_cache* cache, const int32_t* table,
+                                         int64_t cols, int64_t B, const int32_t* idx,
+                                         const int32_t* kept, int64_t budget,
+                                         const vecattn_cache* to, const int32_t* to_table,
+                                         int64_t to_cols, const float* mass, int64_t M,
+                                         float* mass_out, int64_t M_out, int32_t flags,
+                                         void* stream);
 
 /*
  * Attention of rows over another sequence's keys, such as an encoder's states (encoded

@@ -111,6 +111,8 @@ def load() -> ctypes.CDLL:
     lib.vecattn_cache_keep.argtypes = [P, i64, i64, C, P, i64, P, i64, i64, i64, P, P, P,
                                        ctypes.c_size_t, P]
     lib.vecattn_cache_gather.argtypes = [C, P, i64, i64, P, P, i64, C, P, i64, P, i64, P, i32, P]
+    lib.vecattn_cache_gather_wide.argtypes = [C, P, i64, i64, P, P, i64, C, P, i64, P, i64, P, i64,
+                                              i32, P]
     lib.vecattn_cross_attn_workspace_size.argtypes = [D, D, ctypes.POINTER(ctypes.c_size_t)]
     lib.vecattn_cross_attn.argtypes = [P, D, P, D, P, D, P, P, i64, P, i32, f32, P, D, P, P,
                                        ctypes.c_size_t, P]
@@ -128,6 +130,7 @@ def load() -> ctypes.CDLL:
                  "vecattn_cache_attn_workspace_size", "vecattn_cache_attn",
                  "vecattn_cache_mass_workspace_size", "vecattn_cache_mass",
                  "vecattn_cache_keep_workspace_size", "vecattn_cache_keep", "vecattn_cache_gather",
+                 "vecattn_cache_gather_wide",
                  "vecattn_cross_attn_workspace_size", "vecattn_cross_attn",
                  "vecattn_rope_ladder", "vecattn_rope"):
         getattr(lib, name).restype = ctypes.c_int
@@ -767,9 +770,11 @@ def cache_mass(q: torch.Tensor, lse: torch.Tensor, cache: Cache, table: torch.Te
                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The attention weight that the new tokens of q [B, Hq, n, dim] put on each cached token, per
     key/value head (vecattn_cache_mass), added to ``decay`` times ``mass`` (float32 [B, heads, M];
-    0 when not given, M then the table's tokens).  ``lse``: what cache_attn returned for the same
-    q, cache, ``window`` and ``sinks``.  ``out`` may be ``mass``; entries of tokens at or past
-    ``lens`` are left as they were in a given ``out``, and 0 in one made here."""
+    0 when not given, and for tokens past it).  ``lse``: what cache_attn returned for the same
+    q, cache, ``window`` and ``sinks``.  ``out`` may be ``mass``; one made here has an entry for each
+    token of the table (or M, if those are more), in a given one what is put on tokens past its
+    entries is not kept.  Entries of tokens at or past ``lens`` are left as they were in a given
+    ``out``, and 0 in one made here."""
     _bf16_cuda(q, "q")
     B = q.shape[0]
     dev = _cache_args(cache, table, lens, B, n_new)
@@ -779,7 +784,14 @@ def cache_mass(q: torch.Tensor, lse: torch.Tensor, cache: Cache, table: torch.Te
     shape = (B, cache.heads, M)
     flags = 0
     if out is None:
-        out, flags = q.new_empty(shape, dtype=torch.float32), CLEAR_PADDING
+        flags = CLEAR_PADDING
+        if M < cols * cache.page:   # new tokens may lie past what has been collected
+            _fp32_on(mass, shape, dev, "mass")
+            M = cols * cache.page
+            shape = (B, cache.heads, M)
+            out = mass = torch.nn.functional.pad(mass, (0, M - mass.shape[2]))
+        else:
+            out = q.new_empty(shape, dtype=torch.float32)
     _same_device(dev, q=q, workspace=workspace)
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
@@ -819,8 +831,9 @@ def cache_keep(mass: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torc
                budget: int, sinks: int = 0, recent: int = 0,
                workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Which tokens of each head a ``budget`` keeps (vecattn_cache_keep): the first ``sinks``, the
-    last ``recent``, and the heaviest by ``mass`` (float32 [B, heads, M]).  Returns idx (int32 [B,
-    heads, budget], ascending, -1 padded) and kept (int32 [B]), how many each sequence has."""
+    last ``recent``, and the heaviest by ``mass`` (float32 [B, heads, M]; tokens at or past M are
+    never kept, ``recent`` ones neither).  Returns idx (int32 [B, heads, budget], ascending, -1
+    padded) and kept (int32 [B]), how many each sequence has."""
     if mass.dim() != 3:
         raise ValueError("mass must be [B, heads, M]")
     B, M = mass.shape[0], mass.shape[2]
@@ -845,11 +858,13 @@ def cache_keep(mass: torch.Tensor, cache: Cache, table: torch.Tensor, lens: torc
 
 def cache_gather(cache: Cache, table: torch.Tensor, idx: torch.Tensor, kept: torch.Tensor,
                  to_table: torch.Tensor, to: Optional[Cache] = None,
-                 mass: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+                 mass: Optional[torch.Tensor] = None,
+                 entries: Optional[int] = None) -> Optional[torch.Tensor]:
     """Moves tokens ``idx`` (int32 [B, heads, budget], kept[b] of them) of each head into the pages
     of ``to_table``, which no page of ``table`` may be among (vecattn_cache_gather); of the same
-    cache or of ``to``.  With ``mass`` (float32 [B, heads, M]) returns theirs ([B, heads, budget],
-    0 past kept)."""
+    cache or of ``to``.  With ``mass`` (float32 [B, heads, M]) returns theirs ([B, heads, entries],
+    0 past kept); ``entries``: budget (when not given) or more, such as all tokens of ``to_table``, so
+    that those written behind the kept ones have one."""
     if idx.dim() != 3:
         raise ValueError("idx must be [B, heads, budget]")
     to = cache if to is None else to
@@ -861,12 +876,15 @@ def cache_gather(cache: Cache, table: torch.Tensor, idx: torch.Tensor, kept: tor
     if mass is not None:
         M = mass.shape[-1]
         _fp32_on(mass, (B, cache.heads, M), dev, "mass")
-        out = mass.new_empty((B, cache.heads, budget))
-    _call(dev, "cache_gather", load().vecattn_cache_gather,
+        entries = budget if entries is None else int(entries)
+        if entries < budget:
+            raise ValueError("entries must be at least the budget")
+        out = mass.new_empty((B, cache.heads, entries))
+    _call(dev, "cache_gather", load().vecattn_cache_gather_wide,
           cache.desc(), table.data_ptr(), table.shape[1], B, idx.data_ptr(), kept.data_ptr(),
           budget, to.desc(), to_table.data_ptr(), to_table.shape[1],
           None if mass is None else mass.data_ptr(), M, None if out is None else out.data_ptr(),
-          CLEAR_PADDING)
+          0 if out is None else entries, CLEAR_PADDING)
     return out
 
 

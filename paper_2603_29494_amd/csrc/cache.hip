@@ -350,7 +350,8 @@ __global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
                                                       const int32_t* __restrict__ kept,
                                                       int64_t budget,
                                                       const float* __restrict__ mass, int64_t M,
-                                                      float* __restrict__ mass_out, bool clear) {
+                                                      float* __restrict__ mass_out, int64_t M_out,
+                                                      bool clear) {
   using L = CacheLayout<D, BITS>;
   constexpr int RUN = D / 32 * L::kDw;   // dwords of a token's codes of K on a lane
   constexpr int NB = 2, SLOTS = NB * kCacheBlock;
@@ -358,9 +359,14 @@ __global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
   const int h = blockIdx.y;
   const int64_t n = min(max(static_cast<int64_t>(kept[b]), int64_t(0)), budget);
   const int64_t jb = static_cast<int64_t>(blockIdx.x) * NB, j0 = jb * kCacheBlock;
-  if (mass_out && clear && threadIdx.x < SLOTS) {
+  const int64_t bh = b * map.H + h;
+  if (mass_out && clear) {
     const int64_t i = j0 + threadIdx.x;
-    if (i >= n && i < budget) mass_out[(b * map.H + h) * budget + i] = 0.0f;
+    if (threadIdx.x < SLOTS && i >= n && i < budget) mass_out[bh * M_out + i] = 0.0f;
+    // Entries past the budget, of tokens to come.
+    const int64_t step = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t x = budget + blockIdx.x * int64_t(256) + threadIdx.x; x < M_out; x += step)
+      mass_out[bh * M_out + x] = 0.0f;
   }
   if (j0 >= n) return;
   const int count = static_cast<int>(min<int64_t>(n - j0, SLOTS));
@@ -370,7 +376,6 @@ __global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
   __shared__ __align__(16) uint32_t codes[SLOTS][D / 4 + 4];   // V's, a byte each
   __shared__ const uint8_t* s_blk[SLOTS];                      // NULL: no such token
   __shared__ int s_token[SLOTS];                               // within its block
-  const int64_t bh = b * map.H + h;
   if (threadIdx.x < SLOTS) {
     const int slot = threadIdx.x;
     const uint8_t* blk = nullptr;
@@ -379,7 +384,7 @@ __global__ __launch_bounds__(256) void k_cache_gather(PageMap map, GatherTo to,
       j = idx[bh * budget + j0 + slot];
       if (j >= 0) blk = block_ptr<L::kBytes>(map, b, h, j >> 5);
       if (mass_out)
-        mass_out[bh * budget + j0 + slot] =
+        mass_out[bh * M_out + j0 + slot] =
             j >= 0 && j < M ? mass[bh * M + j] : __builtin_nanf("");
     }
     s_blk[slot] = blk;
@@ -518,15 +523,15 @@ hipError_t launch_cache_read(const CacheArgs& c, int64_t start, const Tensor4& k
 
 hipError_t launch_cache_gather(const CacheArgs& c, const CacheArgs& to, int64_t B,
                                const int32_t* idx, const int32_t* kept, int64_t budget,
-                               const float* mass, int64_t M, float* mass_out, bool clear,
-                               hipStream_t stream) {
+                               const float* mass, int64_t M, float* mass_out, int64_t M_out,
+                               bool clear, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>((budget + 2 * kCacheBlock - 1) / (2 * kCacheBlock)),
                   static_cast<unsigned>(c.H), static_cast<unsigned>(B));
   const GatherTo g{static_cast<uint8_t*>(to.data), to.table, to.cols, to.pages,
                    __builtin_ctz(static_cast<unsigned>(to.page))};
   auto run = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, page_map(c), g, idx, kept, budget, mass, M,
-                       mass_out, clear);
+                       mass_out, M_out, clear);
   };
   if (c.D == 128) c.bits == 4 ? run(k_cache_gather<128, 4>) : run(k_cache_gather<128, 8>);
   else c.bits == 4 ? run(k_cache_gather<64, 4>) : run(k_cache_gather<64, 8>);

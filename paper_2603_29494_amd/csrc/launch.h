@@ -191,8 +191,8 @@ hipError_t launch_cache_keep(const CacheArgs& c, int64_t B, const float* mass, i
                              int32_t* kept, void* workspace, hipStream_t stream);
 hipError_t launch_cache_gather(const CacheArgs& c, const CacheArgs& to, int64_t B,
                                const int32_t* idx, const int32_t* kept, int64_t budget,
-                               const float* mass, int64_t M, float* mass_out, bool clear,
-                               hipStream_t stream);
+                               const float* mass, int64_t M, float* mass_out, int64_t M_out,
+                               bool clear, hipStream_t stream);
 
 // Attention over an encoder's states.  How the work is dealt out, and so the
 // workspace, follows from the shape.

@@ -734,11 +734,13 @@ vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
 }
 
-vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* table, int64_t cols,
-                                    int64_t B, const int32_t* idx, const int32_t* kept,
-                                    int64_t budget, const vecattn_cache* to,
-                                    const int32_t* to_table, int64_t to_cols, const float* mass,
-                                    int64_t M, float* mass_out, int32_t flags, void* stream) {
+vecattn_status vecattn_cache_gather_wide(const vecattn_cache* cache, const int32_t* table,
+                                         int64_t cols, int64_t B, const int32_t* idx,
+                                         const int32_t* kept, int64_t budget,
+                                         const vecattn_cache* to, const int32_t* to_table,
+                                         int64_t to_cols, const float* mass, int64_t M,
+                                         float* mass_out, int64_t M_out, int32_t flags,
+                                         void* stream) {
   vecattn_status st;
   if ((st = check_cache(cache, true)) != VECATTN_OK) return st;
   if ((st = check_cache(to, true)) != VECATTN_OK) return st;
@@ -747,14 +749,23 @@ vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* t
   if (!table || !idx || !kept || !to_table || B < 1 || budget < 1 || budget > kMaxN)
     return VECATTN_ERR_INVALID_ARG;
   if (!cols_ok(cols, cache->page) || !cols_ok(to_cols, to->page)) return VECATTN_ERR_INVALID_ARG;
-  if ((mass == nullptr) != (mass_out == nullptr) || (mass && (M < 1 || M > kMaxN)) ||
-      !flags_ok(flags))
+  if ((mass == nullptr) != (mass_out == nullptr) || !flags_ok(flags) ||
+      (mass && (M < 1 || M > kMaxN || M_out < budget || M_out > kMaxN)))
     return VECATTN_ERR_INVALID_ARG;
   if (B > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
   hipError_t e = vecattn::launch_cache_gather(
       to_cache(cache, table, cols, nullptr), to_cache(to, to_table, to_cols, nullptr), B, idx, kept,
-      budget, mass, M, mass_out, flags != 0, static_cast<hipStream_t>(stream));
+      budget, mass, M, mass_out, M_out, flags != 0, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? VECATTN_OK : VECATTN_ERR_DEVICE;
+}
+
+vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* table, int64_t cols,
+                                    int64_t B, const int32_t* idx, const int32_t* kept,
+                                    int64_t budget, const vecattn_cache* to,
+                                    const int32_t* to_table, int64_t to_cols, const float* mass,
+                                    int64_t M, float* mass_out, int32_t flags, void* stream) {
+  return vecattn_cache_gather_wide(cache, table, cols, B, idx, kept, budget, to, to_table, to_cols,
+                                   mass, M, mass_out, budget, flags, stream);
 }
 
 vecattn_status vecattn_cross_attn_workspace_size(const vecattn_tdesc* qd, const vecattn_tdesc* kd,

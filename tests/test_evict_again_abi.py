@@ -1,0 +1,24 @@
+"""Refusals of vecattn_cache_gather_wide: no call below reaches the GPU."""
+import ctypes
+
+import pytest
+
+from paper_2603_29494_amd import _lib
+
+INVALID = 1
+FAKE = 0x100000   # 16-byte aligned address that validation rejects before any use
+
+
+@pytest.mark.parametrize("bad", [
+    dict(M_out=7), dict(M_out=(1 << 30) + 1), dict(M_out=0), dict(M_out=-1), dict(flags=2),
+    dict(mass=None), dict(mass_out=None), dict(M=0), dict(idx=None), dict(kept=None),
+    dict(budget=0, M_out=8), dict(cols=0), dict(to_cols=0), dict(B=0)])
+def test_gather_wide_rejects_bad_arguments(bad):
+    c = _lib.CacheDesc(FAKE, 8, 2, 128, 64, 4)
+    a = dict(cols=4, B=2, idx=FAKE, kept=FAKE, budget=8, to_cols=4, mass=FAKE, M=256, mass_out=FAKE,
+             M_out=8, flags=0)
+    a.update(bad)
+    assert _lib.load().vecattn_cache_gather_wide(
+        ctypes.byref(c), FAKE, a["cols"], a["B"], a["idx"], a["kept"], a["budget"], ctypes.byref(c),
+        FAKE, a["to_cols"], a["mass"], a["M"], a["mass_out"], a["M_out"], a["flags"],
+        None) == INVALID
