@@ -981,6 +981,9 @@ class Rope:
                     float(self.factor), freq, axis)))
         object.__setattr__(self, "_specs", tuple(specs))
 
+    def __reduce__(self):   # copies and saved plans make specs of their own
+        return type(self), (self.layout, self.freq, self.axis, self.factor)
+
     @property
     def axes(self) -> int:
         return max(self.axis) + 1
