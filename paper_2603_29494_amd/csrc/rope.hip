@@ -107,7 +107,8 @@ __global__ __launch_bounds__(256) void k_rope(const RopeParams a) {
   constexpr int ROWS = 64 / TH;       // rows of a wave
   constexpr int PAIRS = LAYOUT == kHalfAny ? 16 : 8;   // angles a thread needs
   const int lane = threadIdx.x & 63, j = lane % TH, r = lane / TH;
-  const int64_t wave = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t block = blockIdx.y * static_cast<int64_t>(gridDim.x) + blockIdx.x;
+  const int64_t wave = block * 4 + (threadIdx.x >> 6);
   const int64_t unit = wave / a.split;
   if (unit >= a.units) return;
   const int part = static_cast<int>(wave % a.split);
@@ -255,7 +256,11 @@ hipError_t launch_rope(const RopeArgs& x, hipStream_t stream) {
   // Few tokens: their heads are shared by as many waves as it takes to fill the chip.
   const int64_t passes = (a.heads + rows / tokens - 1) / (rows / tokens);
   a.split = static_cast<int32_t>(std::min(passes, std::max<int64_t>(1, 8192 / a.units)));
-  const dim3 grid(static_cast<unsigned>((a.units * a.split + 3) / 4));
+  // A dimension of a launch holds fewer than 2^32 threads (the API takes more without an error,
+  // and runs what is left of them).
+  const int64_t blocks = (a.units * a.split + 3) / 4, most = int64_t(1) << 22;
+  const dim3 grid(static_cast<unsigned>(std::min(blocks, most)),
+                  static_cast<unsigned>((blocks + most - 1) / most));
   const int layout = !x.half ? kInterleaved : x.rot % 16 == 0 ? kHalfChunks : kHalfAny;
   // What is turned, in and out, is past 256 MB: no cache holds it until it is read (131072
   // tokens of 32 heads: 399 us through the caches, 377 past them).
