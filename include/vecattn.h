@@ -635,7 +635,8 @@ vecattn_status vecattn_cache_keep(const float* mass, int64_t M, int64_t B,
  * Asynchronous, one launch.
  * Errors: INVALID_ARG (null pointer, other flags, one of mass and mass_out alone, B < 1,
  * budget or M < 1 or > 2^30, caches of other heads, D or bits, a bad cache, cols or to_cols
- * < 1 or more than 2^30 tokens); UNSUPPORTED (more than 65535 sequences or heads).
+ * < 1 or more than 2^30 tokens); UNSUPPORTED (more than 65535 sequences or heads, or a
+ * budget past 2^29).
  */
 vecattn_status vecattn_cache_gather(const vecattn_cache* cache, const int32_t* table, int64_t cols,
                                     int64_t B, const int32_t* idx, const int32_t* kept,

@@ -752,7 +752,8 @@ vecattn_status vecattn_cache_gather_wide(const vecattn_cache* cache, const int32
   if ((mass == nullptr) != (mass_out == nullptr) || !flags_ok(flags) ||
       (mass && (M < 1 || M > kMaxN || M_out < budget || M_out > kMaxN)))
     return VECATTN_ERR_INVALID_ARG;
-  if (B > kMaxGridYZ) return VECATTN_ERR_UNSUPPORTED;
+  // 256 threads per 64 slots, fewer than 2^32 of them.
+  if (B > kMaxGridYZ || budget > kMaxN / 2) return VECATTN_ERR_UNSUPPORTED;
   hipError_t e = vecattn::launch_cache_gather(
       to_cache(cache, table, cols, nullptr), to_cache(to, to_table, to_cols, nullptr), B, idx, kept,
       budget, mass, M, mass_out, M_out, flags != 0, static_cast<hipStream_t>(stream));

@@ -1,4 +1,4 @@
-"""Refusals of vecattn_cache_gather_wide: no call below reaches the GPU."""
+"""Refusals of vecattn_cache_gather and vecattn_cache_gather_wide: no call below reaches the GPU."""
 import ctypes
 
 import pytest
@@ -22,3 +22,13 @@ def test_gather_wide_rejects_bad_arguments(bad):
         ctypes.byref(c), FAKE, a["cols"], a["B"], a["idx"], a["kept"], a["budget"], ctypes.byref(c),
         FAKE, a["to_cols"], a["mass"], a["M"], a["mass_out"], a["M_out"], a["flags"],
         None) == INVALID
+
+
+@pytest.mark.parametrize("budget", [(1 << 29) + 1, 1 << 30])
+def test_gather_refuses_more_slots_than_a_launch_holds(budget):
+    c, f = _lib.CacheDesc(FAKE, 8, 2, 128, 64, 4), ctypes.byref
+    lib, unsupported = _lib.load(), 2
+    assert lib.vecattn_cache_gather(f(c), FAKE, 4, 2, FAKE, FAKE, budget, f(c), FAKE, 4, None, 0,
+                                    None, 0, None) == unsupported
+    assert lib.vecattn_cache_gather_wide(f(c), FAKE, 4, 2, FAKE, FAKE, budget, f(c), FAKE, 4, FAKE,
+                                         256, FAKE, 1 << 30, 0, None) == unsupported
