@@ -672,9 +672,11 @@ vecattn_status vecattn_cache_gather_wide(const vecattn_cache* cache, const int32
  *   workspace : device memory (16-byte aligned) of at least
  *          vecattn_cross_attn_workspace_size bytes for the same qd and kd (0: may be
  *          NULL); contents need not be initialised.  Calls that may overlap need one each.
- * Scores and sums are fp32, the weights bf16 before they meet V.  The result does not
- * depend on the order of execution (no atomics).  What a call does follows lens, mask and
- * n_q on the device, so that a captured call can be replayed as they change.
+ * Scores and sums are fp32, the weights bf16 before they meet V (off by 2^-8 of a weight at
+ * most), or, of up to 16 rows Nq * Hq / Hkv, two bf16 that add up to them (2^-16).  Finite |V|
+ * up to 2^90 leaves finite rows finite.  The result does not depend on the order of
+ * execution (no atomics).  What a call does follows lens, mask and n_q on the device, so
+ * that a captured call can be replayed as they change.
  * Errors: INVALID_ARG (null pointer, shape mismatch, Hq % Hkv != 0, mask_sB < 0, a bad
  * scale, other flags, an output whose sequences or heads share memory, misalignment);
  * CAPACITY (workspace too small); UNSUPPORTED (D not in {64, 128}, Nq * Hq / Hkv > 2^30, more

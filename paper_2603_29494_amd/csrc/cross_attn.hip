@@ -7,8 +7,12 @@
 // its two lanes; K and V go from memory straight to LDS with the swizzle of
 // device_common.h, and V is read back transposed.  Rows of masked keys of V are fetched
 // from past the buffer's end, which reads 0: what such a key holds never meets a
-// product, and its score is set to -inf.  The weights are rounded to bf16 (half a step,
-// 2^-9) before they meet V, as the operands are; their sum is of what was not rounded.
+// product, and its score is set to -inf.  The weights are rounded to bf16 (off by 2^-8 of a
+// weight at most) before they meet V, as the operands are; their sum is of what was not
+// rounded.  Up to 16 rows stand in the products' 32 columns twice, and a weight in two bf16
+// numbers that add up to it (2^-16), which takes no more products.  Of more rows the second half
+// would: 75600 rows of 40 heads over 512 keys 1138 us in place of 860, 4096 over 4096 keys 190
+// in place of 135.
 //
 // Two kernels.  Of more than 32 rows, a workgroup owns 128 of them (a wave 32) and its
 // waves share tiles of 32 keys.  Of up to 32, each of four waves takes tiles of 32 keys
@@ -211,8 +215,9 @@ __device__ __forceinline__ uint32_t fresh(uint32_t x) {
   return x;
 }
 
-// One wave's 32 rows against 32 keys at a time.
-template <int D>
+// One wave's 32 rows against 32 keys at a time; TWICE: 16 rows, each with a weight's rounding to
+// bf16 in one column of the products and the rounding of what that leaves in the other, 16 on.
+template <int D, bool TWICE>
 struct Wave {
   static constexpr int DS = D / 16, DB = D / 32, RB = 2 * D;
   bf16x8 qf[DS];
@@ -220,6 +225,7 @@ struct Wave {
   float m_run, l_run;
   uint32_t kat, vat;   // where the lane's operands lie: of K's first values, of V's first keys
   int g, ln;
+  float second;        // 1 in the columns of the weights' second parts
 
   __device__ __forceinline__ void clear() {
     m_run = kUnseen;
@@ -229,6 +235,7 @@ struct Wave {
   }
   __device__ __forceinline__ void start(int lane) {
     g = lane >> 5, ln = lane & 31;
+    second = TWICE && (ln & 16) ? 1.0f : 0.0f;
     clear();
     kat = ln * RB + 16 * (g ^ swz<D>(ln));
     const int j16 = lane & 15, tq = j16 >> 2, tp = j16 & 3, vhalf = (lane >> 4) & 1;
@@ -315,6 +322,12 @@ struct Wave {
           y[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * x + e], scale_log2, -m_run));
         part[x] = ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
         pb[x] = __builtin_convertvector(y, bf16x8);
+        if constexpr (TWICE) {   // in the second columns what that leaves
+          const f32x8 first = __builtin_convertvector(pb[x], f32x8);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = __builtin_fmaf(-first[e], second, y[e]);
+          pb[x] = __builtin_convertvector(y, bf16x8);
+        }
       }
       sum = part[0] + part[1];
     };
@@ -370,7 +383,7 @@ template <int D, bool MASK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 3 : 4))) void k_cross_many(
     const CrossParams a) {
   constexpr int KEYS = 32, U = KEYS * (D / 8) / 256;   // direct loads per wave and matrix
-  using W = Wave<D>;
+  using W = Wave<D, false>;
   constexpr int DB = W::DB;
   __shared__ __align__(16) uint16_t k_s0[KEYS * D];
   __shared__ __align__(16) uint16_t k_s1[KEYS * D];
@@ -502,11 +515,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 128 ? 
     }
 }
 
-template <int D>
+// Few rows; TWICE: up to 16, each in two columns of the products (weights in two parts).  What it
+// adds are the instructions that take a weight apart: nothing where K and V come from memory (one
+// token of 28 heads over 16 x 16384 keys 48 us with or without), 3% of 12 heads over 257 keys (7.0
+// and 6.8), 7% where they come from the caches (256 heads of 64 over 4000 keys 29.9 and 27.8).
+// Products of their own would take as much more.
+template <int D, bool TWICE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_cross_few(
     const CrossParams a) {
   constexpr int KEYS = kFewKeys, U = KEYS * (D / 8) / 64, ROWS = 32;
-  using W = Wave<D>;
+  using W = Wave<D, TWICE>;
   __shared__ __align__(16) uint16_t k_s0[4][KEYS * D];
   __shared__ __align__(16) uint16_t k_s1[4][KEYS * D];
   __shared__ __align__(16) uint16_t v_s0[4][KEYS * D];
@@ -540,7 +558,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
                  v_row = lane / (D / 8) * v_rowb;
   const uint8_t* mask = a.mask ? a.mask + s.b * a.mask_sB + first : nullptr;
   const int ntiles = (keys + KEYS - 1) / KEYS;
-  const int row = s.rt * ROWS + (lane & 31);
+  const int row = lane & (TWICE ? 15 : 31);
   const bool have = row < s.rows;
   W w;
   w.start(lane);
@@ -573,6 +591,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     see = bits(b0), see1 = bits(b1);
     fetch(t, see, k_s0[wave], v_s0[wave]);
   }
+  bool settled = false;
   auto turn = [&](const uint16_t* k, const uint16_t* v, uint16_t* k1, uint16_t* v1)
                   __attribute__((always_inline)) {
     const int byte2 = key_byte(tile(t + 8));
@@ -582,6 +601,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     bf16x8 pb[2];
     w.score(x, k);
     if (see != ~0u) w.hide(x, see);
+    if (!settled) {   // the first keys of which one is visible, the same for all rows
+      w.m_run = fmaxf(w.m_run, wave_max_xor32(W::largest(x)) * a.scale_log2);
+      settled = see != 0;
+    }
     w.weigh(x, a.scale_log2, pb);
     w.add(pb, v);
     see = see1, see1 = bits(byte2);
@@ -627,8 +650,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     __syncthreads();
   }
   // Eight threads a row.
-  const int r = threadIdx.x >> 3, sr = s.rt * ROWS + r;
-  if (sr >= s.rows) return;
+  const int r = threadIdx.x >> 3;
+  if (r >= s.rows) return;
   float lr = 0.0f, mr = kUnseen;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -640,11 +663,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   for (int i = 0; i < D / 32; ++i) {
     const int d = 32 * i + 4 * (threadIdx.x & 7);
     f32x4 y = *reinterpret_cast<const f32x4*>(buf + r * kSo + d);
+    if constexpr (TWICE) {
+      const f32x4 more = *reinterpret_cast<const f32x4*>(buf + (r + 16) * kSo + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)   // an infinity of V is one of o, whatever the second part makes of it
+        y[e] += fabsf(y[e]) < INFINITY ? more[e] : 0.0f;
+    }
     if (s.count > 1) {
       put_part<D>(a, s, ROWS, r, d, y);
     } else {
       y *= inv;
-      *reinterpret_cast<bf16x4*>(o_row(a, s.b, s.hk, sr) + d) = __builtin_convertvector(y, bf16x4);
+      *reinterpret_cast<bf16x4*>(o_row(a, s.b, s.hk, r) + d) = __builtin_convertvector(y, bf16x4);
     }
   }
   if ((threadIdx.x & 7) == 0) {
@@ -652,7 +681,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       float* ml = part_ml<D>(a, s.index, ROWS, r);
       ml[0] = mr, ml[1] = lr;
     } else {
-      put_lse(a, s.b, s.hk, sr, mr, lr);
+      put_lse(a, s.b, s.hk, r, mr, lr);
     }
   }
 }
@@ -802,7 +831,9 @@ hipError_t launch_cross_attn(const CrossArgs& x, hipStream_t stream) {
   const dim3 grid(a.items);
   auto pick = [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    if (d.few) hipLaunchKernelGGL(k_cross_few<D>, grid, dim3(256), 0, stream, a);
+    if (d.few && a.Nq * a.group <= 16)
+      hipLaunchKernelGGL((k_cross_few<D, true>), grid, dim3(256), 0, stream, a);
+    else if (d.few) hipLaunchKernelGGL((k_cross_few<D, false>), grid, dim3(256), 0, stream, a);
     else if (a.mask) hipLaunchKernelGGL((k_cross_many<D, true>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((k_cross_many<D, false>), grid, dim3(256), 0, stream, a);
     const hipError_t e = hipGetLastError();
