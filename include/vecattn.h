@@ -757,8 +757,9 @@ vecattn_status vecattn_rope_ladder(int32_t rot, double base, int32_t scaling, do
  *     neither: start + r on every axis
  *   n_new : optional int32 [B] device memory (clamped to [0, N]): the rows of sequence b
  *           that exist; those past it are left as they were.  NULL: all N.
- * Angles are taken in 64 bits and reduced exactly, sines and cosines are good to fp32 at
- * any position, and a result is rounded to bf16 once.  Asynchronous, one launch.
+ * Angles are taken in 64 bits (off by 2^-51 of the angle), sines and cosines of what is left
+ * of a quarter turn in fp32, so that they are good to fp32 for angles up to 2^28 radians, and a
+ * result is rounded to bf16 once.  Asynchronous, one launch.
  * Errors: INVALID_ARG (null pointer, shape mismatch, both pos and lens, |start| > 2^30,
  * a bad stride, a spec outside what its comments allow, a factor or frequency that is not
  * finite, |frequency| > 1024, an output that is its input with other strides or whose

@@ -11,7 +11,7 @@
 // Few rows are bound by reading K's half of the cache: four sequences of 131072 tokens in 4
 // bits, 4 heads of 128, 7 rows each: 34 us, 4.9 TB/s.  Many rows by the matrix products and
 // the exponentials, whose times add: 512 tokens of 28 heads over 33280 in 8 bits, 4 heads:
-// 175 us at best, 700 TFLOP/s (13 more with rows of q in fp16 and their powers of two applied
+// 175 to 187 us over the cards it ran on, 650 to 693 TFLOP/s, 7 of them k_mass_rows (13 more with rows of q in fp16 and their powers of two applied
 // to every score; 5 more with the codes fetched by dwords and each sum's lanes added on
 // their own, which also takes 207 us instead of 128 for 126 rows over 4 x 131072 tokens).
 // Three workgroups fit a CU at a time, and 1040 come out uneven there; splitting their rows

@@ -2,10 +2,10 @@
 // the pair's frequency, (a, b) -> f (a cos t - b sin t, a sin t + b cos t), the
 // transposed turn with -t.
 //
-// Angles.  Frequencies come as turns per position in fp64; position x turns less
-// the nearest quarter turn is exact in one fused multiply-add, so that a far
-// position costs no digits, and what is left, at most an eighth of a turn, goes to
-// fp32.  Its sine and cosine are Taylor sums (the next terms are below 2^-29),
+// Angles.  Frequencies come as turns per position in fp64 (off by 2^-52 of themselves);
+// position x turns less the nearest quarter turn is one fused multiply-add, so that the
+// reduction of a far position costs no digits, and what is left, at most an eighth of a
+// turn, goes to fp32.  Its sine and cosine are Taylor sums (the next terms are below 2^-29),
 // swapped and signed by the quarter.  Products and their sum are fp32, rounded
 // to bf16 once.
 //
